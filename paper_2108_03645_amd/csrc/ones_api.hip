@@ -19,16 +19,26 @@
 // per-device address comes from hipGetSymbolAddress (static_scratch_of below).
 static __device__ __align__(256) unsigned char scratch[ONES_STATIC_SCRATCH_BYTES];
 
+namespace ones {
+int hip_fail(hipError_t e, const char *what);
+}
+
 namespace {
 
 using namespace ones;
 
 thread_local char g_hip_msg[256] = "HIP call failed";
 
-int hip_fail(hipError_t e, const char *what) {
+}  // namespace
+
+// For every entry point of the library: keeps the text that ones_strerror(ONES_E_HIP) returns on this thread.
+int ones::hip_fail(hipError_t e, const char *what) {
   snprintf(g_hip_msg, sizeof(g_hip_msg), "HIP call failed: %s: %s", what, hipGetErrorString(e));
   return ONES_E_HIP;
 }
+
+namespace {
+
 #define HIP_TRY(expr)                                         \
   do {                                                        \
     hipError_t e__ = (expr);                                  \
@@ -1291,7 +1301,7 @@ const char *ones_strerror(int code) {
     case ONES_OK: return "ok";
     case ONES_E_INVALID_ARG: return "invalid argument";
     case ONES_E_NOT_POW2: return "bmin, bmax and gpu_max_batch of an active slot must be powers of two";
-    case ONES_E_BOUNDS: return "batch window or model parameter out of bounds";
+    case ONES_E_BOUNDS: return "batch window, model parameter or size out of bounds";
     case ONES_E_NONFINITE: return "NaN or infinity in a job parameter";
     case ONES_E_WORKSPACE_TOO_SMALL: return "workspace too small or not 256-byte aligned";
     case ONES_E_HIP: return g_hip_msg;

@@ -1,0 +1,286 @@
+// Layer norm over the last dimension, forward and backward (ones_layer_norm_*).
+//
+//   mean = sum x / D, rstd = (sum (x - mean)^2 / D + eps)^-1/2, xh = (x - mean) rstd, y = xh w + b
+//   g = dy w, dx = rstd (g - avg(g) - xh avg(g xh)), dw = sum over rows of dy xh, db = sum over rows of dy
+//
+// Both directions touch every element once: a row is held in registers by a wave (D up to 2048), four waves (up to 8192) or
+// sixteen (up to 32768), so that the centred sum of squares (no cancellation, unlike the sum of squares less the square of the
+// mean) and the results need no second read.  What bounds them is memory.  Workgroups take rows in turn, which keeps the
+// weights in registers, and backward the sums of dw and db over a workgroup's rows as well: it leaves one row of partial sums a
+// workgroup, which a second small launch adds up in a fixed order.  No atomics: the results are the same bits every time.
+#include "train_device.h"
+#include "train_host.h"
+
+#include <algorithm>
+
+namespace ones {
+namespace train {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kMostPerThread = 32;
+
+struct NormArgs {
+  const void *x, *dy;
+  void *out;                       // y forward, dx backward
+  const void *weight, *bias;       // may be null (bias is used forward only)
+  float *mean, *rstd;              // written forward, read backward
+  float *partial;                  // backward: [workgroups][2][D]
+  int64_t rows, x_stride, dy_stride;
+  int32_t cols, weight_type;
+  float eps;
+};
+
+// Thread t of a row holds elements (k * TPR + t) * VEC + 0..VEC-1, k < PER / VEC.
+template <typename T, int PER, int VEC, int TPR>
+__device__ __forceinline__ void load_row(const T *row, int t, int cols, float *v) {
+#pragma unroll
+  for (int k = 0; k < PER / VEC; ++k) {
+    const int c = (k * TPR + t) * VEC;
+    if (c < cols) {
+      const Pack<T, VEC> p = load_pack<T, VEC>(row + c);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[k * VEC + i] = static_cast<float>(p.v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[k * VEC + i] = 0.f;
+    }
+  }
+}
+template <typename T, int PER, int VEC, int TPR>
+__device__ __forceinline__ void store_row(T *row, int t, int cols, const float *v) {
+#pragma unroll
+  for (int k = 0; k < PER / VEC; ++k) {
+    const int c = (k * TPR + t) * VEC;
+    if (c < cols) store_pack<T, VEC>(row + c, v + k * VEC);
+  }
+}
+template <int PER, int VEC, int TPR>
+__device__ __forceinline__ void load_weights(const void *p, int type, float otherwise, int t, int cols, float *v) {
+#pragma unroll
+  for (int k = 0; k < PER / VEC; ++k) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const int c = (k * TPR + t) * VEC + i;
+      v[k * VEC + i] = c < cols ? (p ? load_as(p, type, c) : otherwise) : 0.f;
+    }
+  }
+}
+
+template <typename T, int PER, int VEC, int TPR>
+__global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_forward_kernel(NormArgs a) {
+  constexpr int block = TPR > kBlock ? TPR : kBlock, rows_at_once = block / TPR;
+  __shared__ float part[2][2 * (block / kWave)];
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  float w[PER], b[PER];
+  load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
+  load_weights<PER, VEC, TPR>(a.bias, a.weight_type, 0.f, t, a.cols, b);
+  const float n = static_cast<float>(a.cols);
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * rows_at_once + sub; row < a.rows; row += static_cast<int64_t>(gridDim.x) * rows_at_once) {
+    float v[PER];
+    load_row<T, PER, VEC, TPR>(static_cast<const T *>(a.x) + row * a.x_stride, t, a.cols, v);
+    float sum = 0.f, none = 0.f, square = 0.f, rest = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += v[i];
+    row_sum2<TPR>(sum, none, part[0]);
+    float mean = sum / n;
+#pragma unroll
+    for (int k = 0; k < PER / VEC; ++k) {
+      if ((k * TPR + t) * VEC < a.cols) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float d = v[k * VEC + i] - mean;
+          v[k * VEC + i] = d;
+          rest += d;
+          square += d * d;
+        }
+      }
+    }
+    row_sum2<TPR>(square, rest, part[1]);
+    // what the first mean was off by (its rounding, where the values lie far from zero) is the mean of the differences
+    rest /= n;
+    mean += rest;
+    const float rstd = 1.f / sqrtf(fmaxf(square / n - rest * rest, 0.f) + a.eps);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = (v[i] - rest) * rstd * w[i] + b[i];
+    store_row<T, PER, VEC, TPR>(static_cast<T *>(a.out) + row * a.cols, t, a.cols, v);
+    if (t == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
+  }
+}
+
+template <typename T, int PER, int VEC, int TPR>
+__global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_backward_kernel(NormArgs a) {
+  constexpr int block = TPR > kBlock ? TPR : kBlock, rows_at_once = block / TPR;
+  __shared__ float part[2][2 * (block / kWave)];
+  __shared__ float sums[rows_at_once > 1 ? 2 * PER * TPR : 1];
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  float w[PER], dw[PER], db[PER];
+  load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) dw[i] = db[i] = 0.f;
+  const float n = static_cast<float>(a.cols);
+  int turn = 0;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * rows_at_once + sub; row < a.rows; row += static_cast<int64_t>(gridDim.x) * rows_at_once) {
+    float x[PER], dy[PER];
+    load_row<T, PER, VEC, TPR>(static_cast<const T *>(a.x) + row * a.x_stride, t, a.cols, x);
+    load_row<T, PER, VEC, TPR>(static_cast<const T *>(a.dy) + row * a.dy_stride, t, a.cols, dy);
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float sg = 0.f, sgx = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {                 // past the last column dy and w are zero
+      const float xh = (x[i] - mean) * rstd, g = dy[i] * w[i];
+      x[i] = xh;
+      dw[i] += dy[i] * xh;
+      db[i] += dy[i];
+      sg += g;
+      sgx += g * xh;
+    }
+    row_sum2<TPR>(sg, sgx, part[turn]);
+    turn ^= 1;
+    sg /= n;
+    sgx /= n;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) x[i] = rstd * (dy[i] * w[i] - sg - x[i] * sgx);
+    store_row<T, PER, VEC, TPR>(static_cast<T *>(a.out) + row * a.cols, t, a.cols, x);
+  }
+  if constexpr (rows_at_once > 1) {                 // the waves' sums, one after another
+    for (int s = 0; s < rows_at_once; ++s) {
+      if (sub == s) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          float *p = sums + (2 * i) * TPR + t;
+          if (s) { dw[i] += p[0]; db[i] += p[TPR]; }
+          if (s + 1 < rows_at_once) { p[0] = dw[i]; p[TPR] = db[i]; }
+        }
+      }
+      __syncthreads();
+    }
+    if (sub != rows_at_once - 1) return;
+  }
+  float *to = a.partial + static_cast<int64_t>(blockIdx.x) * 2 * a.cols;
+#pragma unroll
+  for (int k = 0; k < PER / VEC; ++k) {
+    const int c = (k * TPR + t) * VEC;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (c + i < a.cols) { to[c + i] = dw[k * VEC + i]; to[a.cols + c + i] = db[k * VEC + i]; }
+  }
+}
+
+// dw and db from n rows of partial sums: 16 threads share 64 of the 2 D columns.
+__global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *partial, int32_t n, int32_t cols, void *dweight, void *dbias, int32_t type) {
+  __shared__ float sums[16][64];
+  const int lane = threadIdx.x % 64, part = threadIdx.x / 64;
+  const int c = blockIdx.x * 64 + lane;
+  float s = 0.f;
+  if (c < 2 * cols) {
+#pragma unroll 4
+    for (int i = part; i < n; i += 16) s += partial[static_cast<int64_t>(i) * 2 * cols + c];
+  }
+  sums[part][lane] = s;
+  __syncthreads();
+  if (part || c >= 2 * cols) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) s += sums[i][lane];
+  void *to = c < cols ? dweight : dbias;
+  if (to) store_as(to, type, c < cols ? c : c - cols, s);
+}
+
+int threads_per_row(int64_t cols) { return cols <= 64 * kMostPerThread ? 64 : cols <= 256 * kMostPerThread ? 256 : 1024; }
+// Workgroups: enough for eight waves a SIMD forward; backward at most so many that their partial sums stay a small part of the
+// traffic.
+int64_t norm_blocks(int64_t rows, int64_t cols, bool backward) {
+  const int64_t tpr = threads_per_row(cols), at_once = tpr > kBlock ? 1 : kBlock / tpr;
+  const int64_t most = backward ? (tpr == 1024 ? 256 : 512) : (tpr == 1024 ? 512 : 2048);
+  return std::min(ceil_div(rows, at_once), most);
+}
+
+template <typename T, int PER, int VEC, int TPR>
+void launch_norm(const NormArgs &a, bool backward, hipStream_t s) {
+  const dim3 grid(static_cast<uint32_t>(norm_blocks(a.rows, a.cols, backward))), block(TPR > kBlock ? TPR : kBlock);
+  if (backward) hipLaunchKernelGGL((norm_backward_kernel<T, PER, VEC, TPR>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_forward_kernel<T, PER, VEC, TPR>), grid, block, 0, s, a);
+}
+
+template <typename T, int VEC, int TPR>
+void launch_norm_per(const NormArgs &a, bool backward, hipStream_t s) {
+  const int64_t per = ceil_div(a.cols, TPR);
+  if constexpr (TPR == 64) {
+    if (per <= 8) return launch_norm<T, 8, VEC, TPR>(a, backward, s);
+  }
+  if (per <= 16) return launch_norm<T, 16, VEC, TPR>(a, backward, s);
+  launch_norm<T, 32, VEC, TPR>(a, backward, s);
+}
+
+template <typename T, int VEC>
+void launch_norm_tpr(const NormArgs &a, bool backward, hipStream_t s) {
+  switch (threads_per_row(a.cols)) {
+    case 64: return launch_norm_per<T, VEC, 64>(a, backward, s);
+    case 256: return launch_norm_per<T, VEC, 256>(a, backward, s);
+    default: return launch_norm_per<T, VEC, 1024>(a, backward, s);
+  }
+}
+
+template <typename T>
+void launch_norm_vec(const NormArgs &a, bool backward, hipStream_t s) {
+  constexpr int vec = 16 / sizeof(T);
+  const bool wide = a.cols % vec == 0 && a.x_stride % vec == 0 && aligned(a.x, 16) && aligned(a.out, 16) &&
+                    (!backward || (a.dy_stride % vec == 0 && aligned(a.dy, 16)));
+  if (wide) launch_norm_tpr<T, vec>(a, backward, s);
+  else launch_norm_tpr<T, 1>(a, backward, s);
+}
+
+void launch_norm_type(const NormArgs &a, int32_t type, bool backward, hipStream_t s) {
+  if (type == ONES_F32) launch_norm_vec<float>(a, backward, s);
+  else if (type == ONES_F16) launch_norm_vec<f16>(a, backward, s);
+  else launch_norm_vec<bf16>(a, backward, s);
+}
+
+int check_norm(int64_t rows, int64_t cols, int64_t stride, int32_t type, int32_t weight_type) {
+  if (int rc = check_rows(rows, cols, stride)) return rc;
+  if (cols < 1 || !is_type(type) || (weight_type != ONES_F32 && weight_type != type)) return ONES_E_INVALID_ARG;
+  return cols > ONES_MAX_NORM_COLUMNS ? ONES_E_BOUNDS : ONES_OK;
+}
+
+}  // namespace
+}  // namespace train
+}  // namespace ones
+
+using namespace ones::train;
+
+extern "C" {
+
+int ones_layer_norm_forward(const void *x, int64_t x_stride, int64_t rows, int64_t cols, int32_t type, const void *weight, const void *bias,
+                            int32_t weight_type, float eps, void *y, float *mean, float *rstd, void *hip_stream) {
+  if (int rc = check_norm(rows, cols, x_stride, type, weight_type)) return rc;
+  if (!(eps >= 0.f)) return ONES_E_INVALID_ARG;
+  if (rows == 0) return ONES_OK;
+  if (!x || !y || !mean || !rstd) return ONES_E_INVALID_ARG;
+  const NormArgs a{x, nullptr, y, weight, bias, mean, rstd, nullptr, rows, x_stride, 0, static_cast<int32_t>(cols), weight_type, eps};
+  launch_norm_type(a, type, false, static_cast<hipStream_t>(hip_stream));
+  return launched("layer norm forward");
+}
+
+size_t ones_layer_norm_workspace_bytes(int64_t rows, int64_t cols) {
+  if (rows < 0 || cols < 1 || cols > ONES_MAX_NORM_COLUMNS) return 0;
+  return align_up(static_cast<size_t>(std::max<int64_t>(1, norm_blocks(rows, cols, true))) * 2 * static_cast<size_t>(cols) * 4);
+}
+
+int ones_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int64_t rows, int64_t cols, int32_t type,
+                             const void *weight, int32_t weight_type, const float *mean, const float *rstd, void *dx, void *dweight,
+                             void *dbias, void *d_workspace, size_t workspace_bytes, void *hip_stream) {
+  if (int rc = check_norm(rows, cols, x_stride, type, weight_type)) return rc;
+  if (int rc = check_rows(rows, cols, dy_stride)) return rc;
+  if (rows && (!dy || !x || !mean || !rstd || !dx)) return ONES_E_INVALID_ARG;
+  if (int rc = check_workspace(d_workspace, workspace_bytes, ones_layer_norm_workspace_bytes(rows, cols))) return rc;
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const NormArgs a{x, dy, dx, weight, nullptr, const_cast<float *>(mean), const_cast<float *>(rstd), static_cast<float *>(d_workspace),
+                   rows, x_stride, dy_stride, static_cast<int32_t>(cols), weight_type, 0.f};
+  if (rows) launch_norm_type(a, type, true, s);
+  if (dweight || dbias)
+    hipLaunchKernelGGL(norm_reduce_kernel, dim3(static_cast<uint32_t>(ceil_div(2 * cols, 64))), dim3(1024), 0, s, a.partial,
+                       static_cast<int32_t>(norm_blocks(rows, cols, true)), a.cols, dweight, dbias, weight_type);
+  return launched("layer norm backward");
+}
+
+}  // extern "C"

@@ -1,0 +1,263 @@
+"""Python binding of libones' operators for a scheduled job's training step (include/ones_train.h): argument checks and
+marshalling only.  The arithmetic runs in the library's HIP kernels; PyTorch supplies the tensors and the stream (the current one
+of the tensors' device).  There is no CPU fallback: without the built library or without a GPU this raises.
+
+The ``*_forward`` and ``*_backward`` functions are the library's calls; ``layer_norm``, ``gated_recurrence`` and
+``linear_cross_entropy`` are the same under autograd.  ``gated_recurrence_step`` is the single-token form,
+``orthogonal_update`` the optimizer's step."""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import ones
+from .ones import OnesError  # noqa: F401
+
+EXPORTS = ["ones_layer_norm_forward", "ones_layer_norm_workspace_bytes", "ones_layer_norm_backward",
+           "ones_recurrence_carry_bytes", "ones_recurrence_workspace_bytes", "ones_recurrence_forward",
+           "ones_recurrence_backward", "ones_recurrence_step"]
+
+_P, _I64, _I32, _F32, _SIZE = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_size_t
+_ARGUMENTS = {
+    "ones_layer_norm_forward": [_P, _I64, _I64, _I64, _I32, _P, _P, _I32, _F32, _P, _P, _P, _P],
+    "ones_layer_norm_workspace_bytes": [_I64, _I64],
+    "ones_layer_norm_backward": [_P, _I64, _P, _I64, _I64, _I64, _I32, _P, _I32, _P, _P, _P, _P, _P, _P, _SIZE, _P],
+    "ones_recurrence_carry_bytes": [_I64, _I64, _I64],
+    "ones_recurrence_workspace_bytes": [_I64, _I64, _I64],
+    "ones_recurrence_forward": [_P, _I64, _I64, _P, _I64, _I64, _I64, _I64, _I64, _I32, _P, _P, _P, _P, _P, _P, _SIZE, _P],
+    "ones_recurrence_backward": [_P, _I64, _I64, _P, _P, _I64, _I64, _P, _I64, _I64, _I64, _I64, _I64, _I32, _P, _P, _P, _P, _P,
+                                 _P, _SIZE, _P],
+    "ones_recurrence_step": [_P, _I64, _P, _I64, _I64, _I64, _I32, _P, _P, _P],
+}
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_lib = None
+
+
+def load():
+    """The library with the argument types of these functions; raises if it has not been built."""
+    global _lib
+    if _lib is None:
+        L = ones.load()
+        for name, arguments in _ARGUMENTS.items():
+            f = getattr(L, name)
+            f.argtypes = arguments
+            f.restype = _SIZE if name.endswith("_bytes") else C.c_int
+        _lib = L
+    return _lib
+
+
+def _call(device, function, *args):
+    """A call of the library with the tensors' device current (it mostly is already), on its current stream."""
+    if torch.cuda.current_device() == device.index:
+        rc = function(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = function(*args, torch.cuda.current_stream().cuda_stream)
+    if rc:
+        raise OnesError(rc, _lib.ones_strerror(rc).decode())
+
+
+def _check(t, name, shape, types, device=None):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: a tensor is wanted")
+    if t.dtype not in types:
+        raise TypeError(f"{name}: {t.dtype} is not one of {', '.join(str(d) for d in types)}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, wanted {tuple(shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the others on {device}")
+    if not t.is_cuda:
+        raise OnesError(-101, f"{name}: on {t.device}; libones has no CPU path")
+
+
+def _dense(t, name, shape, types, device):
+    """Checked, without gaps (copied if it has any), None stays None."""
+    if t is None:
+        return None
+    _check(t, name, shape, types, device)
+    return t.contiguous()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _scratch(nbytes, device):
+    """Workspace of one call from torch's allocator, whose blocks are 512-byte aligned and reused in stream order."""
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _rows(t):
+    """(t as rows of one dimension, elements between two of them); copied where it cannot be seen as such."""
+    d = t.shape[-1]
+    if t.dim() == 2 and (t.stride(1) == 1 or d == 1) and t.stride(0) >= d:
+        return t, t.stride(0)
+    t = t.contiguous()
+    return t.view(-1, d) if d else t.reshape(-1, d), d
+
+
+# ------------------------------------------------------------------ layer norm --------
+def _norm_weights(weight, bias, x):
+    kinds = (torch.float32, x.dtype)
+    d = x.shape[-1]
+    weight, bias = _dense(weight, "weight", (d,), kinds, x.device), _dense(bias, "bias", (d,), kinds, x.device)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError("weight and bias: one type for both")
+    return weight, bias, next((w.dtype for w in (weight, bias) if w is not None), torch.float32)
+
+
+def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
+    """ones_layer_norm_forward over the last dimension: (y, mean, rstd), the latter float32 without that dimension."""
+    _check(x, "x", None, _TYPES)
+    if x.dim() < 1:
+        raise ValueError("x: at least one dimension is wanted")
+    weight, bias, kind = _norm_weights(weight, bias, x)
+    rows, stride = _rows(x)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
+    n, d = rows.shape
+    p = stats.data_ptr()
+    _call(x.device, load().ones_layer_norm_forward, rows.data_ptr(), stride, n, d, _TYPES[x.dtype], _ptr(weight), _ptr(bias),
+          _TYPES[kind], eps, y.data_ptr(), p, p + 4 * n)
+    return y, stats[0], stats[1]
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, want_bias=True):
+    """ones_layer_norm_backward: (dx, dweight, dbias).  dweight has the weight's type (float32 without one); dbias is None if
+    not wanted."""
+    _check(x, "x", None, _TYPES)
+    _check(dy, "dy", x.shape, (x.dtype,), x.device)
+    weight, _, kind = _norm_weights(weight, None, x)
+    mean = _dense(mean, "mean", x.shape[:-1], (torch.float32,), x.device)
+    rstd = _dense(rstd, "rstd", x.shape[:-1], (torch.float32,), x.device)
+    (rows, stride), (grad, grad_stride) = _rows(x), _rows(dy)
+    n, d = rows.shape
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    sums = torch.empty((2, d), dtype=kind, device=x.device)
+    L = load()
+    nbytes = L.ones_layer_norm_workspace_bytes(n, d)
+    scratch = _scratch(nbytes, x.device)
+    p = sums.data_ptr()
+    _call(x.device, L.ones_layer_norm_backward, grad.data_ptr(), grad_stride, rows.data_ptr(), stride, n, d, _TYPES[x.dtype],
+          _ptr(weight), _TYPES[kind], mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), p,
+          p + d * sums.element_size() if want_bias else None, _ptr(scratch), nbytes)
+    return dx, sums[0], sums[1] if want_bias else None
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = layer_norm_forward(x, weight, bias, eps)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.kinds = (weight is not None, bias.dtype if bias is not None else None)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dx, dweight, dbias = layer_norm_backward(dy, x, weight, mean, rstd, ctx.kinds[1] is not None)
+        return dx, dweight if ctx.kinds[0] else None, dbias if dbias is None else dbias.to(ctx.kinds[1]), None
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Layer norm over the last dimension, differentiable in x, weight and bias."""
+    return _LayerNorm.apply(x, weight, bias, eps)
+
+
+# ------------------------------------------------------- gated recurrence --------
+def _steps(t):
+    """(t, elements between sequences, elements between steps); copied if its channels do not lie one after another."""
+    if (t.stride(2) != 1 and t.shape[2] > 1) or min(t.stride()) < 0:
+        t = t.contiguous()
+    return t, t.stride(0), t.stride(1)
+
+
+def _recurrence_inputs(gate, x, lengths):
+    _check(x, "x", None, _TYPES)
+    if x.dim() != 3:
+        raise ValueError(f"x: [batch, steps, channels] is wanted, got {tuple(x.shape)}")
+    _check(gate, "gate", x.shape, (x.dtype,), x.device)
+    return _dense(lengths, "lengths", x.shape[:1], (torch.int32,), x.device)
+
+
+def gated_recurrence_forward(gate, x, state=None, lengths=None):
+    """ones_recurrence_forward over x [batch, steps, channels]: (h, last, carry).  state, last: float32 [batch, channels];
+    lengths: int32 [batch]; carry is what the backward call takes."""
+    lengths = _recurrence_inputs(gate, x, lengths)
+    b, t, c = x.shape
+    state = _dense(state, "state", (b, c), (torch.float32,), x.device)
+    (g, gb, gs), (u, ub, us) = _steps(gate), _steps(x)
+    L = load()
+    h = torch.empty((b, t, c), dtype=x.dtype, device=x.device)
+    last = torch.empty((b, c), dtype=torch.float32, device=x.device)
+    carry = torch.empty(L.ones_recurrence_carry_bytes(b, t, c) // 4, dtype=torch.float32, device=x.device)
+    nbytes = L.ones_recurrence_workspace_bytes(b, t, c)
+    scratch = _scratch(nbytes, x.device)
+    _call(x.device, L.ones_recurrence_forward, g.data_ptr(), gb, gs, u.data_ptr(), ub, us, b, t, c, _TYPES[x.dtype], _ptr(state),
+          _ptr(lengths), h.data_ptr(), last.data_ptr(), carry.data_ptr(), _ptr(scratch), nbytes)
+    return h, last, carry
+
+
+def gated_recurrence_backward(dh, dlast, gate, x, carry, lengths=None):
+    """ones_recurrence_backward: (dgate, dx, dstate).  dlast (of the last state, float32) may be None."""
+    lengths = _recurrence_inputs(gate, x, lengths)
+    b, t, c = x.shape
+    _check(dh, "dh", x.shape, (x.dtype,), x.device)
+    dlast = _dense(dlast, "dlast", (b, c), (torch.float32,), x.device)
+    L = load()
+    carry = _dense(carry, "carry", (L.ones_recurrence_carry_bytes(b, t, c) // 4,), (torch.float32,), x.device)
+    (g, gb, gs), (u, ub, us), (d, db, ds) = _steps(gate), _steps(x), _steps(dh)
+    dgate, dx = (torch.empty((b, t, c), dtype=x.dtype, device=x.device) for _ in range(2))
+    dstate = torch.empty((b, c), dtype=torch.float32, device=x.device)
+    nbytes = L.ones_recurrence_workspace_bytes(b, t, c)
+    scratch = _scratch(nbytes, x.device)
+    _call(x.device, L.ones_recurrence_backward, d.data_ptr(), db, ds, _ptr(dlast), g.data_ptr(), gb, gs, u.data_ptr(), ub, us, b, t, c,
+          _TYPES[x.dtype], carry.data_ptr(), _ptr(lengths), dgate.data_ptr(), dx.data_ptr(), dstate.data_ptr(), _ptr(scratch), nbytes)
+    return dgate, dx, dstate
+
+
+def gated_recurrence_step(gate, x, state):
+    """ones_recurrence_step: one step of every sequence.  gate, x [batch, channels] or [batch, 1, channels]; state (float32
+    [batch, channels], without gaps) is updated in place; returns h shaped like x."""
+    _check(x, "x", None, _TYPES)
+    if x.dim() not in (2, 3) or (x.dim() == 3 and x.shape[1] != 1):
+        raise ValueError(f"x: [batch, channels] or [batch, 1, channels] is wanted, got {tuple(x.shape)}")
+    _check(gate, "gate", x.shape, (x.dtype,), x.device)
+    b, c = x.shape[0], x.shape[-1]
+    _check(state, "state", (b, c), (torch.float32,), x.device)
+    if not state.is_contiguous():
+        raise ValueError("state: updated in place, it may have no gaps")
+    if c > 1 and (gate.stride(-1) != 1 or gate.stride(0) < 0):
+        gate = gate.contiguous()
+    if c > 1 and (x.stride(-1) != 1 or x.stride(0) < 0):
+        x = x.contiguous()
+    h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _call(x.device, load().ones_recurrence_step, gate.data_ptr(), gate.stride(0), x.data_ptr(), x.stride(0), b, c, _TYPES[x.dtype],
+          state.data_ptr(), h.data_ptr())
+    return h
+
+
+class _GatedRecurrence(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gate, x, state, lengths):
+        h, last, carry = gated_recurrence_forward(gate, x, state, lengths)
+        ctx.save_for_backward(gate, x, carry, lengths)
+        ctx.set_materialize_grads(False)
+        return h, last
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh, dlast):
+        gate, x, carry, lengths = ctx.saved_tensors
+        if dh is None:
+            dh = torch.zeros((), dtype=x.dtype, device=x.device).expand(x.shape)
+        dgate, dx, dstate = gated_recurrence_backward(dh, dlast, gate, x, carry, lengths)
+        return dgate, dx, dstate if ctx.needs_input_grad[2] else None, None
+
+
+def gated_recurrence(gate, x, state=None, lengths=None):
+    """h_t = a_t h_{t-1} + (1 - a_t) x_t with a = sigmoid(gate) over the steps of x [batch, steps, channels], differentiable in
+    gate, x and state: (h, last)."""
+    return _GatedRecurrence.apply(gate, x, state, lengths)
