@@ -35,6 +35,10 @@ extern "C" {
 #define ONES_MAX_STEPS        (1 << 30)   /* steps of a sequence                                    */
 #define ONES_MAX_CHANNELS     (1 << 24)   /* channels of a recurrence                               */
 #define ONES_MAX_BATCH        65535       /* sequences of a recurrence                              */
+#define ONES_MAX_LOSS_ROWS    (1 << 24)   /* rows of a cross entropy                                */
+#define ONES_MAX_LOSS_COLUMNS 65536
+#define ONES_MAX_VOCABULARY   (1 << 24)
+#define ONES_MAX_UPDATE_SIDE  65536       /* rows and columns of an orthogonalised update           */
 
 /* Layer norm over the columns of x[rows][cols], 1 <= cols <= ONES_MAX_NORM_COLUMNS:
  *   y = (x - mean) * rstd * weight + bias, mean and rstd = (variance + eps)^-1/2 per row (variance: the mean square of x - mean).
@@ -74,6 +78,38 @@ int ones_recurrence_backward(const void *dh, int64_t dh_batch_stride, int64_t dh
                              void *d_workspace, size_t workspace_bytes, void *hip_stream);
 int ones_recurrence_step(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride,
                          int64_t batch, int64_t channels, int32_t type, float *state, void *h, void *hip_stream);
+
+/* Softmax cross entropy of the logits x[rows][cols] weight[vocabulary][cols]^T, which are not kept:
+ *   lse_i = log sum_v exp(x_i . weight_v), loss_i = lse_i - x_i . weight_target_i.
+ * type (of x, weight, dx, dweight): ONES_F16 or ONES_BF16.  target: int64 [rows]; below 0: the row is ignored (loss 0, no
+ * gradient, and what x holds there does not matter); vocabulary or above: the row's loss, its dx and dweight are NaN.
+ * loss, lse: float [rows].  Backward: dloss float [rows], lse as forward left it; dx[rows][cols] and dweight[vocabulary][cols]
+ * are written.  It goes through the vocabulary in pieces of at most 128 MiB of logits' gradients, rounded to type.
+ * wide: not 0 if cols, both strides and both bases are multiples of 16 bytes; otherwise the workspace has room for copies.
+ * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size above its limit, or the product of two of them above 2^36),
+ * ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
+size_t ones_cross_entropy_forward_workspace_bytes(int64_t rows, int64_t cols, int64_t vocabulary, int32_t wide);
+size_t ones_cross_entropy_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t vocabulary, int32_t wide);
+int ones_cross_entropy_forward(const void *x, int64_t x_stride, const void *weight, int64_t weight_stride,
+                               int64_t rows, int64_t cols, int64_t vocabulary, int32_t type, const int64_t *target,
+                               float *loss, float *lse, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+int ones_cross_entropy_backward(const float *dloss, const void *x, int64_t x_stride, const void *weight, int64_t weight_stride,
+                                int64_t rows, int64_t cols, int64_t vocabulary, int32_t type, const int64_t *target,
+                                const float *lse, void *dx, void *dweight, void *d_workspace, size_t workspace_bytes,
+                                void *hip_stream);
+
+/* The orthogonalised update of `count` weight matrices [rows][cols] that lie one behind the other: momentum and Newton-Schulz products.
+ *   momentum = beta * momentum + grad; u = grad + beta * momentum if nesterov, else momentum; X = u / (|u| + eps), |u| the root of
+ *   the sum of squares of each matrix; `steps` times, with coefficients a, b, c: A = X X^T, X = a X + (b A + c A A) X; update = X
+ * (with X^T X for rows > cols, which gives the same).  grad_type: any; momentum: float, updated in place, or NULL (u = grad);
+ * update_type: ONES_F16 or ONES_BF16.  coefficients: HOST array of three, of size up to 16, that keep the singular values below 8
+ * (they start below 1); products have fp16 operands.  1 <= steps <= 100, 0 <= beta <= 1, eps >= 0.  A matrix of zeros gives zeros
+ * if eps > 0.  Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a side, count above 65535, a coefficient), ONES_E_WORKSPACE_TOO_SMALL,
+ * ONES_E_HIP. */
+size_t ones_orthogonal_update_workspace_bytes(int64_t count, int64_t rows, int64_t cols);
+int ones_orthogonal_update(const void *grad, float *momentum, int64_t count, int64_t rows, int64_t cols, int32_t grad_type,
+                           float beta, int32_t nesterov, int32_t steps, const float *coefficients, float eps,
+                           void *update, int32_t update_type, void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

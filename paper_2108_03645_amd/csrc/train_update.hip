@@ -1,0 +1,318 @@
+// The orthogonalised update of weight matrices (ones_orthogonal_update): momentum, then Newton-Schulz products.
+//
+//   m = beta m + g, u = g + beta m (nesterov) or m, X = u / (|u| + eps)
+//   steps times, with (a, b, c): A = X X^T, B = b A + c A^2, X = a X + B X
+//
+// X is held with the shorter side first (a tall u turned), r x q, r <= q: A is r x r.  A step is r^2 q + r^3 + 2 r^2 q operations
+// when the symmetry of A and A^2 is used: only the tiles on and below the diagonal are computed, and written to both places.
+//
+// The operands are fp16 whatever the gradient's type: X's singular values stay near 1, so the range of bf16 is not needed, and
+// three more bits keep the result of five steps within a fraction of a bf16 step (each step rounds X, A and B).  They are held
+// times 2^11 (X) and 2^10 (A, B): an element of X is at most 1.3 and typically (r q)^-1/2, of A typically r^-1 q^-1/2 off the diagonal, so
+// neither end of fp16's range is near for sides up to the limit and coefficients that keep the singular values below 8.
+//
+// The first launch updates the momentum and sums the squares of u by workgroups; the second adds those sums up in a fixed order
+// and writes X; then three products a step, the last of which writes the result in the caller's type and orientation.  All
+// matrices of a call go through each launch together.
+#include "train_host.h"
+#include "train_matmul.h"
+
+#include <algorithm>
+
+namespace ones {
+namespace train {
+namespace {
+
+constexpr float kUnitX = 2048.f, kUnitA = 1024.f;
+constexpr int kSumBlocks = 64;                // workgroups that share a matrix's sum of squares
+
+struct MomentumArgs {
+  const void *grad;
+  float *momentum;                            // null: u = g
+  float *squares;                             // [matrices][kSumBlocks]
+  int64_t size;                               // elements of a matrix
+  int32_t type, nesterov;
+  float beta;
+};
+
+// u from the momentum as it was (first) or as it is now.
+__device__ __forceinline__ float update_of(float g, float m, float beta, bool nesterov) { return nesterov ? g + beta * m : m; }
+
+template <typename T, int V>
+__global__ __launch_bounds__(256) void momentum_kernel(MomentumArgs a) {
+  __shared__ float part[4];
+  const T *grad = static_cast<const T *>(a.grad) + blockIdx.y * a.size;
+  float *momentum = a.momentum ? a.momentum + blockIdx.y * a.size : nullptr;
+  float sum = 0.f;
+  for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * V; i < a.size; i += kSumBlocks * 256ll * V) {
+    const Pack<T, V> g = load_pack<T, V>(grad + i);
+    float m[V];
+    if (momentum) {
+      const Pack<float, V> old = load_pack<float, V>(momentum + i);
+#pragma unroll
+      for (int k = 0; k < V; ++k) m[k] = a.beta * old.v[k] + static_cast<float>(g.v[k]);
+      store_pack<float, V>(momentum + i, m);
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const float f = static_cast<float>(g.v[k]), u = momentum ? update_of(f, m[k], a.beta, a.nesterov) : f;
+      sum += u * u;
+    }
+  }
+  sum = wave_sum(sum);
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) a.squares[blockIdx.y * kSumBlocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+struct NormaliseArgs {
+  MomentumArgs m;
+  f16 *x;                                     // [matrices][r][q_ld]
+  int32_t rows, cols, r, q, q_ld;             // rows > cols: turned
+  float eps;
+};
+
+// 64 x 64 elements of X a workgroup, through LDS where u is turned.  Columns up to the padded length are written as zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void normalise_kernel(NormaliseArgs a) {
+  __shared__ float tile[64][65];
+  __shared__ float unit;
+  const T *grad = static_cast<const T *>(a.m.grad) + blockIdx.z * a.m.size;
+  const float *momentum = a.m.momentum ? a.m.momentum + blockIdx.z * a.m.size : nullptr;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  if (wave == 0) {
+    const float sum = wave_sum(a.m.squares[blockIdx.z * kSumBlocks + lane]);
+    if (lane == 0) unit = kUnitX / (sqrtf(sum) + a.eps);
+  }
+  const bool turned = a.rows > a.cols;
+  const int q0 = blockIdx.x * 64, r0 = blockIdx.y * 64;                    // of X
+  const int row0 = turned ? q0 : r0, col0 = turned ? r0 : q0;              // of u
+  for (int i = wave; i < 64; i += 4) {
+    const int row = row0 + i, col = col0 + lane;
+    float u = 0.f;
+    if (row < a.rows && col < a.cols) {
+      const int64_t at = static_cast<int64_t>(row) * a.cols + col;
+      const float g = static_cast<float>(grad[at]);
+      u = momentum ? update_of(g, momentum[at], a.m.beta, a.m.nesterov) : g;
+    }
+    tile[i][lane] = u;
+  }
+  __syncthreads();
+  f16 *x = a.x + static_cast<int64_t>(blockIdx.z) * a.r * a.q_ld;
+  for (int i = wave; i < 64; i += 4) {
+    const int row = r0 + i, col = q0 + lane;
+    if (row < a.r && col < a.q_ld) x[static_cast<int64_t>(row) * a.q_ld + col] = static_cast<f16>((turned ? tile[lane][i] : tile[i][lane]) * unit);
+  }
+}
+
+struct ProductArgs {
+  const f16 *x, *a;                           // [matrices][r][q_ld], [matrices][r][r_ld]
+  f16 *to;
+  void *out;                                  // the last step's result instead, [matrices][rows][cols]
+  int32_t r, q, r_ld, q_ld, out_type, turned;
+  float one, two;                             // coefficients
+};
+
+// A = X X^T, or (POLY) B = b A + c A A.  Tiles on and below the diagonal, each written to both places.
+template <typename S, bool POLY>
+__global__ __launch_bounds__(S::threads) void symmetric_kernel(ProductArgs a) {
+  __shared__ __align__(16) unsigned char lds[S::lds];
+  static_assert(S::BM == S::BN);
+  // tile t of the lower triangle: row n, column m <= n
+  const int32_t t = static_cast<int32_t>(blockIdx.x);
+  int32_t n = static_cast<int32_t>((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+  while ((n + 1) * (n + 2) / 2 <= t) ++n;
+  while (n * (n + 1) / 2 > t) --n;
+  const int32_t m = t - n * (n + 1) / 2;
+  const f16 *from = POLY ? a.a + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld : a.x + static_cast<int64_t>(blockIdx.y) * a.r * a.q_ld;
+  const Operand o{from, POLY ? a.r_ld : a.q_ld, a.r, POLY ? a.r_ld : a.q_ld};
+  Sums<S> acc;
+  product<f16, false, false, S>(o, o, m * S::BM, n * S::BN, lds, acc);
+  f16 *to = a.to + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld;
+  const Place<S> at(m * S::BM, n * S::BN);
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j) {
+    const int32_t row = at.n + j * 16;
+    if (row >= a.r_ld) continue;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+      const int32_t c = at.m + i * 16;
+      if (c >= a.r_ld) continue;              // columns (mirrored: rows) from r to r_ld come out as zeros
+      float v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = acc[i][j][k] * (POLY ? a.two / kUnitA : kUnitA / (kUnitX * kUnitX));
+        if (POLY && row < a.r) v[k] += a.one * static_cast<float>(from[static_cast<int64_t>(row) * a.r_ld + c + k]);
+      }
+      if (row < a.r) store_pack<f16, 4>(to + static_cast<int64_t>(row) * a.r_ld + c, v);
+      if (m != n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (c + k < a.r) to[static_cast<int64_t>(c + k) * a.r_ld + row] = static_cast<f16>(v[k]);
+      }
+    }
+  }
+}
+
+// X = a X + B X.
+template <typename S>
+__global__ __launch_bounds__(S::threads) void apply_kernel(ProductArgs a) {
+  __shared__ __align__(16) unsigned char lds[S::lds];
+  const int32_t tm = (a.q + S::BM - 1) / S::BM, tn = (a.r + S::BN - 1) / S::BN;
+  int32_t m, n;
+  tile_of(static_cast<int32_t>(blockIdx.x), tm * tn, tm, tn, m, n);
+  const f16 *x = a.x + static_cast<int64_t>(blockIdx.y) * a.r * a.q_ld, *b = a.a + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld;
+  Sums<S> acc;
+  product<f16, true, false, S>(Operand{x, a.q_ld, a.q_ld, a.r}, Operand{b, a.r_ld, a.r, a.r_ld}, m * S::BM, n * S::BN, lds, acc);
+  const Place<S> at(m * S::BM, n * S::BN);
+  const int64_t size = static_cast<int64_t>(a.r) * a.q;
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j) {
+    const int32_t row = at.n + j * 16;
+    if (row >= a.r) continue;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+      const int32_t c = at.m + i * 16;
+      if (c >= a.q_ld) continue;
+      const int64_t o = static_cast<int64_t>(row) * a.q_ld + c;
+      const Pack<f16, 4> old = load_pack<f16, 4>(x + o);
+      float v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = a.one * static_cast<float>(old.v[k]) + acc[i][j][k] * (1.f / kUnitA);
+      if (!a.out) {
+        store_pack<f16, 4>(a.to + static_cast<int64_t>(blockIdx.y) * a.r * a.q_ld + o, v);
+        continue;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < a.q) {
+          const int64_t to = blockIdx.y * size + (a.turned ? static_cast<int64_t>(c + k) * a.r + row : static_cast<int64_t>(row) * a.q + c + k);
+          store_as(a.out, a.out_type, to, v[k] * (1.f / kUnitX));
+        }
+    }
+  }
+}
+
+struct UpdatePlan {
+  int64_t r, q, r_ld, q_ld;
+  size_t squares, x[2], a[2], total;
+};
+UpdatePlan update_plan(int64_t count, int64_t rows, int64_t cols) {
+  UpdatePlan p{};
+  p.r = std::min(rows, cols);
+  p.q = std::max(rows, cols);
+  p.r_ld = ceil_div(p.r, 8) * 8;
+  p.q_ld = ceil_div(p.q, 8) * 8;
+  size_t off = 0;
+  auto take = [&](int64_t bytes) { const size_t at = off; off = align_up(off + static_cast<size_t>(bytes)); return at; };
+  p.squares = take(count * kSumBlocks * 4);
+  p.x[0] = take(count * p.r * p.q_ld * 2);
+  p.x[1] = take(count * p.r * p.q_ld * 2);
+  p.a[0] = take(count * p.r * p.r_ld * 2);
+  p.a[1] = take(count * p.r * p.r_ld * 2);
+  p.total = off;
+  return p;
+}
+
+int check_update(int64_t count, int64_t rows, int64_t cols) {
+  if (count < 0 || rows < 0 || cols < 0) return ONES_E_INVALID_ARG;
+  if (count > 65535 || rows > ONES_MAX_UPDATE_SIDE || cols > ONES_MAX_UPDATE_SIDE) return ONES_E_BOUNDS;
+  return ONES_OK;
+}
+
+template <typename T>
+void launch_momentum(const MomentumArgs &a, int64_t count, hipStream_t s) {
+  const dim3 grid(kSumBlocks, static_cast<uint32_t>(count));
+  const bool wide = a.size % 4 == 0 && aligned(a.grad, 4 * sizeof(T)) && (!a.momentum || aligned(a.momentum, 16));
+  if (wide) hipLaunchKernelGGL((momentum_kernel<T, 4>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((momentum_kernel<T, 1>), grid, dim3(256), 0, s, a);
+}
+
+// Large tiles where they are enough for most compute units.
+constexpr int64_t kEnoughTiles = 160;
+
+template <bool POLY>
+void launch_symmetric(const ProductArgs &a, int64_t count, hipStream_t s) {
+  const int64_t large = ceil_div(a.r, Large::BM), small = ceil_div(a.r, Small::BM);
+  const int64_t large_tiles = large * (large + 1) / 2, small_tiles = small * (small + 1) / 2;
+  if (count * large_tiles >= kEnoughTiles)
+    hipLaunchKernelGGL((symmetric_kernel<Large, POLY>), dim3(static_cast<uint32_t>(large_tiles), static_cast<uint32_t>(count)), dim3(Large::threads), 0, s, a);
+  else
+    hipLaunchKernelGGL((symmetric_kernel<Small, POLY>), dim3(static_cast<uint32_t>(small_tiles), static_cast<uint32_t>(count)), dim3(Small::threads), 0, s, a);
+}
+void launch_apply(const ProductArgs &a, int64_t count, hipStream_t s) {
+  const int64_t large = ceil_div(a.r, Large::BN) * ceil_div(a.q, Large::BM), small = ceil_div(a.r, Small::BN) * ceil_div(a.q, Small::BM);
+  if (count * large >= kEnoughTiles)
+    hipLaunchKernelGGL((apply_kernel<Large>), dim3(static_cast<uint32_t>(large), static_cast<uint32_t>(count)), dim3(Large::threads), 0, s, a);
+  else
+    hipLaunchKernelGGL((apply_kernel<Small>), dim3(static_cast<uint32_t>(small), static_cast<uint32_t>(count)), dim3(Small::threads), 0, s, a);
+}
+
+}  // namespace
+}  // namespace train
+}  // namespace ones
+
+using namespace ones::train;
+
+extern "C" {
+
+size_t ones_orthogonal_update_workspace_bytes(int64_t count, int64_t rows, int64_t cols) {
+  if (check_update(count, rows, cols) != ONES_OK || !count || !rows || !cols) return 0;
+  return update_plan(count, rows, cols).total;
+}
+
+int ones_orthogonal_update(const void *grad, float *momentum, int64_t count, int64_t rows, int64_t cols, int32_t grad_type, float beta,
+                           int32_t nesterov, int32_t steps, const float *coefficients, float eps, void *update, int32_t update_type,
+                           void *d_workspace, size_t workspace_bytes, void *hip_stream) {
+  if (int rc = check_update(count, rows, cols)) return rc;
+  if (!is_type(grad_type) || (update_type != ONES_F16 && update_type != ONES_BF16) || steps < 1 || steps > 100 || !coefficients || !(eps >= 0.f))
+    return ONES_E_INVALID_ARG;
+  if (!(beta >= 0.f && beta <= 1.f)) return ONES_E_INVALID_ARG;
+  for (int i = 0; i < 3; ++i)
+    if (!(coefficients[i] >= -16.f && coefficients[i] <= 16.f)) return ONES_E_BOUNDS;
+  if (!count || !rows || !cols) return ONES_OK;
+  if (!grad || !update) return ONES_E_INVALID_ARG;
+  const UpdatePlan p = update_plan(count, rows, cols);
+  if (int rc = check_workspace(d_workspace, workspace_bytes, p.total)) return rc;
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  char *ws = static_cast<char *>(d_workspace);
+  f16 *x[2] = {reinterpret_cast<f16 *>(ws + p.x[0]), reinterpret_cast<f16 *>(ws + p.x[1])};
+  f16 *a[2] = {reinterpret_cast<f16 *>(ws + p.a[0]), reinterpret_cast<f16 *>(ws + p.a[1])};
+  NormaliseArgs n{};
+  n.m = MomentumArgs{grad, momentum, reinterpret_cast<float *>(ws + p.squares), rows * cols, grad_type, nesterov, beta};
+  n.x = x[0];
+  n.rows = static_cast<int32_t>(rows); n.cols = static_cast<int32_t>(cols);
+  n.r = static_cast<int32_t>(p.r); n.q = static_cast<int32_t>(p.q); n.q_ld = static_cast<int32_t>(p.q_ld);
+  n.eps = eps;
+  const dim3 grid(static_cast<uint32_t>(ceil_div(p.q_ld, 64)), static_cast<uint32_t>(ceil_div(p.r, 64)), static_cast<uint32_t>(count));
+  if (grad_type == ONES_F32) {
+    launch_momentum<float>(n.m, count, s);
+    hipLaunchKernelGGL((normalise_kernel<float>), grid, dim3(256), 0, s, n);
+  } else if (grad_type == ONES_F16) {
+    launch_momentum<f16>(n.m, count, s);
+    hipLaunchKernelGGL((normalise_kernel<f16>), grid, dim3(256), 0, s, n);
+  } else {
+    launch_momentum<bf16>(n.m, count, s);
+    hipLaunchKernelGGL((normalise_kernel<bf16>), grid, dim3(256), 0, s, n);
+  }
+  ProductArgs q{};
+  q.r = n.r; q.q = n.q; q.r_ld = static_cast<int32_t>(p.r_ld); q.q_ld = n.q_ld;
+  q.out_type = update_type;
+  q.turned = rows > cols;
+  for (int32_t step = 0; step < steps; ++step) {
+    q.x = x[step & 1];
+    q.to = a[0];
+    launch_symmetric<false>(q, count, s);
+    q.a = a[0];
+    q.to = a[1];
+    q.one = coefficients[1]; q.two = coefficients[2];
+    launch_symmetric<true>(q, count, s);
+    q.a = a[1];
+    q.to = x[(step & 1) ^ 1];
+    q.out = step + 1 == steps ? update : nullptr;
+    q.one = coefficients[0];
+    launch_apply(q, count, s);
+  }
+  return launched("orthogonal update");
+}
+
+}  // extern "C"

@@ -16,7 +16,9 @@ from .ones import OnesError  # noqa: F401
 
 EXPORTS = ["ones_layer_norm_forward", "ones_layer_norm_workspace_bytes", "ones_layer_norm_backward",
            "ones_recurrence_carry_bytes", "ones_recurrence_workspace_bytes", "ones_recurrence_forward",
-           "ones_recurrence_backward", "ones_recurrence_step"]
+           "ones_recurrence_backward", "ones_recurrence_step", "ones_cross_entropy_forward_workspace_bytes",
+           "ones_cross_entropy_backward_workspace_bytes", "ones_cross_entropy_forward", "ones_cross_entropy_backward",
+           "ones_orthogonal_update_workspace_bytes", "ones_orthogonal_update"]
 
 _P, _I64, _I32, _F32, _SIZE = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_size_t
 _ARGUMENTS = {
@@ -29,6 +31,12 @@ _ARGUMENTS = {
     "ones_recurrence_backward": [_P, _I64, _I64, _P, _P, _I64, _I64, _P, _I64, _I64, _I64, _I64, _I64, _I32, _P, _P, _P, _P, _P,
                                  _P, _SIZE, _P],
     "ones_recurrence_step": [_P, _I64, _P, _I64, _I64, _I64, _I32, _P, _P, _P],
+    "ones_cross_entropy_forward_workspace_bytes": [_I64, _I64, _I64, _I32],
+    "ones_cross_entropy_backward_workspace_bytes": [_I64, _I64, _I64, _I32],
+    "ones_cross_entropy_forward": [_P, _I64, _P, _I64, _I64, _I64, _I64, _I32, _P, _P, _P, _P, _SIZE, _P],
+    "ones_cross_entropy_backward": [_P, _P, _I64, _P, _I64, _I64, _I64, _I64, _I32, _P, _P, _P, _P, _P, _SIZE, _P],
+    "ones_orthogonal_update_workspace_bytes": [_I64, _I64, _I64],
+    "ones_orthogonal_update": [_P, _P, _I64, _I64, _I64, _I32, _F32, _I32, _I32, _P, _F32, _P, _I32, _P, _SIZE, _P],
 }
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _lib = None
@@ -49,11 +57,12 @@ def load():
 
 def _call(device, function, *args):
     """A call of the library with the tensors' device current (it mostly is already), on its current stream."""
+    stream = torch._C._cuda_getCurrentRawStream(device.index)     # current_stream(device).cuda_stream, at a thirtieth of its time
     if torch.cuda.current_device() == device.index:
-        rc = function(*args, torch.cuda.current_stream().cuda_stream)
+        rc = function(*args, stream)
     else:
         with torch.cuda.device(device):
-            rc = function(*args, torch.cuda.current_stream().cuda_stream)
+            rc = function(*args, stream)
     if rc:
         raise OnesError(rc, _lib.ones_strerror(rc).decode())
 
@@ -261,3 +270,98 @@ def gated_recurrence(gate, x, state=None, lengths=None):
     """h_t = a_t h_{t-1} + (1 - a_t) x_t with a = sigmoid(gate) over the steps of x [batch, steps, channels], differentiable in
     gate, x and state: (h, last)."""
     return _GatedRecurrence.apply(gate, x, state, lengths)
+
+
+# ------------------------------------------- cross entropy over a vocabulary --------
+_HALVES = (torch.bfloat16, torch.float16)
+
+
+def _loss_inputs(x, weight, target):
+    _check(x, "x", None, _HALVES)
+    _check(weight, "weight", None, (x.dtype,), x.device)
+    if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[1]:
+        raise ValueError(f"x [rows, cols] and weight [vocabulary, cols] are wanted, got {tuple(x.shape)} and {tuple(weight.shape)}")
+    _check(target, "target", x.shape[:1], (torch.int64, torch.int32), x.device)
+    (x, x_stride), (weight, w_stride) = _rows(x), _rows(weight)
+    wide = not (x.shape[1] % 8 or x_stride % 8 or w_stride % 8 or x.data_ptr() % 16 or weight.data_ptr() % 16)
+    return x, x_stride, weight, w_stride, target.long().contiguous(), wide
+
+
+def linear_cross_entropy_forward(x, weight, target):
+    """ones_cross_entropy_forward: (loss, lse), float32 per row of x [rows, cols], for logits x weight^T over weight
+    [vocabulary, cols].  Rows with a target below 0 have no loss."""
+    x, x_stride, weight, w_stride, target, wide = _loss_inputs(x, weight, target)
+    (n, d), v = x.shape, weight.shape[0]
+    L = load()
+    out = torch.empty((2, n), dtype=torch.float32, device=x.device)
+    nbytes = L.ones_cross_entropy_forward_workspace_bytes(n, d, v, wide)
+    scratch = _scratch(nbytes, x.device)
+    p = out.data_ptr()
+    _call(x.device, L.ones_cross_entropy_forward, x.data_ptr(), x_stride, weight.data_ptr(), w_stride, n, d, v, _TYPES[x.dtype],
+          target.data_ptr(), p, p + 4 * n, _ptr(scratch), nbytes)
+    return out[0], out[1]
+
+
+def linear_cross_entropy_backward(dloss, x, weight, target, lse):
+    """ones_cross_entropy_backward: (dx, dweight) for the gradient dloss (float32) of every row's loss."""
+    x, x_stride, weight, w_stride, target, wide = _loss_inputs(x, weight, target)
+    (n, d), v = x.shape, weight.shape[0]
+    dloss = _dense(dloss, "dloss", (n,), (torch.float32,), x.device)
+    lse = _dense(lse, "lse", (n,), (torch.float32,), x.device)
+    L = load()
+    dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    dweight = torch.empty((v, d), dtype=x.dtype, device=x.device)
+    nbytes = L.ones_cross_entropy_backward_workspace_bytes(n, d, v, wide)
+    scratch = _scratch(nbytes, x.device)
+    _call(x.device, L.ones_cross_entropy_backward, dloss.data_ptr(), x.data_ptr(), x_stride, weight.data_ptr(), w_stride, n, d, v,
+          _TYPES[x.dtype], target.data_ptr(), lse.data_ptr(), dx.data_ptr(), dweight.data_ptr(), _ptr(scratch), nbytes)
+    return dx, dweight
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, target):
+        loss, lse = linear_cross_entropy_forward(x, weight, target)
+        ctx.save_for_backward(x, weight, target, lse)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        return *linear_cross_entropy_backward(dloss, *ctx.saved_tensors), None
+
+
+def linear_cross_entropy(x, weight, target):
+    """The loss of every row under autograd: the mean over the rows that count is ``loss.sum() / (target >= 0).sum()``."""
+    return _LinearCrossEntropy.apply(x, weight, target)
+
+
+# --------------------------------------------------- orthogonalised update --------
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)      # singular values from 0.01 to 1 end between 0.7 and 1.2 after five steps
+
+
+def orthogonal_update(grad, momentum=None, beta=0.95, nesterov=True, steps=5, coefficients=COEFFICIENTS, eps=1e-7, dtype=None):
+    """ones_orthogonal_update: the update for weights whose gradient is grad [rows, cols] or [count, rows, cols], all matrices of
+    one call together.  momentum (float32, shaped like grad, without gaps) is updated in place; without one grad itself is
+    orthogonalised.  dtype: of the result, bfloat16 or float16 (default: grad's, bfloat16 for float32)."""
+    _check(grad, "grad", None, _TYPES)
+    if grad.dim() not in (2, 3):
+        raise ValueError(f"grad: [rows, cols] or [count, rows, cols] is wanted, got {tuple(grad.shape)}")
+    if momentum is not None:
+        _check(momentum, "momentum", grad.shape, (torch.float32,), grad.device)
+        if not momentum.is_contiguous():
+            raise ValueError("momentum: updated in place, it may have no gaps")
+    dtype = dtype or (grad.dtype if grad.dtype in _HALVES else torch.bfloat16)
+    if dtype not in _HALVES:
+        raise TypeError(f"dtype: {dtype} is not bfloat16 or float16")
+    if len(coefficients) != 3:
+        raise ValueError("coefficients: three numbers are wanted")
+    grad = grad.contiguous()
+    count, (m, n) = (1 if grad.dim() == 2 else grad.shape[0]), grad.shape[-2:]
+    update = torch.empty(grad.shape, dtype=dtype, device=grad.device)
+    L = load()
+    nbytes = L.ones_orthogonal_update_workspace_bytes(count, m, n)
+    scratch = _scratch(nbytes, grad.device)
+    _call(grad.device, L.ones_orthogonal_update, grad.data_ptr(), _ptr(momentum), count, m, n, _TYPES[grad.dtype], beta, int(nesterov),
+          steps, (C.c_float * 3)(*coefficients), eps, update.data_ptr(), _TYPES[dtype], _ptr(scratch), nbytes)
+    return update
