@@ -8,7 +8,8 @@
 // largest logit of a wave's part of the vocabulary and the sum of exponentials below it; a small second launch joins them.
 // Backward goes through the vocabulary in pieces: one launch forms G of a piece, rounded to 16 bits (the operands' type, as
 // a product of that type needs), and one launch its dW and what it adds to dx, which is summed in 32 bits over the pieces.
-// A piece's G has at most 128 MiB, half of the last-level cache, so that the two products that read it mostly find it there.
+// A piece's G, with the sums of products whose k is split, has at most 128 MiB, half of the last-level cache, so that the two
+// products that read it mostly find it there.
 //
 // G is held in units of the largest |dloss| over 2^14 and the products are scaled back in 32 bits.  fp16 would lose small
 // probabilities times small dloss otherwise; and where all dloss are equal, as in a mean, the target's entry comes to
@@ -26,6 +27,7 @@ namespace train {
 namespace {
 
 constexpr int64_t kPieceBytes = 128 << 20;
+constexpr float kLog2E = 1.44269504f;
 
 struct Part { float top, sum; };              // of some logits of a row: the largest, and the sum of exp(z - top)
 
@@ -40,93 +42,120 @@ struct LossArgs {
   int64_t g_ld;
 };
 
-// One tile of logits.  GRADIENT: writes G; otherwise what the loss needs of it.
+// Tiles of logits.  GRADIENT: writes G; otherwise what the loss needs of it.  A workgroup takes tiles in turn and has the next one's
+// first operands on their way while it deals with one's logits.
 template <typename T, typename S, bool GRADIENT>
-__global__ __launch_bounds__(S::threads) void logits_kernel(LossArgs a) {
+__global__ __launch_bounds__(S::threads, S::resident) void logits_kernel(LossArgs a) {
   __shared__ __align__(16) unsigned char lds[S::lds];
-  const int32_t tm = (a.w.extent + S::BM - 1) / S::BM, tn = (a.x.extent + S::BN - 1) / S::BN;
-  int32_t m, n;
-  tile_of(static_cast<int32_t>(blockIdx.x), tm * tn, tm, tn, m, n);
-  const int part = m * S::WM + static_cast<int>(threadIdx.x) / kWave / S::WN;
+  const int32_t tm = (a.w.extent + S::BM - 1) / S::BM, tn = (a.x.extent + S::BN - 1) / S::BN, tiles = tm * tn;
+  int32_t id = static_cast<int32_t>(blockIdx.x), m, n;
+  Product<T, false, false, S> product;
   Sums<S> acc;
-  product<T, false, false, S>(a.w, a.x, m * S::BM, n * S::BN, lds, acc);
-  const Place<S> at(m * S::BM, n * S::BN);
+  tile_of(id, tiles, tm, tn, m, n);
+  product.begin(a.w, a.x, m * S::BM, n * S::BN, 0, a.w.k, lds);
+  const float unit = GRADIENT ? a.scale[0] : 0.f;
+  for (;;) {
+    const Place<S> at(m * S::BM, n * S::BN);
+    const int part = m * S::WM + static_cast<int>(threadIdx.x) / kWave / S::WN;
+    const bool ragged = (m + 1) * S::BM > a.w.extent;
+    // what a row's logits meet: 16 i + r of the target, if that is in this run; -1: not here, -2: ignored (G is 0), -3: beyond the
+    // vocabulary (G is NaN); and backward the row's lse and dloss
+    int32_t hit[S::TN];
+    float lse[S::TN], weight[S::TN];
 #pragma unroll
-  for (int j = 0; j < S::TN; ++j) {
-    const int32_t row = at.n + j * 16;
-    const bool inside = row < a.x.extent;
-    const int64_t target = inside ? a.target[row] : -1;
-    const int32_t hit = target >= 0 && target < a.vocabulary ? static_cast<int32_t>(target) - a.v0 - at.m : -1;   // 16 i + r, if in this run
-    if constexpr (GRADIENT) {
-      if (!inside) continue;
-      const float lse = a.lse[row];
-      const float weight = target < 0 ? 0.f : target >= a.vocabulary ? __builtin_nanf("") : a.dloss[row] * a.scale[0];
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i) {
-        const int32_t v = at.m + i * 16;
-        float g[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = __expf(acc[i][j][r] - lse) - (hit == i * 16 + r ? 1.f : 0.f);
-          g[r] = target < 0 || v + r >= a.w.extent ? 0.f : p * weight;
-        }
-        store_pack<T, 4>(static_cast<T *>(a.g) + row * a.g_ld + v, g);
+    for (int j = 0; j < S::TN; ++j) {
+      const int32_t row = at.n + j * 16;
+      const int64_t target = row < a.x.extent ? a.target[row] : -1;
+      const int32_t in = target >= 0 && target < a.vocabulary ? static_cast<int32_t>(target) - a.v0 - at.m : -1;
+      hit[j] = target < 0 ? -2 : target >= a.vocabulary ? -3 : in >= 0 && in < S::TM * 16 && in % 16 < 4 ? in : -1;
+      if (GRADIENT) {
+        lse[j] = row < a.x.extent ? a.lse[row] : 0.f;
+        weight[j] = row < a.x.extent ? a.dloss[row] * unit : 0.f;
       }
-    } else {
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (hit == i * 16 + r) a.at_target[row] = acc[i][j][r];
-          if (at.m + i * 16 + r >= a.w.extent) acc[i][j][r] = -INFINITY;
-          top = fmaxf(top, acc[i][j][r]);
-        }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float base = top == -INFINITY ? 0.f : top;
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sum += __expf(acc[i][j][r] - base);
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      if (inside && threadIdx.x % kWave < 16) a.parts[static_cast<int64_t>(part) * a.x.extent + row] = Part{top, sum};
     }
+    product.run(lds, acc);
+    id += static_cast<int32_t>(gridDim.x);
+    if (id < tiles) {
+      tile_of(id, tiles, tm, tn, m, n);
+      product.begin(a.w, a.x, m * S::BM, n * S::BN, 0, a.w.k, lds);
+    }
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int32_t row = at.n + j * 16;
+      const bool inside = row < a.x.extent, hits = __any(hit[j] >= 0);      // one of 16 rows, in a few tiles
+      if constexpr (GRADIENT) {
+        if (!inside) continue;
+        const float factor = hit[j] == -3 ? __builtin_nanf("") : weight[j];
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i) {
+          const int32_t v = at.m + i * 16;
+          float g[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse[j]) * kLog2E);
+            if (hits) p -= hit[j] == i * 16 + r ? 1.f : 0.f;
+            g[r] = hit[j] == -2 || (ragged && v + r >= a.w.extent) ? 0.f : p * factor;
+          }
+          store_pack<T, 4>(static_cast<T *>(a.g) + row * a.g_ld + v, g);
+        }
+      } else {
+        if (hits) {
+          float of_target = 0.f;
+#pragma unroll
+          for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) of_target = hit[j] == i * 16 + r ? acc[i][j][r] : of_target;
+          if (hit[j] >= 0) a.at_target[row] = of_target;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (ragged && at.m + i * 16 + r >= a.w.extent) acc[i][j][r] = -INFINITY;
+            top = fmaxf(top, acc[i][j][r]);
+          }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = top == -INFINITY ? 0.f : top * -kLog2E;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2E, base));
+        // top in units of log 2 was rounded: by the same factor in every term
+        sum *= __builtin_amdgcn_exp2f(-__builtin_fmaf(top == -INFINITY ? 0.f : top, kLog2E, base));
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (inside && threadIdx.x % kWave < 16) a.parts[static_cast<int64_t>(part) * a.x.extent + row] = Part{top, sum};
+      }
+    }
+    if (id >= tiles) return;
   }
 }
 
-// The parts of every row joined: 64 rows a workgroup, four threads a row.
-__global__ __launch_bounds__(256) void join_kernel(const Part *parts, int32_t n_parts, int32_t rows, int32_t vocabulary, const int64_t *target,
-                                                   const float *at_target, float *loss, float *lse) {
-  __shared__ Part shared[3][64];
+// The parts of every row joined: 64 rows a workgroup, sixteen threads a row.
+constexpr int kShares = 16;
+__device__ __forceinline__ void join(float &top, float &sum, const Part &one) {
+  const float both = fmaxf(top, one.top);     // skips NaN; the sum has it then
+  sum = both == -INFINITY ? sum + one.sum : sum * __expf(top - both) + one.sum * __expf(one.top - both);
+  top = both;
+}
+__global__ __launch_bounds__(64 * kShares) void join_kernel(const Part *parts, int32_t n_parts, int32_t rows, int32_t vocabulary,
+                                                            const int64_t *target, const float *at_target, float *loss, float *lse) {
+  __shared__ Part shared[kShares][64];
   const int lane = threadIdx.x % 64, share = threadIdx.x / 64;
   const int32_t row = blockIdx.x * 64 + lane;
   float top = -INFINITY, sum = 0.f;
-  bool nan = false;
   if (row < rows) {
 #pragma unroll 4
-    for (int p = share; p < n_parts; p += 4) {
-      const Part one = parts[static_cast<int64_t>(p) * rows + row];
-      const float both = fmaxf(top, one.top);
-      nan |= one.sum != one.sum;              // a maximum skips NaN, a sum does not
-      if (both == -INFINITY) continue;
-      sum = sum * __expf(top - both) + one.sum * __expf(one.top - both);
-      top = both;
-    }
+    for (int p = share; p < n_parts; p += kShares) join(top, sum, parts[static_cast<int64_t>(p) * rows + row]);
   }
-  if (nan) sum = __builtin_nanf("");
-  if (share) shared[share - 1][lane] = Part{top, sum};
+  shared[share][lane] = Part{top, sum};
   __syncthreads();
   if (share || row >= rows) return;
 #pragma unroll
-  for (int s = 0; s < 3; ++s) {
-    const Part one = shared[s][lane];
-    const float both = fmaxf(top, one.top);
-    sum = both == -INFINITY ? sum + one.sum : sum * __expf(top - both) + one.sum * __expf(one.top - both);
-    top = both;
-  }
+  for (int s = 1; s < kShares; ++s) join(top, sum, shared[s][lane]);
   const float all = top + logf(sum);
   const int64_t t = target[row];
   lse[row] = all;
@@ -148,8 +177,12 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
   if (a.scale && blockIdx.x == gridDim.x - 1) {
     __shared__ float part[4];
     float most = 0.f;
-    for (int32_t i = threadIdx.x; i < a.rows[0]; i += 256)
-      if (a.target[i] >= 0) most = fmaxf(most, fabsf(a.dloss[i]));
+#pragma unroll 8
+    for (int32_t i = threadIdx.x; i < a.rows[0]; i += 256) {
+      const int64_t t = a.target[i];
+      const float d = fabsf(a.dloss[i]);
+      most = t >= 0 ? fmaxf(most, d) : most;
+    }
 #pragma unroll
     for (int m = 1; m < kWave; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = most;
@@ -184,39 +217,48 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
   }
 }
 
-struct GradientArgs {
-  Operand w_turned, g, x_turned, g_turned;
-  const int64_t *target;
-  const float *scale;
-  float *sum;                                 // dx over the pieces so far, [rows][cols]
-  void *dx, *dweight;                         // dweight: of the piece's first word
-  int32_t cols, first, last;
+// A product whose k is shared among `splits` workgroups a tile, `k_each` (a multiple of 64) each.
+struct Split {
+  int32_t splits, k_each;
 };
 
-// The tiles of dx first, then those of a piece's dW.
+struct GradientArgs {
+  Operand w_turned, g, x_turned, g_turned;
+  Split of_dx, of_dw;
+  const int64_t *target;
+  const float *scale;
+  float *dx_sum, *dw_sum;                     // [splits][rows][cols], [splits][words][cols]
+  void *dx, *dweight;                         // dweight: of the piece's first word
+  int32_t cols, first, last, wide;            // wide: runs of four of dx and dW can be written at once
+};
+
+// The tiles of dx first, then those of a piece's dW.  dx is added up over the pieces in 32 bits, in as many places as k is split;
+// a product in one part that is complete is rounded and written.
 template <typename T, typename S>
-__global__ __launch_bounds__(S::threads) void gradients_kernel(GradientArgs a) {
+__global__ __launch_bounds__(S::threads, S::resident) void gradients_kernel(GradientArgs a) {
   __shared__ __align__(16) unsigned char lds[S::lds];
-  const int32_t tm = (a.cols + S::BM - 1) / S::BM, of_dx = tm * ((a.g.extent + S::BN - 1) / S::BN);
-  const float back = a.scale[1];
-  const bool wide = a.cols % 4 == 0;
-  const int32_t id = static_cast<int32_t>(blockIdx.x);
+  const int32_t tm = (a.cols + S::BM - 1) / S::BM, dx_tiles = tm * ((a.g.extent + S::BN - 1) / S::BN);
+  const int32_t dw_tiles = tm * ((a.g_turned.extent + S::BN - 1) / S::BN);
+  const bool of_dx = static_cast<int32_t>(blockIdx.x) < dx_tiles * a.of_dx.splits;
+  const int32_t id = static_cast<int32_t>(blockIdx.x) - (of_dx ? 0 : dx_tiles * a.of_dx.splits), tiles = of_dx ? dx_tiles : dw_tiles;
+  const Split split = of_dx ? a.of_dx : a.of_dw;
+  const int32_t part = id / tiles, k0 = part * split.k_each;
   Sums<S> acc;
   int32_t m, n;
-  if (id < of_dx) {
-    tile_of(id, of_dx, tm, of_dx / tm, m, n);
-    product<T, true, false, S>(a.w_turned, a.g, m * S::BM, n * S::BN, lds, acc);
-  } else {
-    const int32_t of_dw = static_cast<int32_t>(gridDim.x) - of_dx;
-    tile_of(id - of_dx, of_dw, tm, of_dw / tm, m, n);
-    product<T, true, true, S>(a.x_turned, a.g_turned, m * S::BM, n * S::BN, lds, acc);
-  }
+  tile_of(id - part * tiles, tiles, tm, tiles / tm, m, n);
+  if (of_dx) product<T, true, false, S>(a.w_turned, a.g, m * S::BM, n * S::BN, k0, min(a.g.k, k0 + split.k_each), lds, acc);
+  else product<T, true, true, S>(a.x_turned, a.g_turned, m * S::BM, n * S::BN, k0, min(a.g_turned.k, k0 + split.k_each), lds, acc);
   const Place<S> at(m * S::BM, n * S::BN);
+  const bool wide = a.wide, whole = split.splits == 1 && (!of_dx || a.last), adds = of_dx && !a.first;
+  const int32_t rows = of_dx ? a.g.extent : a.g_turned.extent;
+  const float back = whole ? a.scale[1] : 1.f;
+  float *sum = (of_dx ? a.dx_sum : a.dw_sum) + static_cast<int64_t>(part) * rows * a.cols;
+  T *to = static_cast<T *>(of_dx ? a.dx : a.dweight);
 #pragma unroll
   for (int j = 0; j < S::TN; ++j) {
     const int32_t row = at.n + j * 16;
-    if (row >= (id < of_dx ? a.g.extent : a.g_turned.extent)) continue;
-    const bool ignored = id < of_dx && a.target[row] < 0;
+    if (row >= rows) continue;
+    const bool ignored = whole && of_dx && a.target[row] < 0;
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
       const int32_t c = at.m + i * 16;
@@ -225,47 +267,124 @@ __global__ __launch_bounds__(S::threads) void gradients_kernel(GradientArgs a) {
       float v[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r];
-      if (id < of_dx && !a.first) {
+      if (adds) {
+        if (wide) {
+          const Pack<float, 4> old = load_pack<float, 4>(sum + o);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) if (c + r < a.cols) v[r] += a.sum[o + r];
+          for (int r = 0; r < 4; ++r) v[r] += old.v[r];
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) if (c + r < a.cols) v[r] += sum[o + r];
+        }
       }
-      if (id < of_dx && !a.last) {
-        if (wide) store_pack<float, 4>(a.sum + o, v);
+      if (whole) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = ignored ? 0.f : v[r] * back;
+        if (wide) store_pack<T, 4>(to + o, v);
         else
 #pragma unroll
-          for (int r = 0; r < 4; ++r) if (c + r < a.cols) a.sum[o + r] = v[r];
-        continue;
+          for (int r = 0; r < 4; ++r) if (c + r < a.cols) to[o + r] = static_cast<T>(v[r]);
+      } else {
+        if (wide) store_pack<float, 4>(sum + o, v);
+        else
+#pragma unroll
+          for (int r = 0; r < 4; ++r) if (c + r < a.cols) sum[o + r] = v[r];
       }
-      T *to = static_cast<T *>(id < of_dx ? a.dx : a.dweight) + o;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = ignored ? 0.f : v[r] * back;
-      if (wide) store_pack<T, 4>(to, v);
-      else
-#pragma unroll
-        for (int r = 0; r < 4; ++r) if (c + r < a.cols) to[r] = static_cast<T>(v[r]);
     }
   }
 }
 
-// Large tiles where they are enough for most compute units, else small ones (four times as many, two a compute unit).
-constexpr int64_t kEnoughTiles = 160;
-bool large_tiles(int64_t m, int64_t n) { return ceil_div(m, Large::BM) * ceil_div(n, Large::BN) >= kEnoughTiles; }
+// The parts of products that were split, added up in order and rounded: dx after the last piece, and the piece's dW.
+struct FinishArgs {
+  const float *sum[2];
+  void *to[2];
+  int64_t size[2];                            // elements; 0: not split
+  int32_t splits[2], cols, wide;
+  const int64_t *target;                      // of the rows of dx
+  const float *scale;
+};
+template <typename T, int V>
+__global__ __launch_bounds__(256) void finish_kernel(FinishArgs a) {
+  int64_t i = (blockIdx.x * 256ll + threadIdx.x) * V;
+  const int which = i >= a.size[0];
+  if (which) i -= a.size[0];
+  if (i >= a.size[which]) return;
+  const float *sum = a.sum[which] + i;
+  float v[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < a.splits[which]; ++s, sum += a.size[which]) {
+    const Pack<float, V> one = load_pack<float, V>(sum);
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] += one.v[k];
+  }
+  const bool ignored = !which && a.target[i / a.cols] < 0;
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = ignored ? 0.f : v[k] * a.scale[1];
+  store_pack<T, V>(static_cast<T *>(a.to[which]) + i, v);
+}
+
+// Which tiles, and into how many parts k is split: by an estimate of the time in microseconds.  A round of workgroups (one a compute
+// unit with large tiles, else two) takes so long for 64 k, and so long for its start and its end.
+struct Cost { int64_t bm, bn, places; double per_64, fixed; };
+constexpr Cost kCosts[] = {{Large::BM, Large::BN, 256, 1.5, 8.0}, {Small::BM, Small::BN, 512, 1.2, 4.0}};
+enum Tiles { kLarge, kSmall };
+
+double logits_time(const Cost &c, int64_t m, int64_t n, int64_t k) {
+  return ceil_div(ceil_div(m, c.bm) * ceil_div(n, c.bn), c.places) * (ceil_div(k, 64) * c.per_64 + c.fixed);
+}
+Tiles logits_tiles(int64_t m, int64_t n, int64_t k) {
+  return logits_time(kCosts[kSmall], m, n, k) < logits_time(kCosts[kLarge], m, n, k) ? kSmall : kLarge;
+}
+
+Split split_of(int64_t k, int64_t most) {
+  const int64_t splits = std::max<int64_t>(1, ceil_div(k, most)), each = std::max<int64_t>(64, ceil_div(ceil_div(k, splits), 64) * 64);
+  return Split{static_cast<int32_t>(std::max<int64_t>(1, ceil_div(k, each))), static_cast<int32_t>(each)};
+}
+
+struct GradientPlan { Tiles tiles; Split of_dx, of_dw; };
+GradientPlan gradient_plan(int64_t rows, int64_t cols, int64_t words) {
+  GradientPlan best{};
+  double best_time = INFINITY;
+  for (Tiles t : {kLarge, kSmall}) {
+    const Cost &c = kCosts[t];
+    const int64_t tm = ceil_div(cols, c.bm), dx = tm * ceil_div(rows, c.bn), dw = tm * ceil_div(words, c.bn);
+    for (int64_t most = std::max<int64_t>(128, ceil_div(std::max(rows, words), 64) * 64); most >= 128; most /= 2) {
+      const GradientPlan p{t, split_of(words, most), split_of(rows, most)};
+      if (p.of_dx.splits > 32 || p.of_dw.splits > 32) break;
+      const int64_t longest = std::max(p.of_dx.k_each, p.of_dw.k_each), items = dx * p.of_dx.splits + dw * p.of_dw.splits;
+      // items of the shorter product make room for others: a round counts by the work in it
+      const double work = (dx * p.of_dx.splits * (p.of_dx.k_each / 64.0 * c.per_64 + c.fixed) + dw * p.of_dw.splits * (p.of_dw.k_each / 64.0 * c.per_64 + c.fixed)) / c.places;
+      double time = std::max(work, longest / 64.0 * c.per_64 + c.fixed);
+      if (items > c.places) time = std::max(time, work * ceil_div(items, c.places) * c.places / items);
+      double bytes = 0;                       // written and read again
+      if (p.of_dx.splits > 1) bytes += 8.0 * p.of_dx.splits * rows * cols;
+      if (p.of_dw.splits > 1) bytes += 8.0 * p.of_dw.splits * words * cols;
+      if (bytes > 0) time += 4.0 + bytes / 4e6;
+      if (time < best_time) { best = p; best_time = time; }
+    }
+  }
+  return best;
+}
 
 struct LossPlan {
   int64_t cols8, parts, piece, pieces;
-  bool large_logits, large_g, large_gradients;
+  Tiles logits, logits_piece;
+  GradientPlan gradients;
   size_t x, w, part, at_target, forward;                       // offsets, and the bytes of the forward pass
-  size_t g, sum, scale, backward;
+  size_t g, dx_sum, dw_sum, scale, backward;
 };
 
 LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool copies_x, bool copies_w) {
   LossPlan p{};
   p.cols8 = ceil_div(cols, 8) * 8;
-  p.large_logits = large_tiles(vocabulary, rows);
-  p.parts = p.large_logits ? ceil_div(vocabulary, Large::BM) * Large::WM : ceil_div(vocabulary, Small::BM) * Small::WM;
+  p.logits = logits_tiles(vocabulary, rows, cols);
+  static_assert(Large::WM == 2 && Small::WM == 2);
+  p.parts = ceil_div(vocabulary, kCosts[p.logits].bm) * 2;
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes); return at; };
-  const size_t n = static_cast<size_t>(rows), d8 = static_cast<size_t>(p.cols8);
+  const size_t n = static_cast<size_t>(rows), d = static_cast<size_t>(cols), d8 = static_cast<size_t>(p.cols8);
   p.x = take(copies_x ? n * d8 * 2 : 0);
   p.w = take(copies_w ? static_cast<size_t>(vocabulary) * d8 * 2 : 0);
   const size_t packed = off;
@@ -273,13 +392,18 @@ LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool copies_x
   p.at_target = take(n * 4);
   p.forward = off;
   off = packed;
-  p.pieces = std::max<int64_t>(1, ceil_div(rows * ceil_div(vocabulary, 256) * 256 * 2, kPieceBytes));
-  p.piece = ceil_div(ceil_div(vocabulary, p.pieces), 256) * 256;
+  for (p.pieces = std::max<int64_t>(1, ceil_div(rows * ceil_div(vocabulary, 256) * 512, kPieceBytes));; ++p.pieces) {
+    p.piece = ceil_div(ceil_div(vocabulary, p.pieces), 256) * 256;
+    p.gradients = gradient_plan(rows, cols, std::min(p.piece, vocabulary));
+    const Split dx = p.gradients.of_dx, dw = p.gradients.of_dw;
+    const int64_t sums = ((dx.splits - 1) * rows + (dw.splits > 1 ? dw.splits * p.piece : 0)) * cols * 4;
+    if (p.piece == 256 || rows * p.piece * 2 + sums <= kPieceBytes) break;
+  }
   p.pieces = ceil_div(vocabulary, p.piece);
-  p.large_g = large_tiles(p.piece, rows);
-  p.large_gradients = ceil_div(cols, Large::BM) * (ceil_div(rows, Large::BN) + ceil_div(p.piece, Large::BN)) >= kEnoughTiles;
+  p.logits_piece = logits_tiles(p.piece, rows, cols);
   p.g = take(n * static_cast<size_t>(p.piece) * 2);
-  p.sum = take(p.pieces > 1 ? n * static_cast<size_t>(cols) * 4 : 0);
+  p.dx_sum = take(p.pieces > 1 || p.gradients.of_dx.splits > 1 ? p.gradients.of_dx.splits * n * d * 4 : 0);
+  p.dw_sum = take(p.gradients.of_dw.splits > 1 ? static_cast<size_t>(p.gradients.of_dw.splits) * std::min(p.piece, vocabulary) * d * 4 : 0);
   p.scale = take(8);
   p.backward = off;
   return p;
@@ -306,22 +430,48 @@ void launch_pack(const PackArgs &a, hipStream_t s) {
 
 template <typename T, typename S, bool GRADIENT>
 void launch_logits(const LossArgs &a, hipStream_t s) {
-  const int64_t blocks = ceil_div(a.w.extent, S::BM) * ceil_div(a.x.extent, S::BN);
+  const int64_t tiles = ceil_div(a.w.extent, S::BM) * ceil_div(a.x.extent, S::BN), blocks = std::min<int64_t>(tiles, 256 * S::resident);
   hipLaunchKernelGGL((logits_kernel<T, S, GRADIENT>), dim3(static_cast<uint32_t>(blocks)), dim3(S::threads), 0, s, a);
 }
-template <bool GRADIENT>
-void launch_logits(const LossArgs &a, int32_t type, bool large, hipStream_t s) {
-  if (type == ONES_F16) large ? launch_logits<f16, Large, GRADIENT>(a, s) : launch_logits<f16, Small, GRADIENT>(a, s);
-  else large ? launch_logits<bf16, Large, GRADIENT>(a, s) : launch_logits<bf16, Small, GRADIENT>(a, s);
+template <typename T, bool GRADIENT>
+void launch_logits(const LossArgs &a, Tiles tiles, hipStream_t s) {
+  if (tiles == kLarge) launch_logits<T, Large, GRADIENT>(a, s);
+  else launch_logits<T, Small, GRADIENT>(a, s);
 }
 template <typename T, typename S>
 void launch_gradients(const GradientArgs &a, hipStream_t s) {
-  const int64_t blocks = ceil_div(a.cols, S::BM) * (ceil_div(a.g.extent, S::BN) + ceil_div(a.g_turned.extent, S::BN));
+  const int64_t blocks = ceil_div(a.cols, S::BM) * (ceil_div(a.g.extent, S::BN) * a.of_dx.splits + ceil_div(a.g_turned.extent, S::BN) * a.of_dw.splits);
   hipLaunchKernelGGL((gradients_kernel<T, S>), dim3(static_cast<uint32_t>(blocks)), dim3(S::threads), 0, s, a);
 }
-void launch_gradients(const GradientArgs &a, int32_t type, bool large, hipStream_t s) {
-  if (type == ONES_F16) large ? launch_gradients<f16, Large>(a, s) : launch_gradients<f16, Small>(a, s);
-  else large ? launch_gradients<bf16, Large>(a, s) : launch_gradients<bf16, Small>(a, s);
+template <typename T>
+void launch_gradients(const GradientArgs &a, Tiles tiles, hipStream_t s) {
+  if (tiles == kLarge) launch_gradients<T, Large>(a, s);
+  else launch_gradients<T, Small>(a, s);
+}
+template <typename T>
+void launch_finish(const FinishArgs &a, hipStream_t s) {
+  const int64_t total = a.size[0] + a.size[1];
+  if (total == 0) return;
+  if (a.wide) hipLaunchKernelGGL((finish_kernel<T, 4>), dim3(static_cast<uint32_t>(ceil_div(total, 1024))), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((finish_kernel<T, 1>), dim3(static_cast<uint32_t>(ceil_div(total, 256))), dim3(256), 0, s, a);
+}
+
+// A piece of the vocabulary: its G, dW, and what it adds to dx.
+template <typename T>
+void launch_piece(const LossArgs &a, const GradientArgs &b, const LossPlan &p, hipStream_t s) {
+  if (a.x.extent) launch_logits<T, true>(a, p.logits_piece, s);
+  launch_gradients<T>(b, p.gradients.tiles, s);
+  FinishArgs f{};
+  f.sum[0] = b.dx_sum; f.sum[1] = b.dw_sum;
+  f.to[0] = b.dx; f.to[1] = b.dweight;
+  f.splits[0] = b.of_dx.splits; f.splits[1] = b.of_dw.splits;
+  f.size[0] = b.of_dx.splits > 1 && b.last ? static_cast<int64_t>(b.g.extent) * b.cols : 0;
+  f.size[1] = b.of_dw.splits > 1 ? static_cast<int64_t>(b.g_turned.extent) * b.cols : 0;
+  f.cols = b.cols;
+  f.wide = b.wide;
+  f.target = b.target;
+  f.scale = b.scale;
+  launch_finish<T>(f, s);
 }
 
 }  // namespace
@@ -366,8 +516,9 @@ int ones_cross_entropy_forward(const void *x, int64_t x_stride, const void *weig
   a.target = target;
   a.parts = reinterpret_cast<Part *>(ws + p.part);
   a.at_target = reinterpret_cast<float *>(ws + p.at_target);
-  launch_logits<false>(a, type, p.large_logits, s);
-  hipLaunchKernelGGL(join_kernel, dim3(static_cast<uint32_t>(ceil_div(rows, 64))), dim3(256), 0, s, a.parts, static_cast<int32_t>(p.parts), n, v,
+  if (type == ONES_F16) launch_logits<f16, false>(a, p.logits, s);
+  else launch_logits<bf16, false>(a, p.logits, s);
+  hipLaunchKernelGGL(join_kernel, dim3(static_cast<uint32_t>(ceil_div(rows, 64))), dim3(64 * kShares), 0, s, a.parts, static_cast<int32_t>(p.parts), n, v,
                      target, a.at_target, loss, lse);
   return launched("cross entropy forward");
 }
@@ -402,20 +553,24 @@ int ones_cross_entropy_backward(const float *dloss, const void *x, int64_t x_str
     a.target = target; a.lse = lse; a.dloss = dloss; a.scale = scale;
     a.g = ws + p.g;
     a.g_ld = p.piece;
-    if (rows) launch_logits<true>(a, type, p.large_g, s);
     GradientArgs b{};
     b.w_turned = Operand{wp, w_ld, d8, words};
     b.g = Operand{ws + p.g, p.piece, n, words};               // the rest of the last eight words is zeros
     b.x_turned = Operand{ws + p.x, d8, d8, n};
     b.g_turned = Operand{ws + p.g, p.piece, words, n};
     b.target = target; b.scale = scale;
-    b.sum = reinterpret_cast<float *>(ws + p.sum);
+    b.of_dx = p.gradients.of_dx;
+    b.of_dw = p.gradients.of_dw;
+    b.dx_sum = reinterpret_cast<float *>(ws + p.dx_sum);
+    b.dw_sum = reinterpret_cast<float *>(ws + p.dw_sum);
     b.dx = dx;
     b.dweight = static_cast<char *>(dweight) + v0 * cols * 2;
     b.cols = static_cast<int32_t>(cols);
+    b.wide = cols % 4 == 0 && aligned(dx, 8) && aligned(dweight, 8);
     b.first = v0 == 0;
     b.last = v0 + p.piece >= vocabulary;
-    launch_gradients(b, type, p.large_gradients, s);
+    if (type == ONES_F16) launch_piece<f16>(a, b, p, s);
+    else launch_piece<bf16>(a, b, p, s);
   }
   return launched("cross entropy backward");
 }

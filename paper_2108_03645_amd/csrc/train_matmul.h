@@ -4,7 +4,7 @@
 //
 // A workgroup computes a BM x BN tile of C in registers, 64 k at a time.  Either operand may lie as rows of k ("rows": L[m][k])
 // or as rows of m or n ("turned": L[k][m]); both come to LDS as they lie, by direct loads of 16 bytes a lane, into two buffers in
-// turn: the next 64 k arrive while the present ones are multiplied.  Rows are read back with 16 bytes a lane, turned operands with
+// turn: the next k arrive while the present ones are multiplied.  Rows are read back with 16 bytes a lane, turned operands with
 // the transposing read (four k of a column to every lane).  So that the lanes of a read fall into different banks, the 16-byte
 // pieces of an LDS row are exchanged by the row's number; a direct load writes LDS in lane order, so the exchange is made in
 // the address that each lane loads from.  What lies outside an operand is loaded from a block of zeros.
@@ -27,8 +27,6 @@ using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 using LdsBytes = __attribute__((address_space(3))) unsigned char;
 using GlobalBytes = __attribute__((address_space(1))) const unsigned char;
 
-constexpr int kK = 64;                        // k of a tile in LDS
-
 // An operand: `extent` values of m (or n), `k` of k; rows `ld` elements apart.  Base and ld are multiples of 16 bytes, and the
 // length of a row (k, or extent where it is turned) is read up to the next multiple of eight.
 struct Operand {
@@ -45,35 +43,40 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
   else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// One operand's tile of B values of m (or n) by 64 k.
-template <bool TURNED, int B, int THREADS>
+// The workgroup meets, and the direct loads to LDS of all its waves have arrived: a barrier alone does not wait for them.
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// One operand's tile of B values of m (or n) by K of k.
+template <bool TURNED, int B, int K, int THREADS>
 struct Tile {
-  static constexpr int bytes = B * kK * 2, loads = bytes / 16 / THREADS, pieces = B / 8;   // pieces: of a turned row
+  static constexpr int bytes = B * K * 2, loads = bytes / 16 / THREADS;
+  static constexpr int pieces = TURNED ? B / 8 : K / 8;            // 16-byte pieces of a row in LDS
   static_assert(loads * 16 * THREADS == bytes);
   const unsigned char *at[loads];             // what this thread loads next
-  int32_t left[loads];                        // k still to come where that is positive; negative: never inside
+  int32_t left[loads];                        // k still to come where that is positive
   int64_t step;
 
-  __device__ __forceinline__ void start(const Operand &o, int32_t first) {
-    step = TURNED ? o.ld * kK * 2 : kK * 2;
+  // The place of logical piece `p` of LDS row `row`, so that the lanes of a read meet different banks.  A read of rows takes the
+  // same piece of eight rows at a time; a transposing read takes 32 bytes (a unit of two pieces) of rows k..k+3, and of k+8.
+  static __device__ __forceinline__ int place(int row, int p) {
+    if constexpr (TURNED) return p ^ ((((row & 3) | ((row >> 1) & 4)) & (B / 16 - 1)) << 1);
+    else return p ^ (row & 7);
+  }
+  __device__ __forceinline__ void start(const Operand &o, int32_t first, int32_t k0) {
+    step = TURNED ? o.ld * K * 2 : K * 2;
 #pragma unroll
     for (int i = 0; i < loads; ++i) {
-      const int u = i * THREADS + static_cast<int>(threadIdx.x);
-      int32_t m, k;
-      if constexpr (TURNED) {
-        k = u / pieces;
-        const int p = u % pieces;
-        m = first + ((((p >> 1) ^ ((k & 3) | ((k >> 1) & 4))) << 1) | (p & 1)) * 8;
-      } else {
-        const int row = u / 8;
-        m = first + row;
-        k = ((u % 8) ^ (row & 7)) * 8;
-      }
+      const int u = i * THREADS + static_cast<int>(threadIdx.x), row = u / pieces, piece = place(row, u % pieces) * 8;
+      const int32_t m = first + (TURNED ? piece : row), k = k0 + (TURNED ? row : piece);
       left[i] = m < o.extent ? o.k - k : 0;
       at[i] = static_cast<const unsigned char *>(o.p) + 2 * (TURNED ? k * o.ld + m : m * o.ld + k);
     }
   }
-  // The next 64 k, into LDS at `to` (the same for the whole workgroup).
+  // The next K, into LDS at `to` (the same for the whole workgroup).
   __device__ __forceinline__ void load(unsigned char *to) {
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
 #pragma unroll
@@ -81,75 +84,119 @@ struct Tile {
       const unsigned char *from = left[i] > 0 ? at[i] : reinterpret_cast<const unsigned char *>(g_zeros);
       __builtin_amdgcn_global_load_lds((GlobalBytes *)from, (LdsBytes *)(to + (i * THREADS + wave * kWave) * 16), 16, 0, 0);
       at[i] += step;
-      left[i] -= kK;
+      left[i] -= K;
     }
   }
   // Eight k of each of 16 values from `first` (a multiple of 16) of the tile on: k = 32 half + 8 (lane / 16) + 0..7.
   static __device__ __forceinline__ s16x8 fragment(const unsigned char *from, int first, int half, int lane) {
     if constexpr (TURNED) {
-      const int q = lane >> 4, j = (lane >> 2) & 3, unit = (first >> 4) ^ (j | ((q & 1) << 2));
-      const unsigned char *p = from + (half * 32 + q * 8 + j) * (B * 2) + unit * 32 + (lane & 3) * 8;
+      const int k = half * 32 + (lane >> 4) * 8 + ((lane >> 2) & 3);
+      const unsigned char *p = from + k * (B * 2) + place(k, first >> 3) * 16 + (lane & 3) * 8;
       typedef __attribute__((address_space(3))) s16x4 Lds;
       const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds *)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds *)(p + 4 * B * 2));
       return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
       const int row = first + (lane & 15);
-      return *reinterpret_cast<const s16x8 *>(from + row * (kK * 2) + (((half * 4 + (lane >> 4)) ^ (lane & 7)) << 4));
+      return *reinterpret_cast<const s16x8 *>(from + row * (K * 2) + place(lane & 15, half * 4 + (lane >> 4)) * 16);
     }
   }
 };
 
-// BM x BN tiles by WM x WN waves.
-template <int BM_, int BN_, int WM_, int WN_>
+// BM x BN tiles by WM x WN waves, K of k at a time; one workgroup or two a compute unit.
+template <int BM_, int BN_, int WM_, int WN_, int K_, int RESIDENT_>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, threads = WM * WN * kWave;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, K = K_, threads = WM * WN * kWave, resident = RESIDENT_;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;       // 16 x 16 products of a wave
-  static constexpr int lds = 2 * (BM + BN) * kK * 2;
+  static constexpr int lds = 2 * (BM + BN) * K * 2;
 };
-using Large = Shape<256, 256, 2, 4>;
-using Small = Shape<128, 128, 2, 2>;
+using Large = Shape<256, 256, 2, 4, 64, 1>;
+using Small = Shape<128, 128, 2, 2, 64, 2>;
 
 template <typename S>
 using Sums = f32x4[S::TM][S::TN];
 
+// The sums over k0 <= k < k1 (k0 a multiple of S::K; k1 the operands' k, or a multiple too).  begin() sets the loads of the first
+// two tiles of k off, run() multiplies; a workgroup may begin its next product before it deals with the sums of the last.
 template <typename T, bool LT, bool RT, typename S>
-__device__ __forceinline__ void product(const Operand &L, const Operand &R, int32_t m0, int32_t n0, unsigned char *lds, Sums<S> &acc) {
-  constexpr int lbytes = S::BM * kK * 2, buffer = (S::BM + S::BN) * kK * 2;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int wm = (wave / S::WN) * (S::BM / S::WM), wn = (wave % S::WN) * (S::BN / S::WN);
-  Tile<LT, S::BM, S::threads> l;
-  Tile<RT, S::BN, S::threads> r;
-  l.start(L, m0);
-  r.start(R, n0);
+struct Product {
+  static constexpr int lbytes = S::BM * S::K * 2, buffer = (S::BM + S::BN) * S::K * 2;
+  Tile<LT, S::BM, S::K, S::threads> l;
+  Tile<RT, S::BN, S::K, S::threads> r;
+  int tiles;
+
+  __device__ __forceinline__ void begin(const Operand &L, const Operand &R, int32_t m0, int32_t n0, int32_t k0, int32_t k1, unsigned char *lds) {
+    l.start(L, m0, k0);
+    r.start(R, n0, k0);
+    tiles = (k1 - k0 + S::K - 1) / S::K;
 #pragma unroll
-  for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-    for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int tiles = (L.k + kK - 1) / kK;
-  if (tiles > 0) {
-    l.load(lds);
-    r.load(lds + lbytes);
+    for (int t = 0; t < 2; ++t)
+      if (t < tiles) {
+        l.load(lds + t * buffer);
+        r.load(lds + t * buffer + lbytes);
+      }
   }
-  for (int t = 0; t < tiles; ++t) {
-    unsigned char *now = lds + (t & 1) * buffer, *next = lds + ((t & 1) ^ 1) * buffer;
-    __syncthreads();                          // the present tile has arrived; the other buffer has been read by all
-    if (t + 1 < tiles) {
-      l.load(next);
-      r.load(next + lbytes);
-    }
+
+  // Phases of up to four fragments of L by all of R: the reads of the next phase are under way while one is multiplied.  The
+  // workgroup meets where the last fragments of a tile have been read: from there on its buffer takes the tile after the
+  // next, and the next tile has arrived.
+  __device__ __forceinline__ void run(unsigned char *lds, Sums<S> &acc) {
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int wm = (wave / S::WN) * (S::BM / S::WM), wn = (wave % S::WN) * (S::BN / S::WN);
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      s16x8 a[S::TM], b[S::TN];
+    for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j) b[j] = r.fragment(now + lbytes, wn + j * 16, half, lane);
+      for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (tiles <= 0) return;
+    constexpr int halves = S::K / 32, together = S::TM < 4 ? S::TM : 4, groups = S::TM / together, phases = halves * groups;
+    static_assert(halves == 2);
+    s16x8 a[2][together], b[2][S::TN];
+    auto read_a = [&](const unsigned char *from, int half, int group, s16x8 *to) {
 #pragma unroll
-      for (int i = 0; i < S::TM; ++i) a[i] = l.fragment(now, wm + i * 16, half, lane);
+      for (int i = 0; i < together; ++i) to[i] = l.fragment(from, wm + (group * together + i) * 16, half, lane);
+    };
+    auto read_b = [&](const unsigned char *from, int half, s16x8 *to) {
 #pragma unroll
-      for (int i = 0; i < S::TM; ++i)
+      for (int j = 0; j < S::TN; ++j) to[j] = r.fragment(from + lbytes, wn + j * 16, half, lane);
+    };
+    meet();
+    read_b(lds, 0, b[0]);
+    read_a(lds, 0, 0, a[0]);
+    for (int t = 0; t < tiles; ++t) {
+      unsigned char *now = lds + (t & 1) * buffer, *next = lds + ((t & 1) ^ 1) * buffer;
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j) acc[i][j] = mfma<T>(a[i], b[j], acc[i][j]);
+      for (int p = 0; p < phases; ++p) {
+        const int half = p / groups;
+        if (p + 1 < phases) {
+          if ((p + 1) % groups == 0) read_b(now, (p + 1) / groups, b[(p + 1) / groups]);
+          read_a(now, (p + 1) / groups, (p + 1) % groups, a[(p + 1) & 1]);
+        } else {
+          meet();
+          if (t + 1 < tiles) {
+            read_b(next, 0, b[0]);
+            read_a(next, 0, 0, a[0]);
+          }
+          if (t + 2 < tiles) {
+            l.load(now);
+            r.load(now + lbytes);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < together; ++i)
+#pragma unroll
+          for (int j = 0; j < S::TN; ++j)
+            acc[(p % groups) * together + i][j] = mfma<T>(a[p & 1][i], b[half][j], acc[(p % groups) * together + i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
+};
+
+template <typename T, bool LT, bool RT, typename S>
+__device__ __forceinline__ void product(const Operand &L, const Operand &R, int32_t m0, int32_t n0, int32_t k0, int32_t k1, unsigned char *lds,
+                                        Sums<S> &acc) {
+  Product<T, LT, RT, S> p;
+  p.begin(L, R, m0, n0, k0, k1, lds);
+  p.run(lds, acc);
 }
 
 // Where a lane's runs of four m start, and its n: of sum (i, j), in the whole of C.

@@ -115,7 +115,7 @@ struct ProductArgs {
 
 // A = X X^T, or (POLY) B = b A + c A A.  Tiles on and below the diagonal, each written to both places.
 template <typename S, bool POLY>
-__global__ __launch_bounds__(S::threads) void symmetric_kernel(ProductArgs a) {
+__global__ __launch_bounds__(S::threads, S::resident) void symmetric_kernel(ProductArgs a) {
   __shared__ __align__(16) unsigned char lds[S::lds];
   static_assert(S::BM == S::BN);
   // tile t of the lower triangle: row n, column m <= n
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(S::threads) void symmetric_kernel(ProductArgs a) {
   const f16 *from = POLY ? a.a + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld : a.x + static_cast<int64_t>(blockIdx.y) * a.r * a.q_ld;
   const Operand o{from, POLY ? a.r_ld : a.q_ld, a.r, POLY ? a.r_ld : a.q_ld};
   Sums<S> acc;
-  product<f16, false, false, S>(o, o, m * S::BM, n * S::BN, lds, acc);
+  product<f16, false, false, S>(o, o, m * S::BM, n * S::BN, 0, o.k, lds, acc);
   f16 *to = a.to + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld;
   const Place<S> at(m * S::BM, n * S::BN);
 #pragma unroll
@@ -155,14 +155,15 @@ __global__ __launch_bounds__(S::threads) void symmetric_kernel(ProductArgs a) {
 
 // X = a X + B X.
 template <typename S>
-__global__ __launch_bounds__(S::threads) void apply_kernel(ProductArgs a) {
+__global__ __launch_bounds__(S::threads, S::resident) void apply_kernel(ProductArgs a) {
   __shared__ __align__(16) unsigned char lds[S::lds];
   const int32_t tm = (a.q + S::BM - 1) / S::BM, tn = (a.r + S::BN - 1) / S::BN;
   int32_t m, n;
   tile_of(static_cast<int32_t>(blockIdx.x), tm * tn, tm, tn, m, n);
   const f16 *x = a.x + static_cast<int64_t>(blockIdx.y) * a.r * a.q_ld, *b = a.a + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld;
   Sums<S> acc;
-  product<f16, true, false, S>(Operand{x, a.q_ld, a.q_ld, a.r}, Operand{b, a.r_ld, a.r, a.r_ld}, m * S::BM, n * S::BN, lds, acc);
+  product<f16, true, false, S>(Operand{x, a.q_ld, a.q_ld, a.r}, Operand{b, a.r_ld, a.r, a.r_ld}, m * S::BM, n * S::BN, 0, a.r,
+                              lds, acc);
   const Place<S> at(m * S::BM, n * S::BN);
   const int64_t size = static_cast<int64_t>(a.r) * a.q;
 #pragma unroll
