@@ -25,7 +25,6 @@ using s16x8 = __attribute__((ext_vector_type(8))) short;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 using LdsBytes = __attribute__((address_space(3))) unsigned char;
-using GlobalBytes = __attribute__((address_space(1))) const unsigned char;
 
 // An operand: `extent` values of m (or n), `k` of k; rows `ld` elements apart.  Base and ld are multiples of 16 bytes, and the
 // length of a row (k, or extent where it is turned) is read up to the next multiple of eight.
@@ -43,6 +42,17 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
   else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// A direct load of 16 bytes a lane to LDS: lane i's land at to + 16 i.  Written as text: with the builtin in flight the compiler
+// waits for all of LDS's reads where it needs the first of them (it takes the load for one that may return through either
+// counter), and the reads ahead would be in vain.  It has no result in registers; meet() waits for it.
+// (s_nop: m0 is written one instruction ahead at least.)
+__device__ __forceinline__ void load_to_lds(const unsigned char *base, uint32_t offset, uint32_t to) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(to) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const unsigned char *from, uint32_t to) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
+}
+
 // The workgroup meets, and the direct loads to LDS of all its waves have arrived: a barrier alone does not wait for them.
 __device__ __forceinline__ void meet() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -55,10 +65,13 @@ template <bool TURNED, int B, int K, int THREADS>
 struct Tile {
   static constexpr int bytes = B * K * 2, loads = bytes / 16 / THREADS;
   static constexpr int pieces = TURNED ? B / 8 : K / 8;            // 16-byte pieces of a row in LDS
-  static_assert(loads * 16 * THREADS == bytes);
-  const unsigned char *at[loads];             // what this thread loads next
-  int32_t left[loads];                        // k still to come where that is positive
-  int64_t step;
+  static constexpr int rows = THREADS / pieces;                    // LDS rows that one load of the workgroup fills
+  static_assert(loads * 16 * THREADS == bytes && rows % (TURNED ? 16 : 8) == 0);
+  const unsigned char *base;                  // of the next load: element (first, k); the same for all threads
+  int64_t row_bytes;                          // from an LDS row to the next in memory
+  uint32_t offset;                            // from there to what this thread loads, in bytes
+  int32_t m, k, m_left, k_left;               // this thread's m and k in the tile, and what is left of the operand there
+  bool plain;                                 // all loads of the product lie inside
 
   // The place of logical piece `p` of LDS row `row`, so that the lanes of a read meet different banks.  A read of rows takes the
   // same piece of eight rows at a time; a transposing read takes 32 bytes (a unit of two pieces) of rows k..k+3, and of k+8.
@@ -66,26 +79,41 @@ struct Tile {
     if constexpr (TURNED) return p ^ ((((row & 3) | ((row >> 1) & 4)) & (B / 16 - 1)) << 1);
     else return p ^ (row & 7);
   }
+  // The loads of a thread lie `rows` LDS rows apart, a multiple of what place() goes by, so they share one offset.
   __device__ __forceinline__ void start(const Operand &o, int32_t first, int32_t k0) {
-    step = TURNED ? o.ld * K * 2 : K * 2;
-#pragma unroll
-    for (int i = 0; i < loads; ++i) {
-      const int u = i * THREADS + static_cast<int>(threadIdx.x), row = u / pieces, piece = place(row, u % pieces) * 8;
-      const int32_t m = first + (TURNED ? piece : row), k = k0 + (TURNED ? row : piece);
-      left[i] = m < o.extent ? o.k - k : 0;
-      at[i] = static_cast<const unsigned char *>(o.p) + 2 * (TURNED ? k * o.ld + m : m * o.ld + k);
+    const int row = static_cast<int>(threadIdx.x) / pieces, piece = place(row, static_cast<int>(threadIdx.x) % pieces) * 8;
+    m = TURNED ? piece : row;
+    k = TURNED ? row : piece;
+    m_left = o.extent - first;
+    k_left = o.k - k0;
+    plain = m_left >= B && k_left % K == 0;
+    row_bytes = o.ld * 2;
+    base = static_cast<const unsigned char *>(o.p) + 2 * (TURNED ? k0 * o.ld + first : first * o.ld + k0);
+    offset = static_cast<uint32_t>(row * row_bytes) + piece * 2;
+  }
+  // One of the loads of the next K, into LDS at `to` (the same for the whole workgroup); advance() behind the last.
+  template <bool PLAIN>
+  __device__ __forceinline__ void load_one(unsigned char *to, int i) {
+    const uint32_t mine = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LdsBytes *)to)) +
+                          __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave) * (kWave * 16);
+    if constexpr (PLAIN) {
+      load_to_lds(base + i * rows * row_bytes, offset, mine + i * THREADS * 16);
+    } else {
+      const bool inside = m + (TURNED ? 0 : i * rows) < m_left && k + (TURNED ? i * rows : 0) < k_left;
+      load_to_lds(inside ? base + i * rows * row_bytes + offset : reinterpret_cast<const unsigned char *>(g_zeros), mine + i * THREADS * 16);
     }
   }
-  // The next K, into LDS at `to` (the same for the whole workgroup).
+  __device__ __forceinline__ void advance() {
+    base += TURNED ? K * row_bytes : K * 2;
+    k_left -= K;
+  }
   __device__ __forceinline__ void load(unsigned char *to) {
-    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
 #pragma unroll
     for (int i = 0; i < loads; ++i) {
-      const unsigned char *from = left[i] > 0 ? at[i] : reinterpret_cast<const unsigned char *>(g_zeros);
-      __builtin_amdgcn_global_load_lds((GlobalBytes *)from, (LdsBytes *)(to + (i * THREADS + wave * kWave) * 16), 16, 0, 0);
-      at[i] += step;
-      left[i] -= K;
+      if (plain) load_one<true>(to, i);
+      else load_one<false>(to, i);
     }
+    advance();
   }
   // Eight k of each of 16 values from `first` (a multiple of 16) of the tile on: k = 32 half + 8 (lane / 16) + 0..7.
   static __device__ __forceinline__ s16x8 fragment(const unsigned char *from, int first, int half, int lane) {
@@ -136,9 +164,52 @@ struct Product {
       }
   }
 
-  // Phases of up to four fragments of L by all of R: the reads of the next phase are under way while one is multiplied.  The
-  // workgroup meets where the last fragments of a tile have been read: from there on its buffer takes the tile after the
-  // next, and the next tile has arrived.
+  static constexpr int kRows = 4, groups = S::TM / kRows, phases = 2 * groups;
+  static_assert(S::K == 64 && S::TM % kRows == 0 && S::TN == 4 && Tile<LT, S::BM, S::K, S::threads>::loads == kRows &&
+                Tile<RT, S::BN, S::K, S::threads>::loads == kRows);
+
+  // The products of one tile of k, in phases of four fragments of L by all of R.  The reads of the next phase, and the loads of the
+  // tile after the next, are put between the rows of products of a phase: a wave issues in order, and behind a run of reads or
+  // loads its products would wait for the queues that all eight waves fill at once.  The workgroup meets where the last fragments
+  // of the tile have been read: from there on its buffer takes the tile after the next, and the next tile has arrived.
+  template <bool MORE, bool PLAIN>            // MORE: a next tile and one after it
+  __device__ __forceinline__ void multiply(unsigned char *now, unsigned char *next, bool reads, int wm, int wn, int lane, s16x8 (&a)[2][kRows],
+                                           s16x8 (&b)[2][S::TN], Sums<S> &acc) {
+#pragma unroll
+    for (int p = 0; p < phases; ++p) {
+      const int half = p / groups, group = p % groups;
+      const bool last = p + 1 == phases, turns = last || (p + 1) % groups == 0;            // turns: to the other half
+      const unsigned char *from = last ? next : now;
+      const int next_half = last ? 0 : (p + 1) / groups, next_group = (p + 1) % groups;
+      if (last) meet();
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        if (MORE || !last || reads) {
+          if (turns && i < 2) {               // R's fragments first: the next phase begins with all of them
+            b[next_half][2 * i] = r.fragment(from + lbytes, wn + 2 * i * 16, next_half, lane);
+            b[next_half][2 * i + 1] = r.fragment(from + lbytes, wn + (2 * i + 1) * 16, next_half, lane);
+          } else {
+#pragma unroll
+            for (int q = turns ? 2 * (i - 2) : i; q < (turns ? 2 * (i - 1) : i + 1); ++q)
+              a[(p + 1) & 1][q] = l.fragment(from, wm + (next_group * kRows + q) * 16, next_half, lane);
+          }
+        }
+        if (MORE && last) {
+          l.template load_one<PLAIN>(now, i);
+          r.template load_one<PLAIN>(now + lbytes, i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) acc[group * kRows + i][j] = mfma<T>(a[p & 1][i], b[half][j], acc[group * kRows + i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (MORE && last) {
+        l.advance();
+        r.advance();
+      }
+    }
+  }
+
   __device__ __forceinline__ void run(unsigned char *lds, Sums<S> &acc) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int wm = (wave / S::WN) * (S::BM / S::WM), wn = (wave % S::WN) * (S::BN / S::WN);
@@ -147,47 +218,18 @@ struct Product {
 #pragma unroll
       for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (tiles <= 0) return;
-    constexpr int halves = S::K / 32, together = S::TM < 4 ? S::TM : 4, groups = S::TM / together, phases = halves * groups;
-    static_assert(halves == 2);
-    s16x8 a[2][together], b[2][S::TN];
-    auto read_a = [&](const unsigned char *from, int half, int group, s16x8 *to) {
-#pragma unroll
-      for (int i = 0; i < together; ++i) to[i] = l.fragment(from, wm + (group * together + i) * 16, half, lane);
-    };
-    auto read_b = [&](const unsigned char *from, int half, s16x8 *to) {
-#pragma unroll
-      for (int j = 0; j < S::TN; ++j) to[j] = r.fragment(from + lbytes, wn + j * 16, half, lane);
-    };
+    s16x8 a[2][kRows], b[2][S::TN];
     meet();
-    read_b(lds, 0, b[0]);
-    read_a(lds, 0, 0, a[0]);
-    for (int t = 0; t < tiles; ++t) {
-      unsigned char *now = lds + (t & 1) * buffer, *next = lds + ((t & 1) ^ 1) * buffer;
 #pragma unroll
-      for (int p = 0; p < phases; ++p) {
-        const int half = p / groups;
-        if (p + 1 < phases) {
-          if ((p + 1) % groups == 0) read_b(now, (p + 1) / groups, b[(p + 1) / groups]);
-          read_a(now, (p + 1) / groups, (p + 1) % groups, a[(p + 1) & 1]);
-        } else {
-          meet();
-          if (t + 1 < tiles) {
-            read_b(next, 0, b[0]);
-            read_a(next, 0, 0, a[0]);
-          }
-          if (t + 2 < tiles) {
-            l.load(now);
-            r.load(now + lbytes);
-          }
-        }
+    for (int j = 0; j < S::TN; ++j) b[0][j] = r.fragment(lds + lbytes, wn + j * 16, 0, lane);
 #pragma unroll
-        for (int i = 0; i < together; ++i)
-#pragma unroll
-          for (int j = 0; j < S::TN; ++j)
-            acc[(p % groups) * together + i][j] = mfma<T>(a[p & 1][i], b[half][j], acc[(p % groups) * together + i][j]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
+    for (int i = 0; i < kRows; ++i) a[0][i] = l.fragment(lds, wm + i * 16, 0, lane);
+    int t = 0;
+    if (l.plain && r.plain)
+      for (; t + 2 < tiles; ++t) multiply<true, true>(lds + (t & 1) * buffer, lds + ((t & 1) ^ 1) * buffer, true, wm, wn, lane, a, b, acc);
+    else
+      for (; t + 2 < tiles; ++t) multiply<true, false>(lds + (t & 1) * buffer, lds + ((t & 1) ^ 1) * buffer, true, wm, wn, lane, a, b, acc);
+    for (; t < tiles; ++t) multiply<false, false>(lds + (t & 1) * buffer, lds + ((t & 1) ^ 1) * buffer, t + 1 < tiles, wm, wn, lane, a, b, acc);
   }
 };
 
