@@ -325,17 +325,14 @@ __global__ __launch_bounds__(256) void finish_kernel(FinishArgs a) {
   store_pack<T, V>(static_cast<T *>(a.to[which]) + i, v);
 }
 
-// Which tiles, and into how many parts k is split: by an estimate of the time in microseconds.  A round of workgroups (one a compute
-// unit with large tiles, else two) takes so long for 64 k, and so long for its start and its end.
-struct Cost { int64_t bm, bn, places; double per_64, fixed; };
-constexpr Cost kCosts[] = {{Large::BM, Large::BN, 256, 1.5, 8.0}, {Small::BM, Small::BN, 512, 1.2, 4.0}};
-enum Tiles { kLarge, kSmall };
+// Which tiles, and into how many parts k is split: the estimate's least.
+constexpr Tiles kUsed[] = {kLarge, kDeep, kSmall, kTiny};
 
-double logits_time(const Cost &c, int64_t m, int64_t n, int64_t k) {
-  return ceil_div(ceil_div(m, c.bm) * ceil_div(n, c.bn), c.places) * (ceil_div(k, 64) * c.per_64 + c.fixed);
-}
 Tiles logits_tiles(int64_t m, int64_t n, int64_t k) {
-  return logits_time(kCosts[kSmall], m, n, k) < logits_time(kCosts[kLarge], m, n, k) ? kSmall : kLarge;
+  auto time = [&](Tiles t) { return launch_time(kTileCosts[t], ceil_div(m, kTileCosts[t].bm) * ceil_div(n, kTileCosts[t].bn), k); };
+  Tiles best = kLarge;
+  for (Tiles t : kUsed) if (time(t) < time(best)) best = t;
+  return best;
 }
 
 Split split_of(int64_t k, int64_t most) {
@@ -347,17 +344,16 @@ struct GradientPlan { Tiles tiles; Split of_dx, of_dw; };
 GradientPlan gradient_plan(int64_t rows, int64_t cols, int64_t words) {
   GradientPlan best{};
   double best_time = INFINITY;
-  for (Tiles t : {kLarge, kSmall}) {
-    const Cost &c = kCosts[t];
+  for (Tiles t : kUsed) {
+    const TileCost &c = kTileCosts[t];
     const int64_t tm = ceil_div(cols, c.bm), dx = tm * ceil_div(rows, c.bn), dw = tm * ceil_div(words, c.bn);
     for (int64_t most = std::max<int64_t>(128, ceil_div(std::max(rows, words), 64) * 64); most >= 128; most /= 2) {
       const GradientPlan p{t, split_of(words, most), split_of(rows, most)};
       if (p.of_dx.splits > 32 || p.of_dw.splits > 32) break;
-      const int64_t longest = std::max(p.of_dx.k_each, p.of_dw.k_each), items = dx * p.of_dx.splits + dw * p.of_dw.splits;
-      // items of the shorter product make room for others: a round counts by the work in it
-      const double work = (dx * p.of_dx.splits * (p.of_dx.k_each / 64.0 * c.per_64 + c.fixed) + dw * p.of_dw.splits * (p.of_dw.k_each / 64.0 * c.per_64 + c.fixed)) / c.places;
-      double time = std::max(work, longest / 64.0 * c.per_64 + c.fixed);
-      if (items > c.places) time = std::max(time, work * ceil_div(items, c.places) * c.places / items);
+      const int64_t dx_items = dx * p.of_dx.splits, dw_items = dw * p.of_dw.splits, items = dx_items + dw_items;
+      const double dx_time = item_time(c, items, p.of_dx.k_each), dw_time = item_time(c, items, p.of_dw.k_each);
+      // rounds of places, each as long as the items' mean, or the longest item
+      double time = std::max(std::max(dx_time, dw_time), ceil_div(items, c.places) * (dx_items * dx_time + dw_items * dw_time) / items);
       double bytes = 0;                       // written and read again
       if (p.of_dx.splits > 1) bytes += 8.0 * p.of_dx.splits * rows * cols;
       if (p.of_dw.splits > 1) bytes += 8.0 * p.of_dw.splits * words * cols;
@@ -380,8 +376,8 @@ LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool copies_x
   LossPlan p{};
   p.cols8 = ceil_div(cols, 8) * 8;
   p.logits = logits_tiles(vocabulary, rows, cols);
-  static_assert(Large::WM == 2 && Small::WM == 2);
-  p.parts = ceil_div(vocabulary, kCosts[p.logits].bm) * 2;
+  static_assert(Large::WM == 2 && Deep::WM == 2 && Small::WM == 2 && Tiny::WM == 2);
+  p.parts = ceil_div(vocabulary, kTileCosts[p.logits].bm) * 2;
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes); return at; };
   const size_t n = static_cast<size_t>(rows), d = static_cast<size_t>(cols), d8 = static_cast<size_t>(p.cols8);
@@ -435,8 +431,12 @@ void launch_logits(const LossArgs &a, hipStream_t s) {
 }
 template <typename T, bool GRADIENT>
 void launch_logits(const LossArgs &a, Tiles tiles, hipStream_t s) {
-  if (tiles == kLarge) launch_logits<T, Large, GRADIENT>(a, s);
-  else launch_logits<T, Small, GRADIENT>(a, s);
+  switch (tiles) {
+    case kLarge: return launch_logits<T, Large, GRADIENT>(a, s);
+    case kDeep: return launch_logits<T, Deep, GRADIENT>(a, s);
+    case kSmall: return launch_logits<T, Small, GRADIENT>(a, s);
+    default: return launch_logits<T, Tiny, GRADIENT>(a, s);
+  }
 }
 template <typename T, typename S>
 void launch_gradients(const GradientArgs &a, hipStream_t s) {
@@ -445,8 +445,12 @@ void launch_gradients(const GradientArgs &a, hipStream_t s) {
 }
 template <typename T>
 void launch_gradients(const GradientArgs &a, Tiles tiles, hipStream_t s) {
-  if (tiles == kLarge) launch_gradients<T, Large>(a, s);
-  else launch_gradients<T, Small>(a, s);
+  switch (tiles) {
+    case kLarge: return launch_gradients<T, Large>(a, s);
+    case kDeep: return launch_gradients<T, Deep>(a, s);
+    case kSmall: return launch_gradients<T, Small>(a, s);
+    default: return launch_gradients<T, Tiny>(a, s);
+  }
 }
 template <typename T>
 void launch_finish(const FinishArgs &a, hipStream_t s) {

@@ -3,8 +3,8 @@
 //   C[n][m] = sum over k of L(m, k) R(n, k)        16-bit operands, 32-bit sums (v_mfma_f32_16x16x32)
 //
 // A workgroup computes a BM x BN tile of C in registers, 64 k at a time.  Either operand may lie as rows of k ("rows": L[m][k])
-// or as rows of m or n ("turned": L[k][m]); both come to LDS as they lie, by direct loads of 16 bytes a lane, into two buffers in
-// turn: the next k arrive while the present ones are multiplied.  Rows are read back with 16 bytes a lane, turned operands with
+// or as rows of m or n ("turned": L[k][m]); both come to LDS as they lie, by direct loads of 16 bytes a lane, into two to
+// four buffers in turn: the next k arrive while the present ones are multiplied.  Rows are read back with 16 bytes a lane, turned operands with
 // the transposing read (four k of a column to every lane).  So that the lanes of a read fall into different banks, the 16-byte
 // pieces of an LDS row are exchanged by the row's number; a direct load writes LDS in lane order, so the exchange is made in
 // the address that each lane loads from.  What lies outside an operand is loaded from a block of zeros.
@@ -53,9 +53,13 @@ __device__ __forceinline__ void load_to_lds(const unsigned char *from, uint32_t 
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
 }
 
-// The workgroup meets, and the direct loads to LDS of all its waves have arrived: a barrier alone does not wait for them.
+// The workgroup meets, and the direct loads to LDS of all its waves, but for the last PENDING of each, have arrived: a barrier
+// alone does not wait for them.  (Memory operations are counted off in the order they were issued in; stores behind the loads
+// make the wait longer, not shorter.)
+template <int PENDING>
 __device__ __forceinline__ void meet() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  static_assert(PENDING < 64);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PENDING) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -130,21 +134,28 @@ struct Tile {
   }
 };
 
-// BM x BN tiles by WM x WN waves, K of k at a time; one workgroup or two a compute unit.
-template <int BM_, int BN_, int WM_, int WN_, int K_, int RESIDENT_>
+// BM x BN tiles by WM x WN waves, K of k at a time in BUFFERS places of LDS; RESIDENT workgroups a compute unit.
+template <int BM_, int BN_, int WM_, int WN_, int BUFFERS_, int RESIDENT_>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, K = K_, threads = WM * WN * kWave, resident = RESIDENT_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, K = 64, threads = WM * WN * kWave, buffers = BUFFERS_, resident = RESIDENT_;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;       // 16 x 16 products of a wave
-  static constexpr int lds = 2 * (BM + BN) * K * 2;
+  static constexpr int lds = buffers * (BM + BN) * K * 2;
 };
-using Large = Shape<256, 256, 2, 4, 64, 1>;
-using Small = Shape<128, 128, 2, 2, 64, 2>;
+// What carries them: two waves a SIMD at least (four waves of 64 x 64 on a tile of 128 x 128 take 1.2 times as long as eight of
+// 64 x 32, although those read half as much again from LDS), and, where a compute unit holds one workgroup, four buffers
+// instead of two (136 tiles of 128 x 128, k 2048: 21 us against 26).  An operand that is turned has 64, 128 or 256 values.
+using Large = Shape<256, 256, 2, 4, 2, 1>;
+using Middle = Shape<192, 128, 4, 2, 3, 1>;
+using MiddleTurned = Shape<128, 192, 2, 4, 3, 1>;
+using Deep = Shape<128, 128, 2, 4, 4, 1>;
+using Small = Shape<128, 128, 2, 4, 2, 2>;
+using Tiny = Shape<64, 64, 2, 2, 4, 2>;
 
 template <typename S>
 using Sums = f32x4[S::TM][S::TN];
 
 // The sums over k0 <= k < k1 (k0 a multiple of S::K; k1 the operands' k, or a multiple too).  begin() sets the loads of the first
-// two tiles of k off, run() multiplies; a workgroup may begin its next product before it deals with the sums of the last.
+// tiles of k off, run() multiplies; a workgroup may begin its next product before it deals with the sums of the last.
 template <typename T, bool LT, bool RT, typename S>
 struct Product {
   static constexpr int lbytes = S::BM * S::K * 2, buffer = (S::BM + S::BN) * S::K * 2;
@@ -157,22 +168,23 @@ struct Product {
     r.start(R, n0, k0);
     tiles = (k1 - k0 + S::K - 1) / S::K;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < S::buffers; ++t)
       if (t < tiles) {
         l.load(lds + t * buffer);
         r.load(lds + t * buffer + lbytes);
       }
   }
 
-  static constexpr int kRows = 4, groups = S::TM / kRows, phases = 2 * groups;
-  static_assert(S::K == 64 && S::TM % kRows == 0 && S::TN == 4 && Tile<LT, S::BM, S::K, S::threads>::loads == kRows &&
-                Tile<RT, S::BN, S::K, S::threads>::loads == kRows);
+  static constexpr int kRows = S::TM <= 5 ? S::TM : S::TM / 2, groups = S::TM / kRows, phases = 2 * groups;
+  static constexpr int l_loads = Tile<LT, S::BM, S::K, S::threads>::loads, r_loads = Tile<RT, S::BN, S::K, S::threads>::loads;
+  static constexpr int of_tile = l_loads + r_loads;
+  static_assert(S::K == 64 && S::TM % kRows == 0);
 
-  // The products of one tile of k, in phases of four fragments of L by all of R.  The reads of the next phase, and the loads of the
-  // tile after the next, are put between the rows of products of a phase: a wave issues in order, and behind a run of reads or
+  // The products of one tile of k, in phases of up to five fragments of L by all of R.  The reads of the next phase, and the loads of a
+  // later tile, are put between the rows of products of a phase: a wave issues in order, and behind a run of reads or
   // loads its products would wait for the queues that all eight waves fill at once.  The workgroup meets where the last fragments
-  // of the tile have been read: from there on its buffer takes the tile after the next, and the next tile has arrived.
-  template <bool MORE, bool PLAIN>            // MORE: a next tile and one after it
+  // of the tile have been read: from there on its buffer takes a later tile, and the next tile has arrived.
+  template <bool MORE, bool PLAIN>            // MORE: there is a tile to load
   __device__ __forceinline__ void multiply(unsigned char *now, unsigned char *next, bool reads, int wm, int wn, int lane, s16x8 (&a)[2][kRows],
                                            s16x8 (&b)[2][S::TN], Sums<S> &acc) {
 #pragma unroll
@@ -181,22 +193,22 @@ struct Product {
       const bool last = p + 1 == phases, turns = last || (p + 1) % groups == 0;            // turns: to the other half
       const unsigned char *from = last ? next : now;
       const int next_half = last ? 0 : (p + 1) / groups, next_group = (p + 1) % groups;
-      if (last) meet();
+      if (last) meet<MORE ? (S::buffers - 2) * of_tile : 0>();
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
-        if (MORE || !last || reads) {
-          if (turns && i < 2) {               // R's fragments first: the next phase begins with all of them
-            b[next_half][2 * i] = r.fragment(from + lbytes, wn + 2 * i * 16, next_half, lane);
-            b[next_half][2 * i + 1] = r.fragment(from + lbytes, wn + (2 * i + 1) * 16, next_half, lane);
-          } else {
+        if (MORE || !last || reads) {         // R's fragments first: the next phase begins with all of them
+          const int bs = turns ? S::TN : 0, n = bs + kRows;
 #pragma unroll
-            for (int q = turns ? 2 * (i - 2) : i; q < (turns ? 2 * (i - 1) : i + 1); ++q)
-              a[(p + 1) & 1][q] = l.fragment(from, wm + (next_group * kRows + q) * 16, next_half, lane);
+          for (int e = i * n / kRows; e < (i + 1) * n / kRows; ++e) {
+            if (e < bs) b[next_half][e] = r.fragment(from + lbytes, wn + e * 16, next_half, lane);
+            else a[(p + 1) & 1][e - bs] = l.fragment(from, wm + (next_group * kRows + e - bs) * 16, next_half, lane);
           }
         }
         if (MORE && last) {
-          l.template load_one<PLAIN>(now, i);
-          r.template load_one<PLAIN>(now + lbytes, i);
+#pragma unroll
+          for (int e = i * l_loads / kRows; e < (i + 1) * l_loads / kRows; ++e) l.template load_one<PLAIN>(now, e);
+#pragma unroll
+          for (int e = i * r_loads / kRows; e < (i + 1) * r_loads / kRows; ++e) r.template load_one<PLAIN>(now + lbytes, e);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -219,17 +231,20 @@ struct Product {
       for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (tiles <= 0) return;
     s16x8 a[2][kRows], b[2][S::TN];
-    meet();
+    if (tiles >= S::buffers) meet<(S::buffers - 1) * of_tile>();
+    else meet<0>();
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) b[0][j] = r.fragment(lds + lbytes, wn + j * 16, 0, lane);
 #pragma unroll
     for (int i = 0; i < kRows; ++i) a[0][i] = l.fragment(lds, wm + i * 16, 0, lane);
+    unsigned char *now = lds, *const end = lds + S::buffers * buffer;
+    auto after = [&](unsigned char *p) { return p + buffer == end ? lds : p + buffer; };
     int t = 0;
     if (l.plain && r.plain)
-      for (; t + 2 < tiles; ++t) multiply<true, true>(lds + (t & 1) * buffer, lds + ((t & 1) ^ 1) * buffer, true, wm, wn, lane, a, b, acc);
+      for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true, true>(now, after(now), true, wm, wn, lane, a, b, acc);
     else
-      for (; t + 2 < tiles; ++t) multiply<true, false>(lds + (t & 1) * buffer, lds + ((t & 1) ^ 1) * buffer, true, wm, wn, lane, a, b, acc);
-    for (; t < tiles; ++t) multiply<false, false>(lds + (t & 1) * buffer, lds + ((t & 1) ^ 1) * buffer, t + 1 < tiles, wm, wn, lane, a, b, acc);
+      for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true, false>(now, after(now), true, wm, wn, lane, a, b, acc);
+    for (; t < tiles; ++t, now = after(now)) multiply<false, false>(now, after(now), t + 1 < tiles, wm, wn, lane, a, b, acc);
   }
 };
 

@@ -24,13 +24,14 @@ namespace train {
 namespace {
 
 constexpr float kUnitX = 2048.f, kUnitA = 1024.f;
-constexpr int kSumBlocks = 64;                // workgroups that share a matrix's sum of squares
+constexpr int64_t kSumBlocks = 1024;          // workgroups that share a matrix's sum of squares, at most
 
 struct MomentumArgs {
   const void *grad;
   float *momentum;                            // null: u = g
-  float *squares;                             // [matrices][kSumBlocks]
+  float *squares;                             // [matrices][blocks]
   int64_t size;                               // elements of a matrix
+  int32_t blocks;
   int32_t type, nesterov;
   float beta;
 };
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(256) void momentum_kernel(MomentumArgs a) {
   const T *grad = static_cast<const T *>(a.grad) + blockIdx.y * a.size;
   float *momentum = a.momentum ? a.momentum + blockIdx.y * a.size : nullptr;
   float sum = 0.f;
-  for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * V; i < a.size; i += kSumBlocks * 256ll * V) {
+  for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * V; i < a.size; i += a.blocks * 256ll * V) {
     const Pack<T, V> g = load_pack<T, V>(grad + i);
     float m[V];
     if (momentum) {
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(256) void momentum_kernel(MomentumArgs a) {
   sum = wave_sum(sum);
   if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) a.squares[blockIdx.y * kSumBlocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+  if (threadIdx.x == 0) a.squares[static_cast<int64_t>(blockIdx.y) * a.blocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 struct NormaliseArgs {
@@ -81,7 +82,10 @@ __global__ __launch_bounds__(256) void normalise_kernel(NormaliseArgs a) {
   const float *momentum = a.m.momentum ? a.m.momentum + blockIdx.z * a.m.size : nullptr;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   if (wave == 0) {
-    const float sum = wave_sum(a.m.squares[blockIdx.z * kSumBlocks + lane]);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = lane; i < a.m.blocks; i += 64) sum += a.m.squares[static_cast<int64_t>(blockIdx.z) * a.m.blocks + i];
+    sum = wave_sum(sum);
     if (lane == 0) unit = kUnitX / (sqrtf(sum) + a.eps);
   }
   const bool turned = a.rows > a.cols;
@@ -113,41 +117,49 @@ struct ProductArgs {
   float one, two;                             // coefficients
 };
 
-// A = X X^T, or (POLY) B = b A + c A A.  Tiles on and below the diagonal, each written to both places.
+// Tiles of rows n that begin at or below the diagonal (the first column is not beyond the last row), before tile row j.
+template <typename S>
+__host__ __device__ inline int32_t tiles_in_row(int32_t j, int32_t tm) {
+  const int32_t n = ((j + 1) * S::BN - 1) / S::BM + 1;
+  return n < tm ? n : tm;
+}
+
+// A = X X^T, or (POLY) B = b A + c A A.  Only the elements on and below the diagonal are computed; each is written to both places.
 template <typename S, bool POLY>
 __global__ __launch_bounds__(S::threads, S::resident) void symmetric_kernel(ProductArgs a) {
   __shared__ __align__(16) unsigned char lds[S::lds];
-  static_assert(S::BM == S::BN);
-  // tile t of the lower triangle: row n, column m <= n
-  const int32_t t = static_cast<int32_t>(blockIdx.x);
-  int32_t n = static_cast<int32_t>((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-  while ((n + 1) * (n + 2) / 2 <= t) ++n;
-  while (n * (n + 1) / 2 > t) --n;
-  const int32_t m = t - n * (n + 1) / 2;
+  const int32_t tm = (a.r_ld + S::BM - 1) / S::BM, total = static_cast<int32_t>(gridDim.x), die = static_cast<int32_t>(blockIdx.x) % 8;
+  int32_t m = die * (total / 8) + min(die, total % 8) + static_cast<int32_t>(blockIdx.x) / 8, n = 0;      // a run of tiles to each die
+  for (int32_t in = tiles_in_row<S>(0, tm); m >= in; in = tiles_in_row<S>(++n, tm)) m -= in;
   const f16 *from = POLY ? a.a + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld : a.x + static_cast<int64_t>(blockIdx.y) * a.r * a.q_ld;
   const Operand o{from, POLY ? a.r_ld : a.q_ld, a.r, POLY ? a.r_ld : a.q_ld};
   Sums<S> acc;
   product<f16, false, false, S>(o, o, m * S::BM, n * S::BN, 0, o.k, lds, acc);
   f16 *to = a.to + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld;
   const Place<S> at(m * S::BM, n * S::BN);
+  const bool below = (m + 1) * S::BM <= n * S::BN;
 #pragma unroll
   for (int j = 0; j < S::TN; ++j) {
     const int32_t row = at.n + j * 16;
-    if (row >= a.r_ld) continue;
+    if (row >= a.r_ld) continue;              // rows from r on come out as zeros, which are the columns beyond r of the others
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
       const int32_t c = at.m + i * 16;
-      if (c >= a.r_ld) continue;              // columns (mirrored: rows) from r to r_ld come out as zeros
+      if (c > row) continue;
       float v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[k] = acc[i][j][k] * (POLY ? a.two / kUnitA : kUnitA / (kUnitX * kUnitX));
-        if (POLY && row < a.r) v[k] += a.one * static_cast<float>(from[static_cast<int64_t>(row) * a.r_ld + c + k]);
-      }
-      if (row < a.r) store_pack<f16, 4>(to + static_cast<int64_t>(row) * a.r_ld + c, v);
-      if (m != n) {
+      for (int k = 0; k < 4; ++k) v[k] = acc[i][j][k] * (POLY ? a.two / kUnitA : kUnitA / (kUnitX * kUnitX));
+      if (POLY && row < a.r) {
+        const Pack<f16, 4> first = load_pack<f16, 4>(from + static_cast<int64_t>(row) * a.r_ld + c);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (c + k < a.r) to[static_cast<int64_t>(c + k) * a.r_ld + row] = static_cast<f16>(v[k]);
+        for (int k = 0; k < 4; ++k) v[k] += a.one * static_cast<float>(first.v[k]);
+      }
+      if (below && row < a.r) store_pack<f16, 4>(to + static_cast<int64_t>(row) * a.r_ld + c, v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (c + k > row) continue;
+        if (!below && row < a.r) to[static_cast<int64_t>(row) * a.r_ld + c + k] = static_cast<f16>(v[k]);
+        if (c + k < row && c + k < a.r) to[static_cast<int64_t>(c + k) * a.r_ld + row] = static_cast<f16>(v[k]);
       }
     }
   }
@@ -195,6 +207,7 @@ __global__ __launch_bounds__(S::threads, S::resident) void apply_kernel(ProductA
 
 struct UpdatePlan {
   int64_t r, q, r_ld, q_ld;
+  int64_t blocks;
   size_t squares, x[2], a[2], total;
 };
 UpdatePlan update_plan(int64_t count, int64_t rows, int64_t cols) {
@@ -205,7 +218,8 @@ UpdatePlan update_plan(int64_t count, int64_t rows, int64_t cols) {
   p.q_ld = ceil_div(p.q, 8) * 8;
   size_t off = 0;
   auto take = [&](int64_t bytes) { const size_t at = off; off = align_up(off + static_cast<size_t>(bytes)); return at; };
-  p.squares = take(count * kSumBlocks * 4);
+  p.blocks = std::min(kSumBlocks, ceil_div(rows * cols, 4096));            // at least four runs of four elements a thread
+  p.squares = take(count * p.blocks * 4);
   p.x[0] = take(count * p.r * p.q_ld * 2);
   p.x[1] = take(count * p.r * p.q_ld * 2);
   p.a[0] = take(count * p.r * p.r_ld * 2);
@@ -222,30 +236,55 @@ int check_update(int64_t count, int64_t rows, int64_t cols) {
 
 template <typename T>
 void launch_momentum(const MomentumArgs &a, int64_t count, hipStream_t s) {
-  const dim3 grid(kSumBlocks, static_cast<uint32_t>(count));
+  const dim3 grid(static_cast<uint32_t>(a.blocks), static_cast<uint32_t>(count));
   const bool wide = a.size % 4 == 0 && aligned(a.grad, 4 * sizeof(T)) && (!a.momentum || aligned(a.momentum, 16));
   if (wide) hipLaunchKernelGGL((momentum_kernel<T, 4>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((momentum_kernel<T, 1>), grid, dim3(256), 0, s, a);
 }
 
-// Large tiles where they are enough for most compute units.
-constexpr int64_t kEnoughTiles = 160;
-
-template <bool POLY>
-void launch_symmetric(const ProductArgs &a, int64_t count, hipStream_t s) {
-  const int64_t large = ceil_div(a.r, Large::BM), small = ceil_div(a.r, Small::BM);
-  const int64_t large_tiles = large * (large + 1) / 2, small_tiles = small * (small + 1) / 2;
-  if (count * large_tiles >= kEnoughTiles)
-    hipLaunchKernelGGL((symmetric_kernel<Large, POLY>), dim3(static_cast<uint32_t>(large_tiles), static_cast<uint32_t>(count)), dim3(Large::threads), 0, s, a);
-  else
-    hipLaunchKernelGGL((symmetric_kernel<Small, POLY>), dim3(static_cast<uint32_t>(small_tiles), static_cast<uint32_t>(count)), dim3(Small::threads), 0, s, a);
+template <typename S>
+int64_t symmetric_tiles(int64_t r_ld) {
+  int64_t tiles = 0;
+  for (int32_t j = 0; j < ceil_div(r_ld, S::BN); ++j) tiles += tiles_in_row<S>(j, static_cast<int32_t>(ceil_div(r_ld, S::BM)));
+  return tiles;
 }
+template <typename S>
+int64_t all_tiles(const ProductArgs &a) { return ceil_div(a.r, S::BN) * ceil_div(a.q, S::BM); }
+
+template <typename S, bool POLY>
+void launch_symmetric(const ProductArgs &a, int64_t count, hipStream_t s) {
+  hipLaunchKernelGGL((symmetric_kernel<S, POLY>), dim3(static_cast<uint32_t>(symmetric_tiles<S>(a.r_ld)), static_cast<uint32_t>(count)), dim3(S::threads), 0, s, a);
+}
+template <bool POLY>
+void launch_symmetric(const ProductArgs &a, Tiles tiles, int64_t count, hipStream_t s) {
+  switch (tiles) {
+    case kLarge: return launch_symmetric<Large, POLY>(a, count, s);
+    case kMiddle: return launch_symmetric<Middle, POLY>(a, count, s);
+    case kDeep: return launch_symmetric<Deep, POLY>(a, count, s);
+    case kSmall: return launch_symmetric<Small, POLY>(a, count, s);
+    default: return launch_symmetric<Tiny, POLY>(a, count, s);
+  }
+}
+template <typename S>
 void launch_apply(const ProductArgs &a, int64_t count, hipStream_t s) {
-  const int64_t large = ceil_div(a.r, Large::BN) * ceil_div(a.q, Large::BM), small = ceil_div(a.r, Small::BN) * ceil_div(a.q, Small::BM);
-  if (count * large >= kEnoughTiles)
-    hipLaunchKernelGGL((apply_kernel<Large>), dim3(static_cast<uint32_t>(large), static_cast<uint32_t>(count)), dim3(Large::threads), 0, s, a);
-  else
-    hipLaunchKernelGGL((apply_kernel<Small>), dim3(static_cast<uint32_t>(small), static_cast<uint32_t>(count)), dim3(Small::threads), 0, s, a);
+  hipLaunchKernelGGL((apply_kernel<S>), dim3(static_cast<uint32_t>(all_tiles<S>(a)), static_cast<uint32_t>(count)), dim3(S::threads), 0, s, a);
+}
+void launch_apply(const ProductArgs &a, Tiles tiles, int64_t count, hipStream_t s) {
+  switch (tiles) {
+    case kLarge: return launch_apply<Large>(a, count, s);
+    case kMiddle: return launch_apply<MiddleTurned>(a, count, s);
+    case kDeep: return launch_apply<Deep>(a, count, s);
+    case kSmall: return launch_apply<Small>(a, count, s);
+    default: return launch_apply<Tiny>(a, count, s);
+  }
+}
+
+// Which tiles: the estimate's least.
+Tiles least(const int64_t (&items)[5], int64_t k) {
+  Tiles best = kLarge;
+  for (Tiles t : {kMiddle, kDeep, kSmall, kTiny})
+    if (launch_time(kTileCosts[t], items[t], k) < launch_time(kTileCosts[best], items[best], k)) best = t;
+  return best;
 }
 
 }  // namespace
@@ -279,7 +318,7 @@ int ones_orthogonal_update(const void *grad, float *momentum, int64_t count, int
   f16 *x[2] = {reinterpret_cast<f16 *>(ws + p.x[0]), reinterpret_cast<f16 *>(ws + p.x[1])};
   f16 *a[2] = {reinterpret_cast<f16 *>(ws + p.a[0]), reinterpret_cast<f16 *>(ws + p.a[1])};
   NormaliseArgs n{};
-  n.m = MomentumArgs{grad, momentum, reinterpret_cast<float *>(ws + p.squares), rows * cols, grad_type, nesterov, beta};
+  n.m = MomentumArgs{grad, momentum, reinterpret_cast<float *>(ws + p.squares), rows * cols, static_cast<int32_t>(p.blocks), grad_type, nesterov, beta};
   n.x = x[0];
   n.rows = static_cast<int32_t>(rows); n.cols = static_cast<int32_t>(cols);
   n.r = static_cast<int32_t>(p.r); n.q = static_cast<int32_t>(p.q); n.q_ld = static_cast<int32_t>(p.q_ld);
@@ -299,19 +338,24 @@ int ones_orthogonal_update(const void *grad, float *momentum, int64_t count, int
   q.r = n.r; q.q = n.q; q.r_ld = static_cast<int32_t>(p.r_ld); q.q_ld = n.q_ld;
   q.out_type = update_type;
   q.turned = rows > cols;
+  const int64_t triangle[] = {count * symmetric_tiles<Large>(p.r_ld), count * symmetric_tiles<Middle>(p.r_ld), count * symmetric_tiles<Deep>(p.r_ld),
+                              count * symmetric_tiles<Small>(p.r_ld), count * symmetric_tiles<Tiny>(p.r_ld)};
+  const int64_t all[] = {count * all_tiles<Large>(q), count * all_tiles<MiddleTurned>(q), count * all_tiles<Deep>(q), count * all_tiles<Small>(q),
+                         count * all_tiles<Tiny>(q)};
+  const Tiles for_gram = least(triangle, p.q), for_poly = least(triangle, p.r), for_apply = least(all, p.r);
   for (int32_t step = 0; step < steps; ++step) {
     q.x = x[step & 1];
     q.to = a[0];
-    launch_symmetric<false>(q, count, s);
+    launch_symmetric<false>(q, for_gram, count, s);
     q.a = a[0];
     q.to = a[1];
     q.one = coefficients[1]; q.two = coefficients[2];
-    launch_symmetric<true>(q, count, s);
+    launch_symmetric<true>(q, for_poly, count, s);
     q.a = a[1];
     q.to = x[(step & 1) ^ 1];
     q.out = step + 1 == steps ? update : nullptr;
     q.one = coefficients[0];
-    launch_apply(q, count, s);
+    launch_apply(q, for_apply, count, s);
   }
   return launched("orthogonal update");
 }
