@@ -18,17 +18,35 @@ struct alignas(sizeof(T) * N) Pack {
   T v[N];
 };
 
-// N elements from p: one wide load (p aligned to the pack).
+// N elements from p: one wide load.  (Global memory takes wide accesses at any multiple of an element's size; the copy says so to
+// the compiler.)
 template <typename T, int N>
 __device__ __forceinline__ Pack<T, N> load_pack(const T *p) {
-  return *reinterpret_cast<const Pack<T, N> *>(p);
+  Pack<T, N> v;
+  __builtin_memcpy(&v, p, sizeof(v));
+  return v;
 }
 template <typename T, int N>
 __device__ __forceinline__ void store_pack(T *p, const float *v) {
   Pack<T, N> out;
 #pragma unroll
   for (int i = 0; i < N; ++i) out.v[i] = static_cast<T>(v[i]);
-  *reinterpret_cast<Pack<T, N> *>(p) = out;
+  __builtin_memcpy(p, &out, sizeof(out));
+}
+// The same where only the first n of the elements are there (n may be 0 or less, or more than N).
+template <typename T, int N>
+__device__ __forceinline__ Pack<T, N> load_some(const T *p, int n) {
+  if (n >= N) return load_pack<T, N>(p);
+  Pack<T, N> v;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v.v[i] = i < n ? p[i] : static_cast<T>(0.f);
+  return v;
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_some(T *p, const float *v, int n) {
+  if (n >= N) return store_pack<T, N>(p, v);
+#pragma unroll
+  for (int i = 0; i < N; ++i) if (i < n) p[i] = static_cast<T>(v[i]);
 }
 
 // An element of an array whose type is only known at run time (weights; read once a workgroup).
@@ -44,10 +62,21 @@ __device__ __forceinline__ void store_as(void *p, int type, int64_t i, float v) 
   else static_cast<bf16 *>(p)[i] = static_cast<bf16>(v);
 }
 
+// v of the lane that lies n before in its row of 16, in a ring.
+template <int N>
+__device__ __forceinline__ float from_row(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, true));
+}
+// The sum over the wave, in every lane: rows of 16 by rotations, then the four rows.
 __device__ __forceinline__ float wave_sum(float v) {
+  v += from_row<8>(v);
+  v += from_row<4>(v);
+  v += from_row<2>(v);
+  v += from_row<1>(v);
+  float rows[4];
 #pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) v += __shfl_xor(v, m);
-  return v;
+  for (int i = 0; i < 4; ++i) rows[i] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16 * i));
+  return (rows[0] + rows[1]) + (rows[2] + rows[3]);
 }
 
 // The sums of two values over the THREADS threads of a row, for all of them.  `part`: 2 * THREADS / 64 words of LDS, which the

@@ -18,7 +18,10 @@ namespace train {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kMostPerThread = 32;
+// Backward, whether the next row is read ahead: not by workgroups of 1024 threads, which have 128 registers a thread; they read the
+// weights for every row, too.  (Forward, waves enough for each other's gaps: reading ahead costs 5 to 15 %.)
+template <int TPR>
+constexpr bool kAhead = TPR < 1024;
 
 struct NormArgs {
   const void *x, *dy;
@@ -31,39 +34,45 @@ struct NormArgs {
   float eps;
 };
 
-// Thread t of a row holds elements (k * TPR + t) * VEC + 0..VEC-1, k < PER / VEC.
+// A row as read: thread t holds elements (k * TPR + t) * VEC + 0..VEC-1, k < PER / VEC; zeros beyond the last column.
 template <typename T, int PER, int VEC, int TPR>
-__device__ __forceinline__ void load_row(const T *row, int t, int cols, float *v) {
+struct Row {
+  Pack<T, VEC> p[PER / VEC];
+  __device__ __forceinline__ void load(const T *row, int t, int cols) {
 #pragma unroll
-  for (int k = 0; k < PER / VEC; ++k) {
-    const int c = (k * TPR + t) * VEC;
-    if (c < cols) {
-      const Pack<T, VEC> p = load_pack<T, VEC>(row + c);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) v[k * VEC + i] = static_cast<float>(p.v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) v[k * VEC + i] = 0.f;
+    for (int k = 0; k < PER / VEC; ++k) {
+      const int c = (k * TPR + t) * VEC;
+      p[k] = load_some<T, VEC>(row + c, cols - c);
     }
   }
-}
+  __device__ __forceinline__ float operator[](int i) const { return static_cast<float>(p[i / VEC].v[i % VEC]); }
+};
 template <typename T, int PER, int VEC, int TPR>
 __device__ __forceinline__ void store_row(T *row, int t, int cols, const float *v) {
 #pragma unroll
   for (int k = 0; k < PER / VEC; ++k) {
     const int c = (k * TPR + t) * VEC;
-    if (c < cols) store_pack<T, VEC>(row + c, v + k * VEC);
+    store_some<T, VEC>(row + c, v + k * VEC, cols - c);
   }
+}
+template <typename W, int PER, int VEC, int TPR>
+__device__ __forceinline__ void load_weights_as(const W *p, int t, int cols, float *v) {
+  Row<W, PER, VEC, TPR> row;
+  row.load(p, t, cols);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) v[i] = row[i];
 }
 template <int PER, int VEC, int TPR>
 __device__ __forceinline__ void load_weights(const void *p, int type, float otherwise, int t, int cols, float *v) {
+  if (!p) {
 #pragma unroll
-  for (int k = 0; k < PER / VEC; ++k) {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const int c = (k * TPR + t) * VEC + i;
-      v[k * VEC + i] = c < cols ? (p ? load_as(p, type, c) : otherwise) : 0.f;
-    }
+    for (int i = 0; i < PER; ++i) v[i] = (i / VEC * TPR + t) * VEC + i % VEC < cols ? otherwise : 0.f;
+  } else if (type == kF32) {
+    load_weights_as<float, PER, VEC, TPR>(static_cast<const float *>(p), t, cols, v);
+  } else if (type == kF16) {
+    load_weights_as<f16, PER, VEC, TPR>(static_cast<const f16 *>(p), t, cols, v);
+  } else {
+    load_weights_as<bf16, PER, VEC, TPR>(static_cast<const bf16 *>(p), t, cols, v);
   }
 }
 
@@ -76,25 +85,25 @@ __global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_forward_kern
   load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
   load_weights<PER, VEC, TPR>(a.bias, a.weight_type, 0.f, t, a.cols, b);
   const float n = static_cast<float>(a.cols);
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * rows_at_once + sub; row < a.rows; row += static_cast<int64_t>(gridDim.x) * rows_at_once) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * rows_at_once;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * rows_at_once + sub;
+  const T *x = static_cast<const T *>(a.x);
+  for (; row < a.rows; row += step) {
+    Row<T, PER, VEC, TPR> now;
+    now.load(x + row * a.x_stride, t, a.cols);
     float v[PER];
-    load_row<T, PER, VEC, TPR>(static_cast<const T *>(a.x) + row * a.x_stride, t, a.cols, v);
     float sum = 0.f, none = 0.f, square = 0.f, rest = 0.f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += v[i];
+    for (int i = 0; i < PER; ++i) sum += v[i] = now[i];
     row_sum2<TPR>(sum, none, part[0]);
     float mean = sum / n;
 #pragma unroll
-    for (int k = 0; k < PER / VEC; ++k) {
-      if ((k * TPR + t) * VEC < a.cols) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float d = v[k * VEC + i] - mean;
-          v[k * VEC + i] = d;
-          rest += d;
-          square += d * d;
-        }
-      }
+    for (int i = 0; i < PER; ++i) {
+      const bool inside = (i / VEC * TPR + t) * VEC + i % VEC < a.cols;
+      const float d = inside ? v[i] - mean : 0.f;
+      v[i] = d;
+      rest += d;
+      square += d * d;
     }
     row_sum2<TPR>(square, rest, part[1]);
     // what the first mean was off by (its rounding, where the values lie far from zero) is the mean of the differences
@@ -115,16 +124,32 @@ __global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_backward_ker
   __shared__ float sums[rows_at_once > 1 ? 2 * PER * TPR : 1];
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float w[PER], dw[PER], db[PER];
-  load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
+  if (kAhead<TPR>) load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
 #pragma unroll
   for (int i = 0; i < PER; ++i) dw[i] = db[i] = 0.f;
   const float n = static_cast<float>(a.cols);
   int turn = 0;
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * rows_at_once + sub; row < a.rows; row += static_cast<int64_t>(gridDim.x) * rows_at_once) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * rows_at_once;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * rows_at_once + sub;
+  Row<T, PER, VEC, TPR> x_now, x_next, dy_now, dy_next;
+  float mean_next = 0.f, rstd_next = 0.f;
+  auto load = [&](int64_t r, Row<T, PER, VEC, TPR> &u, Row<T, PER, VEC, TPR> &v) {
+    u.load(static_cast<const T *>(a.x) + r * a.x_stride, t, a.cols);
+    v.load(static_cast<const T *>(a.dy) + r * a.dy_stride, t, a.cols);
+    mean_next = a.mean[r];
+    rstd_next = a.rstd[r];
+  };
+  if (kAhead<TPR> && row < a.rows) load(row, x_now, dy_now);
+  for (; row < a.rows; row += step) {
+    if (!kAhead<TPR>) {
+      load(row, x_now, dy_now);
+      load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
+    }
+    const float mean = mean_next, rstd = rstd_next;
+    if (kAhead<TPR> && row + step < a.rows) load(row + step, x_next, dy_next);
     float x[PER], dy[PER];
-    load_row<T, PER, VEC, TPR>(static_cast<const T *>(a.x) + row * a.x_stride, t, a.cols, x);
-    load_row<T, PER, VEC, TPR>(static_cast<const T *>(a.dy) + row * a.dy_stride, t, a.cols, dy);
-    const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) { x[i] = x_now[i]; dy[i] = dy_now[i]; }
     float sg = 0.f, sgx = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {                 // past the last column dy and w are zero
@@ -142,6 +167,7 @@ __global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_backward_ker
 #pragma unroll
     for (int i = 0; i < PER; ++i) x[i] = rstd * (dy[i] * w[i] - sg - x[i] * sgx);
     store_row<T, PER, VEC, TPR>(static_cast<T *>(a.out) + row * a.cols, t, a.cols, x);
+    if (kAhead<TPR>) { x_now = x_next; dy_now = dy_next; }
   }
   if constexpr (rows_at_once > 1) {                 // the waves' sums, one after another
     for (int s = 0; s < rows_at_once; ++s) {
@@ -161,9 +187,8 @@ __global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_backward_ker
 #pragma unroll
   for (int k = 0; k < PER / VEC; ++k) {
     const int c = (k * TPR + t) * VEC;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i)
-      if (c + i < a.cols) { to[c + i] = dw[k * VEC + i]; to[a.cols + c + i] = db[k * VEC + i]; }
+    store_some<float, VEC>(to + c, dw + k * VEC, a.cols - c);
+    store_some<float, VEC>(to + a.cols + c, db + k * VEC, a.cols - c);
   }
 }
 
@@ -186,12 +211,20 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *partial,
   if (to) store_as(to, type, c < cols ? c : c - cols, s);
 }
 
-int threads_per_row(int64_t cols) { return cols <= 64 * kMostPerThread ? 64 : cols <= 256 * kMostPerThread ? 256 : 1024; }
-// Workgroups: enough for eight waves a SIMD forward; backward at most so many that their partial sums stay a small part of the
-// traffic.
+// Threads of a row: up to 32 elements a thread forward; up to 16 backward, which keeps four of each in registers (beyond 16384
+// columns 32).
+int threads_per_row(int64_t cols, bool backward) {
+  const int64_t most = backward ? 16 : 32;
+  return cols <= 64 * most ? 64 : cols <= 256 * most ? 256 : 1024;
+}
+// Workgroups.  Forward as many as eight waves a SIMD.  Backward what the registers let run at once, since each leaves partial sums
+// behind: with 8 elements a thread four waves a SIMD, with 16 two or three.
+// (Backward, bf16, 32768 x 2048: 256 threads of 8 elements and 1024 workgroups 95 us, 64 of 32 and 512 125 us, 256 of 8 and 2048
+// 114 us; 16384 x 4096: 256 of 16 and 768 110 us, 1024 of 8 148 us; 65536 x 512: 64 of 8 and 1024 43 us, 512 49 us.)
 int64_t norm_blocks(int64_t rows, int64_t cols, bool backward) {
-  const int64_t tpr = threads_per_row(cols), at_once = tpr > kBlock ? 1 : kBlock / tpr;
-  const int64_t most = backward ? (tpr == 1024 ? 256 : 512) : (tpr == 1024 ? 512 : 2048);
+  const int64_t tpr = threads_per_row(cols, backward), at_once = tpr > kBlock ? 1 : kBlock / tpr;
+  const bool few = cols <= tpr * 8;
+  const int64_t most = !backward ? (tpr == 1024 ? 512 : 2048) : tpr == 1024 ? (few ? 512 : 256) : few ? 1024 : tpr == 256 ? 768 : 512;
   return std::min(ceil_div(rows, at_once), most);
 }
 
@@ -205,35 +238,25 @@ void launch_norm(const NormArgs &a, bool backward, hipStream_t s) {
 template <typename T, int VEC, int TPR>
 void launch_norm_per(const NormArgs &a, bool backward, hipStream_t s) {
   const int64_t per = ceil_div(a.cols, TPR);
-  if constexpr (TPR == 64) {
-    if (per <= 8) return launch_norm<T, 8, VEC, TPR>(a, backward, s);
-  }
+  if (per <= 8) return launch_norm<T, 8, VEC, TPR>(a, backward, s);
   if (per <= 16) return launch_norm<T, 16, VEC, TPR>(a, backward, s);
   launch_norm<T, 32, VEC, TPR>(a, backward, s);
 }
 
-template <typename T, int VEC>
-void launch_norm_tpr(const NormArgs &a, bool backward, hipStream_t s) {
-  switch (threads_per_row(a.cols)) {
-    case 64: return launch_norm_per<T, VEC, 64>(a, backward, s);
-    case 256: return launch_norm_per<T, VEC, 256>(a, backward, s);
-    default: return launch_norm_per<T, VEC, 1024>(a, backward, s);
+template <typename T>
+void launch_norm(const NormArgs &a, bool backward, hipStream_t s) {
+  constexpr int vec = 16 / sizeof(T);
+  switch (threads_per_row(a.cols, backward)) {
+    case 64: return launch_norm_per<T, vec, 64>(a, backward, s);
+    case 256: return launch_norm_per<T, vec, 256>(a, backward, s);
+    default: return launch_norm_per<T, vec, 1024>(a, backward, s);
   }
 }
 
-template <typename T>
-void launch_norm_vec(const NormArgs &a, bool backward, hipStream_t s) {
-  constexpr int vec = 16 / sizeof(T);
-  const bool wide = a.cols % vec == 0 && a.x_stride % vec == 0 && aligned(a.x, 16) && aligned(a.out, 16) &&
-                    (!backward || (a.dy_stride % vec == 0 && aligned(a.dy, 16)));
-  if (wide) launch_norm_tpr<T, vec>(a, backward, s);
-  else launch_norm_tpr<T, 1>(a, backward, s);
-}
-
 void launch_norm_type(const NormArgs &a, int32_t type, bool backward, hipStream_t s) {
-  if (type == ONES_F32) launch_norm_vec<float>(a, backward, s);
-  else if (type == ONES_F16) launch_norm_vec<f16>(a, backward, s);
-  else launch_norm_vec<bf16>(a, backward, s);
+  if (type == ONES_F32) launch_norm<float>(a, backward, s);
+  else if (type == ONES_F16) launch_norm<f16>(a, backward, s);
+  else launch_norm<bf16>(a, backward, s);
 }
 
 int check_norm(int64_t rows, int64_t cols, int64_t stride, int32_t type, int32_t weight_type) {
