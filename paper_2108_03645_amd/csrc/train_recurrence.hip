@@ -6,12 +6,12 @@
 // Steps t past a sequence's length keep the state: a_t = 1, no input, h_t written as 0, no gradients.
 //
 // A run of steps acts on the state as h -> A h + H (A the product of its gates), and on what comes back from behind as
-// r -> A r + Q (r_t = a_t l_t); two runs one after another compose.  A workgroup owns 64 channels of one sequence and takes tiles
-// of 128 steps: a thread keeps eight steps of four channels in registers (32 steps of one where the rows do not allow wide
-// loads) and forms its run's A and H, one wave composes the runs of the tile's thread groups through LDS, and every thread walks
-// its steps again from the state before them.  gate, x and dh are read once and everything is written once.  The state before
-// every tile is kept in 32 bits (1/32 of the bytes of a 16-bit h): backward recomputes h from it, which is neither rounded to 16
-// bits nor read.
+// r -> A r + Q (r_t = a_t l_t); two runs one after another compose.  A workgroup owns 64 (or 32) channels of one sequence and
+// takes tiles of 128 steps: a thread keeps eight (or four) steps of four channels in registers and forms its run's A and H, one
+// wave composes the runs of the tile's thread groups through LDS, and every thread walks its steps again from the state before
+// them.  gate, x and dh are read once and everything is written once.  The state before every tile is kept in 32 bits (one for 128
+// elements): backward recomputes h from it, which is neither rounded to 16 bits nor read.  What bounds it is memory; next to it
+// the arithmetic (an exponential and a reciprocal an element) and the chain through a tile's groups.
 //
 // Where sequences and channels are too few for the compute units, the steps are split into segments of whole tiles as well.  A
 // first launch forms each segment's A and H (or Q), and the workgroups of the second compose those of the segments before (or
@@ -20,12 +20,13 @@
 #include "train_host.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ones {
 namespace train {
 namespace {
 
-constexpr int kThreads = 256, kChannels = 64, kTile = 128;
+constexpr int kThreads = 256, kV = 4, kTile = 128;
 
 struct RecurrenceArgs {
   const void *gate, *x, *dh;
@@ -43,35 +44,53 @@ __device__ __forceinline__ int length_of(const RecurrenceArgs &a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.steps) : a.steps;
 }
 
-// The S steps x V channels of this thread's run, as read.
-template <typename T, int S, int V>
+// The S steps of kV channels of this thread's run, as read; zeros from step `len` on and beyond the last channel.  EDGE: the
+// channels are no multiple of kV.
+template <typename T, int S, bool EDGE>
 struct Run {
-  Pack<T, V> p[S];
+  Pack<T, kV> p[S];
   __device__ __forceinline__ void load(const T *base, int64_t step_stride, int t0, int c, int len, int channels) {
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-      if (t0 + i < len && c < channels) p[i] = load_pack<T, V>(base + (t0 + i) * step_stride + c);
+      const T *from = base + (t0 + i) * step_stride + c;
+      if (EDGE) p[i] = load_some<T, kV>(from, t0 + i < len ? channels - c : 0);
+      else if (t0 + i < len && c < channels) p[i] = load_pack<T, kV>(from);
       else
 #pragma unroll
-        for (int k = 0; k < V; ++k) p[i].v[k] = static_cast<T>(0.f);
+        for (int k = 0; k < kV; ++k) p[i].v[k] = static_cast<T>(0.f);
     }
   }
 };
-
-// a = sigmoid(g) and 1 - a, which keeps its digits where a is close to 1.
-__device__ __forceinline__ void gate_of(float g, float &a, float &keep) {
-  const float e = __expf(-g);
-  a = 1.f / (1.f + e);
-  keep = isinf(e) ? 1.f : e * a;
+template <typename T, bool EDGE>
+__device__ __forceinline__ void store_run(T *base, int channels, int t0, int steps, int c, int i, const float *v) {
+  T *to = base + static_cast<int64_t>(t0 + i) * channels + c;
+  if (EDGE) { if (t0 + i < steps) store_some<T, kV>(to, v, channels - c); }
+  else if (t0 + i < steps && c < channels) store_pack<T, kV>(to, v);
 }
 
-template <typename T, int V, bool FORM>     // FORM: only the segments' A and H
+// a = sigmoid(g) and 1 - a, which keeps its digits where a is close to 1.  (The reciprocal is off by one place of 32 bits at most.)
+__device__ __forceinline__ void gate_of(float g, float &a, float &keep) {
+  const float e = __expf(-g);
+  a = __builtin_amdgcn_rcpf(1.f + e);
+  keep = e > 1.f ? 1.f - a : e * a;
+}
+
+// Which block of channels: with narrow blocks, two that share cache lines go to one die, one after the other.
+template <int LANES>
+__device__ __forceinline__ uint32_t block_of() {
+  if constexpr (LANES == 16) return blockIdx.x;
+  const uint32_t whole = gridDim.x / 16 * 16, id = blockIdx.x;
+  if (id >= whole) return id;
+  return id / 16 * 16 + id % 8 * 2 + id % 16 / 8;
+}
+
+template <typename T, int LANES, bool EDGE, bool FORM>     // FORM: only the segments' A and H
 __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(RecurrenceArgs a) {
-  constexpr int lanes = kChannels / V, groups = kThreads / lanes, S = kTile / groups;
+  constexpr int V = kV, kChannels = LANES * V, groups = kThreads / LANES, S = kTile / groups;
   __shared__ float sa[groups][kChannels], sh[groups][kChannels];
-  const int b = blockIdx.y, segment = blockIdx.z, c0 = blockIdx.x * kChannels;
+  const int b = blockIdx.y, segment = blockIdx.z, c0 = static_cast<int>(block_of<LANES>()) * kChannels;
   if (FORM && segment == a.n_segments - 1) return;   // nothing comes after it
-  const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes, c = c0 + lane * V;
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, c = c0 + lane * V;
   const int len = length_of(a, b);
   const T *gate = static_cast<const T *>(a.gate) + b * a.gate_batch, *x = static_cast<const T *>(a.x) + b * a.x_batch;
   T *h = FORM ? nullptr : static_cast<T *>(a.h) + static_cast<int64_t>(b) * a.steps * a.channels;
@@ -86,17 +105,18 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
 #pragma unroll 4
     for (int s = 0; s < segment; ++s, seg += 2 * a.channels) state = seg[0] * state + seg[a.channels];
   }
-  Run<T, S, V> g, u;
+  Run<T, S, EDGE> g, u;
   g.load(gate, a.gate_step, first * kTile + group * S, c, len, a.channels);
   u.load(x, a.x_step, first * kTile + group * S, c, len, a.channels);
-  for (int tile = first; tile < end; ++tile) {
+  auto body = [&](int tile, auto whole) {          // whole: no step of the tile is past the length
+    constexpr bool all = decltype(whole)::value;
     const int t0 = tile * kTile + group * S;
     float ga[S][V], in[S][V], A[V], H[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) { A[k] = 1.f; H[k] = 0.f; }
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-      const bool live = t0 + i < len;
+      const bool live = all || t0 + i < len;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         float r, q;
@@ -104,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
         ga[i][k] = live ? r : 1.f;
         in[i][k] = live ? q * static_cast<float>(u.p[i].v[k]) : 0.f;
         A[k] *= ga[i][k];
-        H[k] = ga[i][k] * H[k] + in[i][k];
+        H[k] = __builtin_fmaf(ga[i][k], H[k], in[i][k]);
       }
     }
     if (tile + 1 < end) {                        // the next tile's rows arrive while this one is put together
@@ -116,12 +136,15 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
     __syncthreads();
     if (threadIdx.x < kChannels) {
       if (!FORM && keeps && a.carry) a.carry[(static_cast<int64_t>(b) * a.tiles + tile) * a.channels + own] = state;
+      float as[groups], hs[groups];              // all read before the chain
+#pragma unroll
+      for (int s = 0; s < groups; ++s) { as[s] = sa[s][threadIdx.x]; hs[s] = sh[s][threadIdx.x]; }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int s = 0; s < groups; ++s) {
-        const float as = sa[s][threadIdx.x], hs = sh[s][threadIdx.x];
         sh[s][threadIdx.x] = state;              // before the group's first step
-        state = as * state + hs;
-        if (FORM) through *= as;
+        state = __builtin_fmaf(as[s], state, hs[s]);
+        if (FORM) through *= as[s];
       }
     }
     __syncthreads();
@@ -134,13 +157,17 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
         float out[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          now[k] = ga[i][k] * now[k] + in[i][k];
-          out[k] = t0 + i < len ? now[k] : 0.f;
+          now[k] = __builtin_fmaf(ga[i][k], now[k], in[i][k]);
+          out[k] = all || t0 + i < len ? now[k] : 0.f;
         }
-        if (t0 + i < a.steps && c < a.channels) store_pack<T, V>(h + static_cast<int64_t>(t0 + i) * a.channels + c, out);
+        store_run<T, EDGE>(h, a.channels, t0, a.steps, c, i, out);
       }
       __syncthreads();                           // sh is written anew
     }
+  };
+  for (int tile = first; tile < end; ++tile) {
+    if ((tile + 1) * kTile <= len) body(tile, std::true_type{});
+    else body(tile, std::false_type{});
   }
   if (!keeps) return;
   if (FORM) {
@@ -152,21 +179,21 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
   }
 }
 
-template <typename T, int V, bool FORM>     // FORM: only the segments' A and Q
+template <typename T, int LANES, bool EDGE, bool FORM>     // FORM: only the segments' A and Q
 __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(RecurrenceArgs a) {
-  constexpr int lanes = kChannels / V, groups = kThreads / lanes, S = kTile / groups;
+  constexpr int V = kV, kChannels = LANES * V, groups = kThreads / LANES, S = kTile / groups;
   __shared__ float sa[groups][kChannels], sh[groups][kChannels], sq[groups][kChannels];
-  const int b = blockIdx.y, segment = blockIdx.z, c0 = blockIdx.x * kChannels;
+  const int b = blockIdx.y, segment = blockIdx.z, c0 = static_cast<int>(block_of<LANES>()) * kChannels;
   if (FORM && segment == 0) return;                  // nothing comes before it
-  const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes, c = c0 + lane * V;
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, c = c0 + lane * V;
   const int len = length_of(a, b);
   const T *gate = static_cast<const T *>(a.gate) + b * a.gate_batch, *x = static_cast<const T *>(a.x) + b * a.x_batch;
   const T *dh = static_cast<const T *>(a.dh) + b * a.dh_batch;
   const int64_t out = static_cast<int64_t>(b) * a.steps * a.channels;
   const int first = segment * a.tiles_per_segment, end = min(a.tiles, first + a.tiles_per_segment);
   // the second wave keeps what comes back from behind, the first composes the states
-  const int own = c0 + static_cast<int>(threadIdx.x % kChannels);
-  const bool second = threadIdx.x / kChannels == 1, keeps = second && own < a.channels;
+  const int at = static_cast<int>(threadIdx.x) % kWave, own = c0 + at;
+  const bool second = threadIdx.x / kWave == 1, keeps = second && at < kChannels && own < a.channels;
   float back = 0.f, through = 1.f;
   if (!FORM && keeps) {
     if (a.dlast) back = a.dlast[static_cast<int64_t>(b) * a.channels + own];
@@ -174,39 +201,44 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
 #pragma unroll 4
     for (int s = a.n_segments - 1; s > segment; --s, seg -= 2 * a.channels) back = seg[0] * back + seg[a.channels];
   }
-  Run<T, S, V> g, u, d;
+  Run<T, S, EDGE> g, u, d;
+  float carry = 0.f;                             // of the first wave's threads
+  auto load_carry = [&](int tile) {
+    if (!FORM && threadIdx.x < kChannels && own < a.channels) carry = a.carry[(static_cast<int64_t>(b) * a.tiles + tile) * a.channels + own];
+  };
   if (end > first) {                             // always, but for sequences of no steps
+    load_carry(end - 1);
     const int t0 = (end - 1) * kTile + group * S;
     g.load(gate, a.gate_step, t0, c, len, a.channels);
     if (!FORM) u.load(x, a.x_step, t0, c, len, a.channels);
     d.load(dh, a.dh_step, t0, c, len, a.channels);
   }
-  for (int tile = end - 1; tile >= first; --tile) {
+  auto body = [&](int tile, auto whole) {          // whole: no step of the tile is past the length
+    constexpr bool all = decltype(whole)::value;
     const int t0 = tile * kTile + group * S;
-    float ga[S][V], keep[S][V], xs[S][V], ds[S][V], A[V], H[V], Q[V];
+    float ga[S][V], keep[S][V], A[V], H[V], Q[V];
+    const Run<T, S, EDGE> u0 = u, d0 = d;                // as read: half the registers
+    auto xs = [&](int i, int k) { return static_cast<float>(u0.p[i].v[k]); };
+    auto ds = [&](int i, int k) { return static_cast<float>(d0.p[i].v[k]); };
 #pragma unroll
     for (int k = 0; k < V; ++k) { A[k] = 1.f; H[k] = Q[k] = 0.f; }
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-      const bool live = t0 + i < len;
+      const bool live = all || t0 + i < len;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         float r, q;
         gate_of(static_cast<float>(g.p[i].v[k]), r, q);
         ga[i][k] = live ? r : 1.f;
         keep[i][k] = live ? q : 0.f;
-        ds[i][k] = static_cast<float>(d.p[i].v[k]);
         A[k] *= ga[i][k];
-        if (!FORM) {
-          xs[i][k] = static_cast<float>(u.p[i].v[k]);
-          H[k] = ga[i][k] * H[k] + (live ? keep[i][k] * xs[i][k] : 0.f);
-        }
+        if (!FORM) H[k] = __builtin_fmaf(ga[i][k], H[k], live ? keep[i][k] * xs(i, k) : 0.f);
       }
     }
 #pragma unroll
     for (int i = S - 1; i >= 0; --i)
 #pragma unroll
-      for (int k = 0; k < V; ++k) Q[k] = ga[i][k] * (ds[i][k] + Q[k]);
+      for (int k = 0; k < V; ++k) Q[k] = ga[i][k] * (ds(i, k) + Q[k]);
     if (tile > first) {
       g.load(gate, a.gate_step, t0 - kTile, c, len, a.channels);
       if (!FORM) u.load(x, a.x_step, t0 - kTile, c, len, a.channels);
@@ -219,22 +251,28 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
       if (!FORM) sh[group][lane * V + k] = H[k];
     }
     __syncthreads();
-    if (second) {
+    if (second && threadIdx.x % kWave < kChannels) {
+      float as[groups], qs[groups];              // all read before the chain
+#pragma unroll
+      for (int s = 0; s < groups; ++s) { as[s] = sa[s][at]; qs[s] = sq[s][at]; }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int s = groups - 1; s >= 0; --s) {
-        const float as = sa[s][threadIdx.x % kChannels], qs = sq[s][threadIdx.x % kChannels];
-        sq[s][threadIdx.x % kChannels] = back;   // from behind the group's last step
-        back = as * back + qs;
-        if (FORM) through *= as;
+        sq[s][at] = back;                        // from behind the group's last step
+        back = __builtin_fmaf(as[s], back, qs[s]);
+        if (FORM) through *= as[s];
       }
     } else if (!FORM && threadIdx.x < kChannels) {
-      float state = own < a.channels ? a.carry[(static_cast<int64_t>(b) * a.tiles + tile) * a.channels + own] : 0.f;
+      float state = carry, as[groups], hs[groups];
+#pragma unroll
+      for (int s = 0; s < groups; ++s) { as[s] = sa[s][at]; hs[s] = sh[s][at]; }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int s = 0; s < groups; ++s) {
-        const float as = sa[s][threadIdx.x], hs = sh[s][threadIdx.x];
-        sh[s][threadIdx.x] = state;
-        state = as * state + hs;
+        sh[s][at] = state;
+        state = __builtin_fmaf(as[s], state, hs[s]);
       }
+      if (tile > first) load_carry(tile - 1);
     }
     __syncthreads();
     if constexpr (!FORM) {
@@ -246,27 +284,29 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
 #pragma unroll
         for (int i = 0; i < S; ++i) {
           before[i][k] = now;
-          now = ga[i][k] * now + (t0 + i < len ? keep[i][k] * xs[i][k] : 0.f);
+          now = __builtin_fmaf(ga[i][k], now, all || t0 + i < len ? keep[i][k] * xs(i, k) : 0.f);
         }
       }
 #pragma unroll
       for (int i = S - 1; i >= 0; --i) {
-        const bool live = t0 + i < len;
+        const bool live = all || t0 + i < len;
         float dg[V], dx[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const float l = ds[i][k] + r[k];
+          const float l = ds(i, k) + r[k];
           r[k] = ga[i][k] * l;
           dx[k] = live ? keep[i][k] * l : 0.f;
-          dg[k] = live ? r[k] * keep[i][k] * (before[i][k] - xs[i][k]) : 0.f;
+          dg[k] = live ? r[k] * keep[i][k] * (before[i][k] - xs(i, k)) : 0.f;
         }
-        if (t0 + i < a.steps && c < a.channels) {
-          store_pack<T, V>(static_cast<T *>(a.dgate) + out + static_cast<int64_t>(t0 + i) * a.channels + c, dg);
-          store_pack<T, V>(static_cast<T *>(a.dx) + out + static_cast<int64_t>(t0 + i) * a.channels + c, dx);
-        }
+        store_run<T, EDGE>(static_cast<T *>(a.dgate) + out, a.channels, t0, a.steps, c, i, dg);
+        store_run<T, EDGE>(static_cast<T *>(a.dx) + out, a.channels, t0, a.steps, c, i, dx);
       }
     }
     __syncthreads();
+  };
+  for (int tile = end - 1; tile >= first; --tile) {
+    if ((tile + 1) * kTile <= len) body(tile, std::true_type{});
+    else body(tile, std::false_type{});
   }
   if (!keeps) return;
   if (FORM) {
@@ -278,68 +318,74 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
   }
 }
 
-// One step, the state updated in place: an element a thread (four with wide rows).
-template <typename T, int V>
+// One step, the state updated in place: four channels a thread.
+template <typename T>
 __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(const T *gate, const T *x, float *state, T *h, int64_t batch, int32_t channels,
                                                                   int64_t gate_stride, int64_t x_stride) {
-  const int32_t packs = (channels + V - 1) / V;
+  const int32_t packs = (channels + kV - 1) / kV;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
   if (i >= batch * packs) return;
   const int64_t b = i / packs;
-  const int c = static_cast<int>(i - b * packs) * V;
-  const Pack<T, V> g = load_pack<T, V>(gate + b * gate_stride + c), u = load_pack<T, V>(x + b * x_stride + c);
+  const int c = static_cast<int>(i - b * packs) * kV, have = channels - c;
+  const Pack<T, kV> g = load_some<T, kV>(gate + b * gate_stride + c, have), u = load_some<T, kV>(x + b * x_stride + c, have);
   float *s = state + b * channels + c;
-  const Pack<float, V> old = load_pack<float, V>(s);
-  float now[V];
+  const Pack<float, kV> old = load_some<float, kV>(s, have);
+  float now[kV];
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
+  for (int k = 0; k < kV; ++k) {
     float r, q;
     gate_of(static_cast<float>(g.v[k]), r, q);
     now[k] = r * old.v[k] + q * static_cast<float>(u.v[k]);
   }
-  store_pack<float, V>(s, now);
-  store_pack<T, V>(h + b * channels + c, now);
+  store_some<float, kV>(s, now, have);
+  store_some<T, kV>(h + b * channels + c, now, have);
 }
 
 int64_t tiles_of(int64_t steps) { return ceil_div(steps, kTile); }
 
-// Segments: as many as fill the compute units with a few workgroups each, of four tiles at least.
-void split(int64_t batch, int64_t steps, int64_t channels, int32_t &n, int32_t &tiles_each) {
-  const int64_t tiles = tiles_of(steps), chains = batch * ceil_div(channels, kChannels);
-  int64_t want = chains >= 192 ? 1 : std::min(ceil_div(1024, std::max<int64_t>(chains, 1)), tiles / 4);
-  want = std::max<int64_t>(1, want);
-  tiles_each = static_cast<int32_t>(std::max<int64_t>(1, ceil_div(tiles, want)));
-  n = static_cast<int32_t>(std::max<int64_t>(1, ceil_div(tiles, tiles_each)));
+// How the work is cut.  Workgroups of 32 channels (8 lanes to a row) are twice as many as of 64, and two share every cache line
+// of 128 bytes: on the same die, at about the same time.  Where they are enough for most compute units, or the steps too few to
+// split, they are faster forward, and backward (with five arrays instead of three) on short sequences, before two that share
+// lines drift apart (us, 32 against 64 channels, bf16: forward 16 x 2048 x 1024 39 against 44, 64 x 256 x 1024 21 and 22, 8 x 512 x 512
+// 8.7 and 11.5; backward 95 and 80, 33 and 42, 11.4 and 16.2).  Otherwise 64 channels, and segments of four tiles at least that
+// make about two workgroups a compute unit (2 x 65521 x 512: 512 workgroups 136 and 213 us, 1024 153 and 267, 256 159 and 234;
+// with 32 channels 172 and 247).
+struct Cut {
+  int32_t lanes, segments, tiles_each;
+};
+Cut cut_of(int64_t batch, int64_t steps, int64_t channels, bool backward) {
+  const int64_t tiles = tiles_of(steps), narrow = batch * ceil_div(channels, 32), chains = batch * ceil_div(channels, 64);
+  if ((narrow >= 192 || tiles < 8) && (!backward || tiles <= 8)) return Cut{8, 1, static_cast<int32_t>(std::max<int64_t>(1, tiles))};
+  const int64_t want = chains >= 192 ? 1 : std::max<int64_t>(1, std::min(ceil_div(512, std::max<int64_t>(chains, 1)), tiles / 4));
+  const int64_t each = std::max<int64_t>(1, ceil_div(tiles, want));
+  return Cut{16, static_cast<int32_t>(std::max<int64_t>(1, ceil_div(tiles, each))), static_cast<int32_t>(each)};
 }
 
-template <typename T, int V>
+template <typename T, int LANES, bool EDGE, bool FORM>
 void launch_recurrence(const RecurrenceArgs &a, bool backward, hipStream_t s) {
-  const uint32_t blocks = static_cast<uint32_t>(ceil_div(a.channels, kChannels));
-  const dim3 grid(blocks, static_cast<uint32_t>(a.batch), static_cast<uint32_t>(a.n_segments));
-  if (backward) {
-    if (a.n_segments > 1) hipLaunchKernelGGL((recurrence_backward_kernel<T, V, true>), grid, dim3(kThreads), 0, s, a);
-    hipLaunchKernelGGL((recurrence_backward_kernel<T, V, false>), grid, dim3(kThreads), 0, s, a);
-  } else {
-    if (a.n_segments > 1) hipLaunchKernelGGL((recurrence_forward_kernel<T, V, true>), grid, dim3(kThreads), 0, s, a);
-    hipLaunchKernelGGL((recurrence_forward_kernel<T, V, false>), grid, dim3(kThreads), 0, s, a);
-  }
+  const dim3 grid(static_cast<uint32_t>(ceil_div(a.channels, LANES * kV)), static_cast<uint32_t>(a.batch), static_cast<uint32_t>(a.n_segments));
+  if (backward) hipLaunchKernelGGL((recurrence_backward_kernel<T, LANES, EDGE, FORM>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((recurrence_forward_kernel<T, LANES, EDGE, FORM>), grid, dim3(kThreads), 0, s, a);
 }
-
+template <typename T, bool EDGE>
+void launch_recurrence(const RecurrenceArgs &a, int32_t lanes, bool backward, hipStream_t s) {
+  if (lanes == 8) return launch_recurrence<T, 8, EDGE, false>(a, backward, s);
+  if (a.n_segments > 1) launch_recurrence<T, 16, EDGE, true>(a, backward, s);
+  launch_recurrence<T, 16, EDGE, false>(a, backward, s);
+}
 template <typename T>
-void launch_recurrence_vec(const RecurrenceArgs &a, bool backward, hipStream_t s) {
-  const int64_t bytes = 4 * sizeof(T);
-  bool wide = a.channels % 4 == 0 && a.gate_batch % 4 == 0 && a.gate_step % 4 == 0 && a.x_batch % 4 == 0 && a.x_step % 4 == 0 &&
-              aligned(a.gate, bytes) && aligned(a.x, bytes);
-  if (backward) wide = wide && a.dh_batch % 4 == 0 && a.dh_step % 4 == 0 && aligned(a.dh, bytes) && aligned(a.dgate, bytes) && aligned(a.dx, bytes);
-  else wide = wide && aligned(a.h, bytes);
-  if (wide) launch_recurrence<T, 4>(a, backward, s);
-  else launch_recurrence<T, 1>(a, backward, s);
+void launch_recurrence(const RecurrenceArgs &a, int32_t lanes, bool backward, hipStream_t s) {
+  if (a.channels % kV) launch_recurrence<T, true>(a, lanes, backward, s);
+  else launch_recurrence<T, false>(a, lanes, backward, s);
 }
 
-void launch_recurrence_type(const RecurrenceArgs &a, int32_t type, bool backward, hipStream_t s) {
-  if (type == ONES_F32) launch_recurrence_vec<float>(a, backward, s);
-  else if (type == ONES_F16) launch_recurrence_vec<f16>(a, backward, s);
-  else launch_recurrence_vec<bf16>(a, backward, s);
+void launch_recurrence_type(RecurrenceArgs &a, int32_t type, bool backward, hipStream_t s) {
+  const Cut cut = cut_of(a.batch, a.steps, a.channels, backward);
+  a.n_segments = cut.segments;
+  a.tiles_per_segment = cut.tiles_each;
+  if (type == ONES_F32) launch_recurrence<float>(a, cut.lanes, backward, s);
+  else if (type == ONES_F16) launch_recurrence<f16>(a, cut.lanes, backward, s);
+  else launch_recurrence<bf16>(a, cut.lanes, backward, s);
 }
 
 int check_recurrence(int64_t batch, int64_t steps, int64_t channels, int32_t type) {
@@ -356,13 +402,9 @@ int check_strides(int64_t batch_stride, int64_t step_stride, int64_t channels) {
 template <typename T>
 void launch_step(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride, int64_t batch, int64_t channels, float *state, void *h,
                  hipStream_t s) {
-  const bool wide = channels % 4 == 0 && gate_stride % 4 == 0 && x_stride % 4 == 0 && aligned(gate, 4 * sizeof(T)) && aligned(x, 4 * sizeof(T)) &&
-                    aligned(h, 4 * sizeof(T)) && aligned(state, 16);
-  const int64_t packs = batch * (wide ? channels / 4 : channels);
-  const dim3 grid(static_cast<uint32_t>(ceil_div(packs, kThreads)));
-  const T *g = static_cast<const T *>(gate), *u = static_cast<const T *>(x);
-  if (wide) hipLaunchKernelGGL((recurrence_step_kernel<T, 4>), grid, dim3(kThreads), 0, s, g, u, state, static_cast<T *>(h), batch, static_cast<int32_t>(channels), gate_stride, x_stride);
-  else hipLaunchKernelGGL((recurrence_step_kernel<T, 1>), grid, dim3(kThreads), 0, s, g, u, state, static_cast<T *>(h), batch, static_cast<int32_t>(channels), gate_stride, x_stride);
+  const dim3 grid(static_cast<uint32_t>(ceil_div(batch * ceil_div(channels, kV), kThreads)));
+  hipLaunchKernelGGL((recurrence_step_kernel<T>), grid, dim3(kThreads), 0, s, static_cast<const T *>(gate), static_cast<const T *>(x), state,
+                     static_cast<T *>(h), batch, static_cast<int32_t>(channels), gate_stride, x_stride);
 }
 
 size_t carry_floats(int64_t batch, int64_t steps, int64_t channels) { return static_cast<size_t>(batch) * tiles_of(steps) * channels; }
@@ -382,9 +424,8 @@ size_t ones_recurrence_carry_bytes(int64_t batch, int64_t steps, int64_t channel
 
 size_t ones_recurrence_workspace_bytes(int64_t batch, int64_t steps, int64_t channels) {
   if (check_recurrence(batch, steps, channels, ONES_F32) != ONES_OK) return 0;
-  int32_t n, each;
-  split(batch, steps, channels, n, each);
-  return n > 1 ? align_up(static_cast<size_t>(batch) * n * 2 * channels * 4) : 0;
+  const int64_t n = std::max(cut_of(batch, steps, channels, false).segments, cut_of(batch, steps, channels, true).segments);
+  return n > 1 ? align_up(static_cast<size_t>(batch * n * 2 * channels * 4)) : 0;
 }
 
 int ones_recurrence_forward(const void *gate, int64_t gate_batch_stride, int64_t gate_step_stride, const void *x, int64_t x_batch_stride,
@@ -403,7 +444,6 @@ int ones_recurrence_forward(const void *gate, int64_t gate_batch_stride, int64_t
   a.gate_batch = gate_batch_stride; a.gate_step = gate_step_stride; a.x_batch = x_batch_stride; a.x_step = x_step_stride;
   a.batch = static_cast<int32_t>(batch); a.steps = static_cast<int32_t>(steps); a.channels = static_cast<int32_t>(channels);
   a.tiles = static_cast<int32_t>(tiles_of(steps));
-  split(batch, steps, channels, a.n_segments, a.tiles_per_segment);
   launch_recurrence_type(a, type, false, static_cast<hipStream_t>(hip_stream));
   return launched("recurrence forward");
 }
@@ -428,7 +468,6 @@ int ones_recurrence_backward(const void *dh, int64_t dh_batch_stride, int64_t dh
   a.dh_batch = dh_batch_stride; a.dh_step = dh_step_stride;
   a.batch = static_cast<int32_t>(batch); a.steps = static_cast<int32_t>(steps); a.channels = static_cast<int32_t>(channels);
   a.tiles = static_cast<int32_t>(tiles_of(steps));
-  split(batch, steps, channels, a.n_segments, a.tiles_per_segment);
   launch_recurrence_type(a, type, true, static_cast<hipStream_t>(hip_stream));
   return launched("recurrence backward");
 }
