@@ -1,0 +1,54 @@
+"""The job that trains at the local batch the search gives it (paper_2108_03645_amd/elastic_job.py)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2108_03645_amd import elastic_job
+
+
+def test_a_line_through_step_times():
+    a, d = elastic_job.fit([16, 32, 64], [0.010 + 16e-5, 0.010 + 32e-5, 0.010 + 64e-5])
+    assert abs(a - 1e-5) < 1e-12 and abs(d - 0.010) < 1e-12
+    assert elastic_job.fit([8, 16], [2.0, 1.0]) == (0.0, 1.5)         # a falling line: no slope, the mean
+    assert elastic_job.fit([8], [2.0]) == (0.0, 2.0)
+
+
+def test_local_batch_of_a_placement():
+    slots, batches = np.array([2, 2, 0, -1]), np.array([64, 64, 128, 0])
+    assert [elastic_job.local_batch(s, slots, batches) for s in (0, 1, 2)] == [128, 0, 64]
+
+
+@pytest.mark.gpu
+def test_the_model_learns_the_language_and_continues_it(capsys):
+    losses, right = elastic_job.main(steps=60, generations=5)
+    print(capsys.readouterr().out)
+    # a uniform guess costs log 4000 = 8.3, the language itself 0.9 log(1 / 0.9) + 0.1 log(4000 / 0.1) = 1.2
+    assert losses[0] > 7 and losses[-1] < 4 and right > 0.5
+    assert np.isfinite(losses).all()
+
+
+@pytest.mark.gpu
+def test_single_steps_continue_like_the_whole_sequence():
+    model = elastic_job.Model(vocabulary=300, width=64, blocks=2, seed=3)
+    tokens = torch.randint(0, 300, (5, 21), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    answer = model.continue_from(tokens, 6)
+    for n in range(6):
+        with torch.no_grad():
+            y, _ = model.hidden(torch.cat([tokens, answer[:, :n]], 1))
+            z = y[:, -1].float() @ model.output.float().t()
+        # the step's choice is the likeliest word up to the roundings of 16 bits on the way
+        chosen = z.gather(1, answer[:, n:n + 1])[:, 0]
+        assert (z.max(1).values - chosen).max() < 0.25, n
+
+
+@pytest.mark.gpu
+def test_the_batch_may_change_and_padding_does_not_count():
+    model = elastic_job.Model(vocabulary=200, width=64, blocks=1)
+    worker, language = elastic_job.Worker(model), elastic_job.Language(200, 24)
+    for n in (1, 7, 32, 3):
+        assert worker.step(language.batch(n)).isfinite()
+    tokens = language.batch(4)
+    padded = torch.cat([tokens, torch.full((4, 5), -1, device="cuda")], 1)
+    with torch.no_grad():
+        whole, short = model.loss(padded), model.loss(tokens)
+    assert abs(whole - short) < 1e-5 * short
