@@ -14,8 +14,9 @@
 // the arithmetic (an exponential and a reciprocal an element) and the chain through a tile's groups.
 //
 // Where sequences and channels are too few for the compute units, the steps are split into segments of whole tiles as well.  A
-// first launch forms each segment's A and H (or Q), and the workgroups of the second compose those of the segments before (or
-// behind) their own: the inputs are read twice then.  No workgroup waits for another, and the order of all sums is fixed.
+// first launch forms each segment's A and H (or Q), a small second one turns them into the state before (what comes from behind)
+// each, and the third walks along the segments side by side: the inputs are read twice then.  No workgroup waits for another, and
+// the order of all sums is fixed.
 #include "train_device.h"
 #include "train_host.h"
 
@@ -35,7 +36,7 @@ struct RecurrenceArgs {
   float *last, *dstate;            // may be null
   const int32_t *lengths;          // may be null: all steps
   float *carry;                    // [batch][tiles][channels]: the state before every tile; forward may be null
-  float *segments;                 // [batch][segments][2][channels]
+  float *segments;                 // [batch][segments][2][channels]: A and H (Q) of each, then the state before it (from behind it) for H
   int64_t gate_batch, gate_step, x_batch, x_step, dh_batch, dh_step;
   int32_t batch, steps, channels, tiles, n_segments, tiles_per_segment;
 };
@@ -75,21 +76,36 @@ __device__ __forceinline__ void gate_of(float g, float &a, float &keep) {
   keep = e > 1.f ? 1.f - a : e * a;
 }
 
-// Which block of channels: with narrow blocks, two that share cache lines go to one die, one after the other.
+// Which channels, sequence and segment.  Two blocks of 32 channels share cache lines: they go to one die, one right after the
+// other (ids go round the eight dies).
+struct Work {
+  int32_t c0, b, segment;
+  bool any;
+};
 template <int LANES>
-__device__ __forceinline__ uint32_t block_of() {
-  if constexpr (LANES == 16) return blockIdx.x;
-  const uint32_t whole = gridDim.x / 16 * 16, id = blockIdx.x;
-  if (id >= whole) return id;
-  return id / 16 * 16 + id % 8 * 2 + id % 16 / 8;
+__device__ __forceinline__ Work work_of(const RecurrenceArgs &a) {
+  const uint32_t id = blockIdx.x, blocks = (a.channels + LANES * kV - 1) / (LANES * kV);
+  uint32_t rest, block;
+  if constexpr (LANES == 16) {
+    rest = id / blocks;
+    block = id % blocks;
+  } else {
+    const uint32_t pair = id / 16 * 8 + id % 8, pairs = (blocks + 1) / 2;
+    rest = pair / pairs;
+    block = pair % pairs * 2 + id % 16 / 8;
+  }
+  const uint32_t b = rest % static_cast<uint32_t>(a.batch), segment = rest / static_cast<uint32_t>(a.batch);
+  return Work{static_cast<int32_t>(block * LANES * kV), static_cast<int32_t>(b), static_cast<int32_t>(segment),
+              block < blocks && segment < static_cast<uint32_t>(a.n_segments)};
 }
 
 template <typename T, int LANES, bool EDGE, bool FORM>     // FORM: only the segments' A and H
 __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(RecurrenceArgs a) {
   constexpr int V = kV, kChannels = LANES * V, groups = kThreads / LANES, S = kTile / groups;
   __shared__ float sa[groups][kChannels], sh[groups][kChannels];
-  const int b = blockIdx.y, segment = blockIdx.z, c0 = static_cast<int>(block_of<LANES>()) * kChannels;
-  if (FORM && segment == a.n_segments - 1) return;   // nothing comes after it
+  const Work work = work_of<LANES>(a);
+  const int b = work.b, segment = work.segment, c0 = work.c0;
+  if (!work.any || (FORM && segment == a.n_segments - 1)) return;   // nothing comes after the last
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, c = c0 + lane * V;
   const int len = length_of(a, b);
   const T *gate = static_cast<const T *>(a.gate) + b * a.gate_batch, *x = static_cast<const T *>(a.x) + b * a.x_batch;
@@ -100,10 +116,8 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
   const bool keeps = threadIdx.x < kChannels && own < a.channels;
   float state = 0.f, through = 1.f;
   if (!FORM && keeps) {
-    if (a.state) state = a.state[static_cast<int64_t>(b) * a.channels + own];
-    const float *seg = a.segments + static_cast<int64_t>(b) * a.n_segments * 2 * a.channels + own;
-#pragma unroll 4
-    for (int s = 0; s < segment; ++s, seg += 2 * a.channels) state = seg[0] * state + seg[a.channels];
+    if (segment) state = a.segments[((static_cast<int64_t>(b) * a.n_segments + segment) * 2 + 1) * a.channels + own];
+    else if (a.state) state = a.state[static_cast<int64_t>(b) * a.channels + own];
   }
   Run<T, S, EDGE> g, u;
   g.load(gate, a.gate_step, first * kTile + group * S, c, len, a.channels);
@@ -183,8 +197,9 @@ template <typename T, int LANES, bool EDGE, bool FORM>     // FORM: only the seg
 __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(RecurrenceArgs a) {
   constexpr int V = kV, kChannels = LANES * V, groups = kThreads / LANES, S = kTile / groups;
   __shared__ float sa[groups][kChannels], sh[groups][kChannels], sq[groups][kChannels];
-  const int b = blockIdx.y, segment = blockIdx.z, c0 = static_cast<int>(block_of<LANES>()) * kChannels;
-  if (FORM && segment == 0) return;                  // nothing comes before it
+  const Work work = work_of<LANES>(a);
+  const int b = work.b, segment = work.segment, c0 = work.c0;
+  if (!work.any || (FORM && segment == 0)) return;                  // nothing comes before the first
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, c = c0 + lane * V;
   const int len = length_of(a, b);
   const T *gate = static_cast<const T *>(a.gate) + b * a.gate_batch, *x = static_cast<const T *>(a.x) + b * a.x_batch;
@@ -196,10 +211,8 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
   const bool second = threadIdx.x / kWave == 1, keeps = second && at < kChannels && own < a.channels;
   float back = 0.f, through = 1.f;
   if (!FORM && keeps) {
-    if (a.dlast) back = a.dlast[static_cast<int64_t>(b) * a.channels + own];
-    const float *seg = a.segments + (static_cast<int64_t>(b) * a.n_segments + a.n_segments - 1) * 2 * a.channels + own;
-#pragma unroll 4
-    for (int s = a.n_segments - 1; s > segment; --s, seg -= 2 * a.channels) back = seg[0] * back + seg[a.channels];
+    if (segment + 1 < a.n_segments) back = a.segments[((static_cast<int64_t>(b) * a.n_segments + segment) * 2 + 1) * a.channels + own];
+    else if (a.dlast) back = a.dlast[static_cast<int64_t>(b) * a.channels + own];
   }
   Run<T, S, EDGE> g, u, d;
   float carry = 0.f;                             // of the first wave's threads
@@ -318,6 +331,44 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
   }
 }
 
+// The second launch of the split form: the A and H of the segments of 64 channels of a sequence, in sixteen parts; each
+// segment's H becomes the state before it, or (BACK) what comes from behind it.
+constexpr int kParts = 16;
+template <bool BACK>
+__global__ __launch_bounds__(64 * kParts) void recurrence_join_kernel(RecurrenceArgs a) {
+  __shared__ float sa[kParts][64], sh[kParts][64];
+  const int lane = threadIdx.x % 64, part = threadIdx.x / 64, c = blockIdx.x * 64 + lane, b = blockIdx.y;
+  const bool inside = c < a.channels;
+  const int each = (a.n_segments + kParts - 1) / kParts, lo = part * each, n = max(0, min(a.n_segments, lo + each) - lo);
+  float *seg = a.segments + static_cast<int64_t>(b) * a.n_segments * 2 * a.channels + c;
+  // the i-th segment of the part in the order they are passed through; the last one of all passes nothing on
+  auto at = [&](int i) { return seg + static_cast<int64_t>(BACK ? a.n_segments - 1 - (lo + i) : lo + i) * 2 * a.channels; };
+  auto passes = [&](int i) { return lo + i + 1 < a.n_segments; };
+  float A = 1.f, H = 0.f;
+  if (inside) {
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      const float as = passes(i) ? at(i)[0] : 1.f, hs = passes(i) ? at(i)[a.channels] : 0.f;
+      H = __builtin_fmaf(as, H, hs);
+      A *= as;
+    }
+  }
+  sa[part][lane] = A;
+  sh[part][lane] = H;
+  __syncthreads();
+  if (!inside) return;
+  const float *given = BACK ? a.dlast : a.state;
+  float state = given ? given[static_cast<int64_t>(b) * a.channels + c] : 0.f;
+  for (int s = 0; s < part; ++s) state = __builtin_fmaf(sa[s][lane], state, sh[s][lane]);
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    float *p = at(i);
+    const float as = passes(i) ? p[0] : 1.f, hs = passes(i) ? p[a.channels] : 0.f;
+    p[a.channels] = state;
+    state = __builtin_fmaf(as, state, hs);
+  }
+}
+
 // One step, the state updated in place: four channels a thread.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(const T *gate, const T *x, float *state, T *h, int64_t batch, int32_t channels,
@@ -341,57 +392,72 @@ __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(const T *gate
   store_some<T, kV>(h + b * channels + c, now, have);
 }
 
+constexpr int64_t kEnough = 192, kWanted = 512;
 int64_t tiles_of(int64_t steps) { return ceil_div(steps, kTile); }
 
 // How the work is cut.  Workgroups of 32 channels (8 lanes to a row) are twice as many as of 64, and two share every cache line
-// of 128 bytes: on the same die, at about the same time.  Where they are enough for most compute units, or the steps too few to
-// split, they are faster forward, and backward (with five arrays instead of three) on short sequences, before two that share
-// lines drift apart (us, 32 against 64 channels, bf16: forward 16 x 2048 x 1024 39 against 44, 64 x 256 x 1024 21 and 22, 8 x 512 x 512
-// 8.7 and 11.5; backward 95 and 80, 33 and 42, 11.4 and 16.2).  Otherwise 64 channels, and segments of four tiles at least that
-// make about two workgroups a compute unit (2 x 65521 x 512: 512 workgroups 136 and 213 us, 1024 153 and 267, 256 159 and 234;
-// with 32 channels 172 and 247).
+// of 128 bytes: on the same die, at about the same time.  Where they are enough for most compute units, or the tiles too few to
+// split, they walk along whole sequences; backward (with five arrays instead of three) only along short ones, before two that
+// share lines drift apart, and 64 channels along longer ones (us, 32 against 64 channels, bf16: forward 16 x 2048 x 1024 39 against
+// 44, 64 x 256 x 1024 21 and 22, 8 x 512 x 512 8.7 and 11.5; backward 95 and 80, 33 and 42, 11.4 and 16.2).  Otherwise 64 channels, and
+// as many segments as make two workgroups a compute unit (2 x 65521 x 512: 512 workgroups 141 and 220 us, 1024 152 and 231; with 32
+// channels 179 and 250), which is 4.7 TB/s for what they read twice and write.
 struct Cut {
   int32_t lanes, segments, tiles_each;
 };
 Cut cut_of(int64_t batch, int64_t steps, int64_t channels, bool backward) {
-  const int64_t tiles = tiles_of(steps), narrow = batch * ceil_div(channels, 32), chains = batch * ceil_div(channels, 64);
-  if ((narrow >= 192 || tiles < 8) && (!backward || tiles <= 8)) return Cut{8, 1, static_cast<int32_t>(std::max<int64_t>(1, tiles))};
-  const int64_t want = chains >= 192 ? 1 : std::max<int64_t>(1, std::min(ceil_div(512, std::max<int64_t>(chains, 1)), tiles / 4));
-  const int64_t each = std::max<int64_t>(1, ceil_div(tiles, want));
-  return Cut{16, static_cast<int32_t>(std::max<int64_t>(1, ceil_div(tiles, each))), static_cast<int32_t>(each)};
+  const int64_t tiles = std::max<int64_t>(1, tiles_of(steps)), narrow = batch * ceil_div(channels, 32), chains = batch * ceil_div(channels, 64);
+  const int32_t all = static_cast<int32_t>(tiles);
+  if ((narrow >= kEnough || tiles < 8) && (!backward || tiles <= 8)) return Cut{8, 1, all};
+  if (backward && chains >= kEnough) return Cut{16, 1, all};
+  const int64_t each = ceil_div(tiles, std::min(tiles, ceil_div(kWanted, std::max<int64_t>(1, chains))));
+  return Cut{16, static_cast<int32_t>(ceil_div(tiles, each)), static_cast<int32_t>(each)};
+}
+int64_t blocks_of(const Cut &cut, int64_t batch, int64_t channels) {
+  const int64_t blocks = ceil_div(channels, cut.lanes * kV);
+  return cut.lanes == 16 ? blocks * batch * cut.segments : ceil_div(ceil_div(blocks, 2) * batch * cut.segments, 8) * 16;
 }
 
 template <typename T, int LANES, bool EDGE, bool FORM>
-void launch_recurrence(const RecurrenceArgs &a, bool backward, hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(ceil_div(a.channels, LANES * kV)), static_cast<uint32_t>(a.batch), static_cast<uint32_t>(a.n_segments));
+void launch_recurrence(const RecurrenceArgs &a, int64_t blocks, bool backward, hipStream_t s) {
+  const dim3 grid(static_cast<uint32_t>(blocks));
   if (backward) hipLaunchKernelGGL((recurrence_backward_kernel<T, LANES, EDGE, FORM>), grid, dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((recurrence_forward_kernel<T, LANES, EDGE, FORM>), grid, dim3(kThreads), 0, s, a);
 }
 template <typename T, bool EDGE>
-void launch_recurrence(const RecurrenceArgs &a, int32_t lanes, bool backward, hipStream_t s) {
-  if (lanes == 8) return launch_recurrence<T, 8, EDGE, false>(a, backward, s);
-  if (a.n_segments > 1) launch_recurrence<T, 16, EDGE, true>(a, backward, s);
-  launch_recurrence<T, 16, EDGE, false>(a, backward, s);
+void launch_recurrence(const RecurrenceArgs &a, const Cut &cut, bool backward, hipStream_t s) {
+  const int64_t blocks = blocks_of(cut, a.batch, a.channels);
+  if (cut.lanes == 8) return launch_recurrence<T, 8, EDGE, false>(a, blocks, backward, s);
+  if (cut.segments > 1) {
+    launch_recurrence<T, 16, EDGE, true>(a, blocks, backward, s);
+    const dim3 grid(static_cast<uint32_t>(ceil_div(a.channels, 64)), static_cast<uint32_t>(a.batch));
+    if (backward) hipLaunchKernelGGL((recurrence_join_kernel<true>), grid, dim3(64 * kParts), 0, s, a);
+    else hipLaunchKernelGGL((recurrence_join_kernel<false>), grid, dim3(64 * kParts), 0, s, a);
+  }
+  launch_recurrence<T, 16, EDGE, false>(a, blocks, backward, s);
 }
 template <typename T>
-void launch_recurrence(const RecurrenceArgs &a, int32_t lanes, bool backward, hipStream_t s) {
-  if (a.channels % kV) launch_recurrence<T, true>(a, lanes, backward, s);
-  else launch_recurrence<T, false>(a, lanes, backward, s);
+void launch_recurrence(const RecurrenceArgs &a, const Cut &cut, bool backward, hipStream_t s) {
+  if (a.channels % kV) launch_recurrence<T, true>(a, cut, backward, s);
+  else launch_recurrence<T, false>(a, cut, backward, s);
 }
 
 void launch_recurrence_type(RecurrenceArgs &a, int32_t type, bool backward, hipStream_t s) {
   const Cut cut = cut_of(a.batch, a.steps, a.channels, backward);
   a.n_segments = cut.segments;
   a.tiles_per_segment = cut.tiles_each;
-  if (type == ONES_F32) launch_recurrence<float>(a, cut.lanes, backward, s);
-  else if (type == ONES_F16) launch_recurrence<f16>(a, cut.lanes, backward, s);
-  else launch_recurrence<bf16>(a, cut.lanes, backward, s);
+  if (type == ONES_F32) launch_recurrence<float>(a, cut, backward, s);
+  else if (type == ONES_F16) launch_recurrence<f16>(a, cut, backward, s);
+  else launch_recurrence<bf16>(a, cut, backward, s);
 }
 
 int check_recurrence(int64_t batch, int64_t steps, int64_t channels, int32_t type) {
   if (batch < 0 || steps < 0 || channels < 0 || !is_type(type)) return ONES_E_INVALID_ARG;
   if (batch > ONES_MAX_BATCH || steps > ONES_MAX_STEPS || channels > ONES_MAX_CHANNELS) return ONES_E_BOUNDS;
-  return steps && channels && batch > kMaxElements / (steps * channels) ? ONES_E_BOUNDS : ONES_OK;
+  if (steps && channels && batch > kMaxElements / (steps * channels)) return ONES_E_BOUNDS;
+  // workgroups of a launch
+  return std::max(blocks_of(cut_of(batch, steps, channels, false), batch, channels), blocks_of(cut_of(batch, steps, channels, true), batch, channels)) > (1 << 23)
+             ? ONES_E_BOUNDS : ONES_OK;
 }
 // Rows of `channels` elements, `step` elements apart and sequences `batch` elements apart.
 int check_strides(int64_t batch_stride, int64_t step_stride, int64_t channels) {
