@@ -415,8 +415,11 @@ int check_loss(int64_t rows, int64_t cols, int64_t vocabulary, int64_t x_stride,
   return std::max({n * v, d * n, d * v}) > (1 << 22) ? ONES_E_BOUNDS : ONES_OK;
 }
 
-// Rows that the products can load 16 bytes at a time.
-bool loadable(const void *p, int64_t stride, int64_t cols) { return cols % 8 == 0 && stride % 8 == 0 && aligned(p, 16); }
+// Rows that the products can load as they lie: 16 bytes at a time, the rows that a workgroup loads at once (64 at most) inside 2^32
+// bytes, which is what an offset holds.
+bool loadable(const void *p, int64_t stride, int64_t cols) {
+  return cols % 8 == 0 && stride % 8 == 0 && stride <= kMaxLoadableStride && aligned(p, 16);
+}
 
 void launch_pack(const PackArgs &a, hipStream_t s) {
   const int64_t total = (static_cast<int64_t>(a.rows[0]) + a.rows[1]) * (a.to_ld / 8);

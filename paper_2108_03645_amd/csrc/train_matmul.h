@@ -27,7 +27,7 @@ using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 using LdsBytes = __attribute__((address_space(3))) unsigned char;
 
 // An operand: `extent` values of m (or n), `k` of k; rows `ld` elements apart.  Base and ld are multiples of 16 bytes, and the
-// length of a row (k, or extent where it is turned) is read up to the next multiple of eight.
+// length of a row (k, or extent where it is turned) is read up to the next multiple of eight.  ld <= kMaxLoadableStride.
 struct Operand {
   const void *p;
   int64_t ld;
@@ -83,6 +83,7 @@ struct Tile {
     if constexpr (TURNED) return p ^ ((((row & 3) | ((row >> 1) & 4)) & (B / 16 - 1)) << 1);
     else return p ^ (row & 7);
   }
+  static_assert(rows * 2 * kMaxLoadableStride < (int64_t{1} << 32));            // offsets of 32 bits
   // The loads of a thread lie `rows` LDS rows apart, a multiple of what place() goes by, so they share one offset.
   __device__ __forceinline__ void start(const Operand &o, int32_t first, int32_t k0) {
     const int row = static_cast<int>(threadIdx.x) / pieces, piece = place(row, static_cast<int>(threadIdx.x) % pieces) * 8;

@@ -35,6 +35,17 @@ def test_refusals_need_no_gpu(train):  # noqa: F811
     assert L.ones_cross_entropy_backward_workspace_bytes(16384, 512, 131072, 1) < (128 << 20) + 16384 * 512 * 6 + (1 << 20)
 
 
+def test_rows_far_apart_are_copied(train):  # noqa: F811
+    """A workgroup's loads lie up to 63 rows beside each other at offsets of 32 bits: rows further apart need the copies' workspace."""
+    L = train.load()
+    p = C.c_void_p(0x1000)
+    for size, call in ((L.ones_cross_entropy_forward_workspace_bytes, lambda xs, ws, nb: L.ones_cross_entropy_forward(
+            p, xs, p, ws, 4, 64, 100, 2, p, p, p, p, nb, None)),
+            (L.ones_cross_entropy_backward_workspace_bytes, lambda xs, ws, nb: L.ones_cross_entropy_backward(
+                p, p, xs, p, ws, 4, 64, 100, 2, p, p, p, p, p, nb, None))):
+        assert call(64, (1 << 24) + 8, size(4, 64, 100, 1)) == -5
+
+
 def test_the_binding_refuses_wrong_shapes(train):  # noqa: F811
     x, w, t = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(5, 8, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64)
     with pytest.raises(train.OnesError):
@@ -146,6 +157,18 @@ def test_loss_of_strided_unaligned_and_extreme_inputs(train):  # noqa: F811
     x[1, 3] = float("nan")
     loss, lse = train.linear_cross_entropy_forward(x, w, t)
     assert loss[0].isfinite() and loss[1].isnan() and lse[1].isnan() and loss[2] == 0
+
+
+@gpu
+def test_loss_of_rows_that_lie_gigabytes_apart(train):  # noqa: F811
+    """Row 16 begins 2^32 bytes behind row 0: what a 32-bit offset loses."""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    apart = torch.empty(40 << 27, dtype=torch.bfloat16, device="cuda").as_strided((40, 64), (1 << 27, 1))
+    apart.copy_(torch.randn(40, 64, generator=gen, device="cuda"))
+    other = torch.randn(70, 64, generator=gen, device="cuda").bfloat16() * 0.2
+    target = torch.randint(0, 40, (70,), generator=gen, device="cuda")
+    check(train, other, apart, target, torch.rand(70, generator=gen, device="cuda"))
+    check(train, apart, other, target[:40], torch.rand(40, generator=gen, device="cuda"))
 
 
 @gpu
