@@ -34,6 +34,20 @@ __device__ __forceinline__ void store_pack(T *p, const float *v) {
   for (int i = 0; i < N; ++i) out.v[i] = static_cast<T>(v[i]);
   __builtin_memcpy(p, &out, sizeof(out));
 }
+// The same, and, if `past`, not kept in the caches: what is written would push out what is still to be read.  For results of
+// kPastBytes and more, of which a next reader would not find much in the last-level cache of 256 MiB anyway (layer norm, bf16, 32768
+// x 2048: 162 us to 144; recurrence 2 x 65521 x 512: 333 to 316, 16 x 2048 x 1024: 133 to 128).
+constexpr int64_t kPastBytes = 64 << 20;
+template <typename T, int N>
+__device__ __forceinline__ void store_pack(T *p, const float *v, bool past) {
+  if (!past) return store_pack<T, N>(p, v);
+  typedef uint32_t Words __attribute__((ext_vector_type(sizeof(T) * N / 4)));
+  typedef Words Loose __attribute__((aligned(sizeof(T))));
+  Pack<T, N> out;
+#pragma unroll
+  for (int i = 0; i < N; ++i) out.v[i] = static_cast<T>(v[i]);
+  __builtin_nontemporal_store(__builtin_bit_cast(Words, out), reinterpret_cast<Loose *>(p));
+}
 // The same where only the first n of the elements are there (n may be 0 or less, or more than N).
 template <typename T, int N>
 __device__ __forceinline__ Pack<T, N> load_some(const T *p, int n) {
@@ -44,8 +58,8 @@ __device__ __forceinline__ Pack<T, N> load_some(const T *p, int n) {
   return v;
 }
 template <typename T, int N>
-__device__ __forceinline__ void store_some(T *p, const float *v, int n) {
-  if (n >= N) return store_pack<T, N>(p, v);
+__device__ __forceinline__ void store_some(T *p, const float *v, int n, bool past = false) {
+  if (n >= N) return store_pack<T, N>(p, v, past);
 #pragma unroll
   for (int i = 0; i < N; ++i) if (i < n) p[i] = static_cast<T>(v[i]);
 }

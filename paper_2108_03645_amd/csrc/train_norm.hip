@@ -7,7 +7,8 @@
 // sixteen (up to 32768), so that the centred sum of squares (no cancellation, unlike the sum of squares less the square of the
 // mean) and the results need no second read.  What bounds them is memory.  Workgroups take rows in turn, which keeps the
 // weights in registers, and backward the sums of dw and db over a workgroup's rows as well: it leaves one row of partial sums a
-// workgroup, which a second small launch adds up in a fixed order.  No atomics: the results are the same bits every time.
+// workgroup, which a second small launch adds up in a fixed order; few short rows are left to a single workgroup, which writes dw
+// and db itself.  No atomics: the results are the same bits every time.
 #include "train_device.h"
 #include "train_host.h"
 
@@ -18,20 +19,28 @@ namespace train {
 namespace {
 
 constexpr int kBlock = 256;
-// Backward, whether the next row is read ahead: not by workgroups of 1024 threads, which have 128 registers a thread; they read the
-// weights for every row, too.  (Forward, waves enough for each other's gaps: reading ahead costs 5 to 15 %.)
+// Backward, whether the next row is read ahead: not where 1024 threads share a row, as a workgroup of so many has 128 registers a
+// thread; they read the weights for every row, too.  (Forward, waves enough for each other's gaps: reading ahead costs 5 to 15 %.)
 template <int TPR>
 constexpr bool kAhead = TPR < 1024;
+// Backward, what a single workgroup of 16 waves takes: rows of a wave (PER is 8), up to four each.  It saves the launch that adds up
+// the workgroups' sums: in a graph 16 x 512 takes 3.3 us against 5.3, 64 x 256 8.3 against 5.5 (1.5 us for a row of every wave, as all
+// run on one compute unit); calls one after another, where the launches are what the host waits for, 12.4 us against 16.
+constexpr int64_t kAloneCols = 512, kAloneRows = 64;
+template <int TPR, int BLOCK>
+constexpr bool kAlone = TPR < BLOCK && BLOCK > kBlock;
 
 struct NormArgs {
   const void *x, *dy;
   void *out;                       // y forward, dx backward
   const void *weight, *bias;       // may be null (bias is used forward only)
   float *mean, *rstd;              // written forward, read backward
-  float *partial;                  // backward: [workgroups][2][D]
+  float *partial;                  // backward: [workgroups][2][D]; null: one workgroup, which writes dweight and dbias (may be null)
+  void *dweight, *dbias;
   int64_t rows, x_stride, dy_stride;
   int32_t cols, weight_type;
   float eps;
+  bool past;                       // out goes past the caches
 };
 
 // A row as read: thread t holds elements (k * TPR + t) * VEC + 0..VEC-1, k < PER / VEC; zeros beyond the last column.
@@ -48,11 +57,11 @@ struct Row {
   __device__ __forceinline__ float operator[](int i) const { return static_cast<float>(p[i / VEC].v[i % VEC]); }
 };
 template <typename T, int PER, int VEC, int TPR>
-__device__ __forceinline__ void store_row(T *row, int t, int cols, const float *v) {
+__device__ __forceinline__ void store_row(T *row, int t, int cols, const float *v, bool past) {
 #pragma unroll
   for (int k = 0; k < PER / VEC; ++k) {
     const int c = (k * TPR + t) * VEC;
-    store_some<T, VEC>(row + c, v + k * VEC, cols - c);
+    store_some<T, VEC>(row + c, v + k * VEC, cols - c, past);
   }
 }
 template <typename W, int PER, int VEC, int TPR>
@@ -112,16 +121,16 @@ __global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_forward_kern
     const float rstd = 1.f / sqrtf(fmaxf(square / n - rest * rest, 0.f) + a.eps);
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = (v[i] - rest) * rstd * w[i] + b[i];
-    store_row<T, PER, VEC, TPR>(static_cast<T *>(a.out) + row * a.cols, t, a.cols, v);
+    store_row<T, PER, VEC, TPR>(static_cast<T *>(a.out) + row * a.cols, t, a.cols, v, a.past);
     if (t == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
   }
 }
 
-template <typename T, int PER, int VEC, int TPR>
-__global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_backward_kernel(NormArgs a) {
-  constexpr int block = TPR > kBlock ? TPR : kBlock, rows_at_once = block / TPR;
-  __shared__ float part[2][2 * (block / kWave)];
-  __shared__ float sums[rows_at_once > 1 ? 2 * PER * TPR : 1];
+template <typename T, int PER, int VEC, int TPR, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void norm_backward_kernel(NormArgs a) {
+  constexpr int rows_at_once = BLOCK / TPR;
+  __shared__ float part[2][2 * (BLOCK / kWave)];
+  __shared__ __align__(16) float sums[rows_at_once > 1 ? rows_at_once : 1][2][rows_at_once > 1 ? PER * TPR : 1];
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float w[PER], dw[PER], db[PER];
   if (kAhead<TPR>) load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
@@ -131,29 +140,24 @@ __global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_backward_ker
   int turn = 0;
   const int64_t step = static_cast<int64_t>(gridDim.x) * rows_at_once;
   int64_t row = static_cast<int64_t>(blockIdx.x) * rows_at_once + sub;
-  Row<T, PER, VEC, TPR> x_now, x_next, dy_now, dy_next;
-  float mean_next = 0.f, rstd_next = 0.f;
-  auto load = [&](int64_t r, Row<T, PER, VEC, TPR> &u, Row<T, PER, VEC, TPR> &v) {
-    u.load(static_cast<const T *>(a.x) + r * a.x_stride, t, a.cols);
-    v.load(static_cast<const T *>(a.dy) + r * a.dy_stride, t, a.cols);
-    mean_next = a.mean[r];
-    rstd_next = a.rstd[r];
+  struct Read {
+    Row<T, PER, VEC, TPR> x, dy;
+    float mean, rstd;
   };
-  if (kAhead<TPR> && row < a.rows) load(row, x_now, dy_now);
-  for (; row < a.rows; row += step) {
-    if (!kAhead<TPR>) {
-      load(row, x_now, dy_now);
-      load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
-    }
-    const float mean = mean_next, rstd = rstd_next;
-    if (kAhead<TPR> && row + step < a.rows) load(row + step, x_next, dy_next);
+  auto load = [&](int64_t r, Read &to) {
+    to.x.load(static_cast<const T *>(a.x) + r * a.x_stride, t, a.cols);
+    to.dy.load(static_cast<const T *>(a.dy) + r * a.dy_stride, t, a.cols);
+    to.mean = a.mean[r];
+    to.rstd = a.rstd[r];
+  };
+  auto take = [&](int64_t r, const Read &from) {
     float x[PER], dy[PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) { x[i] = x_now[i]; dy[i] = dy_now[i]; }
+    for (int i = 0; i < PER; ++i) { x[i] = from.x[i]; dy[i] = from.dy[i]; }
     float sg = 0.f, sgx = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {                 // past the last column dy and w are zero
-      const float xh = (x[i] - mean) * rstd, g = dy[i] * w[i];
+      const float xh = (x[i] - from.mean) * from.rstd, g = dy[i] * w[i];
       x[i] = xh;
       dw[i] += dy[i] * xh;
       db[i] += dy[i];
@@ -165,25 +169,44 @@ __global__ __launch_bounds__(TPR > kBlock ? TPR : kBlock) void norm_backward_ker
     sg /= n;
     sgx /= n;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) x[i] = rstd * (dy[i] * w[i] - sg - x[i] * sgx);
-    store_row<T, PER, VEC, TPR>(static_cast<T *>(a.out) + row * a.cols, t, a.cols, x);
-    if (kAhead<TPR>) { x_now = x_next; dy_now = dy_next; }
-  }
-  if constexpr (rows_at_once > 1) {                 // the waves' sums, one after another
-    for (int s = 0; s < rows_at_once; ++s) {
-      if (sub == s) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          float *p = sums + (2 * i) * TPR + t;
-          if (s) { dw[i] += p[0]; db[i] += p[TPR]; }
-          if (s + 1 < rows_at_once) { p[0] = dw[i]; p[TPR] = db[i]; }
-        }
-      }
-      __syncthreads();
+    for (int i = 0; i < PER; ++i) x[i] = from.rstd * (dy[i] * w[i] - sg - x[i] * sgx);
+    store_row<T, PER, VEC, TPR>(static_cast<T *>(a.out) + r * a.cols, t, a.cols, x, a.past);
+  };
+  if constexpr (kAhead<TPR>) {
+    Read now, next;
+    if (row < a.rows) load(row, now);
+    for (; row < a.rows; row += step) {
+      if (row + step < a.rows) load(row + step, next);
+      take(row, now);
+      now = next;
     }
-    if (sub != rows_at_once - 1) return;
+  } else {
+    Read now;
+    for (; row < a.rows; row += step) {
+      load(row, now);
+      load_weights<PER, VEC, TPR>(a.weight, a.weight_type, 1.f, t, a.cols, w);
+      take(row, now);
+    }
   }
   float *to = a.partial + static_cast<int64_t>(blockIdx.x) * 2 * a.cols;
+  if constexpr (rows_at_once > 1) {                 // the waves' sums, in order
+#pragma unroll
+    for (int k = 0; k < PER / VEC; ++k) {
+      const int c = (k * TPR + t) * VEC;
+      store_pack<float, VEC>(&sums[sub][0][c], dw + k * VEC);
+      store_pack<float, VEC>(&sums[sub][1][c], db + k * VEC);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.cols; c += BLOCK) {
+      const int which = c >= a.cols, at = which ? c - a.cols : c;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < rows_at_once; ++i) s += sums[i][which][at];
+      if (!kAlone<TPR, BLOCK>) to[c] = s;
+      else if (void *out = which ? a.dbias : a.dweight) store_as(out, a.weight_type, at, s);
+    }
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < PER / VEC; ++k) {
     const int c = (k * TPR + t) * VEC;
@@ -228,11 +251,24 @@ int64_t norm_blocks(int64_t rows, int64_t cols, bool backward) {
   return std::min(ceil_div(rows, at_once), most);
 }
 
+// Whether a single workgroup takes the backward pass.
+bool alone(int64_t rows, int64_t cols) { return rows && rows <= kAloneRows && cols <= kAloneCols; }
+
 template <typename T, int PER, int VEC, int TPR>
 void launch_norm(const NormArgs &a, bool backward, hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(norm_blocks(a.rows, a.cols, backward))), block(TPR > kBlock ? TPR : kBlock);
-  if (backward) hipLaunchKernelGGL((norm_backward_kernel<T, PER, VEC, TPR>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((norm_forward_kernel<T, PER, VEC, TPR>), grid, block, 0, s, a);
+  constexpr int threads = TPR > kBlock ? TPR : kBlock;
+  // what threads_per_row() leaves to each
+  constexpr bool has_forward = TPR == 64 || PER > 8, has_backward = TPR == 1024 || PER <= 16;
+  const dim3 grid(static_cast<uint32_t>(norm_blocks(a.rows, a.cols, backward))), block(threads);
+  if constexpr (TPR == 64 && PER == 8)
+    if (backward && !a.partial) {
+      hipLaunchKernelGGL((norm_backward_kernel<T, PER, VEC, TPR, 1024>), dim3(1), dim3(1024), 0, s, a);
+      return;
+    }
+  if constexpr (has_backward)
+    if (backward) hipLaunchKernelGGL((norm_backward_kernel<T, PER, VEC, TPR, threads>), grid, block, 0, s, a);
+  if constexpr (has_forward)
+    if (!backward) hipLaunchKernelGGL((norm_forward_kernel<T, PER, VEC, TPR>), grid, block, 0, s, a);
 }
 
 template <typename T, int VEC, int TPR>
@@ -259,6 +295,8 @@ void launch_norm_type(const NormArgs &a, int32_t type, bool backward, hipStream_
   else launch_norm<bf16>(a, backward, s);
 }
 
+bool past(int64_t rows, int64_t cols, int32_t type) { return rows * cols * type_bytes(type) >= kPastBytes; }
+
 int check_norm(int64_t rows, int64_t cols, int64_t stride, int32_t type, int32_t weight_type) {
   if (int rc = check_rows(rows, cols, stride)) return rc;
   if (cols < 1 || !is_type(type) || (weight_type != ONES_F32 && weight_type != type)) return ONES_E_INVALID_ARG;
@@ -279,13 +317,14 @@ int ones_layer_norm_forward(const void *x, int64_t x_stride, int64_t rows, int64
   if (!(eps >= 0.f)) return ONES_E_INVALID_ARG;
   if (rows == 0) return ONES_OK;
   if (!x || !y || !mean || !rstd) return ONES_E_INVALID_ARG;
-  const NormArgs a{x, nullptr, y, weight, bias, mean, rstd, nullptr, rows, x_stride, 0, static_cast<int32_t>(cols), weight_type, eps};
+  const NormArgs a{x, nullptr, y, weight, bias, mean, rstd, nullptr, nullptr, nullptr, rows, x_stride, 0, static_cast<int32_t>(cols),
+                   weight_type, eps, past(rows, cols, type)};
   launch_norm_type(a, type, false, static_cast<hipStream_t>(hip_stream));
   return launched("layer norm forward");
 }
 
 size_t ones_layer_norm_workspace_bytes(int64_t rows, int64_t cols) {
-  if (rows < 0 || cols < 1 || cols > ONES_MAX_NORM_COLUMNS) return 0;
+  if (rows < 0 || cols < 1 || cols > ONES_MAX_NORM_COLUMNS || alone(rows, cols)) return 0;
   return align_up(static_cast<size_t>(std::max<int64_t>(1, norm_blocks(rows, cols, true))) * 2 * static_cast<size_t>(cols) * 4);
 }
 
@@ -297,10 +336,11 @@ int ones_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, i
   if (rows && (!dy || !x || !mean || !rstd || !dx)) return ONES_E_INVALID_ARG;
   if (int rc = check_workspace(d_workspace, workspace_bytes, ones_layer_norm_workspace_bytes(rows, cols))) return rc;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const NormArgs a{x, dy, dx, weight, nullptr, const_cast<float *>(mean), const_cast<float *>(rstd), static_cast<float *>(d_workspace),
-                   rows, x_stride, dy_stride, static_cast<int32_t>(cols), weight_type, 0.f};
+  const bool single = alone(rows, cols);
+  const NormArgs a{x, dy, dx, weight, nullptr, const_cast<float *>(mean), const_cast<float *>(rstd),
+                   single ? nullptr : static_cast<float *>(d_workspace), dweight, dbias, rows, x_stride, dy_stride, static_cast<int32_t>(cols), weight_type, 0.f, past(rows, cols, type)};
   if (rows) launch_norm_type(a, type, true, s);
-  if (dweight || dbias)
+  if (!single && (dweight || dbias))
     hipLaunchKernelGGL(norm_reduce_kernel, dim3(static_cast<uint32_t>(ceil_div(2 * cols, 64))), dim3(1024), 0, s, a.partial,
                        static_cast<int32_t>(norm_blocks(rows, cols, true)), a.cols, dweight, dbias, weight_type);
   return launched("layer norm backward");

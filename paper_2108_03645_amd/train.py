@@ -39,6 +39,7 @@ _ARGUMENTS = {
     "ones_orthogonal_update": [_P, _P, _I64, _I64, _I64, _I32, _F32, _I32, _I32, _P, _F32, _P, _I32, _P, _SIZE, _P],
 }
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_FLOAT = (torch.float32,)
 _lib = None
 # current_device() and current_stream(device).cuda_stream, without what these do around it: 3 us of a call's 15
 _device, _stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
@@ -118,11 +119,11 @@ def _rows(t):
 # ------------------------------------------------------------------ layer norm --------
 def _norm_weights(weight, bias, x):
     kinds = (torch.float32, x.dtype)
-    d = x.shape[-1]
-    weight, bias = _dense(weight, "weight", (d,), kinds, x.device), _dense(bias, "bias", (d,), kinds, x.device)
+    shape = x.shape[-1:]
+    weight, bias = _dense(weight, "weight", shape, kinds, x.device), _dense(bias, "bias", shape, kinds, x.device)
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise TypeError("weight and bias: one type for both")
-    return weight, bias, next((w.dtype for w in (weight, bias) if w is not None), torch.float32)
+    return weight, bias, weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
 
 
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
@@ -131,11 +132,11 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     if x.dim() < 1:
         raise ValueError("x: at least one dimension is wanted")
     weight, bias, kind = _norm_weights(weight, bias, x)
-    rows, stride = _rows(x)
+    device, (rows, stride) = x.device, _rows(x)
     y = _like(x)
-    mean, rstd = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device).unbind(0)
+    mean, rstd = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=device).unbind(0)
     n, d = rows.shape
-    _call(x.device, load().ones_layer_norm_forward, rows.data_ptr(), stride, n, d, _TYPES[x.dtype], _ptr(weight), _ptr(bias),
+    _call(device, load().ones_layer_norm_forward, rows.data_ptr(), stride, n, d, _TYPES[x.dtype], _ptr(weight), _ptr(bias),
           _TYPES[kind], eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr())
     return y, mean, rstd
 
@@ -144,21 +145,23 @@ def layer_norm_backward(dy, x, weight, mean, rstd, want_bias=True):
     """ones_layer_norm_backward: (dx, dweight, dbias).  dweight has the weight's type (float32 without one); dbias is None if
     not wanted."""
     _check(x, "x", None, _TYPES)
-    _check(dy, "dy", x.shape, (x.dtype,), x.device)
+    device = x.device
+    _check(dy, "dy", x.shape, (x.dtype,), device)
     weight, _, kind = _norm_weights(weight, None, x)
-    mean = _dense(mean, "mean", x.shape[:-1], (torch.float32,), x.device)
-    rstd = _dense(rstd, "rstd", x.shape[:-1], (torch.float32,), x.device)
+    lead = x.shape[:-1]
+    mean, rstd = _dense(mean, "mean", lead, _FLOAT, device), _dense(rstd, "rstd", lead, _FLOAT, device)
     (rows, stride), (grad, grad_stride) = _rows(x), _rows(dy)
     n, d = rows.shape
     dx = _like(x)
-    dweight, dbias = torch.empty((2, d), dtype=kind, device=x.device).unbind(0)
+    dweight = torch.empty(d, dtype=kind, device=device) if weight is None else torch.empty_like(weight)
+    dbias = torch.empty_like(dweight) if want_bias else None
     L = load()
     nbytes = L.ones_layer_norm_workspace_bytes(n, d)
-    scratch = _scratch(nbytes, x.device)
-    _call(x.device, L.ones_layer_norm_backward, grad.data_ptr(), grad_stride, rows.data_ptr(), stride, n, d, _TYPES[x.dtype],
-          _ptr(weight), _TYPES[kind], mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dweight.data_ptr(),
-          dbias.data_ptr() if want_bias else None, _ptr(scratch), nbytes)
-    return dx, dweight, dbias if want_bias else None
+    scratch = _scratch(nbytes, device)
+    _call(device, L.ones_layer_norm_backward, grad.data_ptr(), grad_stride, rows.data_ptr(), stride, n, d, _TYPES[x.dtype],
+          _ptr(weight), _TYPES[kind], mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dweight.data_ptr(), _ptr(dbias),
+          _ptr(scratch), nbytes)
+    return dx, dweight, dbias
 
 
 class _LayerNorm(torch.autograd.Function):

@@ -374,3 +374,46 @@ def test_another_stream_and_a_captured_graph_give_the_same(train):
         assert all(torch.equal(p, q) for p, q in zip(got, want))
         assert all(torch.equal(p, q) for p, q in zip(all_of_it(), want))
     assert np.isfinite(want[0].float().sum().item())
+
+
+@gpu
+@pytest.mark.parametrize("rows,cols,kind", [(1, 512, torch.float16), (16, 37, torch.float32), (17, 511, torch.float16), (64, 256, torch.float32),
+                                            (64, 512, torch.float16), (65, 512, torch.float16), (64, 513, torch.float16)])
+def test_layer_norm_of_few_rows_sums_its_weights_gradients(train, rows, cols, kind):
+    """Around the sizes that one workgroup takes alone; without weights, and with one of the two gradients only."""
+    gen = torch.Generator(device="cuda").manual_seed(rows + cols)
+    x, dy = (torch.randn(rows, cols, generator=gen, device="cuda").half() for _ in range(2))
+    w = (torch.randn(cols, generator=gen, device="cuda") + 2).to(kind)
+    y, mean, rstd = train.layer_norm_forward(x, w)
+    *_, wdx, wdw, wdb, xh = norm64(x, w, None, 1e-5, dy)
+    dx, dw, db = train.layer_norm_backward(dy, x, w, mean, rstd)
+    assert dw.dtype == db.dtype == kind
+    near(dx, wdx, wdx.abs() + 20, 300, "dx")
+    near(dw, wdw, (dy.double().abs() * (1 + xh.abs())).sum(0), 300, "dweight")
+    near(db, wdb, dy.double().abs().sum(0), 128, "dbias")
+    again = train.layer_norm_backward(dy, x, w, mean, rstd, want_bias=False)
+    assert again[2] is None and torch.equal(again[0], dx) and torch.equal(again[1], dw)
+    assert torch.equal(train.layer_norm_backward(dy, x, None, mean, rstd)[2].to(kind), db)
+
+
+@gpu
+def test_results_that_go_past_the_caches_are_the_same(train):
+    """Results of 64 MiB and more are written with a hint: the same rows in a smaller call give the same bits, odd columns too."""
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    for cols in (1024, 1027):
+        x = torch.randn(33000, cols, generator=gen, device="cuda").bfloat16()
+        y, mean, rstd = train.layer_norm_forward(x)
+        few = train.layer_norm_forward(x[-300:])
+        assert all(torch.equal(p[-300:], q) for p, q in zip((y, mean, rstd), few))
+        dx = train.layer_norm_backward(x, x, None, mean, rstd)[0]
+        assert torch.equal(dx[-300:], train.layer_norm_backward(x[-300:], x[-300:], None, mean[-300:], rstd[-300:])[0])
+    for channels in (256, 259):
+        gate, x, dh = (torch.randn(200, 700, channels, generator=gen, device="cuda").bfloat16() for _ in range(3))
+        lengths = torch.randint(0, 701, (200,), generator=gen, device="cuda", dtype=torch.int32)
+        h, last, carry = train.gated_recurrence_forward(gate, x, None, lengths)
+        back = train.gated_recurrence_backward(dh, None, gate, x, carry, lengths)
+        want, want_last, few = train.gated_recurrence_forward(gate[:50], x[:50], None, lengths[:50])
+        bound = 2 * HALF[torch.bfloat16] * (want.double().abs() + 2.0 ** -8)          # other segments: other roundings of 32 bits
+        assert ((h[:50].double() - want.double()).abs() <= bound).all() and torch.allclose(last[:50], want_last, rtol=1e-4, atol=1e-5)
+        for got, one in zip(back, train.gated_recurrence_backward(dh[:50], None, gate[:50], x[:50], few, lengths[:50])):
+            assert ((got[:50].double() - one.double()).abs() <= 2 * HALF[torch.bfloat16] * (one.double().abs() + 2.0 ** -8)).all()
