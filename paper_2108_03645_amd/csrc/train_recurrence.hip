@@ -15,8 +15,9 @@
 //
 // Where sequences and channels are too few for the compute units, the steps are split into segments of whole tiles as well.  A
 // first launch forms each segment's A and H (or Q), a small second one turns them into the state before (what comes from behind)
-// each, and the third walks along the segments side by side: the inputs are read twice then.  No workgroup waits for another, and
-// the order of all sums is fixed.
+// each, and the third walks along the segments side by side: the inputs are read twice then.  The first launch goes through a segment
+// against the third's direction, so that what it read last, and the caches still have, is what the third reads first (316 us for
+// 2 x 65521 x 512 forward and backward, 328 in the same direction).  No workgroup waits for another, and the order of all sums is fixed.
 #include "train_device.h"
 #include "train_host.h"
 
@@ -62,11 +63,11 @@ struct Run {
     }
   }
 };
-template <typename T, bool EDGE>
+template <typename T, bool EDGE, bool PAST>
 __device__ __forceinline__ void store_run(T *base, int channels, int t0, int steps, int c, int i, const float *v) {
   T *to = base + static_cast<int64_t>(t0 + i) * channels + c;
-  if (EDGE) { if (t0 + i < steps) store_some<T, kV>(to, v, channels - c); }
-  else if (t0 + i < steps && c < channels) store_pack<T, kV>(to, v);
+  if (EDGE) { if (t0 + i < steps) store_some<T, kV>(to, v, channels - c, PAST); }
+  else if (t0 + i < steps && c < channels) store_pack<T, kV>(to, v, PAST);
 }
 
 // a = sigmoid(g) and 1 - a, which keeps its digits where a is close to 1.  (The reciprocal is off by one place of 32 bits at most.)
@@ -99,7 +100,7 @@ __device__ __forceinline__ Work work_of(const RecurrenceArgs &a) {
               block < blocks && segment < static_cast<uint32_t>(a.n_segments)};
 }
 
-template <typename T, int LANES, bool EDGE, bool FORM>     // FORM: only the segments' A and H
+template <typename T, int LANES, bool EDGE, bool FORM, bool PAST>     // FORM: only the segments' A and H; PAST: h goes past the caches
 __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(RecurrenceArgs a) {
   constexpr int V = kV, kChannels = LANES * V, groups = kThreads / LANES, S = kTile / groups;
   __shared__ float sa[groups][kChannels], sh[groups][kChannels];
@@ -119,9 +120,11 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
     if (segment) state = a.segments[((static_cast<int64_t>(b) * a.n_segments + segment) * 2 + 1) * a.channels + own];
     else if (a.state) state = a.state[static_cast<int64_t>(b) * a.channels + own];
   }
+  constexpr int turn = FORM ? -1 : 1;            // FORM goes from the segment's end to its start
+  const int start = FORM ? end - 1 : first, stop = FORM ? first - 1 : end;
   Run<T, S, EDGE> g, u;
-  g.load(gate, a.gate_step, first * kTile + group * S, c, len, a.channels);
-  u.load(x, a.x_step, first * kTile + group * S, c, len, a.channels);
+  g.load(gate, a.gate_step, start * kTile + group * S, c, len, a.channels);
+  u.load(x, a.x_step, start * kTile + group * S, c, len, a.channels);
   auto body = [&](int tile, auto whole) {          // whole: no step of the tile is past the length
     constexpr bool all = decltype(whole)::value;
     const int t0 = tile * kTile + group * S;
@@ -141,9 +144,9 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
         H[k] = __builtin_fmaf(ga[i][k], H[k], in[i][k]);
       }
     }
-    if (tile + 1 < end) {                        // the next tile's rows arrive while this one is put together
-      g.load(gate, a.gate_step, t0 + kTile, c, len, a.channels);
-      u.load(x, a.x_step, t0 + kTile, c, len, a.channels);
+    if (tile + turn != stop) {                   // the next tile's rows arrive while this one is put together
+      g.load(gate, a.gate_step, t0 + turn * kTile, c, len, a.channels);
+      u.load(x, a.x_step, t0 + turn * kTile, c, len, a.channels);
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) { sa[group][lane * V + k] = A[k]; sh[group][lane * V + k] = H[k]; }
@@ -154,11 +157,21 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
 #pragma unroll
       for (int s = 0; s < groups; ++s) { as[s] = sa[s][threadIdx.x]; hs[s] = sh[s][threadIdx.x]; }
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (FORM) {
+        float tile_h = 0.f, tile_a = 1.f;
 #pragma unroll
-      for (int s = 0; s < groups; ++s) {
-        sh[s][threadIdx.x] = state;              // before the group's first step
-        state = __builtin_fmaf(as[s], state, hs[s]);
-        if (FORM) through *= as[s];
+        for (int s = 0; s < groups; ++s) {
+          tile_h = __builtin_fmaf(as[s], tile_h, hs[s]);
+          tile_a *= as[s];
+        }
+        state = __builtin_fmaf(through, tile_h, state);      // the tile, then those behind it
+        through *= tile_a;
+      } else {
+#pragma unroll
+        for (int s = 0; s < groups; ++s) {
+          sh[s][threadIdx.x] = state;            // before the group's first step
+          state = __builtin_fmaf(as[s], state, hs[s]);
+        }
       }
     }
     __syncthreads();
@@ -174,12 +187,12 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
           now[k] = __builtin_fmaf(ga[i][k], now[k], in[i][k]);
           out[k] = all || t0 + i < len ? now[k] : 0.f;
         }
-        store_run<T, EDGE>(h, a.channels, t0, a.steps, c, i, out);
+        store_run<T, EDGE, PAST>(h, a.channels, t0, a.steps, c, i, out);
       }
       __syncthreads();                           // sh is written anew
     }
   };
-  for (int tile = first; tile < end; ++tile) {
+  for (int tile = start; tile != stop; tile += turn) {
     if ((tile + 1) * kTile <= len) body(tile, std::true_type{});
     else body(tile, std::false_type{});
   }
@@ -193,7 +206,7 @@ __global__ __launch_bounds__(kThreads) void recurrence_forward_kernel(Recurrence
   }
 }
 
-template <typename T, int LANES, bool EDGE, bool FORM>     // FORM: only the segments' A and Q
+template <typename T, int LANES, bool EDGE, bool FORM, bool PAST>     // FORM: only the segments' A and Q; PAST: dgate and dx go past the caches
 __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(RecurrenceArgs a) {
   constexpr int V = kV, kChannels = LANES * V, groups = kThreads / LANES, S = kTile / groups;
   __shared__ float sa[groups][kChannels], sh[groups][kChannels], sq[groups][kChannels];
@@ -219,9 +232,11 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
   auto load_carry = [&](int tile) {
     if (!FORM && threadIdx.x < kChannels && own < a.channels) carry = a.carry[(static_cast<int64_t>(b) * a.tiles + tile) * a.channels + own];
   };
+  constexpr int turn = FORM ? 1 : -1;            // FORM goes from the segment's start to its end
+  const int start = FORM ? first : end - 1, stop = FORM ? end : first - 1;
   if (end > first) {                             // always, but for sequences of no steps
-    load_carry(end - 1);
-    const int t0 = (end - 1) * kTile + group * S;
+    load_carry(start);
+    const int t0 = start * kTile + group * S;
     g.load(gate, a.gate_step, t0, c, len, a.channels);
     if (!FORM) u.load(x, a.x_step, t0, c, len, a.channels);
     d.load(dh, a.dh_step, t0, c, len, a.channels);
@@ -252,10 +267,10 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
     for (int i = S - 1; i >= 0; --i)
 #pragma unroll
       for (int k = 0; k < V; ++k) Q[k] = ga[i][k] * (ds(i, k) + Q[k]);
-    if (tile > first) {
-      g.load(gate, a.gate_step, t0 - kTile, c, len, a.channels);
-      if (!FORM) u.load(x, a.x_step, t0 - kTile, c, len, a.channels);
-      d.load(dh, a.dh_step, t0 - kTile, c, len, a.channels);
+    if (tile + turn != stop) {
+      g.load(gate, a.gate_step, t0 + turn * kTile, c, len, a.channels);
+      if (!FORM) u.load(x, a.x_step, t0 + turn * kTile, c, len, a.channels);
+      d.load(dh, a.dh_step, t0 + turn * kTile, c, len, a.channels);
     }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
@@ -269,11 +284,21 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
 #pragma unroll
       for (int s = 0; s < groups; ++s) { as[s] = sa[s][at]; qs[s] = sq[s][at]; }
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (FORM) {
+        float tile_q = 0.f, tile_a = 1.f;
 #pragma unroll
-      for (int s = groups - 1; s >= 0; --s) {
-        sq[s][at] = back;                        // from behind the group's last step
-        back = __builtin_fmaf(as[s], back, qs[s]);
-        if (FORM) through *= as[s];
+        for (int s = groups - 1; s >= 0; --s) {
+          tile_q = __builtin_fmaf(as[s], tile_q, qs[s]);
+          tile_a *= as[s];
+        }
+        back = __builtin_fmaf(through, tile_q, back);        // the tile, then those before it
+        through *= tile_a;
+      } else {
+#pragma unroll
+        for (int s = groups - 1; s >= 0; --s) {
+          sq[s][at] = back;                      // from behind the group's last step
+          back = __builtin_fmaf(as[s], back, qs[s]);
+        }
       }
     } else if (!FORM && threadIdx.x < kChannels) {
       float state = carry, as[groups], hs[groups];
@@ -311,13 +336,13 @@ __global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(Recurrenc
           dx[k] = live ? keep[i][k] * l : 0.f;
           dg[k] = live ? r[k] * keep[i][k] * (before[i][k] - xs(i, k)) : 0.f;
         }
-        store_run<T, EDGE>(static_cast<T *>(a.dgate) + out, a.channels, t0, a.steps, c, i, dg);
-        store_run<T, EDGE>(static_cast<T *>(a.dx) + out, a.channels, t0, a.steps, c, i, dx);
+        store_run<T, EDGE, PAST>(static_cast<T *>(a.dgate) + out, a.channels, t0, a.steps, c, i, dg);
+        store_run<T, EDGE, PAST>(static_cast<T *>(a.dx) + out, a.channels, t0, a.steps, c, i, dx);
       }
     }
     __syncthreads();
   };
-  for (int tile = end - 1; tile >= first; --tile) {
+  for (int tile = start; tile != stop; tile += turn) {
     if ((tile + 1) * kTile <= len) body(tile, std::true_type{});
     else body(tile, std::false_type{});
   }
@@ -418,28 +443,30 @@ int64_t blocks_of(const Cut &cut, int64_t batch, int64_t channels) {
   return cut.lanes == 16 ? blocks * batch * cut.segments : ceil_div(ceil_div(blocks, 2) * batch * cut.segments, 8) * 16;
 }
 
-template <typename T, int LANES, bool EDGE, bool FORM>
+template <typename T, int LANES, bool EDGE, bool FORM, bool PAST>
 void launch_recurrence(const RecurrenceArgs &a, int64_t blocks, bool backward, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(blocks));
-  if (backward) hipLaunchKernelGGL((recurrence_backward_kernel<T, LANES, EDGE, FORM>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((recurrence_forward_kernel<T, LANES, EDGE, FORM>), grid, dim3(kThreads), 0, s, a);
+  if (backward) hipLaunchKernelGGL((recurrence_backward_kernel<T, LANES, EDGE, FORM, PAST>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((recurrence_forward_kernel<T, LANES, EDGE, FORM, PAST>), grid, dim3(kThreads), 0, s, a);
 }
-template <typename T, bool EDGE>
+// PAST is a choice at compile time: as a branch at every store it costs more than it gives (16 x 2048 x 1024: 136 us against 128).
+template <typename T, bool EDGE, bool PAST>
 void launch_recurrence(const RecurrenceArgs &a, const Cut &cut, bool backward, hipStream_t s) {
   const int64_t blocks = blocks_of(cut, a.batch, a.channels);
-  if (cut.lanes == 8) return launch_recurrence<T, 8, EDGE, false>(a, blocks, backward, s);
+  if (cut.lanes == 8) return launch_recurrence<T, 8, EDGE, false, PAST>(a, blocks, backward, s);
   if (cut.segments > 1) {
-    launch_recurrence<T, 16, EDGE, true>(a, blocks, backward, s);
+    launch_recurrence<T, 16, EDGE, true, false>(a, blocks, backward, s);
     const dim3 grid(static_cast<uint32_t>(ceil_div(a.channels, 64)), static_cast<uint32_t>(a.batch));
     if (backward) hipLaunchKernelGGL((recurrence_join_kernel<true>), grid, dim3(64 * kParts), 0, s, a);
     else hipLaunchKernelGGL((recurrence_join_kernel<false>), grid, dim3(64 * kParts), 0, s, a);
   }
-  launch_recurrence<T, 16, EDGE, false>(a, blocks, backward, s);
+  launch_recurrence<T, 16, EDGE, false, PAST>(a, blocks, backward, s);
 }
 template <typename T>
 void launch_recurrence(const RecurrenceArgs &a, const Cut &cut, bool backward, hipStream_t s) {
-  if (a.channels % kV) launch_recurrence<T, true>(a, cut, backward, s);
-  else launch_recurrence<T, false>(a, cut, backward, s);
+  const bool past = static_cast<int64_t>(a.batch) * a.steps * a.channels * static_cast<int64_t>(sizeof(T)) >= kPastBytes;
+  if (a.channels % kV) past ? launch_recurrence<T, true, true>(a, cut, backward, s) : launch_recurrence<T, true, false>(a, cut, backward, s);
+  else past ? launch_recurrence<T, false, true>(a, cut, backward, s) : launch_recurrence<T, false, false>(a, cut, backward, s);
 }
 
 void launch_recurrence_type(RecurrenceArgs &a, int32_t type, bool backward, hipStream_t s) {
