@@ -58,19 +58,17 @@ __global__ __launch_bounds__(S::threads, S::resident) void logits_kernel(LossArg
     const Place<S> at(m * S::BM, n * S::BN);
     const int part = m * S::WM + static_cast<int>(threadIdx.x) / kWave / S::WN;
     const bool ragged = (m + 1) * S::BM > a.w.extent;
-    // what a row's logits meet: 16 i + r of the target, if that is in this run; -1: not here, -2: ignored (G is 0), -3: beyond the
-    // vocabulary (G is NaN); and backward the row's lse and dloss
-    int32_t hit[S::TN];
+    // read ahead of the products, looked at behind them
+    int64_t target[S::TN];
     float lse[S::TN], weight[S::TN];
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
       const int32_t row = at.n + j * 16;
-      const int64_t target = row < a.x.extent ? a.target[row] : -1;
-      const int32_t in = target >= 0 && target < a.vocabulary ? static_cast<int32_t>(target) - a.v0 - at.m : -1;
-      hit[j] = target < 0 ? -2 : target >= a.vocabulary ? -3 : in >= 0 && in < S::TM * 16 && in % 16 < 4 ? in : -1;
+      const bool inside = row < a.x.extent;
+      target[j] = inside ? a.target[row] : -1;
       if (GRADIENT) {
-        lse[j] = row < a.x.extent ? a.lse[row] : 0.f;
-        weight[j] = row < a.x.extent ? a.dloss[row] * unit : 0.f;
+        lse[j] = inside ? a.lse[row] : 0.f;
+        weight[j] = inside ? a.dloss[row] : 0.f;
       }
     }
     product.run(lds, acc);
@@ -79,24 +77,58 @@ __global__ __launch_bounds__(S::threads, S::resident) void logits_kernel(LossArg
       tile_of(id, tiles, tm, tn, m, n);
       product.begin(a.w, a.x, m * S::BM, n * S::BN, 0, a.w.k, lds);
     }
+    // words beyond the last: no logits forward, no G backward.  (Blocks that most tiles skip, ahead of the others: as a condition at
+    // every logit they would be a select at every logit.)
+    if (!GRADIENT && ragged) {
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool beyond = at.m + i * 16 + r >= a.w.extent;
+#pragma unroll
+          for (int j = 0; j < S::TN; ++j) acc[i][j][r] = beyond ? -INFINITY : acc[i][j][r];
+        }
+    }
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
       const int32_t row = at.n + j * 16;
-      const bool inside = row < a.x.extent, hits = __any(hit[j] >= 0);      // one of 16 rows, in a few tiles
+      const bool inside = row < a.x.extent, ignored = target[j] < 0, unknown = target[j] >= a.vocabulary;
+      // 16 i + r of the target, if that is in this lane's runs
+      const int32_t in = ignored || unknown ? -1 : static_cast<int32_t>(target[j]) - a.v0 - at.m;
+      const int32_t hit = in >= 0 && in < S::TM * 16 && in % 16 < 4 ? in : -1;
+      const bool hits = __any(hit >= 0);                      // one of 16 rows, in a few tiles
       if constexpr (GRADIENT) {
+        const float base = lse[j] * -kLog2E;                  // rounded by 2^-24 of lse, as the logits are by more
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2E, base));
+        if (hits) {
+          asm volatile("");                                   // a block of its own, no selects
+#pragma unroll
+          for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][j][r] -= hit == i * 16 + r ? 1.f : 0.f;
+        }
+        const float factor = unknown ? __builtin_nanf("") : weight[j] * unit;
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[i][j][r] *= factor;
+        if (ragged || __any(ignored)) {                       // whatever came out there
+#pragma unroll
+          for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = ignored || at.m + i * 16 + r >= a.w.extent ? 0.f : acc[i][j][r];
+        }
         if (!inside) continue;
-        const float factor = hit[j] == -3 ? __builtin_nanf("") : weight[j];
+        T *to = static_cast<T *>(a.g) + row * a.g_ld + at.m;
 #pragma unroll
         for (int i = 0; i < S::TM; ++i) {
-          const int32_t v = at.m + i * 16;
           float g[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse[j]) * kLog2E);
-            if (hits) p -= hit[j] == i * 16 + r ? 1.f : 0.f;
-            g[r] = hit[j] == -2 || (ragged && v + r >= a.w.extent) ? 0.f : p * factor;
-          }
-          store_pack<T, 4>(static_cast<T *>(a.g) + row * a.g_ld + v, g);
+          for (int r = 0; r < 4; ++r) g[r] = acc[i][j][r];
+          store_pack<T, 4>(to + i * 16, g);
         }
       } else {
         if (hits) {
@@ -104,17 +136,14 @@ __global__ __launch_bounds__(S::threads, S::resident) void logits_kernel(LossArg
 #pragma unroll
           for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) of_target = hit[j] == i * 16 + r ? acc[i][j][r] : of_target;
-          if (hit[j] >= 0) a.at_target[row] = of_target;
+            for (int r = 0; r < 4; ++r) of_target = hit == i * 16 + r ? acc[i][j][r] : of_target;
+          if (hit >= 0) a.at_target[row] = of_target;
         }
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            if (ragged && at.m + i * 16 + r >= a.w.extent) acc[i][j][r] = -INFINITY;
-            top = fmaxf(top, acc[i][j][r]);
-          }
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float base = top == -INFINITY ? 0.f : top * -kLog2E;

@@ -186,8 +186,8 @@ struct Product {
   // loads its products would wait for the queues that all eight waves fill at once.  The workgroup meets where the last fragments
   // of the tile have been read: from there on its buffer takes a later tile, and the next tile has arrived.
   template <bool MORE, bool PLAIN>            // MORE: there is a tile to load
-  __device__ __forceinline__ void multiply(unsigned char *now, unsigned char *next, bool reads, int wm, int wn, int lane, s16x8 (&a)[2][kRows],
-                                           s16x8 (&b)[2][S::TN], Sums<S> &acc) {
+  __device__ __forceinline__ void multiply(unsigned char *now, unsigned char *next, int wm, int wn, int lane, s16x8 (&a)[2][kRows], s16x8 (&b)[2][S::TN],
+                                           Sums<S> &acc) {
 #pragma unroll
     for (int p = 0; p < phases; ++p) {
       const int half = p / groups, group = p % groups;
@@ -197,13 +197,11 @@ struct Product {
       if (last) meet<MORE ? (S::buffers - 2) * of_tile : 0>();
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
-        if (MORE || !last || reads) {         // R's fragments first: the next phase begins with all of them
-          const int bs = turns ? S::TN : 0, n = bs + kRows;
+        const int bs = turns ? S::TN : 0, n = bs + kRows;     // R's fragments first: the next phase begins with all of them
 #pragma unroll
-          for (int e = i * n / kRows; e < (i + 1) * n / kRows; ++e) {
-            if (e < bs) b[next_half][e] = r.fragment(from + lbytes, wn + e * 16, next_half, lane);
-            else a[(p + 1) & 1][e - bs] = l.fragment(from, wm + (next_group * kRows + e - bs) * 16, next_half, lane);
-          }
+        for (int e = i * n / kRows; e < (i + 1) * n / kRows; ++e) {      // behind the last tile: of what lies there, not used
+          if (e < bs) b[next_half][e] = r.fragment(from + lbytes, wn + e * 16, next_half, lane);
+          else a[(p + 1) & 1][e - bs] = l.fragment(from, wm + (next_group * kRows + e - bs) * 16, next_half, lane);
         }
         if (MORE && last) {
 #pragma unroll
@@ -241,11 +239,13 @@ struct Product {
     unsigned char *now = lds, *const end = lds + S::buffers * buffer;
     auto after = [&](unsigned char *p) { return p + buffer == end ? lds : p + buffer; };
     int t = 0;
-    if (l.plain && r.plain)
-      for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true, true>(now, after(now), true, wm, wn, lane, a, b, acc);
-    else
-      for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true, false>(now, after(now), true, wm, wn, lane, a, b, acc);
-    for (; t < tiles; ++t, now = after(now)) multiply<false, false>(now, after(now), t + 1 < tiles, wm, wn, lane, a, b, acc);
+    if (l.plain && r.plain) {
+      for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true, true>(now, after(now), wm, wn, lane, a, b, acc);
+      for (; t < tiles; ++t, now = after(now)) multiply<false, false>(now, after(now), wm, wn, lane, a, b, acc);
+    } else {
+      for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true, false>(now, after(now), wm, wn, lane, a, b, acc);
+      for (; t < tiles; ++t, now = after(now)) multiply<false, false>(now, after(now), wm, wn, lane, a, b, acc);
+    }
   }
 };
 
