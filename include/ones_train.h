@@ -85,7 +85,7 @@ int ones_recurrence_step(const void *gate, int64_t gate_stride, const void *x, i
  * gradient, and what x holds there does not matter); vocabulary or above: the row's loss, its dx and dweight are NaN.
  * loss, lse: float [rows].  Backward: dloss float [rows], lse as forward left it; dx[rows][cols] and dweight[vocabulary][cols]
  * are written.  It goes through the vocabulary in pieces of at most 128 MiB of logits' gradients, rounded to type.
- * wide: not 0 if cols, both strides and both bases are multiples of 16 bytes and no stride is above 2^24 elements; otherwise the
+ * wide: not 0 if cols, both strides and both bases are multiples of 16 bytes and no stride is above 2^20 elements; otherwise the
  * workspace has room for copies.
  * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size above its limit, or the product of two of them above 2^36),
  * ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */

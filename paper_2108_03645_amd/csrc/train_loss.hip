@@ -444,8 +444,8 @@ int check_loss(int64_t rows, int64_t cols, int64_t vocabulary, int64_t x_stride,
   return std::max({n * v, d * n, d * v}) > (1 << 22) ? ONES_E_BOUNDS : ONES_OK;
 }
 
-// Rows that the products can load as they lie: 16 bytes at a time, the rows that a workgroup loads at once (64 at most) inside 2^32
-// bytes, which is what an offset holds.
+// Rows that the products can load as they lie: 16 bytes at a time, the rows of a tile (256 at most) inside 2^31 bytes,
+// below which the loads' offsets lie.
 bool loadable(const void *p, int64_t stride, int64_t cols) {
   return cols % 8 == 0 && stride % 8 == 0 && stride <= kMaxLoadableStride && aligned(p, 16);
 }

@@ -7,7 +7,7 @@
 // four buffers in turn: the next k arrive while the present ones are multiplied.  Rows are read back with 16 bytes a lane, turned operands with
 // the transposing read (four k of a column to every lane).  So that the lanes of a read fall into different banks, the 16-byte
 // pieces of an LDS row are exchanged by the row's number; a direct load writes LDS in lane order, so the exchange is made in
-// the address that each lane loads from.  What lies outside an operand is loaded from a block of zeros.
+// the address that each lane loads from.  What lies outside an operand comes as zeros, by the loads' own bounds.
 //
 // A wave's sums: acc[i][j][r] is C at m = 16 i + 4 (lane / 16) + r, n = 16 j + lane % 16 of the wave's part of the tile, so a
 // lane holds runs of four m, which lie next to each other in C.
@@ -34,23 +34,26 @@ struct Operand {
   int32_t extent, k;
 };
 
-__device__ __align__(16) const uint32_t g_zeros[4] = {0, 0, 0, 0};
-
 template <typename T>
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
   if constexpr (__is_same(T, bf16)) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// A direct load of 16 bytes a lane to LDS: lane i's land at to + 16 i.  Written as text: with the builtin in flight the compiler
+// A value that is the same in all lanes, in a scalar register.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// A direct load of 16 bytes a lane to LDS: lane i's land at to + 16 i, zeros where `offset` is not below the `bytes` from base on that
+// may be read.  Written as text: with the builtin in flight the compiler
 // waits for all of LDS's reads where it needs the first of them (it takes the load for one that may return through either
 // counter), and the reads ahead would be in vain.  It has no result in registers; meet() waits for it.
-// (s_nop: m0 is written one instruction ahead at least.)
-__device__ __forceinline__ void load_to_lds(const unsigned char *base, uint32_t offset, uint32_t to) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "{m0}"(to) : "memory");
-}
-__device__ __forceinline__ void load_to_lds(const unsigned char *from, uint32_t to) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(to) : "memory");
+// (s_nop: a scalar register that a vector instruction wrote, a v_readlane of a spilled one among them, is read five cycles later at
+// the earliest, m0 one instruction later; the compiler sees to neither inside text.)
+__device__ __forceinline__ void load_to_lds(const unsigned char *base, uint32_t bytes, uint32_t offset, uint32_t to) {
+  const uint64_t at = reinterpret_cast<uintptr_t>(base);
+  typedef __attribute__((ext_vector_type(4))) uint32_t Descriptor;      // of a buffer of bytes: address, length, 32-bit data
+  const Descriptor buffer{uniform(static_cast<uint32_t>(at)), uniform(static_cast<uint32_t>(at >> 32)), uniform(bytes), 0x00020000};
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "{m0}"(to) : "memory");
 }
 
 // The workgroup meets, and the direct loads to LDS of all its waves, but for the last PENDING of each, have arrived: a barrier
@@ -71,11 +74,12 @@ struct Tile {
   static constexpr int pieces = TURNED ? B / 8 : K / 8;            // 16-byte pieces of a row in LDS
   static constexpr int rows = THREADS / pieces;                    // LDS rows that one load of the workgroup fills
   static_assert(loads * 16 * THREADS == bytes && rows % (TURNED ? 16 : 8) == 0);
+  static constexpr uint32_t kOutside = 0x80000000;
   const unsigned char *base;                  // of the next load: element (first, k); the same for all threads
-  int64_t row_bytes;                          // from an LDS row to the next in memory
-  uint32_t offset;                            // from there to what this thread loads, in bytes
-  int32_t m, k, m_left, k_left;               // this thread's m and k in the tile, and what is left of the operand there
-  bool plain;                                 // all loads of the product lie inside
+  uint32_t row_bytes;                         // from an LDS row to the next in memory
+  uint32_t offset;                            // from there to what this thread loads, in bytes; kOutside beyond a row's end
+  int32_t piece;                              // this thread's k (m where turned) in the tile
+  int32_t rows_left, k_left;                  // of the operand, LDS rows and k from base on
 
   // The place of logical piece `p` of LDS row `row`, so that the lanes of a read meet different banks.  A read of rows takes the
   // same piece of eight rows at a time; a transposing read takes 32 bytes (a unit of two pieces) of rows k..k+3, and of k+8.
@@ -83,41 +87,33 @@ struct Tile {
     if constexpr (TURNED) return p ^ ((((row & 3) | ((row >> 1) & 4)) & (B / 16 - 1)) << 1);
     else return p ^ (row & 7);
   }
-  static_assert(rows * 2 * kMaxLoadableStride < (int64_t{1} << 32));            // offsets of 32 bits
-  // The loads of a thread lie `rows` LDS rows apart, a multiple of what place() goes by, so they share one offset.
+  static_assert((TURNED ? K : B) * 2 * kMaxLoadableStride < kOutside);          // and so what is added to either never wraps
+  // The loads of a thread lie `rows` LDS rows apart, a multiple of what place() goes by, so they share one offset.  Rows beyond the
+  // operand's are kept out by the length of what may be read, the ends of rows by the offset.
   __device__ __forceinline__ void start(const Operand &o, int32_t first, int32_t k0) {
-    const int row = static_cast<int>(threadIdx.x) / pieces, piece = place(row, static_cast<int>(threadIdx.x) % pieces) * 8;
-    m = TURNED ? piece : row;
-    k = TURNED ? row : piece;
-    m_left = o.extent - first;
+    const int row = static_cast<int>(threadIdx.x) / pieces;
+    piece = place(row, static_cast<int>(threadIdx.x) % pieces) * 8;
     k_left = o.k - k0;
-    plain = m_left >= B && k_left % K == 0;
-    row_bytes = o.ld * 2;
+    rows_left = min(o.extent - first, B);
+    row_bytes = static_cast<uint32_t>(o.ld * 2);
     base = static_cast<const unsigned char *>(o.p) + 2 * (TURNED ? k0 * o.ld + first : first * o.ld + k0);
-    offset = static_cast<uint32_t>(row * row_bytes) + piece * 2;
+    offset = piece < (TURNED ? rows_left : k_left) ? row * row_bytes + piece * 2 : kOutside;
   }
   // One of the loads of the next K, into LDS at `to` (the same for the whole workgroup); advance() behind the last.
-  template <bool PLAIN>
   __device__ __forceinline__ void load_one(unsigned char *to, int i) {
     const uint32_t mine = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LdsBytes *)to)) +
                           __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave) * (kWave * 16);
-    if constexpr (PLAIN) {
-      load_to_lds(base + i * rows * row_bytes, offset, mine + i * THREADS * 16);
-    } else {
-      const bool inside = m + (TURNED ? 0 : i * rows) < m_left && k + (TURNED ? i * rows : 0) < k_left;
-      load_to_lds(inside ? base + i * rows * row_bytes + offset : reinterpret_cast<const unsigned char *>(g_zeros), mine + i * THREADS * 16);
-    }
+    const uint32_t inside = TURNED ? max(min(k_left, K), 0) : rows_left;
+    load_to_lds(base, inside * row_bytes, offset + i * rows * row_bytes, mine + i * THREADS * 16);
   }
   __device__ __forceinline__ void advance() {
-    base += TURNED ? K * row_bytes : K * 2;
+    base += TURNED ? static_cast<uint64_t>(K) * row_bytes : K * 2;
     k_left -= K;
+    if (!TURNED) offset = piece < k_left ? offset : kOutside;
   }
   __device__ __forceinline__ void load(unsigned char *to) {
 #pragma unroll
-    for (int i = 0; i < loads; ++i) {
-      if (plain) load_one<true>(to, i);
-      else load_one<false>(to, i);
-    }
+    for (int i = 0; i < loads; ++i) load_one(to, i);
     advance();
   }
   // Eight k of each of 16 values from `first` (a multiple of 16) of the tile on: k = 32 half + 8 (lane / 16) + 0..7.
@@ -185,7 +181,7 @@ struct Product {
   // later tile, are put between the rows of products of a phase: a wave issues in order, and behind a run of reads or
   // loads its products would wait for the queues that all eight waves fill at once.  The workgroup meets where the last fragments
   // of the tile have been read: from there on its buffer takes a later tile, and the next tile has arrived.
-  template <bool MORE, bool PLAIN>            // MORE: there is a tile to load
+  template <bool MORE>                        // there is a tile to load
   __device__ __forceinline__ void multiply(unsigned char *now, unsigned char *next, int wm, int wn, int lane, s16x8 (&a)[2][kRows], s16x8 (&b)[2][S::TN],
                                            Sums<S> &acc) {
 #pragma unroll
@@ -205,9 +201,9 @@ struct Product {
         }
         if (MORE && last) {
 #pragma unroll
-          for (int e = i * l_loads / kRows; e < (i + 1) * l_loads / kRows; ++e) l.template load_one<PLAIN>(now, e);
+          for (int e = i * l_loads / kRows; e < (i + 1) * l_loads / kRows; ++e) l.load_one(now, e);
 #pragma unroll
-          for (int e = i * r_loads / kRows; e < (i + 1) * r_loads / kRows; ++e) r.template load_one<PLAIN>(now + lbytes, e);
+          for (int e = i * r_loads / kRows; e < (i + 1) * r_loads / kRows; ++e) r.load_one(now + lbytes, e);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -239,13 +235,8 @@ struct Product {
     unsigned char *now = lds, *const end = lds + S::buffers * buffer;
     auto after = [&](unsigned char *p) { return p + buffer == end ? lds : p + buffer; };
     int t = 0;
-    if (l.plain && r.plain) {
-      for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true, true>(now, after(now), wm, wn, lane, a, b, acc);
-      for (; t < tiles; ++t, now = after(now)) multiply<false, false>(now, after(now), wm, wn, lane, a, b, acc);
-    } else {
-      for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true, false>(now, after(now), wm, wn, lane, a, b, acc);
-      for (; t < tiles; ++t, now = after(now)) multiply<false, false>(now, after(now), wm, wn, lane, a, b, acc);
-    }
+    for (; t + S::buffers < tiles; ++t, now = after(now)) multiply<true>(now, after(now), wm, wn, lane, a, b, acc);
+    for (; t < tiles; ++t, now = after(now)) multiply<false>(now, after(now), wm, wn, lane, a, b, acc);
   }
 };
 

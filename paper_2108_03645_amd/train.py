@@ -294,7 +294,7 @@ def _loss_inputs(x, weight, target):
     _check(target, "target", x.shape[:1], (torch.int64, torch.int32), x.device)
     (x, x_stride), (weight, w_stride) = _rows(x), _rows(weight)
     wide = not (x.shape[1] % 8 or x_stride % 8 or w_stride % 8 or x.data_ptr() % 16 or weight.data_ptr() % 16
-                or max(x_stride, w_stride) > 1 << 24)
+                or max(x_stride, w_stride) > 1 << 20)
     return x, x_stride, weight, w_stride, target.long().contiguous(), wide
 
 
