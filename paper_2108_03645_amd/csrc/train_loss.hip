@@ -401,7 +401,7 @@ struct LossPlan {
   size_t g, dx_sum, dw_sum, scale, backward;
 };
 
-LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool copies_x, bool copies_w) {
+LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool copies_x, bool copies_w, bool backward) {
   LossPlan p{};
   p.cols8 = ceil_div(cols, 8) * 8;
   p.logits = logits_tiles(vocabulary, rows, cols);
@@ -416,6 +416,7 @@ LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool copies_x
   p.part = take(static_cast<size_t>(p.parts) * n * sizeof(Part));
   p.at_target = take(n * 4);
   p.forward = off;
+  if (!backward) return p;
   off = packed;
   for (p.pieces = std::max<int64_t>(1, ceil_div(rows * ceil_div(vocabulary, 256) * 512, kPieceBytes));; ++p.pieces) {
     p.piece = ceil_div(ceil_div(vocabulary, p.pieces), 256) * 256;
@@ -520,11 +521,11 @@ extern "C" {
 
 size_t ones_cross_entropy_forward_workspace_bytes(int64_t rows, int64_t cols, int64_t vocabulary, int32_t wide) {
   if (check_loss(rows, cols, vocabulary, cols, cols, ONES_BF16) != ONES_OK) return 0;
-  return loss_plan(rows, cols, vocabulary, !wide, !wide).forward;
+  return loss_plan(rows, cols, vocabulary, !wide, !wide, false).forward;
 }
 size_t ones_cross_entropy_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t vocabulary, int32_t wide) {
   if (check_loss(rows, cols, vocabulary, cols, cols, ONES_BF16) != ONES_OK) return 0;
-  return loss_plan(rows, cols, vocabulary, true, !wide).backward;
+  return loss_plan(rows, cols, vocabulary, true, !wide, true).backward;
 }
 
 int ones_cross_entropy_forward(const void *x, int64_t x_stride, const void *weight, int64_t weight_stride, int64_t rows, int64_t cols,
@@ -534,7 +535,7 @@ int ones_cross_entropy_forward(const void *x, int64_t x_stride, const void *weig
   if (rows == 0) return ONES_OK;
   if (!x || !weight || !target || !loss || !lse) return ONES_E_INVALID_ARG;
   const bool copy_x = !loadable(x, x_stride, cols), copy_w = !loadable(weight, weight_stride, cols);
-  const LossPlan p = loss_plan(rows, cols, vocabulary, copy_x, copy_w);
+  const LossPlan p = loss_plan(rows, cols, vocabulary, copy_x, copy_w, false);
   if (int rc = check_workspace(d_workspace, workspace_bytes, p.forward)) return rc;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   char *ws = static_cast<char *>(d_workspace);
@@ -565,7 +566,7 @@ int ones_cross_entropy_backward(const float *dloss, const void *x, int64_t x_str
   if (int rc = check_loss(rows, cols, vocabulary, x_stride, weight_stride, type)) return rc;
   if (!weight || !dweight || (rows && (!dloss || !x || !target || !lse || !dx))) return ONES_E_INVALID_ARG;
   const bool copy_w = !loadable(weight, weight_stride, cols);
-  const LossPlan p = loss_plan(rows, cols, vocabulary, true, copy_w);
+  const LossPlan p = loss_plan(rows, cols, vocabulary, true, copy_w, true);
   if (int rc = check_workspace(d_workspace, workspace_bytes, p.backward)) return rc;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   char *ws = static_cast<char *>(d_workspace);

@@ -284,47 +284,50 @@ def gated_recurrence(gate, x, state=None, lengths=None):
 
 # ------------------------------------------- cross entropy over a vocabulary --------
 _HALVES = (torch.bfloat16, torch.float16)
+_WHOLE = (torch.int64, torch.int32)
 
 
 def _loss_inputs(x, weight, target):
     _check(x, "x", None, _HALVES)
-    _check(weight, "weight", None, (x.dtype,), x.device)
+    device = x.device
+    _check(weight, "weight", None, (x.dtype,), device)
     if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[1]:
         raise ValueError(f"x [rows, cols] and weight [vocabulary, cols] are wanted, got {tuple(x.shape)} and {tuple(weight.shape)}")
-    _check(target, "target", x.shape[:1], (torch.int64, torch.int32), x.device)
+    _check(target, "target", x.shape[:1], _WHOLE, device)
+    if target.dtype != torch.int64:
+        target = target.long()
     (x, x_stride), (weight, w_stride) = _rows(x), _rows(weight)
-    wide = not (x.shape[1] % 8 or x_stride % 8 or w_stride % 8 or x.data_ptr() % 16 or weight.data_ptr() % 16
-                or max(x_stride, w_stride) > 1 << 20)
-    return x, x_stride, weight, w_stride, target.long().contiguous(), wide
+    n, d = x.shape
+    x_at, w_at = x.data_ptr(), weight.data_ptr()
+    wide = not ((d | x_stride | w_stride) % 8 or (x_at | w_at) % 16 or max(x_stride, w_stride) > 1 << 20)
+    return device, (x_at, x_stride, w_at, w_stride, n, d, weight.shape[0]), wide, (x, weight, target.contiguous())
 
 
 def linear_cross_entropy_forward(x, weight, target):
     """ones_cross_entropy_forward: (loss, lse), float32 per row of x [rows, cols], for logits x weight^T over weight
     [vocabulary, cols].  Rows with a target below 0 have no loss."""
-    x, x_stride, weight, w_stride, target, wide = _loss_inputs(x, weight, target)
-    (n, d), v = x.shape, weight.shape[0]
+    device, operands, wide, (x, weight, target) = _loss_inputs(x, weight, target)
+    n, d, v = operands[4:]
     L = load()
-    loss, lse = torch.empty((2, n), dtype=torch.float32, device=x.device).unbind(0)
+    loss, lse = torch.empty((2, n), dtype=torch.float32, device=device).unbind(0)
     nbytes = L.ones_cross_entropy_forward_workspace_bytes(n, d, v, wide)
-    scratch = _scratch(nbytes, x.device)
-    _call(x.device, L.ones_cross_entropy_forward, x.data_ptr(), x_stride, weight.data_ptr(), w_stride, n, d, v, _TYPES[x.dtype],
-          target.data_ptr(), loss.data_ptr(), lse.data_ptr(), _ptr(scratch), nbytes)
+    scratch = _scratch(nbytes, device)
+    _call(device, L.ones_cross_entropy_forward, *operands, _TYPES[x.dtype], target.data_ptr(), loss.data_ptr(), lse.data_ptr(),
+          _ptr(scratch), nbytes)
     return loss, lse
 
 
 def linear_cross_entropy_backward(dloss, x, weight, target, lse):
     """ones_cross_entropy_backward: (dx, dweight) for the gradient dloss (float32) of every row's loss."""
-    x, x_stride, weight, w_stride, target, wide = _loss_inputs(x, weight, target)
-    (n, d), v = x.shape, weight.shape[0]
-    dloss = _dense(dloss, "dloss", (n,), (torch.float32,), x.device)
-    lse = _dense(lse, "lse", (n,), (torch.float32,), x.device)
+    device, operands, wide, (x, weight, target) = _loss_inputs(x, weight, target)
+    n, d, v = operands[4:]
+    dloss, lse = _dense(dloss, "dloss", x.shape[:1], _FLOAT, device), _dense(lse, "lse", x.shape[:1], _FLOAT, device)
     L = load()
-    dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
-    dweight = torch.empty((v, d), dtype=x.dtype, device=x.device)
+    dx, dweight = _like(x), _like(weight)
     nbytes = L.ones_cross_entropy_backward_workspace_bytes(n, d, v, wide)
-    scratch = _scratch(nbytes, x.device)
-    _call(x.device, L.ones_cross_entropy_backward, dloss.data_ptr(), x.data_ptr(), x_stride, weight.data_ptr(), w_stride, n, d, v,
-          _TYPES[x.dtype], target.data_ptr(), lse.data_ptr(), dx.data_ptr(), dweight.data_ptr(), _ptr(scratch), nbytes)
+    scratch = _scratch(nbytes, device)
+    _call(device, L.ones_cross_entropy_backward, dloss.data_ptr(), *operands, _TYPES[x.dtype], target.data_ptr(), lse.data_ptr(),
+          dx.data_ptr(), dweight.data_ptr(), _ptr(scratch), nbytes)
     return dx, dweight
 
 
