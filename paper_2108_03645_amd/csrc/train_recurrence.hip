@@ -13,11 +13,15 @@
 // elements): backward recomputes h from it, which is neither rounded to 16 bits nor read.  What bounds it is memory; next to it
 // the arithmetic (an exponential and a reciprocal an element) and the chain through a tile's groups.
 //
+// Measured at 16 x 2048 x 1024 bf16: forward 39 us (206 MB with the carry, 5.2 TB/s; a copy of 4 GiB runs at 4.65), backward 65 us (340
+// MB, 5.2 TB/s).  One step of 64 x 1024 is 3 us, a launch's own time.
+//
 // Where sequences and channels are too few for the compute units, the steps are split into segments of whole tiles as well.  A
 // first launch forms each segment's A and H (or Q), a small second one turns them into the state before (what comes from behind)
 // each, and the third walks along the segments side by side: the inputs are read twice then.  The first launch goes through a segment
 // against the third's direction, so that what it read last, and the caches still have, is what the third reads first (316 us for
-// 2 x 65521 x 512 forward and backward, 328 in the same direction).  No workgroup waits for another, and the order of all sums is fixed.
+// 2 x 65521 x 512 forward and backward, 328 in the same direction; the launches take 51, 5 and 62 us
+// forward, 43, 5 and 143 us backward).  No workgroup waits for another, and the order of all sums is fixed.
 #include "train_device.h"
 #include "train_host.h"
 

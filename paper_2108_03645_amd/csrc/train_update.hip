@@ -11,6 +11,14 @@
 // times 2^11 (X) and 2^10 (A, B): an element of X is at most 1.3 and typically (r q)^-1/2, of A typically r^-1 q^-1/2 off the diagonal, so
 // neither end of fp16's range is near for sides up to the limit and coefficients that keep the singular values below 8.
 //
+// The result of five steps is off by 0.9e-3 to 1.8e-3 of the whole (sides 33 to 4100): mostly from X's roundings, which grow with the
+// directions of small singular values; A's and B's diagonals kept apart in 32 bits took 3 to 28 % off that and cost 2 to 6 % of the
+// time.  A bf16 result's own rounding is 1.7e-3.
+//
+// Measured at 4100 x 3000: A 61 us and B 51 us (tiles of 192 x 128 on and below the diagonal, one round), X 96 us (0.77
+// PFLOP/s, 204 tiles of 256 x 256 in one round), momentum 20 us and X's first form 34 us, both at memory's rate.  Eight of 256 x 256:
+// 5 to 5.6 us each of 15 products, which is a launch, the operands' way from the cache and back, and four tiles of k.
+//
 // The first launch updates the momentum and sums the squares of u by workgroups; the second adds those sums up in a fixed order
 // and writes X; then three products a step, the last of which writes the result in the caller's type and orientation.  All
 // matrices of a call go through each launch together.

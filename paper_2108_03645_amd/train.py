@@ -4,7 +4,10 @@ of the tensors' device).  There is no CPU fallback: without the built library or
 
 The ``*_forward`` and ``*_backward`` functions are the library's calls; ``layer_norm``, ``gated_recurrence`` and
 ``linear_cross_entropy`` are the same under autograd.  ``gated_recurrence_step`` is the single-token form,
-``orthogonal_update`` the optimizer's step."""
+``orthogonal_update`` the optimizer's step.
+
+All of them may be captured into a graph.  Autograd's own rule stays: a backward pass under capture must not meet leaves that an eager
+graph still holds; the ``*_backward`` calls know no such state."""
 from __future__ import annotations
 
 import ctypes as C
