@@ -126,14 +126,13 @@ __global__ __launch_bounds__(S::threads, S::resident) void logits_kernel(LossArg
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[i][j][r] = ignored || at.m + i * 16 + r >= a.w.extent ? 0.f : acc[i][j][r];
         }
-        if (!inside) continue;
-        T *to = static_cast<T *>(a.g) + row * a.g_ld + at.m;
+        // a lane has runs of four words, its neighbours' runs of 16 lanes on are next to them: of every two runs one goes to the lane
+        // 16 on or back, so that each writes eight words
+        T *to = static_cast<T *>(a.g) + row * a.g_ld + swapped_m<S>(at.m);
 #pragma unroll
-        for (int i = 0; i < S::TM; ++i) {
-          float g[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) g[r] = acc[i][j][r];
-          store_pack<T, 4>(to + i * 16, g);
+        for (int i = 0; i < S::TM; i += 2) {
+          const Pack<uint32_t, 4> eight = swapped<T>(acc[i][j], acc[i + 1][j]);
+          if (inside) *reinterpret_cast<Pack<uint32_t, 4> *>(to + i * 16) = eight;
         }
       } else {
         if (hits) {

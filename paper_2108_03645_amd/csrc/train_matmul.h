@@ -259,6 +259,25 @@ struct Place {
   }
 };
 
+// The runs of four of two sums (i, j) and (i + 1, j), rounded: lanes of even groups of 16 get the next eight of the first from their
+// own and the next group's run, those of odd groups of the second.  (v_permlane16_swap: odd groups of one register for even ones of another.)
+template <typename T>
+__device__ __forceinline__ Pack<uint32_t, 4> swapped(f32x4 first, f32x4 second) {
+  Pack<T, 4> a, b;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) { a.v[r] = static_cast<T>(first[r]); b.v[r] = static_cast<T>(second[r]); }
+  const uint2 wa = __builtin_bit_cast(uint2, a), wb = __builtin_bit_cast(uint2, b);
+  const auto lo = __builtin_amdgcn_permlane16_swap(wa.x, wb.x, false, false), hi = __builtin_amdgcn_permlane16_swap(wa.y, wb.y, false, false);
+  return Pack<uint32_t, 4>{{lo[0], hi[0], lo[1], hi[1]}};
+}
+// Where those eight start, from Place::m and for i = 0.
+template <typename S>
+__device__ __forceinline__ int32_t swapped_m(int32_t m) {
+  static_assert(S::TM % 2 == 0);
+  const int group = static_cast<int>(threadIdx.x) % kWave >> 4;
+  return m - group * 4 + (group & 1) * 16 + (group >> 1) * 8;
+}
+
 // Tile `id` of tm x tn: ids go round the eight dies, whose L2s are separate, so each die takes a run of neighbouring tiles, by
 // groups of four rows of tiles.
 __device__ __forceinline__ void tile_of(int32_t id, int32_t total, int32_t tm, int32_t tn, int32_t &m, int32_t &n) {
