@@ -373,12 +373,25 @@ Split split_of(int64_t k, int64_t most) {
   return Split{static_cast<int32_t>(std::max<int64_t>(1, ceil_div(k, each))), static_cast<int32_t>(each)};
 }
 
+// The gradients' operands are turned, which takes two reads from LDS a fragment instead of one, and their sums are written: what a tile
+// takes longer for it, from the whole call's time with each of the tiles (rows, columns, words; large, deep, small, tiny, us, with the
+// best split: 1003, 514, 10007: 94, 86, 89, 89; 2048, 512, 8000: 90, 77, 83, 88; 512, 768, 50000: 203, 185, 168, 212; 300, 2048, 16000: 138,
+// 116, 107, 136; 4096, 4096, 4000: 372, 465, 413, 575; 8192, 1024, 32000: 1471, 1781, 1648, 2245).
+TileCost turned_cost(Tiles t) {
+  TileCost c = kTileCosts[t];
+  const double times = t == kTiny ? 1.0 : t == kSmall ? 1.3 : 1.2;
+  c.alone *= times;
+  c.shared *= times;
+  if (t == kLarge) c.fixed += 4.0;
+  return c;
+}
+
 struct GradientPlan { Tiles tiles; Split of_dx, of_dw; };
 GradientPlan gradient_plan(int64_t rows, int64_t cols, int64_t words) {
   GradientPlan best{};
   double best_time = INFINITY;
   for (Tiles t : kUsed) {
-    const TileCost &c = kTileCosts[t];
+    const TileCost c = turned_cost(t);
     const int64_t tm = ceil_div(cols, c.bm), dx = tm * ceil_div(rows, c.bn), dw = tm * ceil_div(words, c.bn);
     for (int64_t most = std::max<int64_t>(128, ceil_div(std::max(rows, words), 64) * 64); most >= 128; most /= 2) {
       const GradientPlan p{t, split_of(words, most), split_of(rows, most)};
