@@ -167,28 +167,34 @@ __global__ __launch_bounds__(S::threads, S::resident) void logits_kernel(LossArg
   }
 }
 
-// The parts of every row joined: 64 rows a workgroup, sixteen threads a row.
-constexpr int kShares = 16;
+// The parts of every row joined: ROWS rows a workgroup, its 1024 threads' shares of them first within the waves, then across.  Eight
+// rows where 64 would leave most compute units without any (us with 64 and 8: one row of 1000 parts 23 and 5.7, 128 of 2000 49 and 9.3,
+// 512 of 392 12 and 5.0, 1000 of 314 10.1 and 4.5, 8192 of 250 9.3 and 10.8, 16000 of 250 9.9 and 18).
+constexpr int kJoinThreads = 1024;
 __device__ __forceinline__ void join(float &top, float &sum, const Part &one) {
   const float both = fmaxf(top, one.top);     // skips NaN; the sum has it then
   sum = both == -INFINITY ? sum + one.sum : sum * __expf(top - both) + one.sum * __expf(one.top - both);
   top = both;
 }
-__global__ __launch_bounds__(64 * kShares) void join_kernel(const Part *parts, int32_t n_parts, int32_t rows, int32_t vocabulary,
+template <int ROWS>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const Part *parts, int32_t n_parts, int32_t rows, int32_t vocabulary,
                                                             const int64_t *target, const float *at_target, float *loss, float *lse) {
-  __shared__ Part shared[kShares][64];
-  const int lane = threadIdx.x % 64, share = threadIdx.x / 64;
-  const int32_t row = blockIdx.x * 64 + lane;
+  constexpr int waves = kJoinThreads / kWave;
+  __shared__ Part shared[waves][ROWS];
+  const int mine = threadIdx.x % ROWS, share = threadIdx.x / ROWS, wave = threadIdx.x / kWave;
+  const int32_t row = blockIdx.x * ROWS + mine;
   float top = -INFINITY, sum = 0.f;
   if (row < rows) {
 #pragma unroll 4
-    for (int p = share; p < n_parts; p += kShares) join(top, sum, parts[static_cast<int64_t>(p) * rows + row]);
+    for (int p = share; p < n_parts; p += kJoinThreads / ROWS) join(top, sum, parts[static_cast<int64_t>(p) * rows + row]);
   }
-  shared[share][lane] = Part{top, sum};
-  __syncthreads();
-  if (share || row >= rows) return;
 #pragma unroll
-  for (int s = 1; s < kShares; ++s) join(top, sum, shared[s][lane]);
+  for (int m = ROWS; m < kWave; m <<= 1) join(top, sum, Part{__shfl_xor(top, m), __shfl_xor(sum, m)});
+  if (static_cast<int>(threadIdx.x) % kWave < ROWS) shared[wave][mine] = Part{top, sum};
+  __syncthreads();
+  if (threadIdx.x >= ROWS || row >= rows) return;
+#pragma unroll
+  for (int s = 1; s < waves; ++s) join(top, sum, shared[s][mine]);
   const float all = top + logf(sum);
   const int64_t t = target[row];
   lse[row] = all;
@@ -572,8 +578,12 @@ int ones_cross_entropy_forward(const void *x, int64_t x_stride, const void *weig
   a.at_target = reinterpret_cast<float *>(ws + p.at_target);
   if (type == ONES_F16) launch_logits<f16, false>(a, p.logits, s);
   else launch_logits<bf16, false>(a, p.logits, s);
-  hipLaunchKernelGGL(join_kernel, dim3(static_cast<uint32_t>(ceil_div(rows, 64))), dim3(64 * kShares), 0, s, a.parts, static_cast<int32_t>(p.parts), n, v,
-                     target, a.at_target, loss, lse);
+  auto join = [&](auto kernel, int64_t each) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(ceil_div(rows, each))), dim3(kJoinThreads), 0, s, a.parts, static_cast<int32_t>(p.parts), n, v,
+                       target, a.at_target, loss, lse);
+  };
+  if (rows < 4096) join(join_kernel<8>, 8);
+  else join(join_kernel<64>, 64);
   return launched("cross entropy forward");
 }
 

@@ -235,3 +235,23 @@ def test_loss_in_a_graph_and_on_another_stream(train):  # noqa: F811
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(got, want)) and all(torch.equal(p, q) for p, q in zip(both(), want))
+
+
+@gpu
+@pytest.mark.parametrize("rows", [4095, 4097])
+def test_loss_where_the_parts_are_joined_otherwise(train, rows):  # noqa: F811
+    """Few rows are joined eight at a time, many 64 at a time; an ignored, an unknown and a NaN row among them."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, 64, generator=gen, device="cuda").bfloat16()
+    w = (torch.randn(3001, 64, generator=gen, device="cuda") * 0.2).bfloat16()
+    t = torch.randint(0, 3001, (rows,), generator=gen, device="cuda")
+    t[7], t[rows - 2], x[rows - 1, 5] = -100, 3001, float("nan")
+    loss, lse = train.linear_cross_entropy_forward(x, w, t)
+    fine = torch.ones(rows, dtype=torch.bool, device="cuda")
+    fine[[7, rows - 2, rows - 1]] = False
+    want, wlse, *_ = loss64(x[fine], w, t[fine], torch.ones(rows - 3, device="cuda"))
+    size = (x[fine].double().abs() @ w.double().abs().t()).amax(1)
+    many = 16 + 4 * 64 ** 0.5 + 3001 / 64
+    near(lse[fine], wlse, size + wlse.abs() + 1, many, "lse")
+    near(loss[fine], want, 2 * size + wlse.abs() + 1, many, "loss")
+    assert loss[7] == 0 and loss[rows - 2].isnan() and lse[rows - 2].isfinite() and loss[rows - 1].isnan() and lse[rows - 1].isnan()
