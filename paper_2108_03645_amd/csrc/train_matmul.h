@@ -78,8 +78,8 @@ struct Tile {
   const unsigned char *base;                  // of the next load: element (first, k); the same for all threads
   uint32_t row_bytes;                         // from an LDS row to the next in memory
   uint32_t offset;                            // from there to what this thread loads, in bytes; kOutside beyond a row's end
-  int32_t piece;                              // this thread's k (m where turned) in the tile
-  int32_t rows_left, k_left;                  // of the operand, LDS rows and k from base on
+  int32_t piece;                              // k (m where turned) in the tile, of what this thread loads
+  int32_t m_left, k_left;                     // what is left of the operand from base on, of m no more than a tile
 
   // The place of logical piece `p` of LDS row `row`, so that the lanes of a read meet different banks.  A read of rows takes the
   // same piece of eight rows at a time; a transposing read takes 32 bytes (a unit of two pieces) of rows k..k+3, and of k+8.
@@ -94,16 +94,16 @@ struct Tile {
     const int row = static_cast<int>(threadIdx.x) / pieces;
     piece = place(row, static_cast<int>(threadIdx.x) % pieces) * 8;
     k_left = o.k - k0;
-    rows_left = min(o.extent - first, B);
+    m_left = min(o.extent - first, B);
     row_bytes = static_cast<uint32_t>(o.ld * 2);
     base = static_cast<const unsigned char *>(o.p) + 2 * (TURNED ? k0 * o.ld + first : first * o.ld + k0);
-    offset = piece < (TURNED ? rows_left : k_left) ? row * row_bytes + piece * 2 : kOutside;
+    offset = piece < (TURNED ? m_left : k_left) ? row * row_bytes + piece * 2 : kOutside;
   }
   // One of the loads of the next K, into LDS at `to` (the same for the whole workgroup); advance() behind the last.
   __device__ __forceinline__ void load_one(unsigned char *to, int i) {
     const uint32_t mine = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LdsBytes *)to)) +
                           __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave) * (kWave * 16);
-    const uint32_t inside = TURNED ? max(min(k_left, K), 0) : rows_left;
+    const uint32_t inside = TURNED ? max(min(k_left, K), 0) : m_left;
     load_to_lds(base, inside * row_bytes, offset + i * rows * row_bytes, mine + i * THREADS * 16);
   }
   __device__ __forceinline__ void advance() {
