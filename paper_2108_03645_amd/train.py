@@ -312,7 +312,8 @@ def linear_cross_entropy_forward(x, weight, target):
     device, operands, wide, (x, weight, target) = _loss_inputs(x, weight, target)
     n, d, v = operands[4:]
     L = load()
-    loss, lse = torch.empty((2, n), dtype=torch.float32, device=device).unbind(0)
+    # two tensors, not views of one: the caller may change the loss in place while lse is kept for the backward call
+    loss, lse = (torch.empty(n, dtype=torch.float32, device=device) for _ in range(2))
     nbytes = L.ones_cross_entropy_forward_workspace_bytes(n, d, v, wide)
     scratch = _scratch(nbytes, device)
     _call(device, L.ones_cross_entropy_forward, *operands, _TYPES[x.dtype], target.data_ptr(), loss.data_ptr(), lse.data_ptr(),

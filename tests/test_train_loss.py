@@ -255,3 +255,38 @@ def test_loss_where_the_parts_are_joined_otherwise(train, rows):  # noqa: F811
     near(lse[fine], wlse, size + wlse.abs() + 1, many, "lse")
     near(loss[fine], want, 2 * size + wlse.abs() + 1, many, "loss")
     assert loss[7] == 0 and loss[rows - 2].isnan() and lse[rows - 2].isfinite() and loss[rows - 1].isnan() and lse[rows - 1].isnan()
+
+
+def test_the_outputs_under_autograd_can_be_changed_in_place(train, monkeypatch):  # noqa: F811
+    """What the binding itself hands out, without a GPU: the library's call is left out, so the values are whatever memory held."""
+    monkeypatch.setattr(train, "_check", lambda *a, **k: None)
+    monkeypatch.setattr(train, "_call", lambda *a: None)
+    x, w = torch.zeros(6, 8).bfloat16().requires_grad_(), torch.zeros(5, 8).bfloat16().requires_grad_()
+    t = torch.tensor([0, 1, -1, 4, 2, -1])
+    loss = train.linear_cross_entropy(x, w, t)
+    loss[t < 0] = 0
+    loss.mul_(0.5)
+    loss.sum().backward()
+    assert x.grad.shape == x.shape and w.grad.shape == w.shape
+    u = torch.zeros(2, 3, 4).requires_grad_()
+    for outputs in ((train.layer_norm(u),), train.gated_recurrence(u, u)):
+        for q in outputs:
+            q.mul_(2)
+        sum(q.sum() for q in outputs).backward()
+
+
+@gpu
+def test_a_loss_changed_in_place_has_the_changed_gradient(train):  # noqa: F811
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    x = torch.randn(40, 64, generator=gen, device="cuda").bfloat16().requires_grad_()
+    w = (torch.randn(90, 64, generator=gen, device="cuda") * 0.2).bfloat16().requires_grad_()
+    t = torch.randint(-1, 90, (40,), generator=gen, device="cuda")
+    weights = torch.rand(40, generator=gen, device="cuda")
+    loss = train.linear_cross_entropy(x, w, t)
+    loss.mul_(weights)
+    loss[:5] = 0
+    loss.sum().backward()
+    weights[:5] = 0
+    _, lse = train.linear_cross_entropy_forward(x.detach(), w.detach(), t)
+    dx, dw = train.linear_cross_entropy_backward(weights, x.detach(), w.detach(), t, lse)
+    assert torch.equal(x.grad, dx) and torch.equal(w.grad, dw)
