@@ -24,7 +24,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
 
 
 HEADERS = [os.path.join(CSRC, h) for h in ("ones_device.h", "ones_sample.h", "ones_candidate.h", "ones_exchange.h", "ones_sort.h",
-                                              "train_device.h", "train_host.h", "train_matmul.h")] + [
+                                              "train_device.h", "train_host.h", "train_matmul.h", "train_plan.h")] + [
            os.path.join(INCLUDE, "ones.h"), os.path.join(INCLUDE, "ones_train.h"),
            os.path.abspath(__file__)]
 

@@ -12,7 +12,6 @@ namespace train {
 using bf16 = __bf16;
 using f16 = _Float16;
 constexpr int kWave = 64;
-constexpr int64_t kMaxLoadableStride = 1 << 20;         // elements between rows that the matrix products load as they lie
 
 template <typename T, int N>
 struct alignas(sizeof(T) * N) Pack {

@@ -31,10 +31,7 @@ namespace ones {
 namespace train {
 namespace {
 
-constexpr int64_t kPieceBytes = 128 << 20;
 constexpr float kLog2E = 1.44269504f;
-
-struct Part { float top, sum; };              // of some logits of a row: the largest, and the sum of exp(z - top)
 
 struct LossArgs {
   Operand w, x;
@@ -256,11 +253,6 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
   }
 }
 
-// A product whose k is shared among `splits` workgroups a tile, `k_each` (a multiple of 64) each.
-struct Split {
-  int32_t splits, k_each;
-};
-
 struct GradientArgs {
   Operand w_turned, g, x_turned, g_turned;
   Split of_dx, of_dw;
@@ -362,110 +354,6 @@ __global__ __launch_bounds__(256) void finish_kernel(FinishArgs a) {
 #pragma unroll
   for (int k = 0; k < V; ++k) v[k] = ignored ? 0.f : v[k] * a.scale[1];
   store_pack<T, V>(static_cast<T *>(a.to[which]) + i, v);
-}
-
-// Which tiles, and into how many parts k is split: the estimate's least.
-constexpr Tiles kUsed[] = {kLarge, kDeep, kSmall, kTiny};
-
-Tiles logits_tiles(int64_t m, int64_t n, int64_t k) {
-  auto time = [&](Tiles t) { return launch_time(kTileCosts[t], ceil_div(m, kTileCosts[t].bm) * ceil_div(n, kTileCosts[t].bn), k); };
-  Tiles best = kLarge;
-  for (Tiles t : kUsed) if (time(t) < time(best)) best = t;
-  return best;
-}
-
-Split split_of(int64_t k, int64_t most) {
-  const int64_t splits = std::max<int64_t>(1, ceil_div(k, most)), each = std::max<int64_t>(64, ceil_div(ceil_div(k, splits), 64) * 64);
-  return Split{static_cast<int32_t>(std::max<int64_t>(1, ceil_div(k, each))), static_cast<int32_t>(each)};
-}
-
-// The gradients' operands are turned, which takes two reads from LDS a fragment instead of one, and their sums are written: what a tile
-// takes longer for it, from the whole call's time with each of the tiles (rows, columns, words; large, deep, small, tiny, us, with the
-// best split: 1003, 514, 10007: 94, 86, 89, 89; 2048, 512, 8000: 90, 77, 83, 88; 512, 768, 50000: 203, 185, 168, 212; 300, 2048, 16000: 138,
-// 116, 107, 136; 4096, 4096, 4000: 372, 465, 413, 575; 8192, 1024, 32000: 1471, 1781, 1648, 2245).
-TileCost turned_cost(Tiles t) {
-  TileCost c = kTileCosts[t];
-  const double times = t == kTiny ? 1.0 : t == kSmall ? 1.3 : 1.2;
-  c.alone *= times;
-  c.shared *= times;
-  if (t == kLarge) c.fixed += 4.0;
-  return c;
-}
-
-struct GradientPlan { Tiles tiles; Split of_dx, of_dw; };
-GradientPlan gradient_plan(int64_t rows, int64_t cols, int64_t words) {
-  GradientPlan best{};
-  double best_time = INFINITY;
-  for (Tiles t : kUsed) {
-    const TileCost c = turned_cost(t);
-    const int64_t tm = ceil_div(cols, c.bm), dx = tm * ceil_div(rows, c.bn), dw = tm * ceil_div(words, c.bn);
-    for (int64_t most = std::max<int64_t>(128, ceil_div(std::max(rows, words), 64) * 64); most >= 128; most /= 2) {
-      const GradientPlan p{t, split_of(words, most), split_of(rows, most)};
-      if (p.of_dx.splits > 32 || p.of_dw.splits > 32) break;
-      const int64_t dx_items = dx * p.of_dx.splits, dw_items = dw * p.of_dw.splits, items = dx_items + dw_items;
-      const double dx_time = item_time(c, items, p.of_dx.k_each), dw_time = item_time(c, items, p.of_dw.k_each);
-      // rounds of places, each as long as the items' mean, or the longest item
-      double time = std::max(std::max(dx_time, dw_time), ceil_div(items, c.places) * (dx_items * dx_time + dw_items * dw_time) / items);
-      double bytes = 0;                       // written and read again
-      if (p.of_dx.splits > 1) bytes += 8.0 * p.of_dx.splits * rows * cols;
-      if (p.of_dw.splits > 1) bytes += 8.0 * p.of_dw.splits * words * cols;
-      if (bytes > 0) time += 4.0 + bytes / 4e6;
-      if (time < best_time) { best = p; best_time = time; }
-    }
-  }
-  return best;
-}
-
-struct LossPlan {
-  int64_t cols8, parts, piece, pieces;
-  Tiles logits, logits_piece;
-  GradientPlan gradients;
-  size_t x, w, part, at_target, forward;                       // offsets, and the bytes of the forward pass
-  size_t g, dx_sum, dw_sum, scale, backward;
-};
-
-LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool copies_x, bool copies_w, bool backward) {
-  LossPlan p{};
-  p.cols8 = ceil_div(cols, 8) * 8;
-  p.logits = logits_tiles(vocabulary, rows, cols);
-  static_assert(Large::WM == 2 && Deep::WM == 2 && Small::WM == 2 && Tiny::WM == 2);
-  p.parts = ceil_div(vocabulary, kTileCosts[p.logits].bm) * 2;
-  size_t off = 0;
-  auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes); return at; };
-  const size_t n = static_cast<size_t>(rows), d = static_cast<size_t>(cols), d8 = static_cast<size_t>(p.cols8);
-  p.x = take(copies_x ? n * d8 * 2 : 0);
-  p.w = take(copies_w ? static_cast<size_t>(vocabulary) * d8 * 2 : 0);
-  const size_t packed = off;
-  p.part = take(static_cast<size_t>(p.parts) * n * sizeof(Part));
-  p.at_target = take(n * 4);
-  p.forward = off;
-  if (!backward) return p;
-  off = packed;
-  for (p.pieces = std::max<int64_t>(1, ceil_div(rows * ceil_div(vocabulary, 256) * 512, kPieceBytes));; ++p.pieces) {
-    p.piece = ceil_div(ceil_div(vocabulary, p.pieces), 256) * 256;
-    p.gradients = gradient_plan(rows, cols, std::min(p.piece, vocabulary));
-    const Split dx = p.gradients.of_dx, dw = p.gradients.of_dw;
-    const int64_t sums = ((dx.splits - 1) * rows + (dw.splits > 1 ? dw.splits * p.piece : 0)) * cols * 4;
-    if (p.piece == 256 || rows * p.piece * 2 + sums <= kPieceBytes) break;
-  }
-  p.pieces = ceil_div(vocabulary, p.piece);
-  p.logits_piece = logits_tiles(p.piece, rows, cols);
-  p.g = take(n * static_cast<size_t>(p.piece) * 2);
-  p.dx_sum = take(p.pieces > 1 || p.gradients.of_dx.splits > 1 ? p.gradients.of_dx.splits * n * d * 4 : 0);
-  p.dw_sum = take(p.gradients.of_dw.splits > 1 ? static_cast<size_t>(p.gradients.of_dw.splits) * std::min(p.piece, vocabulary) * d * 4 : 0);
-  p.scale = take(8);
-  p.backward = off;
-  return p;
-}
-
-int check_loss(int64_t rows, int64_t cols, int64_t vocabulary, int64_t x_stride, int64_t w_stride, int32_t type) {
-  if (int rc = check_rows(rows, cols, x_stride)) return rc;
-  if (int rc = check_rows(vocabulary, cols, w_stride)) return rc;
-  if (cols < 1 || vocabulary < 1 || (type != ONES_F16 && type != ONES_BF16)) return ONES_E_INVALID_ARG;
-  if (rows > ONES_MAX_LOSS_ROWS || vocabulary > ONES_MAX_VOCABULARY || cols > ONES_MAX_LOSS_COLUMNS) return ONES_E_BOUNDS;
-  // tiles of a launch: at most 2^23, of 256 threads
-  const int64_t n = ceil_div(rows, 128), v = ceil_div(vocabulary, 128), d = ceil_div(cols, 128);
-  return std::max({n * v, d * n, d * v}) > (1 << 22) ? ONES_E_BOUNDS : ONES_OK;
 }
 
 // Rows that the products can load as they lie: 16 bytes at a time, the rows of a tile (256 at most) inside 2^31 bytes,

@@ -14,6 +14,7 @@
 #pragma once
 
 #include "train_device.h"
+#include "train_plan.h"
 
 namespace ones {
 namespace train {
@@ -147,6 +148,13 @@ using MiddleTurned = Shape<128, 192, 2, 4, 3, 1>;
 using Deep = Shape<128, 128, 2, 4, 4, 1>;
 using Small = Shape<128, 128, 2, 4, 2, 2>;
 using Tiny = Shape<64, 64, 2, 2, 4, 2>;
+
+// The plans (train_plan.h) count these.
+template <typename S, Tiles T>
+constexpr bool kCounted = S::BM == kTileCosts[T].bm && S::BN == kTileCosts[T].bn && S::resident * 256 == kTileCosts[T].places;
+static_assert(kCounted<Large, kLarge> && kCounted<Middle, kMiddle> && kCounted<Deep, kDeep> && kCounted<Small, kSmall> && kCounted<Tiny, kTiny> &&
+              MiddleTurned::BM == Middle::BN && MiddleTurned::BN == Middle::BM);
+static_assert(Large::WM == 2 && Deep::WM == 2 && Small::WM == 2 && Tiny::WM == 2);      // parts of the loss: two a tile of logits
 
 template <typename S>
 using Sums = f32x4[S::TM][S::TN];

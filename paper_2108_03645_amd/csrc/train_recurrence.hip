@@ -32,7 +32,7 @@ namespace ones {
 namespace train {
 namespace {
 
-constexpr int kThreads = 256, kV = 4, kTile = 128;
+constexpr int kThreads = 256;
 
 struct RecurrenceArgs {
   const void *gate, *x, *dh;
@@ -421,32 +421,6 @@ __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(const T *gate
   store_some<T, kV>(h + b * channels + c, now, have);
 }
 
-constexpr int64_t kEnough = 192, kWanted = 512;
-int64_t tiles_of(int64_t steps) { return ceil_div(steps, kTile); }
-
-// How the work is cut.  Workgroups of 32 channels (8 lanes to a row) are twice as many as of 64, and two share every cache line
-// of 128 bytes: on the same die, at about the same time.  Where they are enough for most compute units, or the tiles too few to
-// split, they walk along whole sequences; backward (with five arrays instead of three) only along short ones, before two that
-// share lines drift apart, and 64 channels along longer ones (us, 32 against 64 channels, bf16: forward 16 x 2048 x 1024 39 against
-// 44, 64 x 256 x 1024 21 and 22, 8 x 512 x 512 8.7 and 11.5; backward 95 and 80, 33 and 42, 11.4 and 16.2).  Otherwise 64 channels, and
-// as many segments as make two workgroups a compute unit (2 x 65521 x 512: 512 workgroups 141 and 220 us, 1024 152 and 231; with 32
-// channels 179 and 250), which is 4.7 TB/s for what they read twice and write.
-struct Cut {
-  int32_t lanes, segments, tiles_each;
-};
-Cut cut_of(int64_t batch, int64_t steps, int64_t channels, bool backward) {
-  const int64_t tiles = std::max<int64_t>(1, tiles_of(steps)), narrow = batch * ceil_div(channels, 32), chains = batch * ceil_div(channels, 64);
-  const int32_t all = static_cast<int32_t>(tiles);
-  if ((narrow >= kEnough || tiles < 8) && (!backward || tiles <= 8)) return Cut{8, 1, all};
-  if (backward && chains >= kEnough) return Cut{16, 1, all};
-  const int64_t each = ceil_div(tiles, std::min(tiles, ceil_div(kWanted, std::max<int64_t>(1, chains))));
-  return Cut{16, static_cast<int32_t>(ceil_div(tiles, each)), static_cast<int32_t>(each)};
-}
-int64_t blocks_of(const Cut &cut, int64_t batch, int64_t channels) {
-  const int64_t blocks = ceil_div(channels, cut.lanes * kV);
-  return cut.lanes == 16 ? blocks * batch * cut.segments : ceil_div(ceil_div(blocks, 2) * batch * cut.segments, 8) * 16;
-}
-
 template <typename T, int LANES, bool EDGE, bool FORM, bool PAST>
 void launch_recurrence(const RecurrenceArgs &a, int64_t blocks, bool backward, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(blocks));
@@ -482,20 +456,6 @@ void launch_recurrence_type(RecurrenceArgs &a, int32_t type, bool backward, hipS
   else launch_recurrence<bf16>(a, cut, backward, s);
 }
 
-int check_recurrence(int64_t batch, int64_t steps, int64_t channels, int32_t type) {
-  if (batch < 0 || steps < 0 || channels < 0 || !is_type(type)) return ONES_E_INVALID_ARG;
-  if (batch > ONES_MAX_BATCH || steps > ONES_MAX_STEPS || channels > ONES_MAX_CHANNELS) return ONES_E_BOUNDS;
-  if (steps && channels && batch > kMaxElements / (steps * channels)) return ONES_E_BOUNDS;
-  // workgroups of a launch
-  return std::max(blocks_of(cut_of(batch, steps, channels, false), batch, channels), blocks_of(cut_of(batch, steps, channels, true), batch, channels)) > (1 << 23)
-             ? ONES_E_BOUNDS : ONES_OK;
-}
-// Rows of `channels` elements, `step` elements apart and sequences `batch` elements apart.
-int check_strides(int64_t batch_stride, int64_t step_stride, int64_t channels) {
-  if (batch_stride < 0 || step_stride < 0) return ONES_E_INVALID_ARG;
-  return batch_stride > (int64_t{1} << 40) || step_stride > (int64_t{1} << 32) ? ONES_E_BOUNDS : ONES_OK;
-}
-
 template <typename T>
 void launch_step(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride, int64_t batch, int64_t channels, float *state, void *h,
                  hipStream_t s) {
@@ -503,8 +463,6 @@ void launch_step(const void *gate, int64_t gate_stride, const void *x, int64_t x
   hipLaunchKernelGGL((recurrence_step_kernel<T>), grid, dim3(kThreads), 0, s, static_cast<const T *>(gate), static_cast<const T *>(x), state,
                      static_cast<T *>(h), batch, static_cast<int32_t>(channels), gate_stride, x_stride);
 }
-
-size_t carry_floats(int64_t batch, int64_t steps, int64_t channels) { return static_cast<size_t>(batch) * tiles_of(steps) * channels; }
 
 }  // namespace
 }  // namespace train

@@ -32,7 +32,6 @@ namespace train {
 namespace {
 
 constexpr float kUnitX = 2048.f, kUnitA = 1024.f;
-constexpr int64_t kSumBlocks = 1024;          // workgroups that share a matrix's sum of squares, at most
 
 struct MomentumArgs {
   const void *grad;
@@ -125,20 +124,13 @@ struct ProductArgs {
   float one, two;                             // coefficients
 };
 
-// Tiles of rows n that begin at or below the diagonal (the first column is not beyond the last row), before tile row j.
-template <typename S>
-__host__ __device__ inline int32_t tiles_in_row(int32_t j, int32_t tm) {
-  const int32_t n = ((j + 1) * S::BN - 1) / S::BM + 1;
-  return n < tm ? n : tm;
-}
-
 // A = X X^T, or (POLY) B = b A + c A A.  Only the elements on and below the diagonal are computed; each is written to both places.
 template <typename S, bool POLY>
 __global__ __launch_bounds__(S::threads, S::resident) void symmetric_kernel(ProductArgs a) {
   __shared__ __align__(16) unsigned char lds[S::lds];
   const int32_t tm = (a.r_ld + S::BM - 1) / S::BM, total = static_cast<int32_t>(gridDim.x), die = static_cast<int32_t>(blockIdx.x) % 8;
   int32_t m = die * (total / 8) + min(die, total % 8) + static_cast<int32_t>(blockIdx.x) / 8, n = 0;      // a run of tiles to each die
-  for (int32_t in = tiles_in_row<S>(0, tm); m >= in; in = tiles_in_row<S>(++n, tm)) m -= in;
+  for (int32_t in = tiles_in_row(0, tm, S::BM, S::BN); m >= in; in = tiles_in_row(++n, tm, S::BM, S::BN)) m -= in;
   const f16 *from = POLY ? a.a + static_cast<int64_t>(blockIdx.y) * a.r * a.r_ld : a.x + static_cast<int64_t>(blockIdx.y) * a.r * a.q_ld;
   const Operand o{from, POLY ? a.r_ld : a.q_ld, a.r, POLY ? a.r_ld : a.q_ld};
   Sums<S> acc;
@@ -213,35 +205,6 @@ __global__ __launch_bounds__(S::threads, S::resident) void apply_kernel(ProductA
   }
 }
 
-struct UpdatePlan {
-  int64_t r, q, r_ld, q_ld;
-  int64_t blocks;
-  size_t squares, x[2], a[2], total;
-};
-UpdatePlan update_plan(int64_t count, int64_t rows, int64_t cols) {
-  UpdatePlan p{};
-  p.r = std::min(rows, cols);
-  p.q = std::max(rows, cols);
-  p.r_ld = ceil_div(p.r, 8) * 8;
-  p.q_ld = ceil_div(p.q, 8) * 8;
-  size_t off = 0;
-  auto take = [&](int64_t bytes) { const size_t at = off; off = align_up(off + static_cast<size_t>(bytes)); return at; };
-  p.blocks = std::min(kSumBlocks, ceil_div(rows * cols, 4096));            // at least four runs of four elements a thread
-  p.squares = take(count * p.blocks * 4);
-  p.x[0] = take(count * p.r * p.q_ld * 2);
-  p.x[1] = take(count * p.r * p.q_ld * 2);
-  p.a[0] = take(count * p.r * p.r_ld * 2);
-  p.a[1] = take(count * p.r * p.r_ld * 2);
-  p.total = off;
-  return p;
-}
-
-int check_update(int64_t count, int64_t rows, int64_t cols) {
-  if (count < 0 || rows < 0 || cols < 0) return ONES_E_INVALID_ARG;
-  if (count > 65535 || rows > ONES_MAX_UPDATE_SIDE || cols > ONES_MAX_UPDATE_SIDE) return ONES_E_BOUNDS;
-  return ONES_OK;
-}
-
 template <typename T>
 void launch_momentum(const MomentumArgs &a, int64_t count, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(a.blocks), static_cast<uint32_t>(count));
@@ -251,17 +214,11 @@ void launch_momentum(const MomentumArgs &a, int64_t count, hipStream_t s) {
 }
 
 template <typename S>
-int64_t symmetric_tiles(int64_t r_ld) {
-  int64_t tiles = 0;
-  for (int32_t j = 0; j < ceil_div(r_ld, S::BN); ++j) tiles += tiles_in_row<S>(j, static_cast<int32_t>(ceil_div(r_ld, S::BM)));
-  return tiles;
-}
-template <typename S>
 int64_t all_tiles(const ProductArgs &a) { return ceil_div(a.r, S::BN) * ceil_div(a.q, S::BM); }
 
 template <typename S, bool POLY>
 void launch_symmetric(const ProductArgs &a, int64_t count, hipStream_t s) {
-  hipLaunchKernelGGL((symmetric_kernel<S, POLY>), dim3(static_cast<uint32_t>(symmetric_tiles<S>(a.r_ld)), static_cast<uint32_t>(count)), dim3(S::threads), 0, s, a);
+  hipLaunchKernelGGL((symmetric_kernel<S, POLY>), dim3(static_cast<uint32_t>(symmetric_tiles(S::BM, S::BN, a.r_ld)), static_cast<uint32_t>(count)), dim3(S::threads), 0, s, a);
 }
 template <bool POLY>
 void launch_symmetric(const ProductArgs &a, Tiles tiles, int64_t count, hipStream_t s) {
@@ -285,14 +242,6 @@ void launch_apply(const ProductArgs &a, Tiles tiles, int64_t count, hipStream_t 
     case kSmall: return launch_apply<Small>(a, count, s);
     default: return launch_apply<Tiny>(a, count, s);
   }
-}
-
-// Which tiles: the estimate's least.
-Tiles least(const int64_t (&items)[5], int64_t k) {
-  Tiles best = kLarge;
-  for (Tiles t : {kMiddle, kDeep, kSmall, kTiny})
-    if (launch_time(kTileCosts[t], items[t], k) < launch_time(kTileCosts[best], items[best], k)) best = t;
-  return best;
 }
 
 }  // namespace
@@ -346,24 +295,20 @@ int ones_orthogonal_update(const void *grad, float *momentum, int64_t count, int
   q.r = n.r; q.q = n.q; q.r_ld = static_cast<int32_t>(p.r_ld); q.q_ld = n.q_ld;
   q.out_type = update_type;
   q.turned = rows > cols;
-  const int64_t triangle[] = {count * symmetric_tiles<Large>(p.r_ld), count * symmetric_tiles<Middle>(p.r_ld), count * symmetric_tiles<Deep>(p.r_ld),
-                              count * symmetric_tiles<Small>(p.r_ld), count * symmetric_tiles<Tiny>(p.r_ld)};
-  const int64_t all[] = {count * all_tiles<Large>(q), count * all_tiles<MiddleTurned>(q), count * all_tiles<Deep>(q), count * all_tiles<Small>(q),
-                         count * all_tiles<Tiny>(q)};
-  const Tiles for_gram = least(triangle, p.q), for_poly = least(triangle, p.r), for_apply = least(all, p.r);
+  const UpdateTiles tiles = update_tiles(count, p.r, p.q);
   for (int32_t step = 0; step < steps; ++step) {
     q.x = x[step & 1];
     q.to = a[0];
-    launch_symmetric<false>(q, for_gram, count, s);
+    launch_symmetric<false>(q, tiles.gram, count, s);
     q.a = a[0];
     q.to = a[1];
     q.one = coefficients[1]; q.two = coefficients[2];
-    launch_symmetric<true>(q, for_poly, count, s);
+    launch_symmetric<true>(q, tiles.poly, count, s);
     q.a = a[1];
     q.to = x[(step & 1) ^ 1];
     q.out = step + 1 == steps ? update : nullptr;
     q.one = coefficients[0];
-    launch_apply(q, for_apply, count, s);
+    launch_apply(q, tiles.apply, count, s);
   }
   return launched("orthogonal update");
 }
