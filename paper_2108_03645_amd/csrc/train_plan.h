@@ -176,7 +176,9 @@ inline LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool c
   p.forward = off;
   if (!backward) return p;
   off = packed;
-  for (p.pieces = std::max<int64_t>(1, ceil_div(rows * ceil_div(vocabulary, 256) * 512, kPieceBytes));; ++p.pieces) {
+  // G's rows are a piece apart, and the products load them as they lie
+  const int64_t least_pieces = std::max(ceil_div(vocabulary, kMaxLoadableStride), ceil_div(rows * ceil_div(vocabulary, 256) * 512, kPieceBytes));
+  for (p.pieces = least_pieces;; ++p.pieces) {
     p.piece = ceil_div(ceil_div(vocabulary, p.pieces), 256) * 256;
     p.gradients = gradient_plan(rows, cols, std::min(p.piece, vocabulary));
     const Split dx = p.gradients.of_dx, dw = p.gradients.of_dw;

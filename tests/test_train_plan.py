@@ -188,3 +188,38 @@ def test_recurrence_of_every_cut(train, sizes, dtype):  # noqa: F811
     near(dx, wdx, (lam * slow).expand_as(wdx), 16, "dx")
     near(dgate, wdgate, (lam * top * slow * 2).expand_as(wdgate), 16, "dgate")
     near(dstate, wdstate, (lam * slow).expand_as(wdstate), 16, "dstate")
+
+
+def test_the_logits_gradients_lie_no_further_apart_than_the_products_load(plans, train):  # noqa: F811
+    """Rows of what the products load lie 2^20 elements apart at most: 256 rows at offsets of 32 bits."""
+    for rows, cols, words in ((1, 8, 1 << 24), (3, 24, (1 << 20) + 1), (2, 8, 1 << 20), (63, 64, 1 << 21), (500, 8, 1 << 24)):
+        *_, piece, pieces = plans("loss", 7, rows, cols, words)
+        assert piece <= 1 << 20 and (pieces - 1) * piece < words <= pieces * piece
+    L, p = train.load(), C.c_void_p(0x1000)
+    wide = L.ones_cross_entropy_forward_workspace_bytes(4, 64, 100, 1)
+    for xs, ws in ((64, (1 << 20) + 8), ((1 << 20) + 8, 64)):
+        assert L.ones_cross_entropy_forward(p, xs, p, ws, 4, 64, 100, 2, p, p, p, p, wide, None) == -5
+    wide = L.ones_cross_entropy_backward_workspace_bytes(4, 64, 100, 1)
+    assert L.ones_cross_entropy_backward(p, p, 64, p, (1 << 20) + 8, 4, 64, 100, 2, p, p, p, p, p, wide, None) == -5
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+def test_loss_of_few_rows_over_a_vocabulary_of_millions(train, dtype):  # noqa: F811
+    words = (1 << 20) + 300
+    gen = torch.Generator(device="cuda").manual_seed(23)
+    x = torch.randn(3, 24, generator=gen, device="cuda").to(dtype)
+    w = (torch.randn(words, 24, generator=gen, device="cuda") * 0.3).to(dtype)
+    check(train, x, w, torch.tensor([words - 1, 5, 1 << 19], device="cuda"), torch.rand(3, generator=gen, device="cuda"))
+
+
+@gpu
+def test_loss_of_rows_as_far_apart_as_the_products_load(train):  # noqa: F811
+    """2^20 elements: loaded as they lie, with the workspace that has no room for copies; eight more: copied."""
+    gen = torch.Generator(device="cuda").manual_seed(29)
+    for stride in (1 << 20, (1 << 20) + 8):
+        apart = torch.empty(300 * stride, dtype=torch.bfloat16, device="cuda").as_strided((300, 64), (stride, 1))
+        apart.copy_(torch.randn(300, 64, generator=gen, device="cuda"))
+        other = (torch.randn(270, 64, generator=gen, device="cuda") * 0.2).bfloat16()
+        check(train, other, apart, torch.randint(0, 300, (270,), generator=gen, device="cuda"), torch.rand(270, generator=gen, device="cuda"))
+        check(train, apart, other, torch.randint(0, 270, (300,), generator=gen, device="cuda"), torch.rand(300, generator=gen, device="cuda"))
