@@ -84,7 +84,8 @@ int ones_recurrence_step(const void *gate, int64_t gate_stride, const void *x, i
  * type (of x, weight, dx, dweight): ONES_F16 or ONES_BF16.  target: int64 [rows]; below 0: the row is ignored (loss 0, no
  * gradient, and what x holds there does not matter); vocabulary or above: the row's loss, its dx and dweight are NaN.
  * loss, lse: float [rows].  Backward: dloss float [rows], lse as forward left it; dx[rows][cols] and dweight[vocabulary][cols]
- * are written.  It goes through the vocabulary in pieces of at most 128 MiB of logits' gradients, rounded to type.
+ * are written.  It goes through the vocabulary in pieces, and through more than 2^18 rows in blocks, so that at most 128 MiB of logits'
+ * gradients, rounded to type, are held at a time.
  * wide: not 0 if cols, both strides and both bases are multiples of 16 bytes and no stride is above 2^20 elements; otherwise the
  * workspace has room for copies.
  * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size above its limit, or the product of two of them above 2^36),

@@ -8,8 +8,9 @@
 // largest logit of a wave's part of the vocabulary and the sum of exponentials below it; a small second launch joins them.
 // Backward goes through the vocabulary in pieces: one launch forms G of a piece, rounded to 16 bits (the operands' type, as
 // a product of that type needs), and one launch its dW and what it adds to dx, which is summed in 32 bits over the pieces.
-// A piece's G, with the sums of products whose k is split, has at most 128 MiB, half of the last-level cache, so that the two
-// products that read it mostly find it there.
+// A piece's G has at most 128 MiB, with the sums of products whose k is split where that leaves more than 256 words: half of the
+// last-level cache, so that the two products that read it mostly find it there.  More than 262144 rows, of which 256 words would be
+// more, are taken in blocks within each piece, and dW is summed in 32 bits over them.
 //
 // Measured, where a large library product reaches 1.35 (8192 cubed) to 1.5 PFLOP/s: logits of 16384 x 32000, k 512, with their
 // epilogue 455 us (1.18 PFLOP/s; a tile of 256 x 256 takes 1.4 us for 64 k and 5 us for its start and its exponentials), 8192 x
@@ -260,11 +261,13 @@ struct GradientArgs {
   const float *scale;
   float *dx_sum, *dw_sum;                     // [splits][rows][cols], [splits][words][cols]
   void *dx, *dweight;                         // dweight: of the piece's first word
-  int32_t cols, first, last, wide;            // wide: runs of four of dx and dW can be written at once
+  int32_t cols, wide;                         // wide: runs of four of dx and dW can be written at once
+  int32_t dx_first, dx_last, dw_first, dw_last;       // of the pieces that dx is summed over, of the blocks of rows that dW is
+  int32_t dw_parts;                           // parts of dW to be added up behind the last block; 0: written here
 };
 
-// The tiles of dx first, then those of a piece's dW.  dx is added up over the pieces in 32 bits, in as many places as k is split;
-// a product in one part that is complete is rounded and written.
+// The tiles of dx of a block of rows first, then those of a piece's dW.  dx is added up over the pieces in 32 bits, dW over the blocks, in
+// as many places as k is split; a product in one part that is complete is rounded and written.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::threads, S::resident) void gradients_kernel(GradientArgs a) {
   __shared__ __align__(16) unsigned char lds[S::lds];
@@ -280,7 +283,7 @@ __global__ __launch_bounds__(S::threads, S::resident) void gradients_kernel(Grad
   if (of_dx) product<T, true, false, S>(a.w_turned, a.g, m * S::BM, n * S::BN, k0, min(a.g.k, k0 + split.k_each), lds, acc);
   else product<T, true, true, S>(a.x_turned, a.g_turned, m * S::BM, n * S::BN, k0, min(a.g_turned.k, k0 + split.k_each), lds, acc);
   const Place<S> at(m * S::BM, n * S::BN);
-  const bool wide = a.wide, whole = split.splits == 1 && (!of_dx || a.last), adds = of_dx && !a.first;
+  const bool wide = a.wide, whole = of_dx ? split.splits == 1 && a.dx_last : !a.dw_parts, adds = !(of_dx ? a.dx_first : a.dw_first);
   const int32_t rows = of_dx ? a.g.extent : a.g_turned.extent;
   const float back = whole ? a.scale[1] : 1.f;
   float *sum = (of_dx ? a.dx_sum : a.dw_sum) + static_cast<int64_t>(part) * rows * a.cols;
@@ -325,7 +328,7 @@ __global__ __launch_bounds__(S::threads, S::resident) void gradients_kernel(Grad
   }
 }
 
-// The parts of products that were split, added up in order and rounded: dx after the last piece, and the piece's dW.
+// The parts of products that were split, added up in order and rounded: dx of a block after the last piece, dW of a piece after the last block.
 struct FinishArgs {
   const float *sum[2];
   void *to[2];
@@ -404,7 +407,7 @@ void launch_finish(const FinishArgs &a, hipStream_t s) {
   else hipLaunchKernelGGL((finish_kernel<T, 1>), dim3(static_cast<uint32_t>(ceil_div(total, 256))), dim3(256), 0, s, a);
 }
 
-// A piece of the vocabulary: its G, dW, and what it adds to dx.
+// A piece of the vocabulary and a block of rows: its G, and what it adds to dW and dx.
 template <typename T>
 void launch_piece(const LossArgs &a, const GradientArgs &b, const LossPlan &p, hipStream_t s) {
   if (a.x.extent) launch_logits<T, true>(a, p.logits_piece, s);
@@ -412,9 +415,9 @@ void launch_piece(const LossArgs &a, const GradientArgs &b, const LossPlan &p, h
   FinishArgs f{};
   f.sum[0] = b.dx_sum; f.sum[1] = b.dw_sum;
   f.to[0] = b.dx; f.to[1] = b.dweight;
-  f.splits[0] = b.of_dx.splits; f.splits[1] = b.of_dw.splits;
-  f.size[0] = b.of_dx.splits > 1 && b.last ? static_cast<int64_t>(b.g.extent) * b.cols : 0;
-  f.size[1] = b.of_dw.splits > 1 ? static_cast<int64_t>(b.g_turned.extent) * b.cols : 0;
+  f.splits[0] = b.of_dx.splits; f.splits[1] = b.dw_parts;
+  f.size[0] = b.of_dx.splits > 1 && b.dx_last ? static_cast<int64_t>(b.g.extent) * b.cols : 0;
+  f.size[1] = b.dw_parts && b.dw_last ? static_cast<int64_t>(b.g_turned.extent) * b.cols : 0;
   f.cols = b.cols;
   f.wide = b.wide;
   f.target = b.target;
@@ -491,38 +494,46 @@ int ones_cross_entropy_backward(const float *dloss, const void *x, int64_t x_str
                 {reinterpret_cast<uint16_t *>(ws + p.x), reinterpret_cast<uint16_t *>(ws + p.w)}, {x_stride, weight_stride},
                 {n, copy_w ? static_cast<int32_t>(vocabulary) : 0}, static_cast<int32_t>(cols), d8, target, dloss, scale};
   launch_pack(pack, s);
-  const Operand xs{ws + p.x, d8, n, d8};
   const char *w = copy_w ? ws + p.w : static_cast<const char *>(weight);
   const int64_t w_ld = copy_w ? d8 : weight_stride;
   for (int64_t v0 = 0; v0 < vocabulary; v0 += p.piece) {
     const int32_t words = static_cast<int32_t>(std::min(p.piece, vocabulary - v0));
     const char *wp = w + v0 * w_ld * 2;
-    LossArgs a{};
-    a.w = Operand{wp, w_ld, words, d8};
-    a.x = xs;
-    a.v0 = static_cast<int32_t>(v0);
-    a.vocabulary = static_cast<int32_t>(vocabulary);
-    a.target = target; a.lse = lse; a.dloss = dloss; a.scale = scale;
-    a.g = ws + p.g;
-    a.g_ld = p.piece;
-    GradientArgs b{};
-    b.w_turned = Operand{wp, w_ld, d8, words};
-    b.g = Operand{ws + p.g, p.piece, n, words};               // the rest of the last eight words is zeros
-    b.x_turned = Operand{ws + p.x, d8, d8, n};
-    b.g_turned = Operand{ws + p.g, p.piece, words, n};
-    b.target = target; b.scale = scale;
-    b.of_dx = p.gradients.of_dx;
-    b.of_dw = p.gradients.of_dw;
-    b.dx_sum = reinterpret_cast<float *>(ws + p.dx_sum);
-    b.dw_sum = reinterpret_cast<float *>(ws + p.dw_sum);
-    b.dx = dx;
-    b.dweight = static_cast<char *>(dweight) + v0 * cols * 2;
-    b.cols = static_cast<int32_t>(cols);
-    b.wide = cols % 4 == 0 && aligned(dx, 8) && aligned(dweight, 8);
-    b.first = v0 == 0;
-    b.last = v0 + p.piece >= vocabulary;
-    if (type == ONES_F16) launch_piece<f16>(a, b, p, s);
-    else launch_piece<bf16>(a, b, p, s);
+    int64_t r0 = 0;
+    do {                                      // once for no rows: dW is zeros then
+      const int32_t some = static_cast<int32_t>(std::min(p.block, rows - r0));
+      const char *xp = ws + p.x + r0 * d8 * 2;
+      LossArgs a{};
+      a.w = Operand{wp, w_ld, words, d8};
+      a.x = Operand{xp, d8, some, d8};
+      a.v0 = static_cast<int32_t>(v0);
+      a.vocabulary = static_cast<int32_t>(vocabulary);
+      a.target = target + r0; a.lse = lse + r0; a.dloss = dloss + r0; a.scale = scale;
+      a.g = ws + p.g;
+      a.g_ld = p.piece;
+      GradientArgs b{};
+      b.w_turned = Operand{wp, w_ld, d8, words};
+      b.g = Operand{ws + p.g, p.piece, some, words};          // the rest of the last eight words is zeros
+      b.x_turned = Operand{xp, d8, d8, some};
+      b.g_turned = Operand{ws + p.g, p.piece, words, some};
+      b.target = target + r0; b.scale = scale;
+      b.of_dx = p.gradients.of_dx;
+      b.of_dw = p.gradients.of_dw;
+      b.dx_sum = reinterpret_cast<float *>(ws + p.dx_sum) + b.of_dx.splits * r0 * cols;
+      b.dw_sum = reinterpret_cast<float *>(ws + p.dw_sum);
+      b.dx = static_cast<char *>(dx) + r0 * cols * 2;
+      b.dweight = static_cast<char *>(dweight) + v0 * cols * 2;
+      b.cols = static_cast<int32_t>(cols);
+      b.wide = cols % 4 == 0 && aligned(dx, 8) && aligned(dweight, 8);
+      b.dx_first = v0 == 0;
+      b.dx_last = v0 + p.piece >= vocabulary;
+      b.dw_first = r0 == 0;
+      b.dw_last = r0 + p.block >= rows;
+      b.dw_parts = p.blocks > 1 || b.of_dw.splits > 1 ? b.of_dw.splits : 0;
+      if (type == ONES_F16) launch_piece<f16>(a, b, p, s);
+      else launch_piece<bf16>(a, b, p, s);
+      r0 += p.block;
+    } while (r0 < rows);
   }
   return launched("cross entropy backward");
 }

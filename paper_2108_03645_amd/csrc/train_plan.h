@@ -152,8 +152,9 @@ inline GradientPlan gradient_plan(int64_t rows, int64_t cols, int64_t words) {
   return best;
 }
 
+// Backward: pieces of the vocabulary, each with all blocks of rows.
 struct LossPlan {
-  int64_t cols8, parts, piece, pieces;
+  int64_t cols8, parts, piece, pieces, block, blocks;
   Tiles logits, logits_piece;
   GradientPlan gradients;
   size_t x, w, part, at_target, forward;                       // offsets, and the bytes of the forward pass
@@ -176,20 +177,24 @@ inline LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool c
   p.forward = off;
   if (!backward) return p;
   off = packed;
+  // a block's G of the smallest piece fills its bytes at most
+  p.blocks = std::max<int64_t>(1, ceil_div(rows * 512, kPieceBytes));
+  p.block = std::max<int64_t>(64, ceil_div(ceil_div(rows, p.blocks), 64) * 64);
+  const int64_t at_once = std::min(rows, p.block);
   // G's rows are a piece apart, and the products load them as they lie
-  const int64_t least_pieces = std::max(ceil_div(vocabulary, kMaxLoadableStride), ceil_div(rows * ceil_div(vocabulary, 256) * 512, kPieceBytes));
+  const int64_t least_pieces = std::max(ceil_div(vocabulary, kMaxLoadableStride), ceil_div(at_once * ceil_div(vocabulary, 256) * 512, kPieceBytes));
   for (p.pieces = least_pieces;; ++p.pieces) {
     p.piece = ceil_div(ceil_div(vocabulary, p.pieces), 256) * 256;
-    p.gradients = gradient_plan(rows, cols, std::min(p.piece, vocabulary));
+    p.gradients = gradient_plan(at_once, cols, std::min(p.piece, vocabulary));
     const Split dx = p.gradients.of_dx, dw = p.gradients.of_dw;
-    const int64_t sums = ((dx.splits - 1) * rows + (dw.splits > 1 ? dw.splits * p.piece : 0)) * cols * 4;
-    if (p.piece == 256 || rows * p.piece * 2 + sums <= kPieceBytes) break;
+    const int64_t sums = ((dx.splits - 1) * at_once + (dw.splits > 1 ? dw.splits * p.piece : 0)) * cols * 4;
+    if (p.piece == 256 || at_once * p.piece * 2 + sums <= kPieceBytes) break;
   }
   p.pieces = ceil_div(vocabulary, p.piece);
-  p.logits_piece = logits_tiles(p.piece, rows, cols);
-  p.g = take(n * static_cast<size_t>(p.piece) * 2);
+  p.logits_piece = logits_tiles(p.piece, at_once, cols);
+  p.g = take(static_cast<size_t>(at_once * p.piece) * 2);
   p.dx_sum = take(p.pieces > 1 || p.gradients.of_dx.splits > 1 ? p.gradients.of_dx.splits * n * d * 4 : 0);
-  p.dw_sum = take(p.gradients.of_dw.splits > 1 ? static_cast<size_t>(p.gradients.of_dw.splits) * std::min(p.piece, vocabulary) * d * 4 : 0);
+  p.dw_sum = take(p.blocks > 1 || p.gradients.of_dw.splits > 1 ? static_cast<size_t>(p.gradients.of_dw.splits) * std::min(p.piece, vocabulary) * d * 4 : 0);
   p.scale = take(8);
   p.backward = off;
   return p;

@@ -28,6 +28,11 @@ void loss(int64_t rows, int64_t cols, int64_t words, int64_t *to) {
   const int64_t out[] = {p.logits, p.logits_piece, p.gradients.tiles, p.gradients.of_dx.splits, p.gradients.of_dw.splits, p.piece, p.pieces};
   std::copy(out, out + 7, to);
 }
+void blocks(int64_t rows, int64_t cols, int64_t words, int64_t *to) {
+  const LossPlan p = loss_plan(rows, cols, words, true, false, true);
+  const int64_t out[] = {p.block, p.blocks, p.piece, static_cast<int64_t>((p.dx_sum ? p.dx_sum : p.backward) - p.g)};
+  std::copy(out, out + 4, to);
+}
 void update(int64_t count, int64_t rows, int64_t cols, int64_t *to) {
   const UpdateTiles t = update_tiles(count, std::min(rows, cols), std::max(rows, cols));
   to[0] = t.gram; to[1] = t.poly; to[2] = t.apply;
@@ -223,3 +228,29 @@ def test_loss_of_rows_as_far_apart_as_the_products_load(train):  # noqa: F811
         other = (torch.randn(270, 64, generator=gen, device="cuda") * 0.2).bfloat16()
         check(train, other, apart, torch.randint(0, 300, (270,), generator=gen, device="cuda"), torch.rand(270, generator=gen, device="cuda"))
         check(train, apart, other, torch.randint(0, 270, (300,), generator=gen, device="cuda"), torch.rand(300, generator=gen, device="cuda"))
+
+
+def test_the_logits_gradients_that_are_held_stay_below_128_mib(plans, train):  # noqa: F811
+    """Whatever the rows: x's copy and the 32-bit sum of dx grow with them, nothing else of the workspace."""
+    size = train.load().ones_cross_entropy_backward_workspace_bytes
+    for rows, cols, words in ((1 << 18, 8, 1000), ((1 << 18) + 1, 8, 1000), (300000, 64, 500), (524288, 8, 1000), (1 << 20, 24, 5000), (1 << 24, 8, 1000),
+                              (1 << 24, 128, 17)):
+        block, blocks, piece, held = plans("blocks", 4, rows, cols, words)
+        assert held <= 128 << 20 and block * piece * 2 <= 128 << 20 and (blocks - 1) * block < rows <= blocks * block
+        assert size(rows, cols, words, 1) <= rows * cols * 6 + (256 << 20)
+    assert plans("blocks", 4, 1 << 18, 8, 1000)[1] == 1 and plans("blocks", 4, (1 << 18) + 1, 8, 1000)[1] == 2
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("cols,words", [(24, 700), (33, 90)])
+def test_loss_of_rows_in_blocks(train, cols, words, dtype):  # noqa: F811
+    """Two blocks of rows with two pieces of the vocabulary, or one; the second block is shorter, a run of ignored rows reaches over both."""
+    rows = (1 << 18) + 301
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randn(rows, cols, generator=gen, device="cuda").to(dtype)
+    w = (torch.randn(words, cols, generator=gen, device="cuda") * 1.5 / cols ** 0.5).to(dtype)
+    t = torch.randint(0, words, (rows,), generator=gen, device="cuda")
+    t[131000:131500], t[-1] = -100, words - 1
+    x[t < 0] = float("nan")
+    check(train, x, w, t, torch.rand(rows, generator=gen, device="cuda") / rows)
