@@ -205,7 +205,8 @@ inline int check_loss(int64_t rows, int64_t cols, int64_t vocabulary, int64_t x_
   if (int rc = check_rows(vocabulary, cols, w_stride)) return rc;
   if (cols < 1 || vocabulary < 1 || (type != ONES_F16 && type != ONES_BF16)) return ONES_E_INVALID_ARG;
   if (rows > ONES_MAX_LOSS_ROWS || vocabulary > ONES_MAX_VOCABULARY || cols > ONES_MAX_LOSS_COLUMNS) return ONES_E_BOUNDS;
-  // tiles of a launch: at most 2^23, of 256 threads
+  // The product of two sizes is at most 2^36, in tiles of 128 x 128 at most 2^22: the tiles that are chosen, with the parts that k is
+  // split into and their 256 or 512 threads, then stay below the 2^32 threads of a launch.
   const int64_t n = ceil_div(rows, 128), v = ceil_div(vocabulary, 128), d = ceil_div(cols, 128);
   return std::max({n * v, d * n, d * v}) > (1 << 22) ? ONES_E_BOUNDS : ONES_OK;
 }

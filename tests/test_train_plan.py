@@ -33,6 +33,19 @@ void blocks(int64_t rows, int64_t cols, int64_t words, int64_t *to) {
   const int64_t out[] = {p.block, p.blocks, p.piece, static_cast<int64_t>((p.dx_sum ? p.dx_sum : p.backward) - p.g)};
   std::copy(out, out + 4, to);
 }
+// Threads of the largest launch of either call.
+void launch(int64_t rows, int64_t cols, int64_t words, int64_t *to) {
+  *to = 0;
+  if (check_loss(rows, cols, words, cols, cols, ONES_BF16) != ONES_OK) return;
+  const LossPlan p = loss_plan(rows, cols, words, true, true, true);
+  const int64_t some = std::min(rows, p.block), piece = std::min(p.piece, words);
+  const Split dx = p.gradients.of_dx, dw = p.gradients.of_dw;
+  const TileCost &c = kTileCosts[p.gradients.tiles], &f = kTileCosts[p.logits];
+  const int64_t threads = p.gradients.tiles == kTiny ? 256 : 512;
+  const int64_t products = ceil_div(cols, c.bm) * (ceil_div(some, c.bn) * dx.splits + ceil_div(piece, c.bn) * dw.splits) * threads;
+  const int64_t finish = (dx.splits > 1 ? some * cols : 0) + (p.blocks > 1 || dw.splits > 1 ? piece * cols : 0);
+  *to = std::max({products, finish, 2 * ceil_div(words, f.bm) * ceil_div(rows, f.bn), rows * 128});      // the logits' tiles have 31 bits; 8 rows a join
+}
 void update(int64_t count, int64_t rows, int64_t cols, int64_t *to) {
   const UpdateTiles t = update_tiles(count, std::min(rows, cols), std::max(rows, cols));
   to[0] = t.gram; to[1] = t.poly; to[2] = t.apply;
@@ -254,3 +267,14 @@ def test_loss_of_rows_in_blocks(train, cols, words, dtype):  # noqa: F811
     t[131000:131500], t[-1] = -100, words - 1
     x[t < 0] = float("nan")
     check(train, x, w, t, torch.rand(rows, generator=gen, device="cuda") / rows)
+
+
+def test_launches_of_every_accepted_size_of_the_loss_fit(plans):
+    """A grid has less than 2^32 threads: at the corners of what is accepted, and between them."""
+    largest = 0
+    sizes = lambda top: [v for k in range(0, top + 1, 2) for v in (1 << k, (1 << k) * 3 // 2 + 1) if v <= 1 << top]  # noqa: E731
+    for rows in sizes(24):
+        for cols in sizes(16):
+            for words in sizes(24):
+                largest = max(largest, *plans("launch", 1, rows, cols, words))
+    assert 1 << 28 < largest < 1 << 32
