@@ -258,7 +258,7 @@ inline UpdatePlan update_plan(int64_t count, int64_t rows, int64_t cols) {
   size_t off = 0;
   auto take = [&](int64_t bytes) { const size_t at = off; off = align_up(off + static_cast<size_t>(bytes)); return at; };
   p.blocks = std::min(kSumBlocks, ceil_div(rows * cols, 4096));            // at least four runs of four elements a thread
-  p.squares = take(count * p.blocks * 4);
+  p.squares = take(count * p.blocks * 8);
   p.x[0] = take(count * p.r * p.q_ld * 2);
   p.x[1] = take(count * p.r * p.q_ld * 2);
   p.a[0] = take(count * p.r * p.r_ld * 2);

@@ -8,8 +8,10 @@
 //
 // The operands are fp16 whatever the gradient's type: X's singular values stay near 1, so the range of bf16 is not needed, and
 // three more bits keep the result of five steps within a fraction of a bf16 step (each step rounds X, A and B).  They are held
-// times 2^11 (X) and 2^10 (A, B): an element of X is at most 1.3 and typically (r q)^-1/2, of A typically r^-1 q^-1/2 off the diagonal, so
-// neither end of fp16's range is near for sides up to the limit and coefficients that keep the singular values below 8.
+// times 2^11 (X) and 2^10 (A, B): an element of X is at most 1.3 and typically (r q)^-1/2, of A typically r^-1 q^-1/2 off the diagonal.  For
+// coefficients that keep the singular values below 7.9 nothing is too large for fp16.  At the other end, with both sides at their limit of
+// 65536, X's elements are typically 2^-5 and A's 2^-14, where fp16's steps cease to shrink: an element is off by 2^-25 at most, as
+// much as half a step is there, and by a larger share only where it is smaller than most.
 //
 // The result of five steps is off by 0.9e-3 to 1.8e-3 of the whole (sides 33 to 4100): mostly from X's roundings, which grow with the
 // directions of small singular values; A's and B's diagonals kept apart in 32 bits took 3 to 28 % off that and cost 2 to 6 % of the
@@ -36,7 +38,7 @@ constexpr float kUnitX = 2048.f, kUnitA = 1024.f;
 struct MomentumArgs {
   const void *grad;
   float *momentum;                            // null: u = g
-  float *squares;                             // [matrices][blocks]
+  double *squares;                            // [matrices][blocks]
   int64_t size;                               // elements of a matrix
   int32_t blocks;
   int32_t type, nesterov;
@@ -46,12 +48,20 @@ struct MomentumArgs {
 // u from the momentum as it was (first) or as it is now.
 __device__ __forceinline__ float update_of(float g, float m, float beta, bool nesterov) { return nesterov ? g + beta * m : m; }
 
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) v += __shfl_xor(v, m);
+  return v;
+}
+
+// The squares are summed in 64 bits: those of elements above 2^64 or below 2^-75 leave the range of 32 (a finite gradient would give an
+// update of zeros, or NaN).  The kernel is bound by memory either way.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void momentum_kernel(MomentumArgs a) {
-  __shared__ float part[4];
+  __shared__ double part[4];
   const T *grad = static_cast<const T *>(a.grad) + blockIdx.y * a.size;
   float *momentum = a.momentum ? a.momentum + blockIdx.y * a.size : nullptr;
-  float sum = 0.f;
+  double sum = 0.;
   for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * V; i < a.size; i += a.blocks * 256ll * V) {
     const Pack<T, V> g = load_pack<T, V>(grad + i);
     float m[V];
@@ -64,10 +74,10 @@ __global__ __launch_bounds__(256) void momentum_kernel(MomentumArgs a) {
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const float f = static_cast<float>(g.v[k]), u = momentum ? update_of(f, m[k], a.beta, a.nesterov) : f;
-      sum += u * u;
+      sum = __builtin_fma(static_cast<double>(u), static_cast<double>(u), sum);
     }
   }
-  sum = wave_sum(sum);
+  sum = wave_sum64(sum);
   if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sum;
   __syncthreads();
   if (threadIdx.x == 0) a.squares[static_cast<int64_t>(blockIdx.y) * a.blocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
@@ -84,16 +94,16 @@ struct NormaliseArgs {
 template <typename T>
 __global__ __launch_bounds__(256) void normalise_kernel(NormaliseArgs a) {
   __shared__ float tile[64][65];
-  __shared__ float unit;
+  __shared__ double unit;
   const T *grad = static_cast<const T *>(a.m.grad) + blockIdx.z * a.m.size;
   const float *momentum = a.m.momentum ? a.m.momentum + blockIdx.z * a.m.size : nullptr;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   if (wave == 0) {
-    float sum = 0.f;
+    double sum = 0.;
 #pragma unroll 4
     for (int i = lane; i < a.m.blocks; i += 64) sum += a.m.squares[static_cast<int64_t>(blockIdx.z) * a.m.blocks + i];
-    sum = wave_sum(sum);
-    if (lane == 0) unit = kUnitX / (sqrtf(sum) + a.eps);
+    sum = wave_sum64(sum);
+    if (lane == 0) unit = kUnitX / (sqrt(sum) + a.eps);
   }
   const bool turned = a.rows > a.cols;
   const int q0 = blockIdx.x * 64, r0 = blockIdx.y * 64;                    // of X
@@ -112,7 +122,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(NormaliseArgs a) {
   f16 *x = a.x + static_cast<int64_t>(blockIdx.z) * a.r * a.q_ld;
   for (int i = wave; i < 64; i += 4) {
     const int row = r0 + i, col = q0 + lane;
-    if (row < a.r && col < a.q_ld) x[static_cast<int64_t>(row) * a.q_ld + col] = static_cast<f16>((turned ? tile[lane][i] : tile[i][lane]) * unit);
+    if (row < a.r && col < a.q_ld) x[static_cast<int64_t>(row) * a.q_ld + col] = static_cast<f16>(static_cast<float>((turned ? tile[lane][i] : tile[i][lane]) * unit));
   }
 }
 
@@ -275,7 +285,7 @@ int ones_orthogonal_update(const void *grad, float *momentum, int64_t count, int
   f16 *x[2] = {reinterpret_cast<f16 *>(ws + p.x[0]), reinterpret_cast<f16 *>(ws + p.x[1])};
   f16 *a[2] = {reinterpret_cast<f16 *>(ws + p.a[0]), reinterpret_cast<f16 *>(ws + p.a[1])};
   NormaliseArgs n{};
-  n.m = MomentumArgs{grad, momentum, reinterpret_cast<float *>(ws + p.squares), rows * cols, static_cast<int32_t>(p.blocks), grad_type, nesterov, beta};
+  n.m = MomentumArgs{grad, momentum, reinterpret_cast<double *>(ws + p.squares), rows * cols, static_cast<int32_t>(p.blocks), grad_type, nesterov, beta};
   n.x = x[0];
   n.rows = static_cast<int32_t>(rows); n.cols = static_cast<int32_t>(cols);
   n.r = static_cast<int32_t>(p.r); n.q = static_cast<int32_t>(p.q); n.q_ld = static_cast<int32_t>(p.q_ld);

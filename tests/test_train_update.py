@@ -153,3 +153,34 @@ def test_update_in_a_graph(train):  # noqa: F811
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, second) and torch.equal(m, end)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("scale", [1e-37, 1e-30, 1e-24, 1e20, 1e30, 1e37])
+@pytest.mark.parametrize("rows,cols", [(200, 136), (33, 71)])
+def test_update_of_gradients_whose_squares_leave_32_bits(train, rows, cols, scale, dtype):  # noqa: F811
+    """Finite gradients of any size: the norm is the root of a sum of squares that 32 bits do not hold."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    g = (torch.randn(2, rows, cols, generator=gen, device="cuda").double() * scale).to(dtype)
+    m = (torch.randn(2, rows, cols, generator=gen, device="cuda").double() * scale).float()
+    eps = 1e-7 if scale > 1 else 0.0
+    for momentum in (None, m):
+        want, _ = update64(g, momentum, 0.95, True, 5, ABC, eps)
+        got = train.orthogonal_update(g, momentum, 0.95, True, 5, ABC, eps, dtype=torch.bfloat16)
+        off = (got.double() - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1)
+        assert off.max() <= 5.7e-3 + HALF[torch.bfloat16], off.max().item()
+
+
+@gpu
+def test_update_of_one_small_matrix_among_large_ones(train):  # noqa: F811
+    """Every matrix has a norm of its own; an infinity makes its own matrix NaN, zeros stay zeros."""
+    gen = torch.Generator(device="cuda").manual_seed(31)
+    one = torch.randn(64, 96, generator=gen, device="cuda")
+    g = torch.stack([one * 1e30, one * 1e-30, one * 0, one])
+    g[3, 5, 6] = float("inf")
+    got = train.orthogonal_update(g, eps=1e-37)
+    want, _ = update64(one, None, 0, False, 5, ABC, 0.0)
+    for k in (0, 1):
+        assert (got[k].double() - want).norm() <= (5.7e-3 + HALF[torch.bfloat16]) * want.norm()
+    assert not got[2].any() and got[3].isnan().all()
