@@ -58,10 +58,13 @@ inline int64_t blocks_of(const Cut &cut, int64_t batch, int64_t channels) {
   return cut.lanes == 16 ? blocks * batch * cut.segments : ceil_div(ceil_div(blocks, 2) * batch * cut.segments, 8) * 16;
 }
 
-inline int check_recurrence(int64_t batch, int64_t steps, int64_t channels, int32_t type) {
+inline int check_sizes(int64_t batch, int64_t steps, int64_t channels, int32_t type) {
   if (batch < 0 || steps < 0 || channels < 0 || !is_type(type)) return ONES_E_INVALID_ARG;
   if (batch > ONES_MAX_BATCH || steps > ONES_MAX_STEPS || channels > ONES_MAX_CHANNELS) return ONES_E_BOUNDS;
-  if (steps && channels && batch > kMaxElements / (steps * channels)) return ONES_E_BOUNDS;
+  return steps && channels && batch > kMaxElements / (steps * channels) ? ONES_E_BOUNDS : ONES_OK;
+}
+inline int check_recurrence(int64_t batch, int64_t steps, int64_t channels, int32_t type) {
+  if (int rc = check_sizes(batch, steps, channels, type)) return rc;
   // workgroups of a launch
   return std::max(blocks_of(cut_of(batch, steps, channels, false), batch, channels), blocks_of(cut_of(batch, steps, channels, true), batch, channels)) > (1 << 23)
              ? ONES_E_BOUNDS : ONES_OK;

@@ -403,22 +403,22 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(const T *gate, const T *x, float *state, T *h, int64_t batch, int32_t channels,
                                                                   int64_t gate_stride, int64_t x_stride) {
   const int32_t packs = (channels + kV - 1) / kV;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= batch * packs) return;
-  const int64_t b = i / packs;
-  const int c = static_cast<int>(i - b * packs) * kV, have = channels - c;
-  const Pack<T, kV> g = load_some<T, kV>(gate + b * gate_stride + c, have), u = load_some<T, kV>(x + b * x_stride + c, have);
-  float *s = state + b * channels + c;
-  const Pack<float, kV> old = load_some<float, kV>(s, have);
-  float now[kV];
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < batch * packs; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+    const int64_t b = i / packs;
+    const int c = static_cast<int>(i - b * packs) * kV, have = channels - c;
+    const Pack<T, kV> g = load_some<T, kV>(gate + b * gate_stride + c, have), u = load_some<T, kV>(x + b * x_stride + c, have);
+    float *s = state + b * channels + c;
+    const Pack<float, kV> old = load_some<float, kV>(s, have);
+    float now[kV];
 #pragma unroll
-  for (int k = 0; k < kV; ++k) {
-    float r, q;
-    gate_of(static_cast<float>(g.v[k]), r, q);
-    now[k] = r * old.v[k] + q * static_cast<float>(u.v[k]);
+    for (int k = 0; k < kV; ++k) {
+      float r, q;
+      gate_of(static_cast<float>(g.v[k]), r, q);
+      now[k] = r * old.v[k] + q * static_cast<float>(u.v[k]);
+    }
+    store_some<float, kV>(s, now, have);
+    store_some<T, kV>(h + b * channels + c, now, have);
   }
-  store_some<float, kV>(s, now, have);
-  store_some<T, kV>(h + b * channels + c, now, have);
 }
 
 template <typename T, int LANES, bool EDGE, bool FORM, bool PAST>
@@ -459,7 +459,7 @@ void launch_recurrence_type(RecurrenceArgs &a, int32_t type, bool backward, hipS
 template <typename T>
 void launch_step(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride, int64_t batch, int64_t channels, float *state, void *h,
                  hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(ceil_div(batch * ceil_div(channels, kV), kThreads)));
+  const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(ceil_div(batch * ceil_div(channels, kV), kThreads), 1 << 16)));
   hipLaunchKernelGGL((recurrence_step_kernel<T>), grid, dim3(kThreads), 0, s, static_cast<const T *>(gate), static_cast<const T *>(x), state,
                      static_cast<T *>(h), batch, static_cast<int32_t>(channels), gate_stride, x_stride);
 }
@@ -529,7 +529,7 @@ int ones_recurrence_backward(const void *dh, int64_t dh_batch_stride, int64_t dh
 
 int ones_recurrence_step(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride, int64_t batch, int64_t channels, int32_t type,
                          float *state, void *h, void *hip_stream) {
-  if (int rc = check_recurrence(batch, 1, channels, type)) return rc;
+  if (int rc = check_sizes(batch, 1, channels, type)) return rc;
   if (int rc = check_strides(gate_stride, 0, channels)) return rc;
   if (int rc = check_strides(x_stride, 0, channels)) return rc;
   if (batch == 0 || channels == 0) return ONES_OK;

@@ -417,3 +417,27 @@ def test_results_that_go_past_the_caches_are_the_same(train):
         assert ((h[:50].double() - want.double()).abs() <= bound).all() and torch.allclose(last[:50], want_last, rtol=1e-4, atol=1e-5)
         for got, one in zip(back, train.gated_recurrence_backward(dh[:50], None, gate[:50], x[:50], few, lengths[:50])):
             assert ((got[:50].double() - one.double()).abs() <= 2 * HALF[torch.bfloat16] * (one.double().abs() + 2.0 ** -8)).all()
+
+
+def test_a_single_token_of_any_size_is_not_refused(train):
+    """Up to the limits of batch and channels; a state that is missing shows that the sizes were taken."""
+    L, p = train.load(), C.c_void_p(0x1000)
+    step = lambda b, c: L.ones_recurrence_step(p, c, p, c, b, c, 2, None, p, None)  # noqa: E731
+    assert step(65535, 8192) == step(65535, 1 << 24) == step(1, 1 << 24) == -1
+    assert step(65536, 8) == step(1, (1 << 24) + 1) == -3
+
+
+@gpu
+@pytest.mark.parametrize("batch,channels", [(65535, 8192), (65535, 1031)])
+def test_a_single_token_of_many_sequences(train, batch, channels):
+    """More than 2^16 workgroups' worth: a thread takes several runs of channels."""
+    gen = torch.Generator(device="cuda").manual_seed(channels)
+    gate, x = (torch.randn(batch, channels, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    state = torch.randn(batch, channels, generator=gen, device="cuda")
+    parts = [slice(0, 300), slice(40000, 40300), slice(batch - 300, batch)]
+    held = [state[rows].clone() for rows in parts]
+    h = train.gated_recurrence_step(gate, x, state)
+    for rows, old in zip(parts, held):
+        want, end, *_ = recurrence64(gate[rows, None], x[rows, None], old, None, x[rows, None], None)
+        near(h[rows], want[:, 0], torch.full_like(end, 8.0), 16, "h")
+        near(state[rows], end, torch.full_like(end, 8.0), 16, "state")
