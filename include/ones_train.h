@@ -61,8 +61,9 @@ int ones_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, i
  * state, last, dlast, dstate: float [batch][channels]; carry: ones_recurrence_carry_bytes, written forward (NULL: not
  * wanted) and read backward, which needs neither state nor h.  lengths: int32 [batch] or NULL; of sequence b only the first
  * lengths[b] steps (pulled into 0..steps) count: the rest is not read, h and the gradients are 0 there, last is the state behind
- * the last step that counts.  last, dstate may be NULL, dlast too (0).  batch <= ONES_MAX_BATCH.
- * ones_recurrence_step: one step of every sequence, gate and x [batch][channels] with a row stride, state updated in place. */
+ * the last step that counts.  last, dstate may be NULL, dlast too (0).  batch <= ONES_MAX_BATCH, batch * channels <= 2^36.
+ * ones_recurrence_step: one step of every sequence, gate and x [batch][channels] with a row stride, state updated in place.
+ * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size or a stride above its limit), ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
 size_t ones_recurrence_carry_bytes(int64_t batch, int64_t steps, int64_t channels);
 size_t ones_recurrence_workspace_bytes(int64_t batch, int64_t steps, int64_t channels);
 int ones_recurrence_forward(const void *gate, int64_t gate_batch_stride, int64_t gate_step_stride,

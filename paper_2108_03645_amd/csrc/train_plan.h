@@ -65,8 +65,8 @@ inline int check_sizes(int64_t batch, int64_t steps, int64_t channels, int32_t t
 }
 inline int check_recurrence(int64_t batch, int64_t steps, int64_t channels, int32_t type) {
   if (int rc = check_sizes(batch, steps, channels, type)) return rc;
-  // workgroups of a launch
-  return std::max(blocks_of(cut_of(batch, steps, channels, false), batch, channels), blocks_of(cut_of(batch, steps, channels, true), batch, channels)) > (1 << 23)
+  // workgroups of a launch, numbered in 32 bits
+  return std::max(blocks_of(cut_of(batch, steps, channels, false), batch, channels), blocks_of(cut_of(batch, steps, channels, true), batch, channels)) > (int64_t{1} << 31)
              ? ONES_E_BOUNDS : ONES_OK;
 }
 // Rows of `channels` elements, `step` elements apart and sequences `batch` elements apart.

@@ -89,7 +89,7 @@ struct Work {
 };
 template <int LANES>
 __device__ __forceinline__ Work work_of(const RecurrenceArgs &a) {
-  const uint32_t id = blockIdx.x, blocks = (a.channels + LANES * kV - 1) / (LANES * kV);
+  const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x, blocks = (a.channels + LANES * kV - 1) / (LANES * kV);
   uint32_t rest, block;
   if constexpr (LANES == 16) {
     rest = id / blocks;
@@ -423,7 +423,9 @@ __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(const T *gate
 
 template <typename T, int LANES, bool EDGE, bool FORM, bool PAST>
 void launch_recurrence(const RecurrenceArgs &a, int64_t blocks, bool backward, hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(blocks));
+  // more workgroups than one dimension takes (2^32 threads): rows of them, the last of which goes past the end
+  const int64_t across = std::min<int64_t>(blocks, 1 << 20);
+  const dim3 grid(static_cast<uint32_t>(across), static_cast<uint32_t>(ceil_div(blocks, across)));
   if (backward) hipLaunchKernelGGL((recurrence_backward_kernel<T, LANES, EDGE, FORM, PAST>), grid, dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((recurrence_forward_kernel<T, LANES, EDGE, FORM, PAST>), grid, dim3(kThreads), 0, s, a);
 }

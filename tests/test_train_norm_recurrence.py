@@ -441,3 +441,28 @@ def test_a_single_token_of_many_sequences(train, batch, channels):
         want, end, *_ = recurrence64(gate[rows, None], x[rows, None], old, None, x[rows, None], None)
         near(h[rows], want[:, 0], torch.full_like(end, 8.0), 16, "h")
         near(state[rows], end, torch.full_like(end, 8.0), 16, "state")
+
+
+def test_many_sequences_of_few_steps_are_not_refused(train):
+    L, p = train.load(), C.c_void_p(0x1000)
+    run = lambda b, t, c: L.ones_recurrence_forward(p, t * c, c, p, t * c, c, b, t, c, 2, None, None, None, None, None, None, 0, None)  # noqa: E731
+    assert run(65535, 2, 8192) == run(4096, 1, 1 << 24) == run(65535, 300, 1 << 20) == -1       # taken, but h is missing
+    assert run(4097, 1, 1 << 24) == -3
+
+
+@gpu
+@pytest.mark.parametrize("channels", [8192, 8190])
+def test_recurrence_of_many_sequences_of_few_steps(train, channels):
+    """2^24 workgroups, more than one dimension of a launch takes; every third sequence has one step only."""
+    batch, steps = 65535, 2
+    gen = torch.Generator(device="cuda").manual_seed(channels)
+    gate, x, dh = (torch.randn(batch, steps, channels, generator=gen, device="cuda").bfloat16() for _ in range(3))
+    lengths = torch.full((batch,), steps, device="cuda", dtype=torch.int32)
+    lengths[::3] = 1
+    state = torch.randn(batch, channels, generator=gen, device="cuda")
+    h, last, carry = train.gated_recurrence_forward(gate, x, state, lengths)
+    dgate, dx, dstate = train.gated_recurrence_backward(dh, state, gate, x, carry, lengths)
+    for rows in (slice(0, 300), slice(32700, 33000), slice(batch - 300, batch)):
+        want = recurrence64(gate[rows], x[rows], state[rows], lengths[rows], dh[rows], state[rows])
+        for got, one, what in zip((h, last, dgate, dx, dstate), want, ("h", "last", "dgate", "dx", "dstate")):
+            near(got[rows], one, torch.full_like(one, 64.0), 32, what)
