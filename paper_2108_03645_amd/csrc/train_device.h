@@ -63,13 +63,8 @@ __device__ __forceinline__ void store_some(T *p, const float *v, int n, bool pas
   for (int i = 0; i < N; ++i) if (i < n) p[i] = static_cast<T>(v[i]);
 }
 
-// An element of an array whose type is only known at run time (weights; read once a workgroup).
+// An element of an array whose type is only known at run time (gradients of weights, an update).
 enum : int { kF32 = 0, kF16 = 1, kBF16 = 2 };
-__device__ __forceinline__ float load_as(const void *p, int type, int64_t i) {
-  if (type == kF32) return static_cast<const float *>(p)[i];
-  if (type == kF16) return static_cast<float>(static_cast<const f16 *>(p)[i]);
-  return static_cast<float>(static_cast<const bf16 *>(p)[i]);
-}
 __device__ __forceinline__ void store_as(void *p, int type, int64_t i, float v) {
   if (type == kF32) static_cast<float *>(p)[i] = v;
   else if (type == kF16) static_cast<f16 *>(p)[i] = static_cast<f16>(v);

@@ -69,8 +69,8 @@ inline int check_recurrence(int64_t batch, int64_t steps, int64_t channels, int3
   return std::max(blocks_of(cut_of(batch, steps, channels, false), batch, channels), blocks_of(cut_of(batch, steps, channels, true), batch, channels)) > (int64_t{1} << 31)
              ? ONES_E_BOUNDS : ONES_OK;
 }
-// Rows of `channels` elements, `step` elements apart and sequences `batch` elements apart.
-inline int check_strides(int64_t batch_stride, int64_t step_stride, int64_t channels) {
+// Elements from a sequence to the next, and from a step to the next.
+inline int check_strides(int64_t batch_stride, int64_t step_stride) {
   if (batch_stride < 0 || step_stride < 0) return ONES_E_INVALID_ARG;
   return batch_stride > (int64_t{1} << 40) || step_stride > (int64_t{1} << 32) ? ONES_E_BOUNDS : ONES_OK;
 }

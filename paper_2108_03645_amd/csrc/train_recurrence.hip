@@ -490,8 +490,8 @@ int ones_recurrence_forward(const void *gate, int64_t gate_batch_stride, int64_t
                             const int32_t *lengths, void *h, float *last, float *carry, void *d_workspace, size_t workspace_bytes,
                             void *hip_stream) {
   if (int rc = check_recurrence(batch, steps, channels, type)) return rc;
-  if (int rc = check_strides(gate_batch_stride, gate_step_stride, channels)) return rc;
-  if (int rc = check_strides(x_batch_stride, x_step_stride, channels)) return rc;
+  if (int rc = check_strides(gate_batch_stride, gate_step_stride)) return rc;
+  if (int rc = check_strides(x_batch_stride, x_step_stride)) return rc;
   if (batch == 0 || channels == 0) return ONES_OK;
   if (steps && (!gate || !x || !h)) return ONES_E_INVALID_ARG;
   if (int rc = check_workspace(d_workspace, workspace_bytes, ones_recurrence_workspace_bytes(batch, steps, channels))) return rc;
@@ -511,9 +511,9 @@ int ones_recurrence_backward(const void *dh, int64_t dh_batch_stride, int64_t dh
                              const int32_t *lengths, void *dgate, void *dx, float *dstate, void *d_workspace, size_t workspace_bytes,
                              void *hip_stream) {
   if (int rc = check_recurrence(batch, steps, channels, type)) return rc;
-  if (int rc = check_strides(dh_batch_stride, dh_step_stride, channels)) return rc;
-  if (int rc = check_strides(gate_batch_stride, gate_step_stride, channels)) return rc;
-  if (int rc = check_strides(x_batch_stride, x_step_stride, channels)) return rc;
+  if (int rc = check_strides(dh_batch_stride, dh_step_stride)) return rc;
+  if (int rc = check_strides(gate_batch_stride, gate_step_stride)) return rc;
+  if (int rc = check_strides(x_batch_stride, x_step_stride)) return rc;
   if (batch == 0 || channels == 0) return ONES_OK;
   if (steps && (!dh || !gate || !x || !carry || !dgate || !dx)) return ONES_E_INVALID_ARG;
   if (int rc = check_workspace(d_workspace, workspace_bytes, ones_recurrence_workspace_bytes(batch, steps, channels))) return rc;
@@ -532,8 +532,8 @@ int ones_recurrence_backward(const void *dh, int64_t dh_batch_stride, int64_t dh
 int ones_recurrence_step(const void *gate, int64_t gate_stride, const void *x, int64_t x_stride, int64_t batch, int64_t channels, int32_t type,
                          float *state, void *h, void *hip_stream) {
   if (int rc = check_sizes(batch, 1, channels, type)) return rc;
-  if (int rc = check_strides(gate_stride, 0, channels)) return rc;
-  if (int rc = check_strides(x_stride, 0, channels)) return rc;
+  if (int rc = check_strides(gate_stride, 0)) return rc;
+  if (int rc = check_strides(x_stride, 0)) return rc;
   if (batch == 0 || channels == 0) return ONES_OK;
   if (!gate || !x || !state || !h) return ONES_E_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
