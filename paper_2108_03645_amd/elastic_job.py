@@ -73,24 +73,28 @@ class Model:
 
 
 class Worker:
-    """Trains a model at a local batch that may change between any two steps."""
+    """Trains a model at a local batch that may change between any two steps.  The learning rate is proportional to the batch: `rate` at
+    `per_sample_rate_at` sequences."""
 
-    def __init__(self, model, rate=0.02, per_sample_rate_at=32):
+    def __init__(self, model, rate=0.02, per_sample_rate_at=512):
         self.model, self.rate, self.at = model, rate, per_sample_rate_at
         self.momentum = torch.zeros_like(model.matrices)
         self.others = torch.optim.AdamW([model.embedding, model.output, model.norms], lr=rate / 4, weight_decay=0.0)
 
+    def rate_of(self, batch):
+        return self.rate * batch / self.at
+
     def step(self, tokens):
-        model, scale = self.model, tokens.shape[0] / self.at          # the learning rate follows the batch
+        model, rate = self.model, self.rate_of(tokens.shape[0])
         model.matrices.grad = None
         self.others.zero_grad(set_to_none=True)
         loss = model.loss(tokens)
         loss.backward()
         update = train.orthogonal_update(model.matrices.grad, self.momentum)
         with torch.no_grad():
-            model.matrices.add_(update, alpha=-self.rate * min(scale, 1.0))
+            model.matrices.add_(update, alpha=-rate)
         for group in self.others.param_groups:
-            group["lr"] = self.rate / 4 * min(scale, 1.0)
+            group["lr"] = rate / 4
         self.others.step()
         return loss.detach()
 

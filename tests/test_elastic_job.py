@@ -52,3 +52,19 @@ def test_the_batch_may_change_and_padding_does_not_count():
     with torch.no_grad():
         whole, short = model.loss(padded), model.loss(tokens)
     assert abs(whole - short) < 1e-5 * short
+
+
+def test_the_learning_rate_is_proportional_to_the_batch(monkeypatch):
+    """At every batch the search may give, for the matrices and for the rest; the operators are stood in for, so no GPU is needed."""
+    monkeypatch.setattr(elastic_job.train, "orthogonal_update", lambda grad, momentum: torch.ones_like(grad))
+    model = elastic_job.Model(vocabulary=7, width=4, blocks=1, device="cpu")
+    monkeypatch.setattr(model, "loss", lambda tokens: sum(p.sum() for p in (model.matrices, model.embedding, model.output, model.norms)))
+    worker = elastic_job.Worker(model)
+    moved, rates = [], []
+    for n in (32, 64, 512, 1024):
+        before = model.matrices.detach().clone()
+        worker.step(torch.zeros(n, 3, dtype=torch.int64))
+        moved.append((before - model.matrices.detach()).mean().item())
+        rates.append(worker.others.param_groups[0]["lr"])
+    assert np.allclose(np.array(moved) / moved[0], [1, 2, 16, 32], rtol=1e-4) and np.allclose(np.array(rates) / rates[0], [1, 2, 16, 32])
+    assert np.allclose(moved, [worker.rate_of(n) for n in (32, 64, 512, 1024)], rtol=1e-4)
