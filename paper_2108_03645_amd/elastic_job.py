@@ -143,9 +143,31 @@ def measure(worker, language, batches, repeats=3):
     return seconds
 
 
-def main(steps=60, generations=20, slot=0):
+def place(a, d, batches, generations=20, slot=0):
+    """The local batch that the search gives a job with these figures, its samples and GPUs, and the cluster's GPUs.  The cluster runs
+    other jobs when this one arrives in `slot`; arrivals are served first.  Raises RuntimeError if the winning schedule lets it wait."""
     from . import ones
 
+    cluster, jobs = workloads.paper_scale()
+    jobs.active[slot] = 0
+    search = ones.Search(cluster, jobs)
+    try:
+        search.generation(generations)
+        jobs.active[slot], jobs.job_id[slot] = 1, jobs.job_id.max() + 1
+        jobs.a[slot], jobs.d[slot], jobs.gpu_max_batch[slot] = a, d, batches[-1]
+        jobs.bmin[slot], jobs.bmax[slot], jobs.remaining[slot] = batches[0], 1024, 1e6
+        search.set_new_jobs_first(True)
+        search.set_jobs(jobs)
+        search.generation(1)
+        batch, (samples, gpus, _) = local_batch(slot, *search.placement()), search.best()
+    finally:
+        search.close()
+    if not batch:
+        raise RuntimeError("the winning schedule lets the job wait")
+    return batch, int(samples[slot]), int(gpus[slot]), cluster.n_gpus
+
+
+def main(steps=60, generations=20, slot=0):
     model = Model(vocabulary=4000, width=512)
     worker, language = Worker(model), Language(model.vocabulary, 256)
     first = worker.step(language.batch(32)).item()
@@ -155,23 +177,10 @@ def main(steps=60, generations=20, slot=0):
     print("steps at local batches", ", ".join(f"{n}: {1e3 * t:.2f} ms" for n, t in zip(batches, seconds)),
           f"-> a = {1e6 * a:.2f} us a sample, d = {1e3 * d:.2f} ms")
 
-    # the cluster runs other jobs when this one arrives; arrivals are served first
-    cluster, jobs = workloads.paper_scale()
-    jobs.active[slot] = 0
-    search = ones.Search(cluster, jobs)
-    search.generation(generations)
-    jobs.active[slot], jobs.job_id[slot] = 1, jobs.job_id.max() + 1
-    jobs.a[slot], jobs.d[slot], jobs.gpu_max_batch[slot] = a, d, batches[-1]
-    jobs.bmin[slot], jobs.bmax[slot], jobs.remaining[slot] = batches[0], 1024, 1e6
-    search.set_new_jobs_first(True)
-    search.set_jobs(jobs)
-    search.generation(1)
-    batch, (b, g, _) = local_batch(slot, *search.placement()), search.best()
-    print(f"the winning schedule gives the job {b[slot]} samples on {g[slot]} of {cluster.n_gpus} GPUs: {batch} a worker"
-          + ("" if batch else " (it waits)"))
-    search.close()
+    batch, samples, gpus, of = place(a, d, batches, generations, slot)
+    print(f"the winning schedule gives the job {samples} samples on {gpus} of {of} GPUs: {batch} a worker")
 
-    losses = [first] + [worker.step(language.batch(batch or batches[0])).item() for _ in range(steps)]
+    losses = [first] + [worker.step(language.batch(batch)).item() for _ in range(steps)]
     print(f"loss {losses[0]:.3f} at first, {losses[1]:.3f} -> {losses[-1]:.3f} in {steps} steps")
     prompt = language.batch(4)[:, :16]
     answer = model.continue_from(prompt, 8)

@@ -68,3 +68,44 @@ def test_the_learning_rate_is_proportional_to_the_batch(monkeypatch):
         rates.append(worker.others.param_groups[0]["lr"])
     assert np.allclose(np.array(moved) / moved[0], [1, 2, 16, 32], rtol=1e-4) and np.allclose(np.array(rates) / rates[0], [1, 2, 16, 32])
     assert np.allclose(moved, [worker.rate_of(n) for n in (32, 64, 512, 1024)], rtol=1e-4)
+
+
+class Waiting:
+    """A search whose winner has no GPU for the job."""
+    closed = False
+
+    def __init__(self, cluster, jobs):
+        self.jobs, self.gpus = len(jobs.active), cluster.n_gpus
+
+    def generation(self, n):
+        pass
+
+    set_jobs = set_new_jobs_first = generation
+
+    def placement(self):
+        return np.full(self.gpus, 1), np.full(self.gpus, 64)
+
+    def best(self):
+        return np.zeros(self.jobs, int), np.zeros(self.jobs, int), 0.0
+
+    def close(self):
+        Waiting.closed = True
+
+
+def test_a_job_that_waits_is_not_trained(monkeypatch):
+    from paper_2108_03645_amd import ones
+    monkeypatch.setattr(ones, "Search", Waiting)
+    monkeypatch.setattr(elastic_job, "Model", lambda **k: type("M", (), {"vocabulary": 4}))
+    monkeypatch.setattr(elastic_job, "Worker", lambda model: type("W", (), {"step": staticmethod(lambda tokens: torch.zeros(()))}))
+    monkeypatch.setattr(elastic_job, "Language", lambda *a: type("L", (), {"batch": staticmethod(lambda n: None)}))
+    monkeypatch.setattr(elastic_job, "measure", lambda *a: [1, 2, 3, 4, 5])
+    with pytest.raises(RuntimeError, match="wait"):
+        elastic_job.main()
+    assert Waiting.closed
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("a,d", [(2e-5, 1e-3), (1e-4, 2e-2)])
+def test_the_search_gives_the_job_a_batch(a, d):
+    batch, samples, gpus, of = elastic_job.place(a, d, [32, 64, 128, 256, 512], generations=5)
+    assert 0 < batch <= 512 and 1 <= gpus <= of and 32 <= samples <= 1024 and batch * gpus >= samples
