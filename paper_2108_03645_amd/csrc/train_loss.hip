@@ -17,7 +17,7 @@
 // 32000, k 1024, 437 us (1.23).  A piece of 8192 rows and words, k 1024: G 120 to 144 us (1.0), its two products 208 to 240 us (1.2
 // to 1.3); joining the parts 4 to 11 us, packing x 3 to 12 us.
 //
-// G is held in units of the largest |dloss| over 2^14 and the products are scaled back in 32 bits.  fp16 would lose small
+// G is held in units of the largest finite |dloss| over 2^14 and the products are scaled back in 32 bits.  fp16 would lose small
 // probabilities times small dloss otherwise; and where all dloss are equal, as in a mean, the target's entry comes to
 // 2^14 (p - 1), next to a power of two for small p, instead of a value whose rounding error is the same in every row (error of
 // fp16 gradients against 64 bits, 1003 rows of 514, 10007 words: 4.1e-4 with a power of two as the unit; half a step's is 2.1e-4).
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
     for (int32_t i = threadIdx.x; i < a.rows[0]; i += 256) {
       const int64_t t = a.target[i];
       const float d = fabsf(a.dloss[i]);
-      most = t >= 0 ? fmaxf(most, d) : most;
+      most = t >= 0 && isfinite(d) ? fmaxf(most, d) : most;      // an infinite one takes no unit away from the others
     }
 #pragma unroll
     for (int m = 1; m < kWave; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
     __syncthreads();
     if (threadIdx.x == 0) {
       most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-      const bool usable = most > 1e-30f && isfinite(most);
+      const bool usable = most > 1e-30f;
       a.scale[0] = usable ? 16384.f / most : 1.f;
       a.scale[1] = usable ? most / 16384.f : 1.f;
     }

@@ -290,3 +290,32 @@ def test_a_loss_changed_in_place_has_the_changed_gradient(train):  # noqa: F811
     _, lse = train.linear_cross_entropy_forward(x.detach(), w.detach(), t)
     dx, dw = train.linear_cross_entropy_backward(weights, x.detach(), w.detach(), t, lse)
     assert torch.equal(x.grad, dx) and torch.equal(w.grad, dw)
+
+
+def row_errors(train, x, w, t, dloss):  # noqa: F811
+    """Per row, what dx is off by and what G's rounding (half a step each, of either sign) and dx's own make of it, as norms; dx, dweight."""
+    loss, lse = train.linear_cross_entropy_forward(x, w, t)
+    dx, dw = train.linear_cross_entropy_backward(dloss, x, w, t, lse)
+    rows = dloss.isfinite()
+    _, wlse, g, p, cx, cw = loss64(x, w, t, torch.where(rows, dloss, torch.zeros_like(dloss)))
+    want, half = g @ cw, HALF[x.dtype]
+    # a logit's error goes into its probability, and with that into all of the row's terms
+    logits = (16 + 4 * x.shape[1] ** 0.5 + w.shape[0] / 64) * U32 * ((cx.abs() @ cw.abs().t()).amax(1) + 2 + wlse.abs())
+    allowed = 2 * half * (g.square() @ cw.square()).sum(1).sqrt() + half * want.norm(dim=1) + logits * (p @ cw.abs()).norm(dim=1)
+    allowed = allowed + (2.0 ** -24 * x.shape[1] ** 0.5 if x.dtype == torch.float16 else 0.0)
+    return (dx.double() - want).norm(dim=1), allowed, dx, dw
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+def test_an_infinite_gradient_of_a_loss_stays_in_its_row_of_dx(train, dtype):  # noqa: F811
+    gen = torch.Generator(device="cuda").manual_seed(37)
+    x = (torch.randn(70, 64, generator=gen, device="cuda") * 0.3).to(dtype)
+    w = (torch.randn(30000, 64, generator=gen, device="cuda") * 0.2 + 0.1).to(dtype)
+    t = torch.randint(0, 30000, (70,), generator=gen, device="cuda")
+    dloss = torch.full((70,), 1e-3, device="cuda")
+    dloss[3], dloss[66] = float("inf"), float("nan")
+    off, allowed, dx, dw = row_errors(train, x, w, t, dloss)
+    assert not dx[[3, 66]].isfinite().any() and not dw.isfinite().any()
+    off[[3, 66]] = 0
+    assert (off <= allowed).all(), (off / allowed).max().item()
