@@ -21,6 +21,10 @@
 // probabilities times small dloss otherwise; and where all dloss are equal, as in a mean, the target's entry comes to
 // 2^14 (p - 1), next to a power of two for small p, instead of a value whose rounding error is the same in every row (error of
 // fp16 gradients against 64 bits, 1003 rows of 514, 10007 words: 4.1e-4 with a power of two as the unit; half a step's is 2.1e-4).
+// A row whose |dloss| lies far below the largest would still lose its small probabilities to fp16's smallest step, and its dx with them
+// (30000 words, a dloss 2^-24 of the largest: all of it).  So from 2^-14 of the largest on, G of the row is held 2^k times as large and x's
+// copy 2^-k times, k up to 12: dW = G^T x stays as it is, the logits and dx are scaled back in 32 bits.
+// (The unit has to be there before x is copied then, by a launch of its own: 1003 rows of 514, 10007 words, both calls 117 us before, 120 now.)
 // Rows whose target is below 0 are copied as zeros first, so that whatever they hold (they are padding) meets the zeros of G
 // as zeros.
 #include "train_host.h"
@@ -40,10 +44,17 @@ struct LossArgs {
   const int64_t *target;
   Part *parts;                                // [parts of the vocabulary][rows]
   float *at_target;
-  const float *lse, *dloss, *scale;           // scale: of G, and back
+  const float *lse, *dloss, *scale;           // scale: of G, back, and the largest |dloss|
   void *g;                                    // [rows][g_ld]
   int64_t g_ld;
 };
+
+// k of a row, above.
+constexpr int kKept = 14, kLift = 12;
+__device__ __forceinline__ int lift_of(float dloss, float most) {
+  const float d = fabsf(dloss);
+  return d > 0.f && d < most ? max(min(ilogbf(most) - ilogbf(d) - kKept, kLift), 0) : 0;
+}
 
 // Tiles of logits.  GRADIENT: writes G; otherwise what the loss needs of it.  A workgroup takes tiles in turn and has the next one's
 // first operands on their way while it deals with one's logits.
@@ -102,10 +113,12 @@ __global__ __launch_bounds__(S::threads, S::resident) void logits_kernel(LossArg
       const bool hits = __any(hit >= 0);                      // one of 16 rows, in a few tiles
       if constexpr (GRADIENT) {
         const float base = lse[j] * -kLog2E;                  // rounded by 2^-24 of lse, as the logits are by more
+        const int lift = __is_same(T, f16) ? lift_of(weight[j], a.scale[2]) : 0;
+        const float slope = __is_same(T, f16) ? ldexpf(kLog2E, lift) : kLog2E;
 #pragma unroll
         for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], kLog2E, base));
+          for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][r], slope, base));
         if (hits) {
           asm volatile("");                                   // a block of its own, no selects
 #pragma unroll
@@ -113,7 +126,7 @@ __global__ __launch_bounds__(S::threads, S::resident) void logits_kernel(LossArg
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[i][j][r] -= hit == i * 16 + r ? 1.f : 0.f;
         }
-        const float factor = unknown ? __builtin_nanf("") : weight[j] * unit;
+        const float factor = unknown ? __builtin_nanf("") : __is_same(T, f16) ? ldexpf(weight[j] * unit, lift) : weight[j] * unit;
 #pragma unroll
         for (int i = 0; i < S::TM; ++i)
 #pragma unroll
@@ -200,7 +213,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Part *parts, i
 }
 
 // Rows of two arrays copied with their columns padded with zeros; x's rows of ignored targets as zeros.  The last workgroup
-// finds G's unit instead.
+// finds G's unit instead, or, for fp16, whose rows are copied by it, a launch of its own.
 struct PackArgs {
   const uint16_t *from[2];
   uint16_t *to[2];
@@ -208,31 +221,35 @@ struct PackArgs {
   int32_t rows[2], cols, to_ld;
   const int64_t *target;                      // of the rows of array 0, or null
   const float *dloss;
-  float *scale;
+  float *scale;                               // null: not wanted
+  int32_t lifts;                              // array 0 is fp16, scale is there already
 };
-__global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
-  if (a.scale && blockIdx.x == gridDim.x - 1) {
-    __shared__ float part[4];
-    float most = 0.f;
+__device__ __forceinline__ void find_unit(const PackArgs &a) {
+  __shared__ float part[4];
+  float most = 0.f;
 #pragma unroll 8
-    for (int32_t i = threadIdx.x; i < a.rows[0]; i += 256) {
-      const int64_t t = a.target[i];
-      const float d = fabsf(a.dloss[i]);
-      most = t >= 0 && isfinite(d) ? fmaxf(most, d) : most;      // an infinite one takes no unit away from the others
-    }
-#pragma unroll
-    for (int m = 1; m < kWave; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
-    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = most;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-      const bool usable = most > 1e-30f;
-      a.scale[0] = usable ? 16384.f / most : 1.f;
-      a.scale[1] = usable ? most / 16384.f : 1.f;
-    }
-    return;
+  for (int32_t i = threadIdx.x; i < a.rows[0]; i += 256) {
+    const int64_t t = a.target[i];
+    const float d = fabsf(a.dloss[i]);
+    most = t >= 0 && isfinite(d) ? fmaxf(most, d) : most;        // an infinite one takes no unit away from the others
   }
-  const int64_t blocks = gridDim.x - (a.scale ? 1 : 0), pieces = a.to_ld / 8, total = (static_cast<int64_t>(a.rows[0]) + a.rows[1]) * pieces;
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+    const bool usable = most > 1e-30f;
+    a.scale[0] = usable ? 16384.f / most : 1.f;
+    a.scale[1] = usable ? most / 16384.f : 1.f;
+    a.scale[2] = usable ? most : 0.f;
+  }
+}
+__global__ __launch_bounds__(256) void unit_kernel(PackArgs a) { find_unit(a); }
+__global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
+  const bool finds = a.scale && !a.lifts;
+  if (finds && blockIdx.x == gridDim.x - 1) return find_unit(a);
+  const int64_t blocks = gridDim.x - (finds ? 1 : 0), pieces = a.to_ld / 8, total = (static_cast<int64_t>(a.rows[0]) + a.rows[1]) * pieces;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += blocks * 256) {
     int64_t row = i / pieces;
     const int32_t c = static_cast<int32_t>(i - row * pieces) * 8;
@@ -250,6 +267,11 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) v.v[k] = c + k < a.cols ? from[k] : uint16_t{0};
     }
+    const int lift = a.lifts && !which && !skip ? lift_of(a.dloss[row], a.scale[2]) : 0;
+    if (lift) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v.v[k] = __builtin_bit_cast(uint16_t, static_cast<f16>(ldexpf(static_cast<float>(__builtin_bit_cast(f16, v.v[k])), -lift)));
+    }
     *reinterpret_cast<Pack<uint16_t, 8> *>(a.to[which] + row * a.to_ld + c) = v;
   }
 }
@@ -258,7 +280,7 @@ struct GradientArgs {
   Operand w_turned, g, x_turned, g_turned;
   Split of_dx, of_dw;
   const int64_t *target;
-  const float *scale;
+  const float *dloss, *scale;
   float *dx_sum, *dw_sum;                     // [splits][rows][cols], [splits][words][cols]
   void *dx, *dweight;                         // dweight: of the piece's first word
   int32_t cols, wide;                         // wide: runs of four of dx and dW can be written at once
@@ -285,7 +307,6 @@ __global__ __launch_bounds__(S::threads, S::resident) void gradients_kernel(Grad
   const Place<S> at(m * S::BM, n * S::BN);
   const bool wide = a.wide, whole = of_dx ? split.splits == 1 && a.dx_last : !a.dw_parts, adds = !(of_dx ? a.dx_first : a.dw_first);
   const int32_t rows = of_dx ? a.g.extent : a.g_turned.extent;
-  const float back = whole ? a.scale[1] : 1.f;
   float *sum = (of_dx ? a.dx_sum : a.dw_sum) + static_cast<int64_t>(part) * rows * a.cols;
   T *to = static_cast<T *>(of_dx ? a.dx : a.dweight);
 #pragma unroll
@@ -293,6 +314,7 @@ __global__ __launch_bounds__(S::threads, S::resident) void gradients_kernel(Grad
     const int32_t row = at.n + j * 16;
     if (row >= rows) continue;
     const bool ignored = whole && of_dx && a.target[row] < 0;
+    const float back = !whole ? 1.f : __is_same(T, f16) && of_dx ? ldexpf(a.scale[1], -lift_of(a.dloss[row], a.scale[2])) : a.scale[1];
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
       const int32_t c = at.m + i * 16;
@@ -335,7 +357,7 @@ struct FinishArgs {
   int64_t size[2];                            // elements; 0: not split
   int32_t splits[2], cols, wide;
   const int64_t *target;                      // of the rows of dx
-  const float *scale;
+  const float *dloss, *scale;
 };
 template <typename T, int V>
 __global__ __launch_bounds__(256) void finish_kernel(FinishArgs a) {
@@ -353,9 +375,11 @@ __global__ __launch_bounds__(256) void finish_kernel(FinishArgs a) {
 #pragma unroll
     for (int k = 0; k < V; ++k) v[k] += one.v[k];
   }
-  const bool ignored = !which && a.target[i / a.cols] < 0;
+  const int64_t row = which ? 0 : i / a.cols;
+  const bool ignored = !which && a.target[row] < 0;
+  const float back = __is_same(T, f16) && !which ? ldexpf(a.scale[1], -lift_of(a.dloss[row], a.scale[2])) : a.scale[1];
 #pragma unroll
-  for (int k = 0; k < V; ++k) v[k] = ignored ? 0.f : v[k] * a.scale[1];
+  for (int k = 0; k < V; ++k) v[k] = ignored ? 0.f : v[k] * back;
   store_pack<T, V>(static_cast<T *>(a.to[which]) + i, v);
 }
 
@@ -367,7 +391,8 @@ bool loadable(const void *p, int64_t stride, int64_t cols) {
 
 void launch_pack(const PackArgs &a, hipStream_t s) {
   const int64_t total = (static_cast<int64_t>(a.rows[0]) + a.rows[1]) * (a.to_ld / 8);
-  const int64_t blocks = std::min<int64_t>(ceil_div(total, 256), 4096) + (a.scale ? 1 : 0);
+  const int64_t blocks = std::min<int64_t>(ceil_div(total, 256), 4096) + (a.scale && !a.lifts ? 1 : 0);
+  if (a.lifts) hipLaunchKernelGGL(unit_kernel, dim3(1), dim3(256), 0, s, a);
   if (blocks) hipLaunchKernelGGL(pack_kernel, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, s, a);
 }
 
@@ -421,6 +446,7 @@ void launch_piece(const LossArgs &a, const GradientArgs &b, const LossPlan &p, h
   f.cols = b.cols;
   f.wide = b.wide;
   f.target = b.target;
+  f.dloss = b.dloss;
   f.scale = b.scale;
   launch_finish<T>(f, s);
 }
@@ -457,7 +483,7 @@ int ones_cross_entropy_forward(const void *x, int64_t x_stride, const void *weig
   if (copy_x || copy_w) {
     PackArgs a{{static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(weight)},
                {reinterpret_cast<uint16_t *>(ws + p.x), reinterpret_cast<uint16_t *>(ws + p.w)}, {x_stride, weight_stride},
-               {copy_x ? n : 0, copy_w ? v : 0}, static_cast<int32_t>(cols), d8, nullptr, nullptr, nullptr};
+               {copy_x ? n : 0, copy_w ? v : 0}, static_cast<int32_t>(cols), d8, nullptr, nullptr, nullptr, 0};
     launch_pack(a, s);
   }
   LossArgs a{};
@@ -492,7 +518,7 @@ int ones_cross_entropy_backward(const float *dloss, const void *x, int64_t x_str
   float *scale = reinterpret_cast<float *>(ws + p.scale);
   PackArgs pack{{static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(weight)},
                 {reinterpret_cast<uint16_t *>(ws + p.x), reinterpret_cast<uint16_t *>(ws + p.w)}, {x_stride, weight_stride},
-                {n, copy_w ? static_cast<int32_t>(vocabulary) : 0}, static_cast<int32_t>(cols), d8, target, dloss, scale};
+                {n, copy_w ? static_cast<int32_t>(vocabulary) : 0}, static_cast<int32_t>(cols), d8, target, dloss, scale, type == ONES_F16};
   launch_pack(pack, s);
   const char *w = copy_w ? ws + p.w : static_cast<const char *>(weight);
   const int64_t w_ld = copy_w ? d8 : weight_stride;
@@ -516,7 +542,7 @@ int ones_cross_entropy_backward(const float *dloss, const void *x, int64_t x_str
       b.g = Operand{ws + p.g, p.piece, some, words};          // the rest of the last eight words is zeros
       b.x_turned = Operand{xp, d8, d8, some};
       b.g_turned = Operand{ws + p.g, p.piece, words, some};
-      b.target = target + r0; b.scale = scale;
+      b.target = target + r0; b.dloss = dloss + r0; b.scale = scale;
       b.of_dx = p.gradients.of_dx;
       b.of_dw = p.gradients.of_dw;
       b.dx_sum = reinterpret_cast<float *>(ws + p.dx_sum) + b.of_dx.splits * r0 * cols;

@@ -198,7 +198,7 @@ inline LossPlan loss_plan(int64_t rows, int64_t cols, int64_t vocabulary, bool c
   p.g = take(static_cast<size_t>(at_once * p.piece) * 2);
   p.dx_sum = take(p.pieces > 1 || p.gradients.of_dx.splits > 1 ? p.gradients.of_dx.splits * n * d * 4 : 0);
   p.dw_sum = take(p.blocks > 1 || p.gradients.of_dw.splits > 1 ? static_cast<size_t>(p.gradients.of_dw.splits) * std::min(p.piece, vocabulary) * d * 4 : 0);
-  p.scale = take(8);
+  p.scale = take(12);
   p.backward = off;
   return p;
 }

@@ -319,3 +319,26 @@ def test_an_infinite_gradient_of_a_loss_stays_in_its_row_of_dx(train, dtype):  #
     assert not dx[[3, 66]].isfinite().any() and not dw.isfinite().any()
     off[[3, 66]] = 0
     assert (off <= allowed).all(), (off / allowed).max().item()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("rows,cols,words", [(140, 64, 30000), (140, 33, 131072), (1329, 2774, 1593), (4103, 250, 12267)])
+def test_rows_of_small_gradients_next_to_large_ones(train, rows, cols, words, dtype):  # noqa: F811
+    """dloss from 2^13 down to 2^-13: dx of every row is right for itself, and dW for words that only a small row has as its target."""
+    gen = torch.Generator(device="cuda").manual_seed(41)
+    x = (torch.randn(rows, cols, generator=gen, device="cuda") * 0.3).to(dtype)
+    w = (torch.randn(words, cols, generator=gen, device="cuda") * 1.6 + 0.8).div(cols ** 0.5).to(dtype)
+    t = torch.randperm(words, generator=gen, device="cuda")[:rows]
+    dloss = 2.0 ** (13 - torch.arange(rows, device="cuda") % 27) * (1 + torch.rand(rows, generator=gen, device="cuda"))
+    t[7] = -1
+    off, allowed, dx, dw = row_errors(train, x, w, t, dloss)
+    off[7] = 0
+    assert (off <= allowed).all(), (off / allowed).max().item()
+    _, _, g, p, cx, _ = loss64(x, w, t, dloss)
+    want, at = g.t() @ cx, t.clamp(min=0)
+    error = (dw.double() - want).norm(dim=1)
+    # G's roundings of either sign, and x's in units of the largest dloss
+    mine = 2 * HALF[dtype] * (g.t().square() @ cx.square()).sum(1).sqrt() + HALF[dtype] * want.norm(dim=1) + 2.0 ** -24 * cols ** 0.5
+    soft = (16 + 4 * cols ** 0.5 + words / 64) * U32 * 8 * (p.t() @ cx.abs()).norm(dim=1)
+    assert (error <= mine + soft)[at].all(), (error / (mine + soft))[at].max().item()
