@@ -105,6 +105,10 @@ def _like(t):
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
+# what autograd has to know of a tensor that a call has written in place: a backward pass that saved it raises then
+_changed = torch.autograd.graph.increment_version
+
+
 def _scratch(nbytes, device):
     """Workspace of one call from torch's allocator, whose blocks are 512-byte aligned and reused in stream order."""
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
@@ -258,6 +262,7 @@ def gated_recurrence_step(gate, x, state):
     h = _like(x)
     _call(x.device, load().ones_recurrence_step, gate.data_ptr(), gate.stride(0), x.data_ptr(), x.stride(0), b, c, _TYPES[x.dtype],
           state.data_ptr(), h.data_ptr())
+    _changed(state)
     return h
 
 
@@ -381,4 +386,6 @@ def orthogonal_update(grad, momentum=None, beta=0.95, nesterov=True, steps=5, co
     scratch = _scratch(nbytes, grad.device)
     _call(grad.device, L.ones_orthogonal_update, grad.data_ptr(), _ptr(momentum), count, m, n, _TYPES[grad.dtype], beta, int(nesterov),
           steps, (C.c_float * 3)(*coefficients), eps, update.data_ptr(), _TYPES[dtype], _ptr(scratch), nbytes)
+    if momentum is not None:
+        _changed(momentum)
     return update

@@ -466,3 +466,20 @@ def test_recurrence_of_many_sequences_of_few_steps(train, channels):
         want = recurrence64(gate[rows], x[rows], state[rows], lengths[rows], dh[rows], state[rows])
         for got, one, what in zip((h, last, dgate, dx, dstate), want, ("h", "last", "dgate", "dx", "dstate")):
             near(got[rows], one, torch.full_like(one, 64.0), 32, what)
+
+
+def test_what_is_updated_in_place_is_known_to_autograd(train, monkeypatch):
+    """A backward pass that needs the old state or momentum raises, as behind torch's own in-place operators; no GPU: the call is left out."""
+    monkeypatch.setattr(train, "_check", lambda *a, **k: None)
+    monkeypatch.setattr(train, "_call", lambda *a: None)
+    x = torch.zeros(2, 8)
+    for shape, change in (((2, 8), lambda t: train.gated_recurrence_step(x, x, t)), ((8, 8), lambda t: train.orthogonal_update(torch.zeros(8, 8), t))):
+        leaf = torch.ones(shape, requires_grad=True)
+        held = leaf * 2
+        loss = held.square().sum()                                    # keeps held
+        with torch.no_grad():
+            change(held)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+        with torch.inference_mode():
+            change(torch.ones(shape))
