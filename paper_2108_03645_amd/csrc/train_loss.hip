@@ -231,7 +231,10 @@ __device__ __forceinline__ void find_unit(const PackArgs &a) {
   for (int32_t i = threadIdx.x; i < a.rows[0]; i += 256) {
     const int64_t t = a.target[i];
     const float d = fabsf(a.dloss[i]);
-    most = t >= 0 && isfinite(d) ? fmaxf(most, d) : most;        // an infinite one takes no unit away from the others
+    // An infinite one takes no unit away from the others.  (Not with &&: as a branch that puts the loads one after another, 8192 rows
+    // 21 us instead of 9.)
+    const bool counts = (t >= 0) & (d < INFINITY);
+    most = counts ? fmaxf(most, d) : most;
   }
 #pragma unroll
   for (int m = 1; m < kWave; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
