@@ -105,8 +105,10 @@ int ones_cross_entropy_backward(const float *dloss, const void *x, int64_t x_str
  *   momentum = beta * momentum + grad; u = grad + beta * momentum if nesterov, else momentum; X = u / (|u| + eps), |u| the root of
  *   the sum of squares of each matrix; `steps` times, with coefficients a, b, c: A = X X^T, X = a X + (b A + c A A) X; update = X
  * (with X^T X for rows > cols, which gives the same).  grad_type: any; momentum: float, updated in place, or NULL (u = grad);
- * update_type: ONES_F16 or ONES_BF16.  coefficients: HOST array of three, of size up to 16, that keep the singular values below 8
- * (they start below 1); products have fp16 operands.  1 <= steps <= 100, 0 <= beta <= 1, eps >= 0.  A matrix of zeros gives zeros
+ * update_type: ONES_F16 or ONES_BF16.  coefficients: HOST array of three, of size up to 16, that keep the singular values below 7.9
+ * (they start below 1).  Products have fp16 operands for ONES_BF16, which puts the result of five steps about as far off again as its own
+ * rounding does (2e-3 of its norm in all), and pairs of fp16 for ONES_F16, three products each, which leaves its own rounding (2e-4).
+ * The workspace is enough for either.  1 <= steps <= 100, 0 <= beta <= 1, eps >= 0.  A matrix of zeros gives zeros
  * if eps > 0.  Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a side, count above 65535, a coefficient), ONES_E_WORKSPACE_TOO_SMALL,
  * ONES_E_HIP. */
 size_t ones_orthogonal_update_workspace_bytes(int64_t count, int64_t rows, int64_t cols);

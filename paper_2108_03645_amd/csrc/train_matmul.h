@@ -225,13 +225,16 @@ struct Product {
     }
   }
 
+  template <bool ADDS = false>                // to what acc holds
   __device__ __forceinline__ void run(unsigned char *lds, Sums<S> &acc) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int wm = (wave / S::WN) * (S::BM / S::WM), wn = (wave % S::WN) * (S::BN / S::WN);
+    if constexpr (!ADDS) {
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i)
+      for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     if (tiles <= 0) return;
     s16x8 a[2][kRows], b[2][S::TN];
     if (tiles >= S::buffers) meet<(S::buffers - 1) * of_tile>();
@@ -248,12 +251,20 @@ struct Product {
   }
 };
 
-template <typename T, bool LT, bool RT, typename S>
+template <typename T, bool LT, bool RT, typename S, bool ADDS = false>
 __device__ __forceinline__ void product(const Operand &L, const Operand &R, int32_t m0, int32_t n0, int32_t k0, int32_t k1, unsigned char *lds,
                                         Sums<S> &acc) {
   Product<T, LT, RT, S> p;
   p.begin(L, R, m0, n0, k0, k1, lds);
-  p.run(lds, acc);
+  p.template run<ADDS>(lds, acc);
+}
+// The same of operands held in pairs, the second what the first was rounded by: three products, without that of the two seconds (2^-22).
+template <typename T, bool LT, bool RT, typename S>
+__device__ __forceinline__ void product_of_pairs(const Operand (&L)[2], const Operand (&R)[2], int32_t m0, int32_t n0, int32_t k0, int32_t k1,
+                                                 unsigned char *lds, Sums<S> &acc) {
+  product<T, LT, RT, S>(L[1], R[0], m0, n0, k0, k1, lds, acc);
+  product<T, LT, RT, S, true>(L[0], R[1], m0, n0, k0, k1, lds, acc);
+  product<T, LT, RT, S, true>(L[0], R[0], m0, n0, k0, k1, lds, acc);
 }
 
 // Where a lane's runs of four m start, and its n: of sum (i, j), in the whole of C.

@@ -237,22 +237,25 @@ inline Tiles least(const int64_t (&items)[5], int64_t k) {
   return best;
 }
 struct UpdateTiles { Tiles gram, poly, apply; };
-inline UpdateTiles update_tiles(int64_t count, int64_t r, int64_t q) {
+inline UpdateTiles update_tiles(int64_t count, int64_t r, int64_t q, bool pairs) {
+  const int64_t products = pairs ? 3 : 1;
   int64_t triangle[5], all[5];
   for (Tiles t : {kLarge, kMiddle, kDeep, kSmall, kTiny}) {
     const TileCost &c = kTileCosts[t];
     triangle[t] = count * symmetric_tiles(c.bm, c.bn, ceil_div(r, 8) * 8);
     all[t] = count * (t == kMiddle ? ceil_div(r, c.bm) * ceil_div(q, c.bn) : ceil_div(r, c.bn) * ceil_div(q, c.bm));
   }
-  return UpdateTiles{least(triangle, q), least(triangle, r), least(all, r)};
+  return UpdateTiles{least(triangle, products * q), least(triangle, products * r), least(all, products * r)};
 }
 
+// pairs: X and A are held in pairs, the second one behind all matrices' first.
 struct UpdatePlan {
   int64_t r, q, r_ld, q_ld;
   int64_t blocks;
+  int64_t x_low, a_low;                       // elements from a first to its second; 0 without
   size_t squares, x[2], a[2], total;
 };
-inline UpdatePlan update_plan(int64_t count, int64_t rows, int64_t cols) {
+inline UpdatePlan update_plan(int64_t count, int64_t rows, int64_t cols, bool pairs) {
   UpdatePlan p{};
   p.r = std::min(rows, cols);
   p.q = std::max(rows, cols);
@@ -262,10 +265,13 @@ inline UpdatePlan update_plan(int64_t count, int64_t rows, int64_t cols) {
   auto take = [&](int64_t bytes) { const size_t at = off; off = align_up(off + static_cast<size_t>(bytes)); return at; };
   p.blocks = std::min(kSumBlocks, ceil_div(rows * cols, 4096));            // at least four runs of four elements a thread
   p.squares = take(count * p.blocks * 8);
-  p.x[0] = take(count * p.r * p.q_ld * 2);
-  p.x[1] = take(count * p.r * p.q_ld * 2);
-  p.a[0] = take(count * p.r * p.r_ld * 2);
-  p.a[1] = take(count * p.r * p.r_ld * 2);
+  const int64_t x = count * p.r * p.q_ld, a = count * p.r * p.r_ld, bytes = pairs ? 4 : 2;
+  p.x_low = pairs ? x : 0;
+  p.a_low = pairs ? a : 0;
+  p.x[0] = take(x * bytes);
+  p.x[1] = take(x * bytes);
+  p.a[0] = take(a * bytes);
+  p.a[1] = take(a * bytes);
   p.total = off;
   return p;
 }

@@ -365,7 +365,8 @@ COEFFICIENTS = (3.4445, -4.7750, 2.0315)      # singular values from 0.01 to 1 e
 def orthogonal_update(grad, momentum=None, beta=0.95, nesterov=True, steps=5, coefficients=COEFFICIENTS, eps=1e-7, dtype=None):
     """ones_orthogonal_update: the update for weights whose gradient is grad [rows, cols] or [count, rows, cols], all matrices of
     one call together.  momentum (float32, shaped like grad, without gaps) is updated in place; without one grad itself is
-    orthogonalised.  dtype: of the result, bfloat16 or float16 (default: grad's, bfloat16 for float32)."""
+    orthogonalised.  dtype: of the result, bfloat16 or float16 (default: grad's, bfloat16 for float32); a float16 result is right to its own
+    rounding and takes up to 2.6 times as long, a bfloat16 one is off by 1.4 times its own rounding."""
     _check(grad, "grad", None, _TYPES)
     if grad.dim() not in (2, 3):
         raise ValueError(f"grad: [rows, cols] or [count, rows, cols] is wanted, got {tuple(grad.shape)}")

@@ -14,7 +14,7 @@ import torch
 
 from test_train_loss import check
 from test_train_norm_recurrence import HALF, U32, near, recurrence64, train  # noqa: F401
-from test_train_update import ABC, update64
+from test_train_update import ABC, IN_PAIRS, update64
 
 gpu = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -47,7 +47,11 @@ void launch(int64_t rows, int64_t cols, int64_t words, int64_t *to) {
   *to = std::max({products, finish, 2 * ceil_div(words, f.bm) * ceil_div(rows, f.bn), rows * 128});      // the logits' tiles have 31 bits; 8 rows a join
 }
 void update(int64_t count, int64_t rows, int64_t cols, int64_t *to) {
-  const UpdateTiles t = update_tiles(count, std::min(rows, cols), std::max(rows, cols));
+  const UpdateTiles t = update_tiles(count, std::min(rows, cols), std::max(rows, cols), false);
+  to[0] = t.gram; to[1] = t.poly; to[2] = t.apply;
+}
+void update_in_pairs(int64_t count, int64_t rows, int64_t cols, int64_t *to) {
+  const UpdateTiles t = update_tiles(count, std::min(rows, cols), std::max(rows, cols), true);
   to[0] = t.gram; to[1] = t.poly; to[2] = t.apply;
 }
 void recurrence(int64_t batch, int64_t steps, int64_t channels, int64_t backward, int64_t *to) {
@@ -108,6 +112,18 @@ UPDATES = {
     (1, 3001, 2999): (MIDDLE, MIDDLE, LARGE),
     (2, 4101, 2047): (MIDDLE, MIDDLE, MIDDLE),
 }
+# the same where the operands are held in pairs (fp16 results)
+PAIRS = {
+    (2, 131, 65): (TINY, TINY, TINY),
+    (40, 267, 269): (DEEP, DEEP, SMALL),
+    (40, 415, 417): (SMALL, SMALL, LARGE),
+    (5, 3287, 70): (TINY, TINY, DEEP),
+    (8, 4177, 131): (TINY, TINY, LARGE),
+    (3, 3599, 349): (TINY, TINY, MIDDLE),
+    (16, 643, 645): (MIDDLE, MIDDLE, LARGE),
+    (40, 541, 543): (LARGE, LARGE, SMALL),
+    (2, 4101, 2047): (MIDDLE, MIDDLE, MIDDLE),
+}
 # (batch, steps, channels): lanes and segments forward, and backward
 RECURRENCES = {
     (96, 1101, 130): (8, 1, 16, 1),
@@ -130,6 +146,11 @@ def test_tiles_of_the_update(plans, sizes):
     assert plans("update", 3, *sizes) == UPDATES[sizes]
 
 
+@pytest.mark.parametrize("sizes", PAIRS, ids=str)
+def test_tiles_of_the_update_in_pairs(plans, sizes):
+    assert plans("update_in_pairs", 3, *sizes) == PAIRS[sizes]
+
+
 @pytest.mark.parametrize("sizes", RECURRENCES, ids=str)
 def test_cuts_of_the_recurrence(plans, sizes):
     assert plans("recurrence", 2, *sizes, 0) + plans("recurrence", 2, *sizes, 1) == RECURRENCES[sizes]
@@ -137,7 +158,7 @@ def test_cuts_of_the_recurrence(plans, sizes):
 
 def test_the_sizes_reach_every_shape_of_every_product():
     for shapes, of in (((LARGE, DEEP, SMALL, TINY), [[p[k] for p in LOSSES.values()] for k in range(3)]),
-                       (range(5), [[p[k] for p in UPDATES.values()] for k in range(3)])):
+                       (range(5), [[p[k] for p in UPDATES.values()] for k in range(3)]), (range(5), [[p[k] for p in PAIRS.values()] for k in range(3)])):
         assert all(set(shapes) == set(reached) for reached in of)
     # dx added up over pieces of the vocabulary and rounded behind the last, by each of the tiles that large calls take
     assert {p[2] for p in LOSSES.values() if p[3] == 1 and p[5] > 1} == {LARGE, DEEP, SMALL}
@@ -278,3 +299,16 @@ def test_launches_of_every_accepted_size_of_the_loss_fit(plans):
             for words in sizes(24):
                 largest = max(largest, *plans("launch", 1, rows, cols, words))
     assert 1 << 28 < largest < 1 << 32
+
+
+@gpu
+@pytest.mark.parametrize("sizes", PAIRS, ids=str)
+def test_update_of_every_shape_in_pairs(train, sizes):  # noqa: F811
+    """Element by element: half a step of fp16, and eight times (as above) what 22 bits leave of the whole."""
+    gen = torch.Generator(device="cuda").manual_seed(sum(sizes))
+    g = torch.randn(*sizes, generator=gen, device="cuda") * 1e-2
+    m = torch.randn(*sizes, generator=gen, device="cuda") * 0.1
+    want, _ = update64(g, m, 0.95, True, 5, ABC, 1e-7)
+    got = train.orthogonal_update(g, m, 0.95, True, 5, ABC, 1e-7, dtype=torch.float16)
+    off, mean = (got.double() - want).abs(), want.square().mean((1, 2), keepdim=True).sqrt()
+    assert (off <= HALF[torch.float16] * want.abs() * (1 + 2.0 ** -7) + 8 * IN_PAIRS * mean + 2.0 ** -24).all(), (off / mean).max().item()

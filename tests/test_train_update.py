@@ -184,3 +184,23 @@ def test_update_of_one_small_matrix_among_large_ones(train):  # noqa: F811
     for k in (0, 1):
         assert (got[k].double() - want).norm() <= (5.7e-3 + HALF[torch.bfloat16]) * want.norm()
     assert not got[2].any() and got[3].isnan().all()
+
+
+# What products of pairs and sums of 32 bits make of the whole over five steps: 45 (see the top of the file) times half a step of 22 bits
+# and, for up to 4096 terms of either sign, 2^-24 times a quarter of the root of their number.
+IN_PAIRS = 45 * (2.0 ** -22 + 16 * U32)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("count,rows,cols", SIZES)
+def test_an_fp16_result_has_the_precision_of_fp16(train, count, rows, cols, dtype):  # noqa: F811
+    gen = torch.Generator(device="cuda").manual_seed(rows * 7 + cols)
+    rank = max(1, min(rows, cols) // 8)
+    signal = torch.randn(count, rows, rank, generator=gen, device="cuda").double() @ torch.randn(count, rank, cols, generator=gen, device="cuda").double()
+    g = ((signal / rank ** 0.5 + torch.randn(count, rows, cols, generator=gen, device="cuda")) * 1e-3).to(dtype)
+    m = ((signal * 8 / rank ** 0.5 + 3 * torch.randn(count, rows, cols, generator=gen, device="cuda")) * 1e-3).float() if rows % 3 else None
+    want, _ = update64(g, m, 0.95, True, 5, ABC, 1e-7)
+    got = train.orthogonal_update(g, m, 0.95, True, 5, ABC, 1e-7, dtype=torch.float16)
+    off = (got.double() - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1)
+    assert off.max() <= HALF[torch.float16] + IN_PAIRS, off.max().item()
