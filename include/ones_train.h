@@ -86,7 +86,8 @@ int ones_recurrence_step(const void *gate, int64_t gate_stride, const void *x, i
  * gradient, and what x holds there does not matter); vocabulary or above: the row's loss, its dx and dweight are NaN.
  * loss, lse: float [rows].  Backward: dloss float [rows], lse as forward left it; dx[rows][cols] and dweight[vocabulary][cols]
  * are written.  It goes through the vocabulary in pieces, and through more than 2^18 rows in blocks, so that at most 128 MiB of logits'
- * gradients, rounded to type, are held at a time.
+ * gradients, rounded to type, are held at a time (in units of dloss: in fp16 dx of a row is as exact as fp16 is while the row's |dloss|
+ * is above 2^-26 of the largest).
  * wide: not 0 if cols, both strides and both bases are multiples of 16 bytes and no stride is above 2^20 elements; otherwise the
  * workspace has room for copies.
  * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size above its limit, or the product of two of them above 2^36),
@@ -107,7 +108,7 @@ int ones_cross_entropy_backward(const float *dloss, const void *x, int64_t x_str
  * (with X^T X for rows > cols, which gives the same).  grad_type: any; momentum: float, updated in place, or NULL (u = grad);
  * update_type: ONES_F16 or ONES_BF16.  coefficients: HOST array of three, of size up to 16, that keep the singular values below 7.9
  * (they start below 1).  Products have fp16 operands for ONES_BF16, which puts the result of five steps about as far off again as its own
- * rounding does (2e-3 of its norm in all), and pairs of fp16 for ONES_F16, three products each, which leaves its own rounding (2e-4).
+ * rounding does (2.4e-3 of its norm in all), and pairs of fp16 for ONES_F16, three products each, which leaves its own rounding (2e-4).
  * The workspace is enough for either.  1 <= steps <= 100, 0 <= beta <= 1, eps >= 0.  A matrix of zeros gives zeros
  * if eps > 0.  Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a side, count above 65535, a coefficient), ONES_E_WORKSPACE_TOO_SMALL,
  * ONES_E_HIP. */

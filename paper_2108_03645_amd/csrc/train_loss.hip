@@ -15,7 +15,7 @@
 // Measured, where a large library product reaches 1.35 (8192 cubed) to 1.5 PFLOP/s: logits of 16384 x 32000, k 512, with their
 // epilogue 455 us (1.18 PFLOP/s; a tile of 256 x 256 takes 1.4 us for 64 k and 5 us for its start and its exponentials), 8192 x
 // 32000, k 1024, 437 us (1.23).  A piece of 8192 rows and words, k 1024: G 120 to 144 us (1.0), its two products 208 to 240 us (1.2
-// to 1.3); joining the parts 4 to 11 us, packing x 3 to 12 us.
+// to 1.3); joining the parts 4 to 11 us, packing x 3 to 9 us.
 //
 // G is held in units of the largest finite |dloss| over 2^14 and the products are scaled back in 32 bits.  fp16 would lose small
 // probabilities times small dloss otherwise; and where all dloss are equal, as in a mean, the target's entry comes to
