@@ -312,10 +312,10 @@ def _own(s):
         dq, dk, dqw, dkw = train.head_norm_rotation_backward(s["dq"], s["dk"], s["q"], s["k"], *common)
         return {"q": q, "dq": dq, "dqw": dqw, "k": k, "dk": dk, "dkw": dkw}
     if case["op"] == "attention":
-        o, lse = train.attention_forward(s["q"], s["k"], s["v"], s["offsets"])
+        o, lse, rest = train.attention_forward(s["q"], s["k"], s["v"], s["offsets"], keep_rest=case["backward"])
         if not case["backward"]:
             return {"o": o, "lse": lse}
-        dq, dk, dv = train.attention_backward(s["do"], s["q"], s["k"], s["v"], o, lse, s["offsets"])
+        dq, dk, dv = train.attention_backward(s["do"], s["q"], s["k"], s["v"], o, lse, rest, s["offsets"])
         return {"o": o, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
     if case["op"] == "step":
         o = train.attention_step(s["q"], s["k"], s["v"], s["keys"], s["values"], s["lengths"])
