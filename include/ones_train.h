@@ -3,8 +3,9 @@
  *
  * The search (ones.h) decides at which batch a job trains and describes the job by its iteration time
  * t(B,g) = a*B/g + c*log2(g) + d.  These are the parts of such an iteration: layer norm, a gated linear recurrence over the
- * steps of a sequence and the loss over a large vocabulary, whose work grows with the local batch B/g (a), and the
- * orthogonalised update of a weight matrix, whose work does not (d).
+ * steps of a sequence, causal attention with the norms and the rotation of its queries and keys, and the loss over a large vocabulary,
+ * whose work grows with the local batch B/g (a), and the clipping of the gradients and the orthogonalised update of a weight matrix,
+ * whose work does not (d).
  *
  * Conventions.  Every function returns ONES_OK (0) or a negative ONES_E_* code of ones.h; nothing aborts or throws across this
  * boundary, all sizes are checked before the first launch and nothing is launched on error.  All arrays are DEVICE pointers
@@ -39,6 +40,11 @@ extern "C" {
 #define ONES_MAX_LOSS_COLUMNS 65536
 #define ONES_MAX_VOCABULARY   (1 << 24)
 #define ONES_MAX_UPDATE_SIDE  65536       /* rows and columns of an orthogonalised update           */
+#define ONES_MAX_TOKENS       (1 << 30)   /* tokens of a call, places of a cache                     */
+#define ONES_MAX_HEADS        1024
+#define ONES_MAX_HEAD_DIM     512         /* elements of a head's row: head norms with the rotation  */
+#define ONES_MAX_ATTENTION_DIM 128        /* attention                                              */
+#define ONES_MAX_GRADIENTS    (1 << 20)   /* tensors of a clipping                                  */
 
 /* Layer norm over the columns of x[rows][cols], 1 <= cols <= ONES_MAX_NORM_COLUMNS:
  *   y = (x - mean) * rstd * weight + bias, mean and rstd = (variance + eps)^-1/2 per row (variance: the mean square of x - mean).
@@ -116,6 +122,73 @@ size_t ones_orthogonal_update_workspace_bytes(int64_t count, int64_t rows, int64
 int ones_orthogonal_update(const void *grad, float *momentum, int64_t count, int64_t rows, int64_t cols, int32_t grad_type,
                            float beta, int32_t nesterov, int32_t steps, const float *coefficients, float eps,
                            void *update, int32_t update_type, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Norms of queries and keys for each head, and their rotation by positions.  Of every row x of `dim` elements (a head of a token):
+ *   n = x * r * weight, r = (mean(x^2) + eps)^-1/2; the first 2 * pairs elements in pairs (n1, n2), i = 0 .. pairs - 1, turned by the
+ *   angle position * frequencies[i]: y1 = n1 cos - n2 sin, y2 = n2 cos + n1 sin; the others as they are.
+ * Pairs are elements (i, i + pairs), or with `neighbours` (2 i, 2 i + 1).  q: [tokens][heads][dim], k: [tokens][kv_heads][dim], with
+ * strides between tokens and between heads; outputs without gaps.  type: any; q_weight, k_weight: dim elements of weight_type, type or
+ * ONES_F32.  positions: int32 [tokens], any; frequencies: float [pairs], radians a position (the angle is formed in 64 bits: off by
+ * less than 2^-24 turns up to 2^29 turns).  0 <= 2 * pairs <= dim <= ONES_MAX_HEAD_DIM.
+ * Backward: dq_out, dk_out are the gradients of the results; dq, dk and the sums over tokens and heads dq_weight, dk_weight are written
+ * (the latter may be NULL).  Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS, ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
+int ones_head_norm_rotation_forward(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride,
+                                    int64_t k_head_stride, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type,
+                                    const void *q_weight, const void *k_weight, int32_t weight_type, float eps, const int32_t *positions,
+                                    const float *frequencies, int64_t pairs, int32_t neighbours, void *q_out, void *k_out, void *hip_stream);
+size_t ones_head_norm_rotation_workspace_bytes(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim);
+int ones_head_norm_rotation_backward(const void *dq_out, int64_t dq_stride, int64_t dq_head_stride, const void *dk_out, int64_t dk_stride,
+                                     int64_t dk_head_stride, const void *q, int64_t q_stride, int64_t q_head_stride, const void *k,
+                                     int64_t k_stride, int64_t k_head_stride, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim,
+                                     int32_t type, const void *q_weight, const void *k_weight, int32_t weight_type, float eps,
+                                     const int32_t *positions, const float *frequencies, int64_t pairs, int32_t neighbours, void *dq, void *dk,
+                                     void *dq_weight, void *dk_weight, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Causal attention over packed sequences.  q: [tokens][heads][dim], k, v: [tokens][kv_heads][dim]; query head h reads key head
+ * h / (heads / kv_heads).  offsets: int32 [sequences + 1], rising (pulled into 0 .. tokens): sequence s has the rows offsets[s] ..
+ * offsets[s + 1] - 1, none or more.  For a row i of it, over the rows j <= i of the same sequence:
+ *   z_j = scale * q_i . k_j, lse_i = log sum_j exp z_j, o_i = sum_j exp(z_j - lse_i) v_j
+ * lse: float [heads][tokens].  Rows in front of the first and behind the last sequence are not read; o and the gradients are 0 there and
+ * lse is -infinity.  rest, or NULL: what the rounding took from o, in its type; backward takes it for the sums that it needs o for (without it
+ * the gradients of short sequences are off by up to three times their own rounding).  o, rest, dq, dk, dv have no gaps.
+ * type: ONES_F16 or ONES_BF16; exponentials and the scores' gradients are rounded to it where a product takes them (in fp16 in units that
+ * keep them from its ends).  dim: 8 .. ONES_MAX_ATTENTION_DIM, a multiple of 8; bases multiples of 16 bytes, strides of 8 elements, between
+ * tokens at least dim and at most 2^20.  heads: a multiple of kv_heads.  scale: 1e-30 to 1e30.
+ * Backward: dout is the gradient of o; dk and dv are summed over the query heads of a key head.
+ * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size or stride above its limit; (tokens / 128 + sequences + 2) * (heads + kv_heads)
+ * of 2^24 or more), ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
+int ones_attention_forward(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride, int64_t k_head_stride,
+                           const void *v, int64_t v_stride, int64_t v_head_stride, int64_t tokens, int64_t heads, int64_t kv_heads,
+                           int64_t dim, int32_t type, const int32_t *offsets, int64_t sequences, float scale, void *o, void *rest,
+                           float *lse, void *hip_stream);
+size_t ones_attention_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim);
+int ones_attention_backward(const void *dout, int64_t do_stride, int64_t do_head_stride, const void *q, int64_t q_stride, int64_t q_head_stride,
+                            const void *k, int64_t k_stride, int64_t k_head_stride, const void *v, int64_t v_stride, int64_t v_head_stride,
+                            int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, const int32_t *offsets,
+                            int64_t sequences, float scale, const void *o, const void *rest, const float *lse, void *dq, void *dk, void *dv,
+                            void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* One more token of every sequence: its k and v [batch][kv_heads][dim] are written to place lengths[b] of the caches keys and values
+ * [batch][capacity][kv_heads][dim], and its q [batch][heads][dim] attends over places 0 .. lengths[b].  lengths: int32 [batch], as it is
+ * before the token; it is not changed.  Below 0: the sequence is left out, o is 0 and its cache stays; capacity or above: there is no room,
+ * o is NaN and its cache stays.  Places behind lengths[b] are not read.  o [batch][heads][dim] has no gaps.  type, dim, heads, scale, bases
+ * and strides as for ones_attention_forward (the caches' stride: between places; batch strides multiples of 8 elements).
+ * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size or stride, batch * heads above 2^22), ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
+size_t ones_attention_step_workspace_bytes(int64_t batch, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim);
+int ones_attention_step(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride, int64_t k_head_stride,
+                        const void *v, int64_t v_stride, int64_t v_head_stride, void *keys, int64_t keys_batch_stride, int64_t keys_stride,
+                        int64_t keys_head_stride, void *values, int64_t values_batch_stride, int64_t values_stride, int64_t values_head_stride,
+                        const int32_t *lengths, int64_t batch, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type,
+                        float scale, void *o, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Clipping of `tensors` gradients by their global norm, in place: norm = the root of the sum of all squares, summed in 64 bits; where
+ * norm + eps > limit every element is multiplied by limit / (norm + eps) and rounded.  A norm that is not finite changes nothing.
+ * gradients, counts, types: HOST arrays of the tensors' addresses (multiples of an element's size), their numbers of elements and their types (any); no two of
+ * them may overlap.  norm: float, one, on the device (infinity above the largest float).  limit: at least 0; infinity: only the norm.  eps >= 0.
+ * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (tensors, or an element count above 2^46), ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
+size_t ones_clip_gradients_workspace_bytes(int64_t tensors);
+int ones_clip_gradients(void *const *gradients, const int64_t *counts, const int32_t *types, int64_t tensors, float limit, float eps,
+                        float *norm, void *d_workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,571 @@
+// Causal attention over packed sequences, query heads in groups that share a key head, with its gradients (ones_attention_*).
+//
+//   z_ij = scale q_i . k_j for j <= i, lse_i = log sum_j exp z_ij, p_ij = exp(z_ij - lse_i), o_i = sum_j p_ij v_j
+//   delta_i = do_i . o_i, ds_ij = p_ij (do_i . v_j - delta_i)
+//   dv_j = sum_i p_ij do_i, dk_j = scale sum_i ds_ij q_i (both over the heads of a group, too), dq_i = scale sum_j ds_ij k_j
+#include "train_attention.h"
+#include "train_host.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+namespace ones {
+namespace train {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttentionArgs {
+  const void *q, *k, *v, *dout;
+  int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head, do_stride, do_head;      // elements
+  void *o, *rest;
+  float *lse;
+  void *dq, *dk, *dv;
+  float *delta, *dout_norm, *v_norm;          // delta, |do| of every row; the largest |do| and |v| of every slot (fp16)
+  const int32_t *offsets;
+  int32_t sequences, tokens, heads, kv_heads, dim;
+  float scale;
+};
+
+template <typename T>
+__device__ __forceinline__ const T *at(const void *p, int64_t row, int64_t stride, int32_t head, int64_t head_stride) {
+  return static_cast<const T *>(p) + row * stride + head * head_stride;
+}
+
+// fp16 keeps 2^-24 and up: the exponentials below the row's largest are held in units of 2^-8.
+template <typename T>
+constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;
+
+constexpr int kQueries = kAttentionRows, kKeys = 64;       // of a workgroup; of a step
+
+template <typename T, int D, bool REST>
+__global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs a) {
+  using Tile = RowTile<D, kKeys, 256>;
+  __shared__ __attribute__((aligned(256))) unsigned char lds[4 * Tile::bytes];
+  const Turn turn = turn_of(blockIdx.x, a.heads, a.kv_heads);
+  const int32_t last_slot = static_cast<int32_t>(slots_of(a.tokens, a.sequences, kQueries)) - 1;
+  const Rows rows = rows_of<kQueries>(a.offsets, a.sequences, a.tokens, last_slot - turn.slot);      // the longest tiles first
+  if (rows.at >= rows.length || rows.at < 0) return;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t out_stride = static_cast<int64_t>(a.heads) * a.dim;
+  const int32_t here = rows.first + rows.at, count = min(rows.length - rows.at, kQueries);
+  T *const o = const_cast<T *>(at<T>(a.o, here, out_stride, turn.head, a.dim)), *const rest = a.rest ? const_cast<T *>(at<T>(a.rest, here, out_stride, turn.head, a.dim)) : nullptr;
+  float *const lse = a.lse + static_cast<int64_t>(turn.head) * a.tokens + here;
+  if (!rows.real) {
+    write_zeros(o, out_stride, count, a.dim);
+    write_zeros(rest, out_stride, count, a.dim);
+    for (int i = threadIdx.x; i < count; i += 256) lse[i] = -INFINITY;
+    return;
+  }
+  Tile k, v;
+  k.start(at<T>(a.k, rows.first, a.k_stride, turn.kv, a.k_head), a.k_stride, rows.length, a.dim);
+  v.start(at<T>(a.v, rows.first, a.v_stride, turn.kv, a.v_head), a.v_stride, rows.length, a.dim);
+  k.load(lds);
+  v.load(lds + 2 * Tile::bytes);
+  const int mine = wave * 32;                 // the wave's first row in the tile
+  s16x8 q[2][D / 32];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+    read_rows<D>(at<T>(a.q, here + mine + n * 16, a.q_stride, turn.head, a.q_head), a.q_stride, count - mine - n * 16, a.dim, lane, q[n]);
+  int along[D / 32], across[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) along[s] = Tile::along(lane, s);
+#pragma unroll
+  for (int b = 0; b < D / 16; ++b) across[b] = Tile::across(lane, b);
+  const float c = a.scale * kLog2e;
+  f32x4 acc[D / 16][2], total[2];             // total: the rounded exponentials' sums, by a product with ones
+  float top[2], sum[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    top[n] = -INFINITY;
+    sum[n] = 0.f;
+    total[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) acc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  Pack<T, 8> one;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) one.v[i] = static_cast<T>(1.f);
+  const s16x8 ones = __builtin_bit_cast(s16x8, one);
+  const int steps = (rows.at + count + kKeys - 1) / kKeys, first_row = rows.at + mine;
+  for (int step = 0; step < steps; ++step) {
+    meet<0>();
+    const unsigned char *ks = lds + (step & 1) * Tile::bytes, *vs = ks + 2 * Tile::bytes;
+    if (step + 1 < steps) {
+      k.load(lds + (~step & 1) * Tile::bytes);
+      v.load(lds + (2 + (~step & 1)) * Tile::bytes);
+    }
+    const int key = step * kKeys;
+    if (key > first_row + 31) continue;       // keys behind all of the wave's rows
+    f32x4 z[4][2];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) z[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        const s16x8 f = Tile::read_along(ks, b * 16, along[s]);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) z[b][n] = mfma<T>(f, q[n][s], z[b][n]);
+      }
+    }
+    if (key + kKeys - 1 > first_row) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int row = first_row + n * 16 + (lane & 15) - key;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (b * 16 + (lane >> 4) * 4 + r > row) z[b][n][r] = -INFINITY;
+      }
+    }
+    s16x8 p[2][2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      float most = z[0][n][0];
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) most = fmaxf(most, z[b][n][r]);
+      most = fmaxf(top[n], across_max(most));
+      if (__any(most > top[n])) {
+        const float factor = most == top[n] ? 1.f : __builtin_amdgcn_exp2f((top[n] - most) * c);
+        sum[n] *= factor;
+        total[n] *= factor;
+#pragma unroll
+        for (int b = 0; b < D / 16; ++b) acc[b][n] *= factor;
+        top[n] = most;
+      }
+      const float base = (top[n] == -INFINITY ? 0.f : top[n] * c) - kShift<T>;
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          z[b][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][n][r], c, -base));
+          sum[n] += z[b][n][r];
+        }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) p[h][n] = rounded<T>(z[2 * h][n], z[2 * h + 1][n]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int b = 0; b < D / 16; ++b) {
+        const s16x8 f = Tile::read_across(vs, h * 32, across[b]);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) acc[b][n] = mfma<T>(f, p[h][n], acc[b][n]);
+      }
+      if constexpr (REST) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) total[n] = mfma<T>(ones, p[h][n], total[n]);
+      }
+    }
+  }
+  float factor[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const float s = across_sum(sum[n]);
+    factor[n] = 1.f / (REST ? total[n][0] : s);
+    const int r = mine + n * 16 + (lane & 15);
+    if (lane < 16 && r < count) lse[r] = (top[n] * c - kShift<T> + __builtin_amdgcn_logf(s)) * kLn2;
+  }
+  write_rows<T, D, 2, REST>(acc, factor, o + mine * out_stride, rest ? rest + mine * out_stride : nullptr, out_stride, count - mine, a.dim, lane);
+}
+
+// delta of every row of a slot and head, and its |do|; of a key head, the largest |v|.  (fp16 scales by the norms, see unit_of().)
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
+  constexpr int lanes = D / 8, at_once = 256 / lanes;
+  constexpr bool norms = __is_same(T, f16);
+  __shared__ float part[4];
+  const int32_t all = a.heads + (norms ? a.kv_heads : 0);
+  const int32_t slot = blockIdx.x / all, head = blockIdx.x % all;
+  const Rows rows = rows_of<kQueries>(a.offsets, a.sequences, a.tokens, slot);
+  if (rows.at >= rows.length || rows.at < 0 || !rows.real) return;
+  const int32_t here = rows.first + rows.at, count = min(rows.length - rows.at, kQueries);
+  const int p = threadIdx.x % lanes, r0 = threadIdx.x / lanes;
+  const bool inside = p * 8 < a.dim;
+  float most = 0.f;
+  if (head < a.heads) {
+    const int64_t stride = static_cast<int64_t>(a.heads) * a.dim;
+    const T *g = at<T>(a.dout, here, a.do_stride, head, a.do_head) + p * 8, *o = at<T>(a.o, here, stride, head, a.dim) + p * 8;
+    const T *rest = a.rest ? at<T>(a.rest, here, stride, head, a.dim) + p * 8 : nullptr;
+    for (int r = r0; r < (count + at_once - 1) / at_once * at_once; r += at_once) {
+      float dot = 0.f, square = 0.f;
+      if (inside && r < count) {
+        const Pack<T, 8> x = *reinterpret_cast<const Pack<T, 8> *>(g + r * a.do_stride), y = *reinterpret_cast<const Pack<T, 8> *>(o + r * stride);
+        Pack<T, 8> z{};
+        if (rest) z = *reinterpret_cast<const Pack<T, 8> *>(rest + r * stride);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float d = static_cast<float>(x.v[i]);
+          dot = __builtin_fmaf(d, static_cast<float>(y.v[i]) + static_cast<float>(z.v[i]), dot);
+          square = __builtin_fmaf(d, d, square);
+        }
+      }
+#pragma unroll
+      for (int m = 1; m < lanes; m *= 2) { dot += __shfl_xor(dot, m); square += __shfl_xor(square, m); }
+      if (p == 0 && r < count) a.delta[static_cast<int64_t>(head) * a.tokens + here + r] = dot;
+      if (norms && square < INFINITY) most = fmaxf(most, square);
+      if (norms && p == 0 && r < count) a.dout_norm[static_cast<int64_t>(head) * a.tokens + here + r] = square < INFINITY ? sqrtf(square) : 0.f;
+    }
+    if (!norms) return;
+  } else {
+    const T *v = at<T>(a.v, here, a.v_stride, head - a.heads, a.v_head) + p * 8;
+    for (int r = r0; r < (count + at_once - 1) / at_once * at_once; r += at_once) {
+      float square = 0.f;
+      if (inside && r < count) {
+        const Pack<T, 8> x = *reinterpret_cast<const Pack<T, 8> *>(v + r * a.v_stride);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { const float d = static_cast<float>(x.v[i]); square = __builtin_fmaf(d, d, square); }
+      }
+#pragma unroll
+      for (int m = 1; m < lanes; m *= 2) square += __shfl_xor(square, m);
+      if (square < INFINITY) most = fmaxf(most, square);
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < kWave; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    most = sqrtf(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
+    a.v_norm[static_cast<int64_t>(slot) * all + head] = most;      // of do's heads as well
+  }
+}
+
+// The unit that ds is held in where it is rounded to fp16: a power of two that brings |ds| <= 2 |do| |v| to at most 2^14.  (bf16 has the
+// exponents of 32 bits: 1.)
+__device__ __forceinline__ float unit_of(float bound) {
+  if (!(bound > 0.f) || !(bound < INFINITY)) return 1.f;
+  int e;
+  frexpf(bound, &e);                          // bound < 2^e
+  return ldexpf(1.f, min(max(13 - e, -100), 100));
+}
+// The largest of the norms that the slots of a sequence have for `heads` heads from `head` on.
+__device__ __forceinline__ float largest_norm(const float *norms, int32_t all, int32_t head, int32_t heads, int32_t slot, int32_t slots) {
+  float most = 0.f;
+  const int lane = threadIdx.x % kWave;
+  for (int32_t i = lane; i < slots * heads; i += kWave) most = fmaxf(most, norms[static_cast<int64_t>(slot + i / heads) * all + head + i % heads]);
+#pragma unroll
+  for (int m = 1; m < kWave; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+  return most;
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint32_t id, unsigned char *lds) {
+  using Tile = RowTile<D, kKeys, 256>;
+  const Turn turn = turn_of(id, a.heads, a.kv_heads);
+  const int32_t slot = static_cast<int32_t>(slots_of(a.tokens, a.sequences, kQueries)) - 1 - turn.slot;
+  const Rows rows = rows_of<kQueries>(a.offsets, a.sequences, a.tokens, slot);
+  if (rows.at >= rows.length || rows.at < 0) return;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t out_stride = static_cast<int64_t>(a.heads) * a.dim;
+  const int32_t here = rows.first + rows.at, count = min(rows.length - rows.at, kQueries);
+  T *const dq = const_cast<T *>(at<T>(a.dq, here, out_stride, turn.head, a.dim));
+  if (!rows.real) return write_zeros(dq, out_stride, count, a.dim);
+  Tile k, v;
+  k.start(at<T>(a.k, rows.first, a.k_stride, turn.kv, a.k_head), a.k_stride, rows.length, a.dim);
+  v.start(at<T>(a.v, rows.first, a.v_stride, turn.kv, a.v_head), a.v_stride, rows.length, a.dim);
+  k.load(lds);
+  v.load(lds + 2 * Tile::bytes);
+  const int mine = wave * 32;
+  const float c = a.scale * kLog2e;
+  float v_most = 0.f;
+  if constexpr (__is_same(T, f16)) {
+    const int32_t all = a.heads + a.kv_heads;
+    v_most = largest_norm(a.v_norm, all, a.heads + turn.kv, 1, slot - rows.at / kQueries, (rows.length + kQueries - 1) / kQueries);
+  }
+  s16x8 q[2][D / 32], g[2][D / 32];
+  float lse[2], delta[2], unit[2], factor[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int r = mine + n * 16;
+    read_rows<D>(at<T>(a.q, here + r, a.q_stride, turn.head, a.q_head), a.q_stride, count - r, a.dim, lane, q[n]);
+    read_rows<D>(at<T>(a.dout, here + r, a.do_stride, turn.head, a.do_head), a.do_stride, count - r, a.dim, lane, g[n]);
+    const int64_t i = static_cast<int64_t>(turn.head) * a.tokens + here + min(r + (lane & 15), count - 1);
+    lse[n] = a.lse[i] * kLog2e;
+    delta[n] = a.delta[i];
+    unit[n] = 1.f;
+    if constexpr (__is_same(T, f16)) unit[n] = unit_of(2.f * a.dout_norm[i] * v_most);
+    factor[n] = a.scale / unit[n];
+  }
+  int along[D / 32], across[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) along[s] = Tile::along(lane, s);
+#pragma unroll
+  for (int b = 0; b < D / 16; ++b) across[b] = Tile::across(lane, b);
+  f32x4 acc[D / 16][2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) acc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int steps = (rows.at + count + kKeys - 1) / kKeys, first_row = rows.at + mine;
+  for (int step = 0; step < steps; ++step) {
+    meet<0>();
+    const unsigned char *ks = lds + (step & 1) * Tile::bytes, *vs = ks + 2 * Tile::bytes;
+    if (step + 1 < steps) {
+      k.load(lds + (~step & 1) * Tile::bytes);
+      v.load(lds + (2 + (~step & 1)) * Tile::bytes);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int key = step * kKeys + h * 32;
+      if (key > first_row + 31) break;
+      f32x4 z[2][2], d[2][2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) z[b][n] = d[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+          const s16x8 f = Tile::read_along(ks, h * 32 + b * 16, along[s]), e = Tile::read_along(vs, h * 32 + b * 16, along[s]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            z[b][n] = mfma<T>(f, q[n][s], z[b][n]);
+            d[b][n] = mfma<T>(e, g[n][s], d[b][n]);
+          }
+        }
+      }
+      s16x8 ds[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int row = first_row + n * 16 + (lane & 15) - key;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][n][r], c, -lse[n]));
+            const float s = p * (d[b][n][r] - delta[n]) * unit[n];
+            z[b][n][r] = b * 16 + (lane >> 4) * 4 + r > row ? 0.f : s;
+          }
+        ds[n] = rounded<T>(z[0][n], z[1][n]);
+      }
+#pragma unroll
+      for (int b = 0; b < D / 16; ++b) {
+        const s16x8 f = Tile::read_across(ks, h * 32, across[b]);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) acc[b][n] = mfma<T>(f, ds[n], acc[b][n]);
+      }
+    }
+  }
+  write_rows<T, D, 2>(acc, factor, dq + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+}
+
+constexpr int kStepRows = 32;                 // queries of a step of the keys' gradients
+
+template <typename T, int D>
+__device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_t id, unsigned char *lds) {
+  using Tile = RowTile<D, kStepRows, 256>;
+  const int32_t slot = static_cast<int32_t>(id / a.kv_heads), kv = static_cast<int32_t>(id % a.kv_heads), group = a.heads / a.kv_heads;
+  const Rows rows = rows_of<kQueries>(a.offsets, a.sequences, a.tokens, slot);
+  if (rows.at >= rows.length || rows.at < 0) return;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t out_stride = static_cast<int64_t>(a.kv_heads) * a.dim;
+  const int32_t here = rows.first + rows.at, count = min(rows.length - rows.at, kQueries);
+  T *const dk = const_cast<T *>(at<T>(a.dk, here, out_stride, kv, a.dim)), *const dv = const_cast<T *>(at<T>(a.dv, here, out_stride, kv, a.dim));
+  if (!rows.real) {
+    write_zeros(dk, out_stride, count, a.dim);
+    write_zeros(dv, out_stride, count, a.dim);
+    return;
+  }
+  const int mine = wave * 32;
+  const float c = a.scale * kLog2e;
+  float unit = 1.f;
+  if constexpr (__is_same(T, f16)) {
+    const int32_t all = a.heads + a.kv_heads, first = slot - rows.at / kQueries, slots = (rows.length + kQueries - 1) / kQueries;
+    unit = unit_of(2.f * largest_norm(a.v_norm, all, kv * group, group, first, slots) * largest_norm(a.v_norm, all, a.heads + kv, 1, first, slots));
+  }
+  constexpr float kWeights = __is_same(T, f16) ? 16384.f : 1.f;       // the unit of p, at most 1 and a rounding
+  s16x8 k[2][D / 32], v[2][D / 32];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int r = mine + n * 16;
+    read_rows<D>(at<T>(a.k, here + r, a.k_stride, kv, a.k_head), a.k_stride, count - r, a.dim, lane, k[n]);
+    read_rows<D>(at<T>(a.v, here + r, a.v_stride, kv, a.v_head), a.v_stride, count - r, a.dim, lane, v[n]);
+  }
+  int along[D / 32], across[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) along[s] = Tile::along(lane, s);
+#pragma unroll
+  for (int b = 0; b < D / 16; ++b) across[b] = Tile::across(lane, b);
+  f32x4 of_k[D / 16][2], of_v[D / 16][2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) of_k[b][n] = of_v[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // the queries from the tile's first key on, head after head
+  const int steps = (rows.length - rows.at + kStepRows - 1) / kStepRows, all_steps = steps * group;
+  Tile q, g;
+  auto begin = [&](int head) {
+    q.start(at<T>(a.q, here, a.q_stride, kv * group + head, a.q_head), a.q_stride, rows.length - rows.at, a.dim);
+    g.start(at<T>(a.dout, here, a.do_stride, kv * group + head, a.do_head), a.do_stride, rows.length - rows.at, a.dim);
+  };
+  begin(0);
+  q.load(lds);
+  g.load(lds + 2 * Tile::bytes);
+  int head = 0, step = 0;
+  for (int t = 0; t < all_steps; ++t) {
+    meet<0>();
+    const unsigned char *qs = lds + (t & 1) * Tile::bytes, *gs = qs + 2 * Tile::bytes;
+    const int this_head = kv * group + head, first = step * kStepRows;       // from the tile's first key on
+    if (++step == steps) {
+      step = 0;
+      if (++head < group) begin(head);
+    }
+    if (t + 1 < all_steps) {
+      q.load(lds + (~t & 1) * Tile::bytes);
+      g.load(lds + (2 + (~t & 1)) * Tile::bytes);
+    }
+    if (first + kStepRows - 1 < mine) continue;                              // queries in front of all of the wave's keys
+    f32x4 z[2][2], d[2][2];
+    const int64_t row0 = static_cast<int64_t>(this_head) * a.tokens + here;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) z[b][n] = d[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        const s16x8 f = Tile::read_along(qs, b * 16, along[s]), e = Tile::read_along(gs, b * 16, along[s]);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          z[b][n] = mfma<T>(f, k[n][s], z[b][n]);
+          d[b][n] = mfma<T>(e, v[n][s], d[b][n]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = first + b * 16 + (lane >> 4) * 4 + r;
+        const int64_t j = row0 + min(i, rows.length - rows.at - 1);
+        const float lse = a.lse[j] * kLog2e, delta = a.delta[j];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const bool live = i >= mine + n * 16 + (lane & 15) && i < rows.length - rows.at;
+          const float p = live ? __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][n][r], c, -lse)) : 0.f;
+          z[b][n][r] = p * kWeights;
+          d[b][n][r] = live ? p * (d[b][n][r] - delta) * unit : 0.f;
+        }
+      }
+    }
+    s16x8 p[2], ds[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      p[n] = rounded<T>(z[0][n], z[1][n]);
+      ds[n] = rounded<T>(d[0][n], d[1][n]);
+    }
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) {
+      const s16x8 f = Tile::read_across(gs, 0, across[b]), e = Tile::read_across(qs, 0, across[b]);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        of_v[b][n] = mfma<T>(f, p[n], of_v[b][n]);
+        of_k[b][n] = mfma<T>(e, ds[n], of_k[b][n]);
+      }
+    }
+  }
+  const float k_factor[2] = {a.scale / unit, a.scale / unit}, v_factor[2] = {1.f / kWeights, 1.f / kWeights};
+  write_rows<T, D, 2>(of_k, k_factor, dk + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+  write_rows<T, D, 2>(of_v, v_factor, dv + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a) {
+  __shared__ __attribute__((aligned(256))) unsigned char lds[4 * RowTile<D, kKeys, 256>::bytes];
+  gradient_of_queries<T, D>(a, blockIdx.x, lds);
+}
+template <typename T, int D>
+__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionArgs a) {
+  __shared__ __attribute__((aligned(256))) unsigned char lds[4 * RowTile<D, kStepRows, 256>::bytes];
+  gradient_of_keys<T, D>(a, blockIdx.x, lds);
+}
+
+template <typename T, int D>
+void launch_forward(const AttentionArgs &a, hipStream_t s) {
+  const dim3 grid(static_cast<uint32_t>(slots_of(a.tokens, a.sequences, kQueries) * a.heads)), block(256);
+  if (a.rest) hipLaunchKernelGGL((attention_forward_kernel<T, D, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attention_forward_kernel<T, D, false>), grid, block, 0, s, a);
+}
+template <typename T, int D>
+void launch_backward(const AttentionArgs &a, hipStream_t s) {
+  const int64_t slots = slots_of(a.tokens, a.sequences, kQueries), all = a.heads + (__is_same(T, f16) ? a.kv_heads : 0);
+  hipLaunchKernelGGL((attention_delta_kernel<T, D>), dim3(static_cast<uint32_t>(slots * all)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.kv_heads)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((attention_dq_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.heads)), dim3(256), 0, s, a);
+}
+template <typename T>
+void launch(const AttentionArgs &a, bool backward, hipStream_t s) {
+  if (a.dim <= 64) backward ? launch_backward<T, 64>(a, s) : launch_forward<T, 64>(a, s);
+  else backward ? launch_backward<T, 128>(a, s) : launch_forward<T, 128>(a, s);
+}
+void launch_type(const AttentionArgs &a, int32_t type, bool backward, hipStream_t s) {
+  if (type == ONES_F16) launch<f16>(a, backward, s);
+  else launch<bf16>(a, backward, s);
+}
+
+}  // namespace
+}  // namespace train
+}  // namespace ones
+
+using namespace ones::train;
+
+extern "C" {
+
+int ones_attention_forward(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride, int64_t k_head_stride,
+                           const void *v, int64_t v_stride, int64_t v_head_stride, int64_t tokens, int64_t heads, int64_t kv_heads,
+                           int64_t dim, int32_t type, const int32_t *offsets, int64_t sequences, float scale, void *o, void *rest,
+                           float *lse, void *hip_stream) {
+  if (int rc = check_attention(tokens, heads, kv_heads, dim, type, sequences, scale)) return rc;
+  if (tokens == 0) return ONES_OK;
+  if (int rc = check_head_rows(q, q_stride, q_head_stride, heads, dim)) return rc;
+  if (int rc = check_head_rows(k, k_stride, k_head_stride, kv_heads, dim)) return rc;
+  if (int rc = check_head_rows(v, v_stride, v_head_stride, kv_heads, dim)) return rc;
+  if (!offsets || !o || !lse || !aligned(o, 16) || !aligned(rest, 16)) return ONES_E_INVALID_ARG;
+  AttentionArgs a{};
+  a.q = q; a.k = k; a.v = v;
+  a.q_stride = q_stride; a.q_head = q_head_stride; a.k_stride = k_stride; a.k_head = k_head_stride; a.v_stride = v_stride; a.v_head = v_head_stride;
+  a.o = o; a.rest = rest; a.lse = lse; a.offsets = offsets;
+  a.sequences = static_cast<int32_t>(sequences); a.tokens = static_cast<int32_t>(tokens); a.heads = static_cast<int32_t>(heads);
+  a.kv_heads = static_cast<int32_t>(kv_heads); a.dim = static_cast<int32_t>(dim); a.scale = scale;
+  launch_type(a, type, false, static_cast<hipStream_t>(hip_stream));
+  return launched("attention forward");
+}
+
+size_t ones_attention_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim) {
+  if (check_attention(tokens, heads, kv_heads, dim, ONES_F16, sequences, 1.f)) return 0;
+  return attention_plan(tokens, sequences, heads, kv_heads).bytes;
+}
+
+int ones_attention_backward(const void *dout, int64_t do_stride, int64_t do_head_stride, const void *q, int64_t q_stride, int64_t q_head_stride,
+                            const void *k, int64_t k_stride, int64_t k_head_stride, const void *v, int64_t v_stride, int64_t v_head_stride,
+                            int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, const int32_t *offsets,
+                            int64_t sequences, float scale, const void *o, const void *rest, const float *lse, void *dq, void *dk, void *dv,
+                            void *d_workspace, size_t workspace_bytes, void *hip_stream) {
+  if (int rc = check_attention(tokens, heads, kv_heads, dim, type, sequences, scale)) return rc;
+  if (tokens == 0) return ONES_OK;
+  if (int rc = check_head_rows(dout, do_stride, do_head_stride, heads, dim)) return rc;
+  if (int rc = check_head_rows(q, q_stride, q_head_stride, heads, dim)) return rc;
+  if (int rc = check_head_rows(k, k_stride, k_head_stride, kv_heads, dim)) return rc;
+  if (int rc = check_head_rows(v, v_stride, v_head_stride, kv_heads, dim)) return rc;
+  if (!offsets || !o || !lse || !dq || !dk || !dv) return ONES_E_INVALID_ARG;
+  if (!aligned(o, 16) || !aligned(rest, 16) || !aligned(dq, 16) || !aligned(dk, 16) || !aligned(dv, 16)) return ONES_E_INVALID_ARG;
+  const AttentionPlan plan = attention_plan(tokens, sequences, heads, kv_heads);
+  if (int rc = check_workspace(d_workspace, workspace_bytes, plan.bytes)) return rc;
+  AttentionArgs a{};
+  a.dout = dout; a.q = q; a.k = k; a.v = v;
+  a.do_stride = do_stride; a.do_head = do_head_stride;
+  a.q_stride = q_stride; a.q_head = q_head_stride; a.k_stride = k_stride; a.k_head = k_head_stride; a.v_stride = v_stride; a.v_head = v_head_stride;
+  a.o = const_cast<void *>(o); a.rest = const_cast<void *>(rest); a.lse = const_cast<float *>(lse); a.offsets = offsets;
+  a.dq = dq; a.dk = dk; a.dv = dv;
+  unsigned char *const w = static_cast<unsigned char *>(d_workspace);
+  a.delta = reinterpret_cast<float *>(w + plan.delta);
+  a.dout_norm = reinterpret_cast<float *>(w + plan.dout_norm);
+  a.v_norm = reinterpret_cast<float *>(w + plan.slot_norms);
+  a.sequences = static_cast<int32_t>(sequences); a.tokens = static_cast<int32_t>(tokens); a.heads = static_cast<int32_t>(heads);
+  a.kv_heads = static_cast<int32_t>(kv_heads); a.dim = static_cast<int32_t>(dim); a.scale = scale;
+  launch_type(a, type, true, static_cast<hipStream_t>(hip_stream));
+  return launched("attention backward");
+}
+
+}  // extern "C"

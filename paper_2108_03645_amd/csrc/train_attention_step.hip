@@ -1,0 +1,305 @@
+// One more token of every sequence over its cache (ones_attention_step).
+//
+//   o = sum_{j <= n} p_j v_j, p = softmax(scale q . k_j), n the place of the new token
+//
+// A workgroup takes a part of one sequence's cache for up to 16 query heads of one key head, which are the columns of the products; its waves
+// take tiles of 32 keys in turn, each by itself: the tiles come to the wave's own place in LDS by direct loads, the next while the present one is worked
+// on.  The sums of the waves, then those of the parts, are joined at the end.  The new token's key and value are
+// arguments; the wave that begins the cache begins with them, and the same workgroup writes them to the cache.
+#include "train_attention.h"
+#include "train_host.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+namespace ones {
+namespace train {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct StepArgs {
+  const void *q, *k, *v;
+  void *keys, *values, *o;
+  int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head;
+  int64_t keys_batch, keys_stride, keys_head, values_batch, values_stride, values_head;
+  const int32_t *lengths;
+  float *tops, *sums, *outputs;               // of the parts: [batch][heads][splits], outputs with dim
+  int32_t batch, capacity, heads, kv_heads, dim, blocks_of_heads, splits;
+  float scale;
+};
+
+template <typename T>
+constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;      // as in train_attention.hip
+
+// A wave's tile of 32 rows: like RowTile, but a load of the wave fills fewer than 16 rows, so that the exchange differs from load to load.
+template <int D>
+struct WaveTile {
+  using Tile = RowTile<D, 32, 256>;           // places of the reads
+  static constexpr int bytes = Tile::bytes, pieces = D / 8, at_once = kWave / pieces, loads = 32 / at_once, kinds = at_once < 8 ? 4 : 1;
+  static_assert(at_once == 4 || at_once == 8);
+  uint32_t row_bytes, offset[kinds];
+  __device__ __forceinline__ void start(int64_t stride, int32_t dim, int lane) {
+    row_bytes = static_cast<uint32_t>(stride * 2);
+#pragma unroll
+    for (int i = 0; i < kinds; ++i) {
+      const int r = lane / pieces + i * at_once, p = (lane % pieces) ^ Tile::exchange(r);
+      offset[i] = p * 8 < dim ? r * row_bytes + p * 16 : Tile::kOutside;
+    }
+  }
+  // Rows of which `left` are there.
+  __device__ __forceinline__ void load(const unsigned char *base, int32_t left, unsigned char *to) const {
+    const uint32_t mine = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LdsBytes *)to)));
+    const uint32_t inside = static_cast<uint32_t>(max(min(left, 32), 0)) * row_bytes;
+#pragma unroll
+    for (int i = 0; i < loads; ++i)
+      load_to_lds(base, inside, offset[i % kinds] + (i / kinds) * kinds * at_once * row_bytes, mine + i * kWave * 16);
+  }
+};
+
+template <int PENDING>
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PENDING) : "memory");
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
+  using Load = WaveTile<D>;
+  using Tile = typename Load::Tile;
+  constexpr int waves = kStepWaves;
+  __shared__ __attribute__((aligned(256))) unsigned char lds[waves * 4 * Load::bytes];
+  __shared__ float tops[waves][16], sums[waves][16];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+  // key heads of a sequence follow each other, then the parts
+  uint32_t id = blockIdx.x;
+  const int32_t kv = id % a.kv_heads;
+  id /= a.kv_heads;
+  const int32_t of = id % a.blocks_of_heads;
+  id /= a.blocks_of_heads;
+  const int32_t split = id % a.splits, b = id / a.splits;
+  const int32_t group = a.heads / a.kv_heads, head = kv * group + of * 16, heads = min(group - of * 16, 16);
+  const int32_t length = a.lengths[b];
+  const int64_t part0 = (static_cast<int64_t>(b) * a.heads + head) * a.splits + split;      // of the first head; `splits` apart
+  T *const out = static_cast<T *>(a.o) + (static_cast<int64_t>(b) * a.heads + head) * a.dim;
+  if (length < 0 || length >= a.capacity) {
+    const float fill = length < 0 ? 0.f : NAN;
+    if (split == 0)
+      for (int i = threadIdx.x; i < heads * a.dim; i += 256) out[i] = static_cast<T>(fill);
+    return;
+  }
+  // whole tiles of the workgroup, evenly over the parts
+  const int32_t all = (length + kStepKeys * waves - 1) / (kStepKeys * waves);
+  const int32_t begin = static_cast<int32_t>(static_cast<int64_t>(all) * split / a.splits), end = static_cast<int32_t>(static_cast<int64_t>(all) * (split + 1) / a.splits);
+  if (begin == end && split) {
+    if (threadIdx.x < heads) a.tops[part0 + threadIdx.x * a.splits] = -INFINITY;
+    return;
+  }
+  const T *const k_new = static_cast<const T *>(a.k) + b * a.k_stride + kv * a.k_head, *const v_new = static_cast<const T *>(a.v) + b * a.v_stride + kv * a.v_head;
+  const unsigned char *ks = reinterpret_cast<const unsigned char *>(static_cast<const T *>(a.keys) + b * a.keys_batch + kv * a.keys_head);
+  const unsigned char *vs = reinterpret_cast<const unsigned char *>(static_cast<const T *>(a.values) + b * a.values_batch + kv * a.values_head);
+  Load k, v;
+  k.start(a.keys_stride, a.dim, lane);
+  v.start(a.values_stride, a.dim, lane);
+  unsigned char *const mine = lds + wave * 4 * Load::bytes;
+  auto load = [&](int32_t tile, int to) {     // the wave's tile of the workgroup's `tile`
+    const int32_t first = (tile * waves + wave) * kStepKeys;
+    k.load(ks + static_cast<int64_t>(first) * k.row_bytes, length - first, mine + to * 2 * Load::bytes);
+    v.load(vs + static_cast<int64_t>(first) * v.row_bytes, length - first, mine + to * 2 * Load::bytes + Load::bytes);
+  };
+  s16x8 q[D / 32];
+  read_rows<D>(static_cast<const T *>(a.q) + b * a.q_stride + head * a.q_head, a.q_head, heads, a.dim, lane, q);
+  const float c = a.scale * kLog2e;
+  f32x4 acc[D / 16];
+  float top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (split == 0 && wave == 0) {              // the new token: row 0 of a product, weight 1
+    s16x8 f[D / 32];
+    read_rows<D>(k_new, 0, 1, a.dim, lane, f);
+    f32x4 z{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) z = mfma<T>(f[s], q[s], z);
+    top = __shfl(z[0], lane & 15);
+    const float weight = top == -INFINITY ? 0.f : top - top == 0.f ? __builtin_amdgcn_exp2f(kShift<T>) : NAN;
+    if (lane < 16) sum = weight;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = i * 16 + (lane >> 4) * 4 + r;
+        acc[i][r] = d < a.dim && weight != 0.f ? static_cast<float>(v_new[d]) * weight : 0.f;
+      }
+  }
+  if (split == 0 && of == 0 && threadIdx.x < 2 * (D / 8)) {
+    const int which = threadIdx.x / (D / 8), d = threadIdx.x % (D / 8) * 8;
+    T *to = which ? static_cast<T *>(a.values) + b * a.values_batch + length * a.values_stride + kv * a.values_head
+                  : static_cast<T *>(a.keys) + b * a.keys_batch + length * a.keys_stride + kv * a.keys_head;
+    if (d < a.dim) *reinterpret_cast<Pack<uint32_t, 4> *>(to + d) = *reinterpret_cast<const Pack<uint32_t, 4> *>((which ? v_new : k_new) + d);
+  }
+  if (begin < end) load(begin, 0);
+  int along[D / 32], across[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) along[s] = Tile::along(lane, s);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) across[i] = Tile::across(lane, i);
+  for (int32_t tile = begin; tile < end; ++tile) {
+    const int now = (tile - begin) & 1;
+    if (tile + 1 < end) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // its place has been read
+      load(tile + 1, now ^ 1);
+      arrived<2 * Load::loads>();
+    } else {
+      arrived<0>();
+    }
+    const int32_t left = length - (tile * waves + wave) * kStepKeys;
+    if (left <= 0) continue;
+    const unsigned char *kt = mine + now * 2 * Load::bytes, *vt = kt + Load::bytes;
+    f32x4 z[2];
+    float most = top;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      z[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) z[i] = mfma<T>(Tile::read_along(kt, i * 16, along[s]), q[s], z[i]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (i * 16 + (lane >> 4) * 4 + r >= left) z[i][r] = -INFINITY;
+        most = fmaxf(most, z[i][r]);
+      }
+    }
+    most = across_max(most);
+    if (__any(most > top)) {
+      const float factor = most == top ? 1.f : __builtin_amdgcn_exp2f((top - most) * c);
+      sum *= factor;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) acc[i] *= factor;
+      top = most;
+    }
+    const float base = (top == -INFINITY ? 0.f : top * c) - kShift<T>;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        z[i][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][r], c, -base));
+        sum += z[i][r];
+      }
+    const s16x8 p = rounded<T>(z[0], z[1]);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) acc[i] = mfma<T>(Tile::read_across(vt, 0, across[i]), p, acc[i]);
+  }
+  sum = across_sum(sum);
+  __syncthreads();                            // the tiles' places take the sums
+  float *const parts = reinterpret_cast<float *>(lds);        // [wave][head][D]
+  if (lane < 16) {
+    tops[wave][lane] = top;
+    sums[wave][lane] = sum;
+  }
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+    *reinterpret_cast<f32x4 *>(parts + ((wave * 16 + (lane & 15)) * D + i * 16 + (lane >> 4) * 4)) = acc[i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < heads * D; i += 256) {
+    const int h = i / D, d = i % D;
+    float most = tops[0][h];
+#pragma unroll
+    for (int w = 1; w < waves; ++w) most = fmaxf(most, tops[w][h]);
+    float all_sum = 0.f, x = 0.f;
+#pragma unroll
+    for (int w = 0; w < waves; ++w) {
+      const float f = tops[w][h] == most ? 1.f : __builtin_amdgcn_exp2f((tops[w][h] - most) * c);
+      all_sum += sums[w][h] * f;
+      x += parts[(w * 16 + h) * D + d] * f;
+    }
+    if (d >= a.dim) continue;
+    if (a.splits == 1) out[h * a.dim + d] = static_cast<T>(x / all_sum);
+    else {
+      const int64_t at = part0 + static_cast<int64_t>(h) * a.splits;
+      a.outputs[at * a.dim + d] = x;
+      if (d == 0) { a.tops[at] = most; a.sums[at] = all_sum; }
+    }
+  }
+}
+
+// The parts of a head, in order.
+template <typename T>
+__global__ __launch_bounds__(128) void step_join_kernel(StepArgs a) {
+  const int32_t b = blockIdx.x / a.heads;
+  const int32_t length = a.lengths[b];
+  if (length < 0 || length >= a.capacity || static_cast<int>(threadIdx.x) >= a.dim) return;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * a.splits;
+  float most = a.tops[at];
+  for (int i = 1; i < a.splits; ++i) most = fmaxf(most, a.tops[at + i]);
+  float sum = 0.f, x = 0.f;
+  for (int i = 0; i < a.splits; ++i) {
+    const float top = a.tops[at + i];
+    if (i && top == -INFINITY) continue;      // none
+    const float f = top == most ? 1.f : __builtin_amdgcn_exp2f((top - most) * (a.scale * kLog2e));
+    sum += a.sums[at + i] * f;
+    x += a.outputs[(at + i) * a.dim + threadIdx.x] * f;
+  }
+  static_cast<T *>(a.o)[static_cast<int64_t>(blockIdx.x) * a.dim + threadIdx.x] = static_cast<T>(x / sum);
+}
+
+template <typename T>
+void launch(const StepArgs &a, hipStream_t s) {
+  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.batch) * a.splits * a.blocks_of_heads * a.kv_heads)), block(256);
+  if (a.dim <= 64) hipLaunchKernelGGL((step_kernel<T, 64>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((step_kernel<T, 128>), grid, block, 0, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((step_join_kernel<T>), dim3(static_cast<uint32_t>(a.batch * a.heads)), dim3(128), 0, s, a);
+}
+
+}  // namespace
+}  // namespace train
+}  // namespace ones
+
+using namespace ones::train;
+
+extern "C" {
+
+size_t ones_attention_step_workspace_bytes(int64_t batch, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim) {
+  if (check_step(batch, capacity, heads, kv_heads, dim, ONES_F16, 1.f)) return 0;
+  return step_plan(batch, capacity, heads, kv_heads, dim).bytes;
+}
+
+int ones_attention_step(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride, int64_t k_head_stride,
+                        const void *v, int64_t v_stride, int64_t v_head_stride, void *keys, int64_t keys_batch_stride, int64_t keys_stride,
+                        int64_t keys_head_stride, void *values, int64_t values_batch_stride, int64_t values_stride, int64_t values_head_stride,
+                        const int32_t *lengths, int64_t batch, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type,
+                        float scale, void *o, void *d_workspace, size_t workspace_bytes, void *hip_stream) {
+  if (int rc = check_step(batch, capacity, heads, kv_heads, dim, type, scale)) return rc;
+  if (batch == 0) return ONES_OK;
+  if (int rc = check_token_rows(q, q_stride, q_head_stride, batch, heads)) return rc;
+  if (int rc = check_token_rows(k, k_stride, k_head_stride, batch, kv_heads)) return rc;
+  if (int rc = check_token_rows(v, v_stride, v_head_stride, batch, kv_heads)) return rc;
+  if (!lengths || !o || !aligned(o, 16)) return ONES_E_INVALID_ARG;
+  if (capacity) {
+    if (int rc = check_head_rows(keys, keys_stride, keys_head_stride, kv_heads, dim)) return rc;
+    if (int rc = check_head_rows(values, values_stride, values_head_stride, kv_heads, dim)) return rc;
+  }
+  for (const int64_t stride : {keys_batch_stride, values_batch_stride})
+    if (batch > 1 && (stride < 0 || stride % 8)) return ONES_E_INVALID_ARG;
+    else if (batch > 1 && stride > kMaxElements / batch) return ONES_E_BOUNDS;
+  const StepPlan plan = step_plan(batch, capacity, heads, kv_heads, dim);
+  if (int rc = check_workspace(d_workspace, workspace_bytes, plan.bytes)) return rc;
+  unsigned char *const w = static_cast<unsigned char *>(d_workspace);
+  StepArgs a{};
+  a.q = q; a.k = k; a.v = v; a.keys = keys; a.values = values; a.o = o;
+  a.q_stride = q_stride; a.q_head = q_head_stride; a.k_stride = k_stride; a.k_head = k_head_stride; a.v_stride = v_stride; a.v_head = v_head_stride;
+  a.keys_batch = keys_batch_stride; a.keys_stride = keys_stride; a.keys_head = keys_head_stride;
+  a.values_batch = values_batch_stride; a.values_stride = values_stride; a.values_head = values_head_stride;
+  a.lengths = lengths;
+  if (plan.splits > 1) {
+    a.tops = reinterpret_cast<float *>(w + plan.tops);
+    a.sums = reinterpret_cast<float *>(w + plan.sums);
+    a.outputs = reinterpret_cast<float *>(w + plan.outputs);
+  }
+  a.batch = static_cast<int32_t>(batch); a.capacity = static_cast<int32_t>(capacity); a.heads = static_cast<int32_t>(heads);
+  a.kv_heads = static_cast<int32_t>(kv_heads); a.dim = static_cast<int32_t>(dim);
+  a.blocks_of_heads = static_cast<int32_t>(plan.blocks_of_heads); a.splits = static_cast<int32_t>(plan.splits); a.scale = scale;
+  if (type == ONES_F16) launch<f16>(a, static_cast<hipStream_t>(hip_stream));
+  else launch<bf16>(a, static_cast<hipStream_t>(hip_stream));
+  return launched("attention step");
+}
+
+}  // extern "C"

@@ -282,5 +282,104 @@ inline int check_update(int64_t count, int64_t rows, int64_t cols) {
   return ONES_OK;
 }
 
+// ------------------------------------------------ head norms and rotation --------
+constexpr int64_t kRotationBlocks = 1024;               // workgroups that leave sums of the weights' gradients behind
+
+struct RotationPlan {
+  int32_t vec, lanes, per, parts;             // pairs of a load (1: element by element), lanes of a row, loads of a lane; waves of a token
+  int64_t blocks;
+};
+// Wide loads where the pairs that turn, and those that do not, are whole vectors; a power of two of lanes to a row.  A wave takes a
+// token, with few tokens a part of its heads.
+inline RotationPlan rotation_plan(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int64_t turned, bool neighbours, int64_t bytes, bool backward) {
+  RotationPlan p{};
+  const int64_t vec = 16 / bytes, pairs = (dim + 1) / 2;
+  const bool wide = dim % (2 * vec) == 0 && turned % vec == 0;
+  p.vec = static_cast<int32_t>(wide ? vec : 1);
+  p.lanes = 16;
+  if (wide)
+    for (p.lanes = 4; p.lanes * vec < pairs; p.lanes *= 2) {}
+  p.per = static_cast<int32_t>(wide ? 1 : ceil_div(pairs, 16));
+  const int64_t rows = 64 / p.lanes, turns = ceil_div(heads, rows) + ceil_div(kv_heads, rows);
+  p.parts = static_cast<int32_t>(tokens >= 2048 ? 1 : std::max<int64_t>(1, turns));
+  const int64_t most = backward ? kRotationBlocks : 2048;
+  p.blocks = std::max<int64_t>(1, std::min(ceil_div(tokens * p.parts, 4), most));
+  return p;
+}
+// Elements between tokens and between heads.
+inline int check_rows_of_heads(int64_t stride, int64_t head_stride) {
+  if (stride < 0 || head_stride < 0) return ONES_E_INVALID_ARG;
+  return stride > (int64_t{1} << 32) || head_stride > (int64_t{1} << 40) ? ONES_E_BOUNDS : ONES_OK;
+}
+inline int check_rotation(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, int32_t weight_type, float eps, int64_t pairs) {
+  if (tokens < 0 || heads < 0 || kv_heads < 0 || dim < 1 || pairs < 0 || 2 * pairs > dim || !is_type(type) || (weight_type != ONES_F32 && weight_type != type) || !(eps >= 0.f))
+    return ONES_E_INVALID_ARG;
+  return tokens > ONES_MAX_TOKENS || heads > ONES_MAX_HEADS || kv_heads > ONES_MAX_HEADS || dim > ONES_MAX_HEAD_DIM ? ONES_E_BOUNDS : ONES_OK;
+}
+
+// ---------------------------------------------------------------- attention --------
+constexpr int64_t kAttentionRows = 128;       // rows of a workgroup
+
+inline int check_attention(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, int64_t sequences, float scale) {
+  if (tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || dim < 8 || dim % 8 || sequences < 0 || (type != ONES_F16 && type != ONES_BF16) ||
+      !(scale >= 1e-30f) || scale > 1e30f)
+    return ONES_E_INVALID_ARG;
+  if (tokens > ONES_MAX_TOKENS || heads > ONES_MAX_HEADS || dim > ONES_MAX_ATTENTION_DIM || sequences > ONES_MAX_TOKENS) return ONES_E_BOUNDS;
+  // threads of a launch, numbered in 32 bits
+  return (tokens / kAttentionRows + sequences + 2) * (heads + kv_heads) >= (int64_t{1} << 24) ? ONES_E_BOUNDS : ONES_OK;
+}
+// Rows that are loaded to LDS as they lie.
+inline int check_head_rows(const void *p, int64_t stride, int64_t head_stride, int64_t heads, int64_t dim) {
+  if (!p || reinterpret_cast<uintptr_t>(p) % 16 || stride < dim || stride % 8 || (heads > 1 && (head_stride < 0 || head_stride % 8))) return ONES_E_INVALID_ARG;
+  return stride > kMaxLoadableStride || head_stride > (int64_t{1} << 40) ? ONES_E_BOUNDS : ONES_OK;
+}
+// Of a single token of every sequence: rows `stride` apart, and heads.
+inline int check_token_rows(const void *p, int64_t stride, int64_t head_stride, int64_t batch, int64_t heads) {
+  if (!p || reinterpret_cast<uintptr_t>(p) % 16 || (batch > 1 && (stride < 0 || stride % 8)) || (heads > 1 && (head_stride < 0 || head_stride % 8))) return ONES_E_INVALID_ARG;
+  return stride > (int64_t{1} << 40) || head_stride > (int64_t{1} << 40) ? ONES_E_BOUNDS : ONES_OK;
+}
+struct AttentionPlan {
+  size_t delta, dout_norm, slot_norms, bytes;
+};
+inline AttentionPlan attention_plan(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads) {
+  AttentionPlan p{};
+  const size_t rows = align_up(static_cast<size_t>(tokens) * heads * 4);
+  p.dout_norm = rows;
+  p.slot_norms = 2 * rows;
+  p.bytes = p.slot_norms + align_up(static_cast<size_t>(tokens / kAttentionRows + sequences + 2) * (heads + kv_heads) * 4);
+  return p;
+}
+
+// ------------------------------------------- a token's attention over a cache --------
+constexpr int64_t kStepKeys = 32, kStepWaves = 4, kStepHeads = 16;         // keys of a wave's tile; waves; query heads of a workgroup
+
+struct StepPlan {
+  int64_t blocks_of_heads, splits;
+  size_t tops, sums, outputs, bytes;          // of the parts, where the keys are split
+};
+inline StepPlan step_plan(int64_t batch, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim) {
+  StepPlan p{};
+  p.blocks_of_heads = ceil_div(heads / kv_heads, kStepHeads);
+  const int64_t chains = std::max<int64_t>(1, batch * kv_heads * p.blocks_of_heads), tiles = ceil_div(capacity, kStepKeys * kStepWaves);
+  p.splits = std::max<int64_t>(1, std::min(ceil_div(512, chains), tiles / 2));
+  if (p.splits > 1) {
+    const size_t parts = static_cast<size_t>(batch) * heads * p.splits;
+    p.sums = align_up(parts * 4);
+    p.outputs = 2 * p.sums;
+    p.bytes = p.outputs + align_up(parts * dim * 4);
+  }
+  return p;
+}
+inline int check_step(int64_t batch, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, float scale) {
+  if (batch < 0 || capacity < 0) return ONES_E_INVALID_ARG;
+  if (int rc = check_attention(0, heads, kv_heads, dim, type, 0, scale)) return rc;
+  return batch > ONES_MAX_BATCH || capacity > ONES_MAX_TOKENS || batch * heads > (int64_t{1} << 22) ? ONES_E_BOUNDS : ONES_OK;
+}
+
+// ------------------------------------------------------- the global norm --------
+constexpr int64_t kClipTable = 128, kClipPiece = 8192, kClipBlocks = 1024;      // tensors of a launch; elements of a piece; workgroups of all launches
+
+inline size_t clip_workspace(int64_t tensors) { return align_up(static_cast<size_t>(kClipBlocks + ceil_div(tensors, kClipTable)) * 8); }
+
 }  // namespace train
 }  // namespace ones

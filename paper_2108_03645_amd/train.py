@@ -2,9 +2,9 @@
 marshalling only.  The arithmetic runs in the library's HIP kernels; PyTorch supplies the tensors and the stream (the current one
 of the tensors' device).  There is no CPU fallback: without the built library or without a GPU this raises.
 
-The ``*_forward`` and ``*_backward`` functions are the library's calls; ``layer_norm``, ``gated_recurrence`` and
-``linear_cross_entropy`` are the same under autograd.  ``gated_recurrence_step`` is the single-token form,
-``orthogonal_update`` the optimizer's step.
+The ``*_forward`` and ``*_backward`` functions are the library's calls; ``layer_norm``, ``gated_recurrence``,
+``head_norm_rotation``, ``attention`` and ``linear_cross_entropy`` are the same under autograd.  ``gated_recurrence_step`` and
+``attention_step`` are the single-token forms, ``clip_gradients`` and ``orthogonal_update`` the optimizer's step.
 
 All of them may be captured into a graph.  Autograd's own rule stays: a backward pass under capture must not meet leaves that an eager
 graph still holds; the ``*_backward`` calls know no such state."""
@@ -21,7 +21,10 @@ EXPORTS = ["ones_layer_norm_forward", "ones_layer_norm_workspace_bytes", "ones_l
            "ones_recurrence_carry_bytes", "ones_recurrence_workspace_bytes", "ones_recurrence_forward",
            "ones_recurrence_backward", "ones_recurrence_step", "ones_cross_entropy_forward_workspace_bytes",
            "ones_cross_entropy_backward_workspace_bytes", "ones_cross_entropy_forward", "ones_cross_entropy_backward",
-           "ones_orthogonal_update_workspace_bytes", "ones_orthogonal_update"]
+           "ones_orthogonal_update_workspace_bytes", "ones_orthogonal_update", "ones_head_norm_rotation_forward",
+           "ones_head_norm_rotation_workspace_bytes", "ones_head_norm_rotation_backward", "ones_attention_forward",
+           "ones_attention_workspace_bytes", "ones_attention_backward", "ones_attention_step_workspace_bytes", "ones_attention_step",
+           "ones_clip_gradients_workspace_bytes", "ones_clip_gradients"]
 
 _P, _I64, _I32, _F32, _SIZE = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_size_t
 _ARGUMENTS = {
@@ -40,6 +43,17 @@ _ARGUMENTS = {
     "ones_cross_entropy_backward": [_P, _P, _I64, _P, _I64, _I64, _I64, _I64, _I32, _P, _P, _P, _P, _P, _SIZE, _P],
     "ones_orthogonal_update_workspace_bytes": [_I64, _I64, _I64],
     "ones_orthogonal_update": [_P, _P, _I64, _I64, _I64, _I32, _F32, _I32, _I32, _P, _F32, _P, _I32, _P, _SIZE, _P],
+    "ones_head_norm_rotation_forward": [_P, _I64, _I64] * 2 + [_I64, _I64, _I64, _I64, _I32, _P, _P, _I32, _F32, _P, _P, _I64, _I32, _P, _P, _P],
+    "ones_head_norm_rotation_workspace_bytes": [_I64, _I64, _I64, _I64],
+    "ones_head_norm_rotation_backward": [_P, _I64, _I64] * 4 + [_I64, _I64, _I64, _I64, _I32, _P, _P, _I32, _F32, _P, _P, _I64, _I32,
+                                                               _P, _P, _P, _P, _P, _SIZE, _P],
+    "ones_attention_forward": [_P, _I64, _I64] * 3 + [_I64, _I64, _I64, _I64, _I32, _P, _I64, _F32, _P, _P, _P, _P],
+    "ones_attention_workspace_bytes": [_I64, _I64, _I64, _I64, _I64],
+    "ones_attention_backward": [_P, _I64, _I64] * 4 + [_I64, _I64, _I64, _I64, _I32, _P, _I64, _F32, _P, _P, _P, _P, _P, _P, _P, _SIZE, _P],
+    "ones_attention_step_workspace_bytes": [_I64, _I64, _I64, _I64, _I64],
+    "ones_attention_step": [_P, _I64, _I64] * 3 + [_P, _I64, _I64, _I64] * 2 + [_P, _I64, _I64, _I64, _I64, _I64, _I32, _F32, _P, _P, _SIZE, _P],
+    "ones_clip_gradients_workspace_bytes": [_I64],
+    "ones_clip_gradients": [_P, _P, _P, _I64, _F32, _F32, _P, _P, _SIZE, _P],
 }
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _FLOAT = (torch.float32,)
@@ -390,3 +404,250 @@ def orthogonal_update(grad, momentum=None, beta=0.95, nesterov=True, steps=5, co
     if momentum is not None:
         _changed(momentum)
     return update
+
+
+# ------------------------------------------- head norms and rotation --------
+def _heads(t, kinds, name, tokens=None, dim=None, device=None, dtype=None):
+    """Checked to be [tokens, heads, dim]; (t, elements between tokens, between heads), copied if its rows have gaps."""
+    _check(t, name, None, kinds if dtype is None else (dtype,), device)
+    if t.dim() != 3 or (tokens is not None and t.shape[0] != tokens) or (dim is not None and t.shape[2] != dim):
+        raise ValueError(f"{name}: [{'tokens' if tokens is None else tokens}, heads, {'dim' if dim is None else dim}] is wanted, got {tuple(t.shape)}")
+    if (t.stride(2) != 1 and t.shape[2] > 1) or min(t.stride()) < 0:
+        t = t.contiguous()
+    return t, t.stride(0), t.stride(1)
+
+
+def _rotation_inputs(q, k, q_weight, k_weight, positions, frequencies):
+    q, q_stride, q_head = _heads(q, _TYPES, "q")
+    tokens, heads, dim = q.shape
+    k, k_stride, k_head = _heads(k, None, "k", tokens, dim, q.device, q.dtype)
+    kinds = (torch.float32, q.dtype)
+    q_weight = _dense(q_weight, "q_weight", (dim,), kinds, q.device)
+    k_weight = _dense(k_weight, "k_weight", (dim,), kinds, q.device)
+    if q_weight is None or k_weight is None or q_weight.dtype != k_weight.dtype:
+        raise TypeError("q_weight and k_weight: tensors of one type are wanted")
+    _check(positions, "positions", (tokens,), _WHOLE, q.device)
+    _check(frequencies, "frequencies", None, _FLOAT, q.device)
+    if frequencies.dim() != 1 or 2 * frequencies.shape[0] > dim:
+        raise ValueError(f"frequencies: one for each of up to {dim // 2} pairs, got {tuple(frequencies.shape)}")
+    positions, frequencies = positions.int().contiguous(), frequencies.contiguous()
+    sizes = (tokens, heads, k.shape[1], dim, _TYPES[q.dtype], q_weight.data_ptr(), k_weight.data_ptr(), _TYPES[q_weight.dtype])
+    turns = (positions.data_ptr(), frequencies.data_ptr(), frequencies.shape[0])
+    return (q.data_ptr(), q_stride, q_head, k.data_ptr(), k_stride, k_head), sizes, turns, (q, k, q_weight, k_weight, positions, frequencies)
+
+
+def head_norm_rotation_forward(q, k, q_weight, k_weight, positions, frequencies, eps=1e-6, interleaved=False):
+    """ones_head_norm_rotation_forward over q [tokens, heads, dim] and k [tokens, kv_heads, dim]: (q, k), every head's row divided by its
+    root mean square, weighted, and its first 2 * len(frequencies) elements turned in pairs by position * frequency (pairs are the two halves
+    of these elements, or with interleaved neighbours).  positions: whole numbers [tokens] of 32 bits; frequencies: float32."""
+    rows, sizes, turns, kept = _rotation_inputs(q, k, q_weight, k_weight, positions, frequencies)
+    q, k = kept[:2]
+    q_out, k_out = _like(q), _like(k)
+    _call(q.device, load().ones_head_norm_rotation_forward, *rows, *sizes, eps, *turns, int(interleaved), q_out.data_ptr(), k_out.data_ptr())
+    return q_out, k_out
+
+
+def head_norm_rotation_backward(dq_out, dk_out, q, k, q_weight, k_weight, positions, frequencies, eps=1e-6, interleaved=False):
+    """ones_head_norm_rotation_backward: (dq, dk, dq_weight, dk_weight) for the gradients of the two results."""
+    rows, sizes, turns, kept = _rotation_inputs(q, k, q_weight, k_weight, positions, frequencies)
+    q, k, q_weight, k_weight = kept[:4]
+    (dq_out, dq_stride, dq_head), (dk_out, dk_stride, dk_head) = (
+        _heads(_checked(g, name, t), None, name, dtype=t.dtype) for g, name, t in ((dq_out, "dq_out", q), (dk_out, "dk_out", k)))
+    dq, dk, dq_weight, dk_weight = _like(q), _like(k), torch.empty_like(q_weight), torch.empty_like(k_weight)
+    L = load()
+    nbytes = L.ones_head_norm_rotation_workspace_bytes(*sizes[:4])
+    scratch = _scratch(nbytes, q.device)
+    _call(q.device, L.ones_head_norm_rotation_backward, dq_out.data_ptr(), dq_stride, dq_head, dk_out.data_ptr(), dk_stride, dk_head, *rows, *sizes, eps,
+          *turns, int(interleaved), dq.data_ptr(), dk.data_ptr(), dq_weight.data_ptr(), dk_weight.data_ptr(), _ptr(scratch), nbytes)
+    return dq, dk, dq_weight, dk_weight
+
+
+def _checked(g, name, t):
+    """The gradient of something shaped like t."""
+    _check(g, name, t.shape, (t.dtype,), t.device)
+    return g
+
+
+class _HeadNormRotation(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, frequencies, eps, interleaved):
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions, frequencies)
+        ctx.settings = (eps, interleaved)
+        return head_norm_rotation_forward(q, k, q_weight, k_weight, positions, frequencies, eps, interleaved)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        return *head_norm_rotation_backward(dq_out, dk_out, *ctx.saved_tensors, *ctx.settings), None, None, None, None
+
+
+def head_norm_rotation(q, k, q_weight, k_weight, positions, frequencies, eps=1e-6, interleaved=False):
+    """The norms of queries and keys for each head with their rotation, differentiable in q, k and the weights: (q, k)."""
+    return _HeadNormRotation.apply(q, k, q_weight, k_weight, positions, frequencies, eps, interleaved)
+
+
+# ---------------------------------------------------------- attention --------
+_STRIDE = 1 << 20                                 # of elements between tokens, at most
+
+
+def _attended(t, name, tokens=None, dim=None, like=None):
+    """As _heads, copied as well if its rows cannot be loaded as they lie."""
+    t, stride, head = _heads(t, _HALVES, name, tokens, dim, None if like is None else like.device, None if like is None else like.dtype)
+    if stride % 8 or head % 8 or stride > _STRIDE or stride < t.shape[2] or t.data_ptr() % 16:
+        t = t.contiguous() if not t.is_contiguous() else t.clone()
+        stride, head = t.shape[1] * t.shape[2], t.shape[2]
+    return t, stride, head
+
+
+def _attention_inputs(q, k, v, offsets, scale):
+    q, q_stride, q_head = _attended(q, "q")
+    tokens, heads, dim = q.shape
+    k, k_stride, k_head = _attended(k, "k", tokens, dim, q)
+    v, v_stride, v_head = _attended(v, "v", tokens, dim, q)
+    if k.shape[1] != v.shape[1] or not k.shape[1] or heads % k.shape[1]:
+        raise ValueError(f"{heads} query heads, {k.shape[1]} key heads and {v.shape[1]} value heads do not go together")
+    if dim % 8:
+        raise ValueError(f"dim: a multiple of 8 is wanted, got {dim}")
+    if offsets is None:
+        offsets = torch.zeros(2, dtype=torch.int32, device=q.device)
+        offsets[1:].fill_(tokens)
+    _check(offsets, "offsets", None, (torch.int32,), q.device)
+    if offsets.dim() != 1 or not offsets.shape[0]:
+        raise ValueError("offsets: [sequences + 1] is wanted")
+    offsets = offsets.contiguous()
+    sizes = (tokens, heads, k.shape[1], dim, _TYPES[q.dtype], offsets.data_ptr(), offsets.shape[0] - 1, dim ** -0.5 if scale is None else scale)
+    return (q.data_ptr(), q_stride, q_head, k.data_ptr(), k_stride, k_head, v.data_ptr(), v_stride, v_head), sizes, (q, k, v, offsets)
+
+
+def attention_forward(q, k, v, offsets=None, scale=None, keep_rest=False):
+    """ones_attention_forward: causal attention of q [tokens, heads, dim] over k, v [tokens, kv_heads, dim]: (o, lse, rest), lse float32
+    [heads, tokens].  offsets (int32 [sequences + 1]): where the packed sequences begin and the last one ends; None: one sequence.  rest (None
+    unless kept) is what o was rounded by, which the backward call takes.  scale: dim ** -0.5 if None."""
+    rows, sizes, (q, k, v, offsets) = _attention_inputs(q, k, v, offsets, scale)
+    o = _like(q)
+    rest = _like(q) if keep_rest else None
+    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    _call(q.device, load().ones_attention_forward, *rows, *sizes, o.data_ptr(), _ptr(rest), lse.data_ptr())
+    return o, lse, rest
+
+
+def attention_backward(do, q, k, v, o, lse, rest=None, offsets=None, scale=None):
+    """ones_attention_backward: (dq, dk, dv) for the gradient do of o, with o, lse and rest as forward left them."""
+    rows, sizes, (q, k, v, offsets) = _attention_inputs(q, k, v, offsets, scale)
+    device = q.device
+    do, do_stride, do_head = _attended(_checked(do, "do", q), "do", like=q)
+    o, rest = (_dense(t, name, q.shape, (q.dtype,), device) for t, name in ((o, "o"), (rest, "rest")))
+    lse = _dense(lse, "lse", (q.shape[1], q.shape[0]), _FLOAT, device)
+    dq, dk, dv = _like(q), _like(k), _like(v)
+    L = load()
+    nbytes = L.ones_attention_workspace_bytes(sizes[0], sizes[6], *sizes[1:4])
+    scratch = _scratch(nbytes, device)
+    _call(device, L.ones_attention_backward, do.data_ptr(), do_stride, do_head, *rows, *sizes, o.data_ptr(), _ptr(rest), lse.data_ptr(), dq.data_ptr(),
+          dk.data_ptr(), dv.data_ptr(), _ptr(scratch), nbytes)
+    return dq, dk, dv
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, offsets, scale):
+        o, lse, rest = attention_forward(q, k, v, offsets, scale, keep_rest=any(ctx.needs_input_grad[:3]))
+        ctx.save_for_backward(q, k, v, o, lse, rest, offsets)
+        ctx.scale = scale
+        return o
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, do):
+        return *attention_backward(do, *ctx.saved_tensors, ctx.scale), None, None
+
+
+def attention(q, k, v, offsets=None, scale=None):
+    """Causal attention over packed sequences, differentiable in q, k and v: o [tokens, heads, dim]."""
+    return _Attention.apply(q, k, v, offsets, scale)
+
+
+def _cache(t, name, batch, capacity, kv_heads, dim, like):
+    """Checked: a cache is written in place, so its rows have to be loadable as they lie."""
+    _check(t, name, (batch, capacity, kv_heads, dim), (like.dtype,), like.device)
+    b, s, h, d = t.stride()
+    if t.numel() and ((d != 1 and dim > 1) or (b | s | (h if kv_heads > 1 else 0)) % 8 or s < dim or s > _STRIDE or t.data_ptr() % 16):
+        raise ValueError(f"{name}: updated in place; its base has to be a multiple of 16 bytes, strides of 8 elements, rows without gaps")
+    return t.data_ptr(), b, s, h
+
+
+def attention_step(q, k, v, keys, values, lengths, scale=None):
+    """ones_attention_step: one more token of every sequence.  k, v [batch, kv_heads, dim] are written to place lengths[b] of keys, values
+    [batch, capacity, kv_heads, dim], and q [batch, heads, dim] attends over places 0 .. lengths[b]; returns o, shaped like q.  lengths (int32
+    [batch]) is not changed; below 0 a sequence is left out (o is 0), at capacity and above it has no room (o is NaN)."""
+    q, q_stride, q_head = _step_rows(q, "q")
+    batch, heads, dim = q.shape
+    k, k_stride, k_head = _step_rows(k, "k", batch, dim, q)
+    v, v_stride, v_head = _step_rows(v, "v", batch, dim, q)
+    kv_heads = k.shape[1]
+    if kv_heads != v.shape[1] or not kv_heads or heads % kv_heads:
+        raise ValueError(f"{heads} query heads, {kv_heads} key heads and {v.shape[1]} value heads do not go together")
+    if dim % 8:
+        raise ValueError(f"dim: a multiple of 8 is wanted, got {dim}")
+    if not isinstance(keys, torch.Tensor) or keys.dim() != 4:
+        raise ValueError("keys: [batch, capacity, kv_heads, dim] is wanted")
+    capacity = keys.shape[1]
+    of_keys, of_values = (_cache(t, name, batch, capacity, kv_heads, dim, q) for t, name in ((keys, "keys"), (values, "values")))
+    lengths = _dense(lengths, "lengths", (batch,), (torch.int32,), q.device)
+    o = _like(q)
+    L = load()
+    nbytes = L.ones_attention_step_workspace_bytes(batch, capacity, heads, kv_heads, dim)
+    scratch = _scratch(nbytes, q.device)
+    _call(q.device, L.ones_attention_step, q.data_ptr(), q_stride, q_head, k.data_ptr(), k_stride, k_head, v.data_ptr(), v_stride, v_head,
+          *of_keys, *of_values, lengths.data_ptr(), batch, capacity, heads, kv_heads, dim, _TYPES[q.dtype], dim ** -0.5 if scale is None else scale,
+          o.data_ptr(), _ptr(scratch), nbytes)
+    _changed(keys)
+    _changed(values)
+    return o
+
+
+def _step_rows(t, name, batch=None, dim=None, like=None):
+    t, stride, head = _heads(t, _HALVES, name, batch, dim, None if like is None else like.device, None if like is None else like.dtype)
+    if (stride | head) % 8 or t.data_ptr() % 16:
+        t = t.contiguous() if not t.is_contiguous() else t.clone()
+        stride, head = t.shape[1] * t.shape[2], t.shape[2]
+    return t, stride, head
+
+
+# ----------------------------------------------------- the global norm --------
+def clip_gradients(gradients, limit, eps=1e-6):
+    """ones_clip_gradients: scales the gradients (a list of tensors of any of the types, on one device) in place by limit / (norm + eps) where that is
+    below 1, norm the root of the sum of all squares; returns norm, float32, on the device.  A norm that is not finite changes
+    nothing; limit may be infinity.  None among them is passed over; a gradient may lie in any order, but without gaps, and no two
+    may share memory."""
+    gradients = [g for g in gradients if g is not None]
+    if not gradients:
+        raise ValueError("gradients: one at least is wanted")
+    first = gradients[0]
+    _check(first, "gradients", None, _TYPES)
+    device = first.device
+    for g in gradients:
+        _check(g, "gradients", None, _TYPES, device)
+        if not g.is_contiguous() and not _whole(g):
+            raise ValueError("gradients: updated in place, they may have no gaps")
+    n = len(gradients)
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    L = load()
+    nbytes = L.ones_clip_gradients_workspace_bytes(n)
+    scratch = _scratch(nbytes, device)
+    _call(device, L.ones_clip_gradients, (C.c_void_p * n)(*[g.data_ptr() for g in gradients]), (C.c_int64 * n)(*[g.numel() for g in gradients]),
+          (C.c_int32 * n)(*[_TYPES[g.dtype] for g in gradients]), n, limit, eps, norm.data_ptr(), _ptr(scratch), nbytes)
+    for g in gradients:
+        _changed(g)
+    return norm
+
+
+def _whole(t):
+    """Whether the elements of t fill one run of memory, in whatever order of dimensions."""
+    if not t.numel():
+        return True
+    step = 1
+    for stride, size in sorted((stride, size) for stride, size in zip(t.stride(), t.shape) if size > 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
