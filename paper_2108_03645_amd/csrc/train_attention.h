@@ -14,6 +14,14 @@ namespace ones {
 namespace train {
 namespace {
 
+// As load_to_lds, four bytes a lane.
+__device__ __forceinline__ void load_words_to_lds(const unsigned char *base, uint32_t bytes, uint32_t offset, uint32_t to) {
+  const uint64_t at = reinterpret_cast<uintptr_t>(base);
+  typedef __attribute__((ext_vector_type(4))) uint32_t Descriptor;
+  const Descriptor buffer{uniform(static_cast<uint32_t>(at)), uniform(static_cast<uint32_t>(at >> 32)), uniform(bytes), 0x00020000};
+  asm volatile("s_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer), "{m0}"(to) : "memory");
+}
+
 // A tile of ROWS rows of D elements (a head's rows of consecutive tokens).  The 16-byte pieces of a row are exchanged by the row's
 // number so that the lanes of a read meet different banks, whichever way they read: eight rows at one piece, or two pieces of four rows.
 template <int D, int ROWS, int THREADS>

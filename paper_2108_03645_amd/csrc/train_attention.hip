@@ -22,9 +22,11 @@ struct AttentionArgs {
   void *o, *rest;
   float *lse;
   void *dq, *dk, *dv;
-  float *delta, *dout_norm, *v_norm;          // delta, |do| of every row; the largest |do| and |v| of every slot (fp16)
+  float2 *terms;                              // of every row: lse in base 2, delta
+  float *dout_norm, *v_norm;                  // |do| of every row; the largest |do| and |v| of every slot (fp16)
+  float *partial;                             // dk and dv of parts of a group's heads, in 32 bits
   const int32_t *offsets;
-  int32_t sequences, tokens, heads, kv_heads, dim;
+  int32_t sequences, tokens, heads, kv_heads, dim, parts;
   float scale;
 };
 
@@ -207,7 +209,10 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
       }
 #pragma unroll
       for (int m = 1; m < lanes; m *= 2) { dot += __shfl_xor(dot, m); square += __shfl_xor(square, m); }
-      if (p == 0 && r < count) a.delta[static_cast<int64_t>(head) * a.tokens + here + r] = dot;
+      if (p == 0 && r < count) {
+        const int64_t i = static_cast<int64_t>(head) * a.tokens + here + r;
+        a.terms[i] = make_float2(a.lse[i] * kLog2e, dot);
+      }
       if (norms && square < INFINITY) most = fmaxf(most, square);
       if (norms && p == 0 && r < count) a.dout_norm[static_cast<int64_t>(head) * a.tokens + here + r] = square < INFINITY ? sqrtf(square) : 0.f;
     }
@@ -286,8 +291,9 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
     read_rows<D>(at<T>(a.q, here + r, a.q_stride, turn.head, a.q_head), a.q_stride, count - r, a.dim, lane, q[n]);
     read_rows<D>(at<T>(a.dout, here + r, a.do_stride, turn.head, a.do_head), a.do_stride, count - r, a.dim, lane, g[n]);
     const int64_t i = static_cast<int64_t>(turn.head) * a.tokens + here + min(r + (lane & 15), count - 1);
-    lse[n] = a.lse[i] * kLog2e;
-    delta[n] = a.delta[i];
+    const float2 terms = a.terms[i];
+    lse[n] = terms.x;
+    delta[n] = terms.y;
     unit[n] = 1.f;
     if constexpr (__is_same(T, f16)) unit[n] = unit_of(2.f * a.dout_norm[i] * v_most);
     factor[n] = a.scale / unit[n];
@@ -357,16 +363,22 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
 constexpr int kStepRows = 32;                 // queries of a step of the keys' gradients
 
 template <typename T, int D>
+constexpr int kKeysLds = 4 * RowTile<D, kStepRows, 256>::bytes + 2 * kStepRows * 8;
+
+template <typename T, int D>
 __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_t id, unsigned char *lds) {
   using Tile = RowTile<D, kStepRows, 256>;
-  const int32_t slot = static_cast<int32_t>(id / a.kv_heads), kv = static_cast<int32_t>(id % a.kv_heads), group = a.heads / a.kv_heads;
+  const int32_t kv = static_cast<int32_t>(id % a.kv_heads), group = a.heads / a.kv_heads;
+  id /= a.kv_heads;
+  const int32_t part = static_cast<int32_t>(id % a.parts), slot = static_cast<int32_t>(id / a.parts);
   const Rows rows = rows_of<kQueries>(a.offsets, a.sequences, a.tokens, slot);
   if (rows.at >= rows.length || rows.at < 0) return;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const int64_t out_stride = static_cast<int64_t>(a.kv_heads) * a.dim;
   const int32_t here = rows.first + rows.at, count = min(rows.length - rows.at, kQueries);
   T *const dk = const_cast<T *>(at<T>(a.dk, here, out_stride, kv, a.dim)), *const dv = const_cast<T *>(at<T>(a.dv, here, out_stride, kv, a.dim));
   if (!rows.real) {
+    if (part) return;
     write_zeros(dk, out_stride, count, a.dim);
     write_zeros(dv, out_stride, count, a.dim);
     return;
@@ -386,88 +398,135 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     read_rows<D>(at<T>(a.k, here + r, a.k_stride, kv, a.k_head), a.k_stride, count - r, a.dim, lane, k[n]);
     read_rows<D>(at<T>(a.v, here + r, a.v_stride, kv, a.v_head), a.v_stride, count - r, a.dim, lane, v[n]);
   }
-  int along[D / 32], across[D / 16];
-#pragma unroll
-  for (int s = 0; s < D / 32; ++s) along[s] = Tile::along(lane, s);
-#pragma unroll
-  for (int b = 0; b < D / 16; ++b) across[b] = Tile::across(lane, b);
+  int along0 = Tile::along(lane, 0), across0 = Tile::across(lane, 0);
   f32x4 of_k[D / 16][2], of_v[D / 16][2];
 #pragma unroll
   for (int n = 0; n < 2; ++n)
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) of_k[b][n] = of_v[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   // the queries from the tile's first key on, head after head
-  const int steps = (rows.length - rows.at + kStepRows - 1) / kStepRows, all_steps = steps * group;
+  const int32_t left = rows.length - rows.at;
+  const int steps = (left + kStepRows - 1) / kStepRows, each = (group + a.parts - 1) / a.parts, head0 = kv * group + part * each;
+  const int heads = min(each, group - part * each), all_steps = steps * max(heads, 0);
   Tile q, g;
+  const unsigned char *terms;
   auto begin = [&](int head) {
-    q.start(at<T>(a.q, here, a.q_stride, kv * group + head, a.q_head), a.q_stride, rows.length - rows.at, a.dim);
-    g.start(at<T>(a.dout, here, a.do_stride, kv * group + head, a.do_head), a.do_stride, rows.length - rows.at, a.dim);
+    q.start(at<T>(a.q, here, a.q_stride, head0 + head, a.q_head), a.q_stride, left, a.dim);
+    g.start(at<T>(a.dout, here, a.do_stride, head0 + head, a.do_head), a.do_stride, left, a.dim);
+    terms = reinterpret_cast<const unsigned char *>(a.terms + static_cast<int64_t>(head0 + head) * a.tokens + here);
   };
-  begin(0);
-  q.load(lds);
-  g.load(lds + 2 * Tile::bytes);
+  auto load = [&](int to) {
+    if (wave == 0) {
+      const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LdsBytes *)(lds + 4 * Tile::bytes + to * kStepRows * 8)));
+      load_words_to_lds(terms, static_cast<uint32_t>(max(min(q.left, kStepRows), 0)) * 8, lane * 4, at);
+    }
+    terms += kStepRows * 8;
+    q.load(lds + to * Tile::bytes);
+    g.load(lds + (2 + to) * Tile::bytes);
+  };
+  if (all_steps) {
+    begin(0);
+    load(0);
+  }
   int head = 0, step = 0;
   for (int t = 0; t < all_steps; ++t) {
     meet<0>();
     const unsigned char *qs = lds + (t & 1) * Tile::bytes, *gs = qs + 2 * Tile::bytes;
-    const int this_head = kv * group + head, first = step * kStepRows;       // from the tile's first key on
+    const float *ts = reinterpret_cast<const float *>(lds + 4 * Tile::bytes + (t & 1) * kStepRows * 8) + (lane >> 4) * 8;
+    const int first = step * kStepRows;                                      // from the tile's first key on
     if (++step == steps) {
       step = 0;
-      if (++head < group) begin(head);
+      if (++head < heads) begin(head);
     }
-    if (t + 1 < all_steps) {
-      q.load(lds + (~t & 1) * Tile::bytes);
-      g.load(lds + (2 + (~t & 1)) * Tile::bytes);
-    }
+    if (t + 1 < all_steps) load(~t & 1);
     if (first + kStepRows - 1 < mine) continue;                              // queries in front of all of the wave's keys
-    f32x4 z[2][2], d[2][2];
-    const int64_t row0 = static_cast<int64_t>(this_head) * a.tokens + here;
+    const bool border = first < mine + 31;
+    asm volatile("" : "+v"(along0), "+v"(across0));      // places are formed from these two where they are needed: registers are short
+    Pack<T, 8> p[2], ds[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
+      f32x4 z[2], d[2];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) z[b][n] = d[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < 2; ++n) z[n] = d[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) {
-        const s16x8 f = Tile::read_along(qs, b * 16, along[s]), e = Tile::read_along(gs, b * 16, along[s]);
+        const s16x8 f = Tile::read_along(qs, b * 16, along0 ^ (s << 6)), e = Tile::read_along(gs, b * 16, along0 ^ (s << 6));
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-          z[b][n] = mfma<T>(f, k[n][s], z[b][n]);
-          d[b][n] = mfma<T>(e, v[n][s], d[b][n]);
+          z[n] = mfma<T>(f, k[n][s], z[n]);
+          d[n] = mfma<T>(e, v[n][s], d[n]);
         }
       }
+      const f32x4 t0 = *reinterpret_cast<const f32x4 *>(ts + b * 32), t1 = *reinterpret_cast<const f32x4 *>(ts + b * 32 + 4);
+      const float lse[4] = {t0[0], t0[2], t1[0], t1[2]}, delta[4] = {t0[1], t0[3], t1[1], t1[3]};
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = first + b * 16 + (lane >> 4) * 4 + r;
-        const int64_t j = row0 + min(i, rows.length - rows.at - 1);
-        const float lse = a.lse[j] * kLog2e, delta = a.delta[j];
+      for (int n = 0; n < 2; ++n) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const bool live = i >= mine + n * 16 + (lane & 15) && i < rows.length - rows.at;
-          const float p = live ? __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][n][r], c, -lse)) : 0.f;
-          z[b][n][r] = p * kWeights;
-          d[b][n][r] = live ? p * (d[b][n][r] - delta) * unit : 0.f;
+        for (int r = 0; r < 4; ++r) {
+          z[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[n][r], c, -lse[r]));
+          d[n][r] = z[n][r] * (d[n][r] - delta[r]);
+          if constexpr (__is_same(T, f16)) { z[n][r] *= kWeights; d[n][r] *= unit; }
+        }
+        if (border) {
+          const int row = mine + n * 16 + (lane & 15) - first - b * 16 - (lane >> 4) * 4;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (r < row) z[n][r] = d[n][r] = 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          p[n].v[b * 4 + r] = static_cast<T>(z[n][r]);
+          ds[n].v[b * 4 + r] = static_cast<T>(d[n][r]);
         }
       }
-    }
-    s16x8 p[2], ds[2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      p[n] = rounded<T>(z[0][n], z[1][n]);
-      ds[n] = rounded<T>(d[0][n], d[1][n]);
     }
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) {
-      const s16x8 f = Tile::read_across(gs, 0, across[b]), e = Tile::read_across(qs, 0, across[b]);
+      const s16x8 f = Tile::read_across(gs, 0, across0 ^ (b << 5)), e = Tile::read_across(qs, 0, across0 ^ (b << 5));
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        of_v[b][n] = mfma<T>(f, p[n], of_v[b][n]);
-        of_k[b][n] = mfma<T>(e, ds[n], of_k[b][n]);
+        of_v[b][n] = mfma<T>(f, __builtin_bit_cast(s16x8, p[n]), of_v[b][n]);
+        of_k[b][n] = mfma<T>(e, __builtin_bit_cast(s16x8, ds[n]), of_k[b][n]);
       }
     }
   }
   const float k_factor[2] = {a.scale / unit, a.scale / unit}, v_factor[2] = {1.f / kWeights, 1.f / kWeights};
-  write_rows<T, D, 2>(of_k, k_factor, dk + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
-  write_rows<T, D, 2>(of_v, v_factor, dv + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+  if (a.parts == 1) {
+    write_rows<T, D, 2>(of_k, k_factor, dk + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+    write_rows<T, D, 2>(of_v, v_factor, dv + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int r = mine + n * 16 + (lane & 15);
+    if (r >= count) continue;
+    float *to = a.partial + ((static_cast<int64_t>(part) * a.tokens + here + r) * a.kv_heads + kv) * 2 * a.dim;
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) {
+      const int i = b * 16 + (lane >> 4) * 4;
+      if (i >= a.dim) continue;
+      *reinterpret_cast<f32x4 *>(to + i) = of_k[b][n] * k_factor[n];
+      *reinterpret_cast<f32x4 *>(to + a.dim + i) = of_v[b][n] * v_factor[n];
+    }
+  }
+}
+
+// The parts of dk and dv, in order.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
+  const int64_t n = static_cast<int64_t>(a.tokens) * a.kv_heads * a.dim / 4, step = static_cast<int64_t>(gridDim.x) * 256;
+  const int32_t first = min(max(a.offsets[0], 0), a.tokens), end = min(max(a.offsets[a.sequences], 0), a.tokens);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < 2 * n; i += step) {
+    const int64_t row = i / (a.dim / 2), in = i % (a.dim / 2) * 4;       // of [tokens][kv_heads], 2 dim elements
+    const int64_t token = row / a.kv_heads;
+    if (token < first || token >= end) continue;
+    f32x4 s{0.f, 0.f, 0.f, 0.f};
+    for (int32_t p = 0; p < a.parts; ++p)
+      s += *reinterpret_cast<const f32x4 *>(a.partial + ((static_cast<int64_t>(p) * a.tokens * a.kv_heads + row) * 2 * a.dim + in));
+    T *to = in < a.dim ? static_cast<T *>(a.dk) + row * a.dim + in : static_cast<T *>(a.dv) + row * a.dim + in - a.dim;
+    const float v[4] = {s[0], s[1], s[2], s[3]};
+    store_pack<T, 4>(to, v);
+  }
 }
 
 template <typename T, int D>
@@ -476,8 +535,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a) {
   gradient_of_queries<T, D>(a, blockIdx.x, lds);
 }
 template <typename T, int D>
-__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionArgs a) {
-  __shared__ __attribute__((aligned(256))) unsigned char lds[4 * RowTile<D, kStepRows, 256>::bytes];
+__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a) {
+  __shared__ __attribute__((aligned(256))) unsigned char lds[kKeysLds<T, D>];
   gradient_of_keys<T, D>(a, blockIdx.x, lds);
 }
 
@@ -491,7 +550,8 @@ template <typename T, int D>
 void launch_backward(const AttentionArgs &a, hipStream_t s) {
   const int64_t slots = slots_of(a.tokens, a.sequences, kQueries), all = a.heads + (__is_same(T, f16) ? a.kv_heads : 0);
   hipLaunchKernelGGL((attention_delta_kernel<T, D>), dim3(static_cast<uint32_t>(slots * all)), dim3(256), 0, s, a);
-  hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.kv_heads)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.kv_heads * a.parts)), dim3(256), 0, s, a);
+  if (a.parts > 1) hipLaunchKernelGGL((attention_join_kernel<T>), dim3(2048), dim3(256), 0, s, a);
   hipLaunchKernelGGL((attention_dq_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.heads)), dim3(256), 0, s, a);
 }
 template <typename T>
@@ -534,7 +594,7 @@ int ones_attention_forward(const void *q, int64_t q_stride, int64_t q_head_strid
 
 size_t ones_attention_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim) {
   if (check_attention(tokens, heads, kv_heads, dim, ONES_F16, sequences, 1.f)) return 0;
-  return attention_plan(tokens, sequences, heads, kv_heads).bytes;
+  return attention_plan(tokens, sequences, heads, kv_heads, dim).bytes;
 }
 
 int ones_attention_backward(const void *dout, int64_t do_stride, int64_t do_head_stride, const void *q, int64_t q_stride, int64_t q_head_stride,
@@ -550,7 +610,7 @@ int ones_attention_backward(const void *dout, int64_t do_stride, int64_t do_head
   if (int rc = check_head_rows(v, v_stride, v_head_stride, kv_heads, dim)) return rc;
   if (!offsets || !o || !lse || !dq || !dk || !dv) return ONES_E_INVALID_ARG;
   if (!aligned(o, 16) || !aligned(rest, 16) || !aligned(dq, 16) || !aligned(dk, 16) || !aligned(dv, 16)) return ONES_E_INVALID_ARG;
-  const AttentionPlan plan = attention_plan(tokens, sequences, heads, kv_heads);
+  const AttentionPlan plan = attention_plan(tokens, sequences, heads, kv_heads, dim);
   if (int rc = check_workspace(d_workspace, workspace_bytes, plan.bytes)) return rc;
   AttentionArgs a{};
   a.dout = dout; a.q = q; a.k = k; a.v = v;
@@ -559,7 +619,9 @@ int ones_attention_backward(const void *dout, int64_t do_stride, int64_t do_head
   a.o = const_cast<void *>(o); a.rest = const_cast<void *>(rest); a.lse = const_cast<float *>(lse); a.offsets = offsets;
   a.dq = dq; a.dk = dk; a.dv = dv;
   unsigned char *const w = static_cast<unsigned char *>(d_workspace);
-  a.delta = reinterpret_cast<float *>(w + plan.delta);
+  a.terms = reinterpret_cast<float2 *>(w + plan.terms);
+  a.partial = reinterpret_cast<float *>(w + plan.partial);
+  a.parts = static_cast<int32_t>(plan.parts);
   a.dout_norm = reinterpret_cast<float *>(w + plan.dout_norm);
   a.v_norm = reinterpret_cast<float *>(w + plan.slot_norms);
   a.sequences = static_cast<int32_t>(sequences); a.tokens = static_cast<int32_t>(tokens); a.heads = static_cast<int32_t>(heads);

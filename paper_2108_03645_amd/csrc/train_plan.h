@@ -319,6 +319,7 @@ inline int check_rotation(int64_t tokens, int64_t heads, int64_t kv_heads, int64
 
 // ---------------------------------------------------------------- attention --------
 constexpr int64_t kAttentionRows = 128;       // rows of a workgroup
+constexpr int64_t kPartsWanted = 2048;        // workgroups of the keys' gradients
 
 inline int check_attention(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, int64_t sequences, float scale) {
   if (tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || dim < 8 || dim % 8 || sequences < 0 || (type != ONES_F16 && type != ONES_BF16) ||
@@ -339,14 +340,19 @@ inline int check_token_rows(const void *p, int64_t stride, int64_t head_stride, 
   return stride > (int64_t{1} << 40) || head_stride > (int64_t{1} << 40) ? ONES_E_BOUNDS : ONES_OK;
 }
 struct AttentionPlan {
-  size_t delta, dout_norm, slot_norms, bytes;
+  int64_t parts;                              // of a group's heads, whose dk and dv are summed in 32 bits behind
+  size_t terms, dout_norm, slot_norms, partial, bytes;
 };
-inline AttentionPlan attention_plan(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads) {
+inline AttentionPlan attention_plan(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t dim) {
   AttentionPlan p{};
   const size_t rows = align_up(static_cast<size_t>(tokens) * heads * 4);
-  p.dout_norm = rows;
-  p.slot_norms = 2 * rows;
-  p.bytes = p.slot_norms + align_up(static_cast<size_t>(tokens / kAttentionRows + sequences + 2) * (heads + kv_heads) * 4);
+  const int64_t slots = tokens / kAttentionRows + sequences + 2;
+  p.parts = std::max<int64_t>(1, std::min(heads / kv_heads, kPartsWanted / std::max<int64_t>(1, ceil_div(tokens, kAttentionRows) * kv_heads)));
+  p.parts = ceil_div(heads / kv_heads, ceil_div(heads / kv_heads, p.parts));
+  p.dout_norm = 2 * rows;
+  p.slot_norms = 3 * rows;
+  p.partial = p.slot_norms + align_up(static_cast<size_t>(slots) * (heads + kv_heads) * 4);
+  p.bytes = p.partial + (p.parts > 1 ? align_up(static_cast<size_t>(tokens) * kv_heads * dim * p.parts * 8) : 0);
   return p;
 }
 
