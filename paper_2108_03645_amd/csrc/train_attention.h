@@ -94,6 +94,27 @@ __device__ __forceinline__ s16x8 rounded(f32x4 a, f32x4 b) {
   return __builtin_bit_cast(s16x8, v);
 }
 
+// What the rounding took from them.
+template <typename T>
+__device__ __forceinline__ s16x8 remainder(f32x4 a, f32x4 b, s16x8 of) {
+  const Pack<T, 8> w = __builtin_bit_cast(Pack<T, 8>, of);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) { a[r] -= static_cast<float>(w.v[r]); b[r] -= static_cast<float>(w.v[4 + r]); }
+  return rounded<T>(a, b);
+}
+
+template <int D, int TN>
+__device__ __forceinline__ bool any_nan(const f32x4 (&acc)[D / 16][TN]) {
+  bool found = false;
+#pragma unroll
+  for (int b = 0; b < D / 16; ++b)
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) found |= acc[b][n][r] != acc[b][n][r];
+  return found;
+}
+
 // Over the four lanes of a wave that hold the same n.
 __device__ __forceinline__ float across_max(float v) {
   const uint32_t b = __float_as_uint(v);

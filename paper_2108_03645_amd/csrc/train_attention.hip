@@ -39,6 +39,47 @@ __device__ __forceinline__ const T *at(const void *p, int64_t row, int64_t strid
 template <typename T>
 constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;
 
+// A weight of 0 does not take a row out of a product where that row has infinities or NaN, so those of a token would reach the rows
+// that it is masked for, as far as they share a step with it.  Each kernel looks for NaN in what it has summed.  Where there is some, the rows
+// that have it are summed once more without products of matrices, over what they do see, which is slow and right:
+//   sums[e] = sum over y of weights(r, y)[e] * element d of row(e, y)
+// for the rows 0 <= r < rows of the workgroup, elements d < dim, and 0 <= y < last(r).  has(r, d): whether element d of row r asks for it;
+// weights(r, y, w): whether row r sees y at all; write(r, d, sums).
+template <int N, class Has, class Last, class Weights, class Row, class Write>
+__device__ __forceinline__ void sum_by_rows(unsigned char *lds, int32_t rows, int32_t dim, Has has, Last last, Weights weights, Row row, Write write) {
+  struct Held {
+    float w[N];
+    int32_t seen;
+  };
+  Held *const held = reinterpret_cast<Held *>(lds);
+  const int d = threadIdx.x;
+  for (int32_t r = 0; r < rows; ++r) {
+    if (!__syncthreads_or(d < dim && has(r, d))) continue;
+    const int32_t end = last(r);
+    float sums[N] = {};
+    for (int32_t y0 = 0; y0 < end; y0 += 256) {
+      Held mine{};
+      if (y0 + d < end) mine.seen = weights(r, y0 + d, mine.w);
+      __syncthreads();
+      held[d] = mine;
+      __syncthreads();
+      if (d >= dim) continue;
+      for (int32_t y = y0; y < min(end, y0 + 256); ++y)
+        if (held[y - y0].seen) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) sums[e] += held[y - y0].w[e] * static_cast<float>(row(e, y)[d]);
+        }
+    }
+    if (d < dim) write(r, d, sums);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float dot(const T *a, const T *b, int32_t dim) {
+  float s = 0.f;
+  for (int i = 0; i < dim; ++i) s = __builtin_fmaf(static_cast<float>(a[i]), static_cast<float>(b[i]), s);
+  return s;
+}
+
 constexpr int kQueries = kAttentionRows, kKeys = 64;       // of a workgroup; of a step
 
 template <typename T, int D, bool REST>
@@ -76,20 +117,15 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
 #pragma unroll
   for (int b = 0; b < D / 16; ++b) across[b] = Tile::across(lane, b);
   const float c = a.scale * kLog2e;
-  f32x4 acc[D / 16][2], total[2];             // total: the rounded exponentials' sums, by a product with ones
+  f32x4 acc[D / 16][2];
   float top[2], sum[2];
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     top[n] = -INFINITY;
     sum[n] = 0.f;
-    total[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) acc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  Pack<T, 8> one;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) one.v[i] = static_cast<T>(1.f);
-  const s16x8 ones = __builtin_bit_cast(s16x8, one);
   const int steps = (rows.at + count + kKeys - 1) / kKeys, first_row = rows.at + mine;
   for (int step = 0; step < steps; ++step) {
     meet<0>();
@@ -123,7 +159,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
             if (b * 16 + (lane >> 4) * 4 + r > row) z[b][n][r] = -INFINITY;
       }
     }
-    s16x8 p[2][2];
+    s16x8 p[2][2], lost[2][2];                // lost: what the rounding takes from the exponentials
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       float most = z[0][n][0];
@@ -135,7 +171,6 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
       if (__any(most > top[n])) {
         const float factor = most == top[n] ? 1.f : __builtin_amdgcn_exp2f((top[n] - most) * c);
         sum[n] *= factor;
-        total[n] *= factor;
 #pragma unroll
         for (int b = 0; b < D / 16; ++b) acc[b][n] *= factor;
         top[n] = most;
@@ -149,7 +184,10 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
           sum[n] += z[b][n][r];
         }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) p[h][n] = rounded<T>(z[2 * h][n], z[2 * h + 1][n]);
+      for (int h = 0; h < 2; ++h) {
+        p[h][n] = rounded<T>(z[2 * h][n], z[2 * h + 1][n]);
+        if constexpr (REST) lost[h][n] = remainder<T>(z[2 * h][n], z[2 * h + 1][n], p[h][n]);
+      }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -157,11 +195,10 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
       for (int b = 0; b < D / 16; ++b) {
         const s16x8 f = Tile::read_across(vs, h * 32, across[b]);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) acc[b][n] = mfma<T>(f, p[h][n], acc[b][n]);
-      }
-      if constexpr (REST) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) total[n] = mfma<T>(ones, p[h][n], total[n]);
+        for (int n = 0; n < 2; ++n) {
+          acc[b][n] = mfma<T>(f, p[h][n], acc[b][n]);
+          if constexpr (REST) acc[b][n] = mfma<T>(f, lost[h][n], acc[b][n]);
+        }
       }
     }
   }
@@ -169,11 +206,28 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const float s = across_sum(sum[n]);
-    factor[n] = 1.f / (REST ? total[n][0] : s);
+    factor[n] = 1.f / s;
     const int r = mine + n * 16 + (lane & 15);
     if (lane < 16 && r < count) lse[r] = (top[n] * c - kShift<T> + __builtin_amdgcn_logf(s)) * kLn2;
   }
   write_rows<T, D, 2, REST>(acc, factor, o + mine * out_stride, rest ? rest + mine * out_stride : nullptr, out_stride, count - mine, a.dim, lane);
+  if (__syncthreads_or(any_nan<D, 2>(acc))) {
+    __syncthreads();
+    const T *const q0 = at<T>(a.q, here, a.q_stride, turn.head, a.q_head), *const k0 = at<T>(a.k, rows.first, a.k_stride, turn.kv, a.k_head);
+    const T *const v0 = at<T>(a.v, rows.first, a.v_stride, turn.kv, a.v_head);
+    sum_by_rows<1>(
+        lds, count, a.dim, [&](int32_t r, int d) { const float x = static_cast<float>(o[r * out_stride + d]); return x != x && lse[r] == lse[r]; },
+        [&](int32_t r) { return rows.at + r + 1; },
+        [&](int32_t r, int32_t y, float (&w)[1]) {
+          w[0] = __builtin_amdgcn_exp2f(dot(q0 + r * a.q_stride, k0 + y * a.k_stride, a.dim) * c - lse[r] * kLog2e);
+          return true;
+        },
+        [&](int, int32_t y) { return v0 + y * a.v_stride; },
+        [&](int32_t r, int d, const float (&sums)[1]) {
+          o[r * out_stride + d] = static_cast<T>(sums[0]);
+          if (rest) rest[r * out_stride + d] = static_cast<T>(sums[0] - static_cast<float>(static_cast<T>(sums[0])));
+        });
+  }
 }
 
 // delta of every row of a slot and head, and its |do|; of a key head, the largest |v|.  (fp16 scales by the norms, see unit_of().)
@@ -358,6 +412,23 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
     }
   }
   write_rows<T, D, 2>(acc, factor, dq + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+  if (__syncthreads_or(any_nan<D, 2>(acc))) {
+    __syncthreads();
+    const T *const q0 = at<T>(a.q, here, a.q_stride, turn.head, a.q_head), *const k0 = at<T>(a.k, rows.first, a.k_stride, turn.kv, a.k_head);
+    const T *const g0 = at<T>(a.dout, here, a.do_stride, turn.head, a.do_head), *const v0 = at<T>(a.v, rows.first, a.v_stride, turn.kv, a.v_head);
+    const float2 *const terms = a.terms + static_cast<int64_t>(turn.head) * a.tokens + here;
+    sum_by_rows<1>(
+        lds, count, a.dim,
+        [&](int32_t r, int d) { const float x = static_cast<float>(dq[r * out_stride + d]), t = terms[r].x + terms[r].y; return x != x && t == t; },
+        [&](int32_t r) { return rows.at + r + 1; },
+        [&](int32_t r, int32_t y, float (&w)[1]) {
+          const float p = __builtin_amdgcn_exp2f(dot(q0 + r * a.q_stride, k0 + y * a.k_stride, a.dim) * c - terms[r].x);
+          w[0] = p * (dot(g0 + r * a.do_stride, v0 + y * a.v_stride, a.dim) - terms[r].y);
+          return true;
+        },
+        [&](int, int32_t y) { return k0 + y * a.k_stride; },
+        [&](int32_t r, int d, const float (&sums)[1]) { dq[r * out_stride + d] = static_cast<T>(sums[0] * a.scale); });
+  }
 }
 
 constexpr int kStepRows = 32;                 // queries of a step of the keys' gradients
@@ -494,13 +565,14 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
   if (a.parts == 1) {
     write_rows<T, D, 2>(of_k, k_factor, dk + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
     write_rows<T, D, 2>(of_v, v_factor, dv + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
-    return;
   }
+  float *const partial = a.partial + ((static_cast<int64_t>(part) * a.tokens + here) * a.kv_heads + kv) * 2 * a.dim;
+  const int64_t partial_stride = static_cast<int64_t>(a.kv_heads) * 2 * a.dim;
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     const int r = mine + n * 16 + (lane & 15);
-    if (r >= count) continue;
-    float *to = a.partial + ((static_cast<int64_t>(part) * a.tokens + here + r) * a.kv_heads + kv) * 2 * a.dim;
+    if (a.parts == 1 || r >= count) continue;
+    float *to = partial + r * partial_stride;
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) {
       const int i = b * 16 + (lane >> 4) * 4;
@@ -508,6 +580,40 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
       *reinterpret_cast<f32x4 *>(to + i) = of_k[b][n] * k_factor[n];
       *reinterpret_cast<f32x4 *>(to + a.dim + i) = of_v[b][n] * v_factor[n];
     }
+  }
+  if (__syncthreads_or(any_nan<D, 2>(of_k) || any_nan<D, 2>(of_v))) {
+    __syncthreads();
+    const T *const k0 = at<T>(a.k, here, a.k_stride, kv, a.k_head), *const v0 = at<T>(a.v, here, a.v_stride, kv, a.v_head);
+    // the queries of all heads in a row, from the tile's first key on
+    sum_by_rows<2>(
+        lds, count, a.dim,
+        [&](int32_t r, int d) {
+          const float x = a.parts == 1 ? static_cast<float>(dk[r * out_stride + d]) + static_cast<float>(dv[r * out_stride + d])
+                                       : partial[r * partial_stride + d] + partial[r * partial_stride + a.dim + d];
+          const float own = dot(k0 + r * a.k_stride, v0 + r * a.v_stride, a.dim);
+          return x != x && own - own == 0.f;  // a key or value that is not finite has no other gradient
+        },
+        [&](int32_t) { return all_steps ? heads * left : 0; },
+        [&](int32_t r, int32_t y, float (&w)[2]) {
+          const int32_t h = head0 + y / left, i = y % left;
+          if (i < r) return false;
+          const float2 terms = a.terms[static_cast<int64_t>(h) * a.tokens + here + i];
+          w[1] = __builtin_amdgcn_exp2f(dot(at<T>(a.q, here + i, a.q_stride, h, a.q_head), k0 + r * a.k_stride, a.dim) * c - terms.x);
+          w[0] = w[1] * (dot(at<T>(a.dout, here + i, a.do_stride, h, a.do_head), v0 + r * a.v_stride, a.dim) - terms.y) * a.scale;
+          return true;
+        },
+        [&](int e, int32_t y) {
+          return e ? at<T>(a.dout, here + y % left, a.do_stride, head0 + y / left, a.do_head) : at<T>(a.q, here + y % left, a.q_stride, head0 + y / left, a.q_head);
+        },
+        [&](int32_t r, int d, const float (&sums)[2]) {
+          if (a.parts > 1) {
+            partial[r * partial_stride + d] = sums[0];
+            partial[r * partial_stride + a.dim + d] = sums[1];
+          } else {
+            dk[r * out_stride + d] = static_cast<T>(sums[0]);
+            dv[r * out_stride + d] = static_cast<T>(sums[1]);
+          }
+        });
   }
 }
 

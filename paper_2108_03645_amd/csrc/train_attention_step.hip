@@ -64,7 +64,7 @@ __device__ __forceinline__ void arrived() {
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
+__global__ __launch_bounds__(kStepWaves * 64) void step_kernel(StepArgs a) {
   using Load = WaveTile<D>;
   using Tile = typename Load::Tile;
   constexpr int waves = kStepWaves;
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
   if (length < 0 || length >= a.capacity) {
     const float fill = length < 0 ? 0.f : NAN;
     if (split == 0)
-      for (int i = threadIdx.x; i < heads * a.dim; i += 256) out[i] = static_cast<T>(fill);
+      for (int i = threadIdx.x; i < heads * a.dim; i += kStepWaves * 64) out[i] = static_cast<T>(fill);
     return;
   }
   // whole tiles of the workgroup, evenly over the parts
@@ -107,6 +107,7 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
     k.load(ks + static_cast<int64_t>(first) * k.row_bytes, length - first, mine + to * 2 * Load::bytes);
     v.load(vs + static_cast<int64_t>(first) * v.row_bytes, length - first, mine + to * 2 * Load::bytes + Load::bytes);
   };
+  if (begin < end) load(begin, 0);
   s16x8 q[D / 32];
   read_rows<D>(static_cast<const T *>(a.q) + b * a.q_stride + head * a.q_head, a.q_head, heads, a.dim, lane, q);
   const float c = a.scale * kLog2e;
@@ -137,7 +138,6 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
                   : static_cast<T *>(a.keys) + b * a.keys_batch + length * a.keys_stride + kv * a.keys_head;
     if (d < a.dim) *reinterpret_cast<Pack<uint32_t, 4> *>(to + d) = *reinterpret_cast<const Pack<uint32_t, 4> *>((which ? v_new : k_new) + d);
   }
-  if (begin < end) load(begin, 0);
   int along[D / 32], across[D / 16];
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) along[s] = Tile::along(lane, s);
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
   for (int i = 0; i < D / 16; ++i)
     *reinterpret_cast<f32x4 *>(parts + ((wave * 16 + (lane & 15)) * D + i * 16 + (lane >> 4) * 4)) = acc[i];
   __syncthreads();
-  for (int i = threadIdx.x; i < heads * D; i += 256) {
+  for (int i = threadIdx.x; i < heads * D; i += kStepWaves * 64) {
     const int h = i / D, d = i % D;
     float most = tops[0][h];
 #pragma unroll
@@ -221,32 +221,48 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs a) {
   }
 }
 
-// The parts of a head, in order.
+// The parts of a head: 128 elements by 8 groups of parts, added up in order.
 template <typename T>
-__global__ __launch_bounds__(128) void step_join_kernel(StepArgs a) {
-  const int32_t b = blockIdx.x / a.heads;
-  const int32_t length = a.lengths[b];
-  if (length < 0 || length >= a.capacity || static_cast<int>(threadIdx.x) >= a.dim) return;
+__global__ __launch_bounds__(1024) void step_join_kernel(StepArgs a) {
+  __shared__ float factors[kStepMaxSplits], most_of[16], sums[8], outputs[8][128];
+  const int32_t b = blockIdx.x / a.heads, length = a.lengths[b];
+  if (length < 0 || length >= a.capacity) return;
   const int64_t at = static_cast<int64_t>(blockIdx.x) * a.splits;
-  float most = a.tops[at];
-  for (int i = 1; i < a.splits; ++i) most = fmaxf(most, a.tops[at + i]);
+  const int i = threadIdx.x, d = i % 128, group = i / 128;
+  const float top = i < a.splits ? a.tops[at + i] : -INFINITY;       // -infinity: a part without keys, whose sums are not there
+  float most = across_max(top);
+#pragma unroll
+  for (int m = 1; m < 16; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+  if (i % kWave == 0) most_of[i / kWave] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) most = fmaxf(most, most_of[w]);
+  if (i < a.splits) factors[i] = i && top == -INFINITY ? 0.f : top == most ? 1.f : __builtin_amdgcn_exp2f((top - most) * (a.scale * kLog2e));
+  __syncthreads();
   float sum = 0.f, x = 0.f;
-  for (int i = 0; i < a.splits; ++i) {
-    const float top = a.tops[at + i];
-    if (i && top == -INFINITY) continue;      // none
-    const float f = top == most ? 1.f : __builtin_amdgcn_exp2f((top - most) * (a.scale * kLog2e));
-    sum += a.sums[at + i] * f;
-    x += a.outputs[(at + i) * a.dim + threadIdx.x] * f;
+  const int e = min(d, a.dim - 1);
+#pragma unroll 4
+  for (int p = group; p < a.splits; p += 8) {
+    const float f = factors[p], s = a.sums[at + p], y = a.outputs[(at + p) * a.dim + e];
+    sum += f == 0.f ? 0.f : s * f;
+    x += f == 0.f ? 0.f : y * f;
   }
-  static_cast<T *>(a.o)[static_cast<int64_t>(blockIdx.x) * a.dim + threadIdx.x] = static_cast<T>(x / sum);
+  outputs[group][d] = x;
+  if (d == 0) sums[group] = sum;
+  __syncthreads();
+  if (group || d >= a.dim) return;
+  sum = sums[0];
+#pragma unroll
+  for (int g = 1; g < 8; ++g) { x += outputs[g][d]; sum += sums[g]; }
+  static_cast<T *>(a.o)[static_cast<int64_t>(blockIdx.x) * a.dim + d] = static_cast<T>(x / sum);
 }
 
 template <typename T>
 void launch(const StepArgs &a, hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.batch) * a.splits * a.blocks_of_heads * a.kv_heads)), block(256);
+  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.batch) * a.splits * a.blocks_of_heads * a.kv_heads)), block(kStepWaves * 64);
   if (a.dim <= 64) hipLaunchKernelGGL((step_kernel<T, 64>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((step_kernel<T, 128>), grid, block, 0, s, a);
-  if (a.splits > 1) hipLaunchKernelGGL((step_join_kernel<T>), dim3(static_cast<uint32_t>(a.batch * a.heads)), dim3(128), 0, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((step_join_kernel<T>), dim3(static_cast<uint32_t>(a.batch * a.heads)), dim3(1024), 0, s, a);
 }
 
 }  // namespace

@@ -357,7 +357,8 @@ inline AttentionPlan attention_plan(int64_t tokens, int64_t sequences, int64_t h
 }
 
 // ------------------------------------------- a token's attention over a cache --------
-constexpr int64_t kStepKeys = 32, kStepWaves = 4, kStepHeads = 16;         // keys of a wave's tile; waves; query heads of a workgroup
+constexpr int64_t kStepKeys = 32, kStepWaves = 2, kStepHeads = 16;         // keys of a wave's tile; waves; query heads of a workgroup
+constexpr int64_t kStepMaxSplits = 512;
 
 struct StepPlan {
   int64_t blocks_of_heads, splits;
@@ -366,8 +367,8 @@ struct StepPlan {
 inline StepPlan step_plan(int64_t batch, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim) {
   StepPlan p{};
   p.blocks_of_heads = ceil_div(heads / kv_heads, kStepHeads);
-  const int64_t chains = std::max<int64_t>(1, batch * kv_heads * p.blocks_of_heads), tiles = ceil_div(capacity, kStepKeys * kStepWaves);
-  p.splits = std::max<int64_t>(1, std::min(ceil_div(512, chains), tiles / 2));
+  const int64_t chains = std::max<int64_t>(1, batch * kv_heads * p.blocks_of_heads);
+  p.splits = std::max<int64_t>(1, std::min(ceil_div(kStepMaxSplits, chains), capacity / 512));
   if (p.splits > 1) {
     const size_t parts = static_cast<size_t>(batch) * heads * p.splits;
     p.sums = align_up(parts * 4);

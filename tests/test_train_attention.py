@@ -194,6 +194,38 @@ def test_a_sequence_does_not_see_its_neighbours(train):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_a_row_does_not_see_what_comes_behind_it(train, bad, dtype):
+    """Infinities and NaN of a token reach its own row of o and dq and those behind it, its own of dk and dv and those before it, and no other.
+    Rows that share a step with it are summed another way: either way is off by a share of h, so they differ by up to two (rest: by as much as o)."""
+    def alike(got, right, what):
+        size = want[0].float().norm() if what[1] == "rest" else right.float().norm()
+        assert got.isfinite().all() and (got.float() - right.float()).norm() <= 2 * HALF[dtype] * size, what
+
+    n, at = 200, 77
+    clean = inputs(30, n, 2, 1, 128, dtype)
+    ends = offsets_of([n])
+    offsets = torch.tensor(ends, device="cuda", dtype=torch.int32)
+    want = check(train, *clean[:3], ends, clean[3])
+    for which in range(4):                                           # q, k, v, do
+        t = [x.clone() for x in clean]
+        t[which][at, 0, 5:7] = bad
+        o, lse, rest = train.attention_forward(*t[:3], offsets, keep_rest=True)
+        dq, dk, dv = train.attention_backward(t[3], *t[:3], o, lse, rest, offsets)
+        for name, got, right in (("o", o, want[0]), ("lse", lse.t(), want[1].t()), ("rest", rest, want[2]), ("dq", dq, want[3])):
+            same = [i for i in range(n) if i < at or (which in (0, 3) and i != at)]
+            alike(got[same], right[same], (which, name))
+        if which in (0, 3):                                          # of a query: only the keys up to it
+            alike(dk[at + 1:], want[4][at + 1:], (which, "dk"))
+            alike(dv[at + 1:], want[5][at + 1:], (which, "dv"))
+        if which == 2:
+            assert not o[at:, 0, 5:7].isfinite().any() and o[at:, 0, 7:].isfinite().all()
+        elif which == 3:
+            assert not dv[:at + 1, 0, 5:7].isfinite().any() and dv[:, 0, 7:].isfinite().all()
+
+
+@gpu
 def test_many_sequences_and_offsets_that_do_not_rise(train):
     lengths = [(i * 7) % 4 for i in range(9001)]
     q, k, v, do = inputs(7, sum(lengths), 1, 1, 8, FP16)
