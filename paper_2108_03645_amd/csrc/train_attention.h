@@ -23,7 +23,9 @@ __device__ __forceinline__ void load_words_to_lds(const unsigned char *base, uin
 }
 
 // A tile of ROWS rows of D elements (a head's rows of consecutive tokens).  The 16-byte pieces of a row are exchanged by the row's
-// number so that the lanes of a read meet different banks, whichever way they read: eight rows at one piece, or two pieces of four rows.
+// number so that the lanes of a read meet different banks (of 64, 256 bytes at a time), whichever way they read: two pieces of eight rows, or
+// along the rows one piece of rows 0..3 and 12..15 with the next of rows 4..11 (lanes 0..3, 12..15 and 20..27 read at the same time).  (D 64: two
+// rows are 256 bytes.)
 template <int D, int ROWS, int THREADS>
 struct RowTile {
   static constexpr int row = D * 2, bytes = ROWS * row, pieces = D / 8, at_once = THREADS / pieces, loads = (ROWS + at_once - 1) / at_once;
@@ -33,7 +35,9 @@ struct RowTile {
   uint32_t row_bytes, offset;                 // between rows in memory; what this thread loads, kOutside beyond a row's end
   int32_t left;                               // rows from base on
 
-  static __device__ __forceinline__ int exchange(int r) { return (((r & 3) << 1) | ((r >> 2) & 1) | (pieces > 8 ? r & 8 : 0)); }
+  static __device__ __forceinline__ int exchange(int r) {
+    return pieces > 8 ? ((r & 7) << 1) ^ (r & 8 ? 9 : 0) : (r & 6) ^ (r & 8 ? 5 : 0);
+  }
   __device__ __forceinline__ void start(const void *first, int64_t stride, int32_t rows, int32_t dim) {
     const int r = static_cast<int>(threadIdx.x) / pieces, p = (static_cast<int>(threadIdx.x) % pieces) ^ exchange(r);
     base = static_cast<const unsigned char *>(first);

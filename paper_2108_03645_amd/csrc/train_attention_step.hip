@@ -37,7 +37,7 @@ constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;      // as in train_atte
 template <int D>
 struct WaveTile {
   using Tile = RowTile<D, 32, 256>;           // places of the reads
-  static constexpr int bytes = Tile::bytes, pieces = D / 8, at_once = kWave / pieces, loads = 32 / at_once, kinds = at_once < 8 ? 4 : 1;
+  static constexpr int bytes = Tile::bytes, pieces = D / 8, at_once = kWave / pieces, loads = 32 / at_once, kinds = 16 / at_once;
   static_assert(at_once == 4 || at_once == 8);
   uint32_t row_bytes, offset[kinds];
   __device__ __forceinline__ void start(int64_t stride, int32_t dim, int lane) {
