@@ -144,9 +144,13 @@ __device__ __forceinline__ float across_sum(float v) {
 __host__ __device__ inline int64_t slots_of(int64_t tokens, int64_t sequences, int64_t tile) { return tokens / tile + sequences + 2; }
 
 struct Rows {
-  int32_t first, length, at;                  // of the sequence: its first row, its rows; the slot's first row in it
+  int32_t sequence, first, length, at;        // the sequence: its first row, its rows; the slot's first row in it
   bool real;                                  // a sequence; or rows outside all of them
 };
+// The first slot of sequence s, which begins at row `first`.
+template <int TILE>
+__device__ __forceinline__ int32_t slot_of(int32_t s, int32_t first) { return s < 0 ? 0 : first / TILE + s + 1; }
+
 template <int TILE>
 __device__ __forceinline__ Rows rows_of(const int32_t *offsets, int32_t sequences, int32_t tokens, int32_t slot) {
   const int lane = static_cast<int>(threadIdx.x) % kWave;
@@ -154,7 +158,7 @@ __device__ __forceinline__ Rows rows_of(const int32_t *offsets, int32_t sequence
   int32_t lo = 0, n = sequences + 1;          // the number of s whose first slot is not above this one, 64 probes at a time
   while (n > 0) {
     const int32_t stride = (n + kWave - 1) / kWave, mine = lane * stride + stride - 1;
-    const bool below = mine < n && offset(lo + mine) / TILE + lo + mine + 1 <= slot;
+    const bool below = mine < n && slot_of<TILE>(lo + mine, offset(lo + mine)) <= slot;
     const int32_t c = __popcll(__ballot(below));
     lo += c * stride;
     n = stride == 1 ? 0 : min(stride, n - c * stride);
@@ -165,8 +169,8 @@ __device__ __forceinline__ Rows rows_of(const int32_t *offsets, int32_t sequence
   const int32_t end = s < 0 ? offset(0) : s >= sequences ? tokens : offset(s + 1);
   r.first = __builtin_amdgcn_readfirstlane(r.first);
   r.length = max(__builtin_amdgcn_readfirstlane(end) - r.first, 0);
-  const int32_t slots = s < 0 ? 0 : r.first / TILE + s + 1;
-  r.at = (slot - slots) * TILE;
+  r.sequence = s;
+  r.at = (slot - slot_of<TILE>(s, r.first)) * TILE;
   r.real = s >= 0 && s < sequences;
   return r;
 }

@@ -39,6 +39,8 @@ __device__ __forceinline__ const T *at(const void *p, int64_t row, int64_t strid
 template <typename T>
 constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;
 
+constexpr float kSlack = 6.f;                 // 2^(kShift + kSlack) is far from fp16's end
+
 // A weight of 0 does not take a row out of a product where that row has infinities or NaN, so those of a token would reach the rows
 // that it is masked for, as far as they share a step with it.  Each kernel looks for NaN in what it has summed.  Where there is some, the rows
 // that have it are summed once more without products of matrices, over what they do see, which is slow and right:
@@ -51,20 +53,21 @@ __device__ __forceinline__ void sum_by_rows(unsigned char *lds, int32_t rows, in
     float w[N];
     int32_t seen;
   };
+  constexpr int kChunk = 256;
   Held *const held = reinterpret_cast<Held *>(lds);
   const int d = threadIdx.x;
   for (int32_t r = 0; r < rows; ++r) {
     if (!__syncthreads_or(d < dim && has(r, d))) continue;
     const int32_t end = last(r);
     float sums[N] = {};
-    for (int32_t y0 = 0; y0 < end; y0 += 256) {
+    for (int32_t y0 = 0; y0 < end; y0 += kChunk) {
       Held mine{};
-      if (y0 + d < end) mine.seen = weights(r, y0 + d, mine.w);
+      if (d < kChunk && y0 + d < end) mine.seen = weights(r, y0 + d, mine.w);
       __syncthreads();
-      held[d] = mine;
+      if (d < kChunk) held[d] = mine;
       __syncthreads();
       if (d >= dim) continue;
-      for (int32_t y = y0; y < min(end, y0 + 256); ++y)
+      for (int32_t y = y0; y < min(end, y0 + kChunk); ++y)
         if (held[y - y0].seen) {
 #pragma unroll
           for (int e = 0; e < N; ++e) sums[e] += held[y - y0].w[e] * static_cast<float>(row(e, y)[d]);
@@ -84,7 +87,8 @@ constexpr int kQueries = kAttentionRows, kKeys = 64;       // of a workgroup; of
 
 template <typename T, int D, bool REST>
 __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs a) {
-  using Tile = RowTile<D, kKeys, 256>;
+  constexpr int TN = 2, kThreads = 256, kMine = 16 * TN;
+  using Tile = RowTile<D, kKeys, kThreads>;
   __shared__ __attribute__((aligned(256))) unsigned char lds[4 * Tile::bytes];
   const Turn turn = turn_of(blockIdx.x, a.heads, a.kv_heads);
   const int32_t last_slot = static_cast<int32_t>(slots_of(a.tokens, a.sequences, kQueries)) - 1;
@@ -98,7 +102,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
   if (!rows.real) {
     write_zeros(o, out_stride, count, a.dim);
     write_zeros(rest, out_stride, count, a.dim);
-    for (int i = threadIdx.x; i < count; i += 256) lse[i] = -INFINITY;
+    for (int i = threadIdx.x; i < count; i += kThreads) lse[i] = -INFINITY;
     return;
   }
   Tile k, v;
@@ -106,10 +110,10 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
   v.start(at<T>(a.v, rows.first, a.v_stride, turn.kv, a.v_head), a.v_stride, rows.length, a.dim);
   k.load(lds);
   v.load(lds + 2 * Tile::bytes);
-  const int mine = wave * 32;                 // the wave's first row in the tile
-  s16x8 q[2][D / 32];
+  const int mine = wave * kMine;                 // the wave's first row in the tile
+  s16x8 q[TN][D / 32];
 #pragma unroll
-  for (int n = 0; n < 2; ++n)
+  for (int n = 0; n < TN; ++n)
     read_rows<D>(at<T>(a.q, here + mine + n * 16, a.q_stride, turn.head, a.q_head), a.q_stride, count - mine - n * 16, a.dim, lane, q[n]);
   int along[D / 32], across[D / 16];
 #pragma unroll
@@ -117,10 +121,10 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
 #pragma unroll
   for (int b = 0; b < D / 16; ++b) across[b] = Tile::across(lane, b);
   const float c = a.scale * kLog2e;
-  f32x4 acc[D / 16][2];
-  float top[2], sum[2];
+  f32x4 acc[D / 16][TN];
+  float top[TN], sum[TN];
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
+  for (int n = 0; n < TN; ++n) {
     top[n] = -INFINITY;
     sum[n] = 0.f;
 #pragma unroll
@@ -135,22 +139,22 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
       v.load(lds + (2 + (~step & 1)) * Tile::bytes);
     }
     const int key = step * kKeys;
-    if (key > first_row + 31) continue;       // keys behind all of the wave's rows
-    f32x4 z[4][2];
+    if (key > first_row + kMine - 1) continue;       // keys behind all of the wave's rows
+    f32x4 z[4][TN];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n) z[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < TN; ++n) z[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) {
         const s16x8 f = Tile::read_along(ks, b * 16, along[s]);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) z[b][n] = mfma<T>(f, q[n][s], z[b][n]);
+        for (int n = 0; n < TN; ++n) z[b][n] = mfma<T>(f, q[n][s], z[b][n]);
       }
     }
     if (key + kKeys - 1 > first_row) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
+      for (int n = 0; n < TN; ++n) {
         const int row = first_row + n * 16 + (lane & 15) - key;
 #pragma unroll
         for (int b = 0; b < 4; ++b)
@@ -159,30 +163,44 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
             if (b * 16 + (lane >> 4) * 4 + r > row) z[b][n][r] = -INFINITY;
       }
     }
-    s16x8 p[2][2], lost[2][2];                // lost: what the rounding takes from the exponentials
+    // the largest score: taken over where it has grown by more than 2^kSlack, which exponentials may exceed 1 by
+    float most[TN];
+    bool grown = false;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      float most = z[0][n][0];
+    for (int n = 0; n < TN; ++n) {
+      float m[2] = {fmaxf(z[0][n][0], z[0][n][1]), fmaxf(z[1][n][0], z[1][n][1])};
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+      for (int h = 0; h < 2; ++h) {
+        m[h] = fmaxf(fmaxf(m[h], z[h][n][2]), z[h][n][3]);
+        m[h] = fmaxf(fmaxf(m[h], z[2 + h][n][0]), z[2 + h][n][1]);
+        m[h] = fmaxf(fmaxf(m[h], z[2 + h][n][2]), z[2 + h][n][3]);
+      }
+      most[n] = across_max(fmaxf(m[0], m[1]));
+      grown |= (most[n] - top[n]) * c > kSlack;
+    }
+    if (__any(grown)) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) most = fmaxf(most, z[b][n][r]);
-      most = fmaxf(top[n], across_max(most));
-      if (__any(most > top[n])) {
-        const float factor = most == top[n] ? 1.f : __builtin_amdgcn_exp2f((top[n] - most) * c);
+      for (int n = 0; n < TN; ++n) {
+        const float next = fmaxf(top[n], most[n]), factor = next == top[n] ? 1.f : __builtin_amdgcn_exp2f((top[n] - next) * c);
         sum[n] *= factor;
 #pragma unroll
         for (int b = 0; b < D / 16; ++b) acc[b][n] *= factor;
-        top[n] = most;
+        top[n] = next;
       }
+    }
+    s16x8 p[2][TN], lost[2][TN];              // lost: what the rounding takes from the exponentials
+#pragma unroll
+    for (int n = 0; n < TN; ++n) {
       const float base = (top[n] == -INFINITY ? 0.f : top[n] * c) - kShift<T>;
+      float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           z[b][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][n][r], c, -base));
-          sum[n] += z[b][n][r];
+          sums[r] += z[b][n][r];
         }
+      sum[n] += (sums[0] + sums[1]) + (sums[2] + sums[3]);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         p[h][n] = rounded<T>(z[2 * h][n], z[2 * h + 1][n]);
@@ -195,23 +213,23 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
       for (int b = 0; b < D / 16; ++b) {
         const s16x8 f = Tile::read_across(vs, h * 32, across[b]);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < TN; ++n) {
           acc[b][n] = mfma<T>(f, p[h][n], acc[b][n]);
           if constexpr (REST) acc[b][n] = mfma<T>(f, lost[h][n], acc[b][n]);
         }
       }
     }
   }
-  float factor[2];
+  float factor[TN];
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
+  for (int n = 0; n < TN; ++n) {
     const float s = across_sum(sum[n]);
     factor[n] = 1.f / s;
     const int r = mine + n * 16 + (lane & 15);
     if (lane < 16 && r < count) lse[r] = (top[n] * c - kShift<T> + __builtin_amdgcn_logf(s)) * kLn2;
   }
-  write_rows<T, D, 2, REST>(acc, factor, o + mine * out_stride, rest ? rest + mine * out_stride : nullptr, out_stride, count - mine, a.dim, lane);
-  if (__syncthreads_or(any_nan<D, 2>(acc))) {
+  write_rows<T, D, TN, REST>(acc, factor, o + mine * out_stride, rest ? rest + mine * out_stride : nullptr, out_stride, count - mine, a.dim, lane);
+  if (__syncthreads_or(any_nan<D, TN>(acc))) {
     __syncthreads();
     const T *const q0 = at<T>(a.q, here, a.q_stride, turn.head, a.q_head), *const k0 = at<T>(a.k, rows.first, a.k_stride, turn.kv, a.k_head);
     const T *const v0 = at<T>(a.v, rows.first, a.v_stride, turn.kv, a.v_head);
@@ -335,7 +353,7 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
   float v_most = 0.f;
   if constexpr (__is_same(T, f16)) {
     const int32_t all = a.heads + a.kv_heads;
-    v_most = largest_norm(a.v_norm, all, a.heads + turn.kv, 1, slot - rows.at / kQueries, (rows.length + kQueries - 1) / kQueries);
+    v_most = largest_norm(a.v_norm, all, a.heads + turn.kv, 1, slot_of<kQueries>(rows.sequence, rows.first), (rows.length + kQueries - 1) / kQueries);
   }
   s16x8 q[2][D / 32], g[2][D / 32];
   float lse[2], delta[2], unit[2], factor[2];
@@ -431,22 +449,27 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
   }
 }
 
-constexpr int kStepRows = 32;                 // queries of a step of the keys' gradients
+constexpr int kStepRows = 32, kKeyRows = kAttentionKeys;        // of the keys' gradients: queries of a step; keys of a workgroup
+#ifndef DKV_TN
+#define DKV_TN 1
+#define DKV_OCC 3
+#endif
 
 template <typename T, int D>
-constexpr int kKeysLds = 4 * RowTile<D, kStepRows, 256>::bytes + 2 * kStepRows * 8;
+constexpr int kKeysLds = 4 * RowTile<D, kStepRows, 4 * kKeyRows / DKV_TN>::bytes + 2 * kStepRows * 8;
 
 template <typename T, int D>
 __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_t id, unsigned char *lds) {
-  using Tile = RowTile<D, kStepRows, 256>;
+  constexpr int TN = DKV_TN, kMine = 16 * TN;
+  using Tile = RowTile<D, kStepRows, 4 * kKeyRows / TN>;
   const int32_t kv = static_cast<int32_t>(id % a.kv_heads), group = a.heads / a.kv_heads;
   id /= a.kv_heads;
   const int32_t part = static_cast<int32_t>(id % a.parts), slot = static_cast<int32_t>(id / a.parts);
-  const Rows rows = rows_of<kQueries>(a.offsets, a.sequences, a.tokens, slot);
+  const Rows rows = rows_of<kKeyRows>(a.offsets, a.sequences, a.tokens, slot);
   if (rows.at >= rows.length || rows.at < 0) return;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const int64_t out_stride = static_cast<int64_t>(a.kv_heads) * a.dim;
-  const int32_t here = rows.first + rows.at, count = min(rows.length - rows.at, kQueries);
+  const int32_t here = rows.first + rows.at, count = min(rows.length - rows.at, kKeyRows);
   T *const dk = const_cast<T *>(at<T>(a.dk, here, out_stride, kv, a.dim)), *const dv = const_cast<T *>(at<T>(a.dv, here, out_stride, kv, a.dim));
   if (!rows.real) {
     if (part) return;
@@ -454,25 +477,25 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     write_zeros(dv, out_stride, count, a.dim);
     return;
   }
-  const int mine = wave * 32;
+  const int mine = wave * kMine;
   const float c = a.scale * kLog2e;
   float unit = 1.f;
   if constexpr (__is_same(T, f16)) {
-    const int32_t all = a.heads + a.kv_heads, first = slot - rows.at / kQueries, slots = (rows.length + kQueries - 1) / kQueries;
+    const int32_t all = a.heads + a.kv_heads, first = slot_of<kQueries>(rows.sequence, rows.first), slots = (rows.length + kQueries - 1) / kQueries;
     unit = unit_of(2.f * largest_norm(a.v_norm, all, kv * group, group, first, slots) * largest_norm(a.v_norm, all, a.heads + kv, 1, first, slots));
   }
   constexpr float kWeights = __is_same(T, f16) ? 16384.f : 1.f;       // the unit of p, at most 1 and a rounding
-  s16x8 k[2][D / 32], v[2][D / 32];
+  s16x8 k[TN][D / 32], v[TN][D / 32];
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
+  for (int n = 0; n < TN; ++n) {
     const int r = mine + n * 16;
     read_rows<D>(at<T>(a.k, here + r, a.k_stride, kv, a.k_head), a.k_stride, count - r, a.dim, lane, k[n]);
     read_rows<D>(at<T>(a.v, here + r, a.v_stride, kv, a.v_head), a.v_stride, count - r, a.dim, lane, v[n]);
   }
   int along0 = Tile::along(lane, 0), across0 = Tile::across(lane, 0);
-  f32x4 of_k[D / 16][2], of_v[D / 16][2];
+  f32x4 of_k[D / 16][TN], of_v[D / 16][TN];
 #pragma unroll
-  for (int n = 0; n < 2; ++n)
+  for (int n = 0; n < TN; ++n)
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) of_k[b][n] = of_v[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   // the queries from the tile's first key on, head after head
@@ -511,19 +534,19 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     }
     if (t + 1 < all_steps) load(~t & 1);
     if (first + kStepRows - 1 < mine) continue;                              // queries in front of all of the wave's keys
-    const bool border = first < mine + 31;
+    const bool border = first < mine + kMine - 1;
     asm volatile("" : "+v"(along0), "+v"(across0));      // places are formed from these two where they are needed: registers are short
-    Pack<T, 8> p[2], ds[2];
+    Pack<T, 8> p[TN], ds[TN];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      f32x4 z[2], d[2];
+      f32x4 z[TN], d[TN];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) z[n] = d[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < TN; ++n) z[n] = d[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) {
         const s16x8 f = Tile::read_along(qs, b * 16, along0 ^ (s << 6)), e = Tile::read_along(gs, b * 16, along0 ^ (s << 6));
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < TN; ++n) {
           z[n] = mfma<T>(f, k[n][s], z[n]);
           d[n] = mfma<T>(e, v[n][s], d[n]);
         }
@@ -531,7 +554,7 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
       const f32x4 t0 = *reinterpret_cast<const f32x4 *>(ts + b * 32), t1 = *reinterpret_cast<const f32x4 *>(ts + b * 32 + 4);
       const float lse[4] = {t0[0], t0[2], t1[0], t1[2]}, delta[4] = {t0[1], t0[3], t1[1], t1[3]};
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
+      for (int n = 0; n < TN; ++n) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           z[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[n][r], c, -lse[r]));
@@ -555,21 +578,26 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     for (int b = 0; b < D / 16; ++b) {
       const s16x8 f = Tile::read_across(gs, 0, across0 ^ (b << 5)), e = Tile::read_across(qs, 0, across0 ^ (b << 5));
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
+      for (int n = 0; n < TN; ++n) {
         of_v[b][n] = mfma<T>(f, __builtin_bit_cast(s16x8, p[n]), of_v[b][n]);
         of_k[b][n] = mfma<T>(e, __builtin_bit_cast(s16x8, ds[n]), of_k[b][n]);
       }
     }
   }
-  const float k_factor[2] = {a.scale / unit, a.scale / unit}, v_factor[2] = {1.f / kWeights, 1.f / kWeights};
+  float k_factor[TN], v_factor[TN];
+#pragma unroll
+  for (int n = 0; n < TN; ++n) {
+    k_factor[n] = a.scale / unit;
+    v_factor[n] = 1.f / kWeights;
+  }
   if (a.parts == 1) {
-    write_rows<T, D, 2>(of_k, k_factor, dk + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
-    write_rows<T, D, 2>(of_v, v_factor, dv + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+    write_rows<T, D, TN>(of_k, k_factor, dk + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+    write_rows<T, D, TN>(of_v, v_factor, dv + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
   }
   float *const partial = a.partial + ((static_cast<int64_t>(part) * a.tokens + here) * a.kv_heads + kv) * 2 * a.dim;
   const int64_t partial_stride = static_cast<int64_t>(a.kv_heads) * 2 * a.dim;
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {
+  for (int n = 0; n < TN; ++n) {
     const int r = mine + n * 16 + (lane & 15);
     if (a.parts == 1 || r >= count) continue;
     float *to = partial + r * partial_stride;
@@ -581,7 +609,7 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
       *reinterpret_cast<f32x4 *>(to + a.dim + i) = of_v[b][n] * v_factor[n];
     }
   }
-  if (__syncthreads_or(any_nan<D, 2>(of_k) || any_nan<D, 2>(of_v))) {
+  if (__syncthreads_or(any_nan<D, TN>(of_k) || any_nan<D, TN>(of_v))) {
     __syncthreads();
     const T *const k0 = at<T>(a.k, here, a.k_stride, kv, a.k_head), *const v0 = at<T>(a.v, here, a.v_stride, kv, a.v_head);
     // the queries of all heads in a row, from the tile's first key on
@@ -641,7 +669,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a) {
   gradient_of_queries<T, D>(a, blockIdx.x, lds);
 }
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(4 * kKeyRows / DKV_TN, DKV_OCC) void attention_dkv_kernel(AttentionArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char lds[kKeysLds<T, D>];
   gradient_of_keys<T, D>(a, blockIdx.x, lds);
 }
@@ -656,7 +684,7 @@ template <typename T, int D>
 void launch_backward(const AttentionArgs &a, hipStream_t s) {
   const int64_t slots = slots_of(a.tokens, a.sequences, kQueries), all = a.heads + (__is_same(T, f16) ? a.kv_heads : 0);
   hipLaunchKernelGGL((attention_delta_kernel<T, D>), dim3(static_cast<uint32_t>(slots * all)), dim3(256), 0, s, a);
-  hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.kv_heads * a.parts)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(static_cast<uint32_t>(slots_of(a.tokens, a.sequences, kKeyRows) * a.kv_heads * a.parts)), dim3(4 * kKeyRows / DKV_TN), 0, s, a);
   if (a.parts > 1) hipLaunchKernelGGL((attention_join_kernel<T>), dim3(2048), dim3(256), 0, s, a);
   hipLaunchKernelGGL((attention_dq_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.heads)), dim3(256), 0, s, a);
 }

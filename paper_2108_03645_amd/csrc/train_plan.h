@@ -318,8 +318,14 @@ inline int check_rotation(int64_t tokens, int64_t heads, int64_t kv_heads, int64
 }
 
 // ---------------------------------------------------------------- attention --------
-constexpr int64_t kAttentionRows = 128;       // rows of a workgroup
-constexpr int64_t kPartsWanted = 2048;        // workgroups of the keys' gradients
+#ifndef KEYROWS
+#define KEYROWS 64
+#endif
+constexpr int64_t kAttentionRows = 128, kAttentionKeys = KEYROWS;      // rows of a workgroup; of one of the keys' gradients
+#ifndef PARTS
+#define PARTS 2048
+#endif
+constexpr int64_t kPartsWanted = PARTS;        // workgroups of the keys' gradients
 
 inline int check_attention(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, int64_t sequences, float scale) {
   if (tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || dim < 8 || dim % 8 || sequences < 0 || (type != ONES_F16 && type != ONES_BF16) ||
@@ -327,7 +333,7 @@ inline int check_attention(int64_t tokens, int64_t heads, int64_t kv_heads, int6
     return ONES_E_INVALID_ARG;
   if (tokens > ONES_MAX_TOKENS || heads > ONES_MAX_HEADS || dim > ONES_MAX_ATTENTION_DIM || sequences > ONES_MAX_TOKENS) return ONES_E_BOUNDS;
   // threads of a launch, numbered in 32 bits
-  return (tokens / kAttentionRows + sequences + 2) * (heads + kv_heads) >= (int64_t{1} << 24) ? ONES_E_BOUNDS : ONES_OK;
+  return std::max((tokens / kAttentionRows + sequences + 2) * (heads + kv_heads), (tokens / kAttentionKeys + sequences + 2) * heads) >= (int64_t{1} << 24) ? ONES_E_BOUNDS : ONES_OK;
 }
 // Rows that are loaded to LDS as they lie.
 inline int check_head_rows(const void *p, int64_t stride, int64_t head_stride, int64_t heads, int64_t dim) {
@@ -347,7 +353,7 @@ inline AttentionPlan attention_plan(int64_t tokens, int64_t sequences, int64_t h
   AttentionPlan p{};
   const size_t rows = align_up(static_cast<size_t>(tokens) * heads * 4);
   const int64_t slots = tokens / kAttentionRows + sequences + 2;
-  p.parts = std::max<int64_t>(1, std::min(heads / kv_heads, kPartsWanted / std::max<int64_t>(1, ceil_div(tokens, kAttentionRows) * kv_heads)));
+  p.parts = std::max<int64_t>(1, std::min(heads / kv_heads, kPartsWanted / std::max<int64_t>(1, ceil_div(tokens, kAttentionKeys) * kv_heads)));
   p.parts = ceil_div(heads / kv_heads, ceil_div(heads / kv_heads, p.parts));
   p.dout_norm = 2 * rows;
   p.slot_norms = 3 * rows;
