@@ -15,7 +15,7 @@ UNITS = [("ones_api.hip", "ones_api.o", []), ("ones_select.hip", "ones_select.o"
          ("ones_sample.hip", "ones_sample.o", []), ("ones_fused.hip", "ones_fused.o", [])] + [
     ("ones_evolve.hip", f"ones_evolve_{g}.o", [f"-DONES_ROW_GROUP={g}"]) for g in range(4)] + [
     ("ones_resident.hip", f"ones_resident_{q}.o", [f"-DONES_RESIDENT_WORDS={q}"]) for q in range(1, 5)] + [
-    (f"train_{name}.hip", f"train_{name}.o", []) for name in ("norm", "recurrence", "loss", "update", "rotation", "attention", "attention_step", "clip")]
+    (f"train_{name}.hip", f"train_{name}.o", []) for name in ("norm", "recurrence", "loss", "update", "rotation", "attention", "attention_backward", "attention_step", "clip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -24,7 +24,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
 
 
 HEADERS = [os.path.join(CSRC, h) for h in ("ones_device.h", "ones_sample.h", "ones_candidate.h", "ones_exchange.h", "ones_sort.h",
-                                              "train_device.h", "train_host.h", "train_matmul.h", "train_attention.h", "train_plan.h")] + [
+                                              "train_device.h", "train_host.h", "train_matmul.h", "train_attention.h", "train_attention_sequences.h", "train_plan.h")] + [
            os.path.join(INCLUDE, "ones.h"), os.path.join(INCLUDE, "ones_train.h"),
            os.path.abspath(__file__)]
 

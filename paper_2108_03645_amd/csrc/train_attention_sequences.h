@@ -1,0 +1,89 @@
+// What the attention kernels over packed sequences share (train_attention.hip forward, train_attention_backward.hip): their arguments, and the sums
+// of rows that products of matrices cannot give.
+#pragma once
+
+#include "train_attention.h"
+#include "train_host.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+namespace ones {
+namespace train {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttentionArgs {
+  const void *q, *k, *v, *dout;
+  int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head, do_stride, do_head;      // elements
+  void *o, *rest;
+  float *lse;
+  void *dq, *dk, *dv;
+  float2 *terms;                              // of every row: lse in base 2, delta
+  float *dout_norm, *v_norm;                  // |do| of every row; the largest |do| and |v| of every slot (fp16)
+  float *partial;                             // dk and dv of parts of a group's heads, in 32 bits
+  const int32_t *offsets;
+  int32_t sequences, tokens, heads, kv_heads, dim, parts;
+  float scale;
+};
+
+template <typename T>
+__device__ __forceinline__ const T *at(const void *p, int64_t row, int64_t stride, int32_t head, int64_t head_stride) {
+  return static_cast<const T *>(p) + row * stride + head * head_stride;
+}
+
+// fp16 keeps 2^-24 and up: the exponentials below the row's largest are held in units of 2^-8.
+template <typename T>
+constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;
+
+constexpr float kSlack = 6.f;                 // 2^(kShift + kSlack) is far from fp16's end
+
+// A weight of 0 does not take a row out of a product where that row has infinities or NaN, so those of a token would reach the rows
+// that it is masked for, as far as they share a step with it.  Each kernel looks for NaN in what it has summed.  Where there is some, the rows
+// that have it are summed once more without products of matrices, over what they do see, which is slow and right:
+//   sums[e] = sum over y of weights(r, y)[e] * element d of row(e, y)
+// for the rows 0 <= r < rows of the workgroup, elements d < dim, and 0 <= y < last(r).  has(r, d): whether element d of row r asks for it;
+// weights(r, y, w): whether row r sees y at all; write(r, d, sums).
+template <int N, class Has, class Last, class Weights, class Row, class Write>
+__device__ __forceinline__ void sum_by_rows(unsigned char *lds, int32_t rows, int32_t dim, Has has, Last last, Weights weights, Row row, Write write) {
+  struct Held {
+    float w[N];
+    int32_t seen;
+  };
+  constexpr int kChunk = 256;
+  Held *const held = reinterpret_cast<Held *>(lds);
+  const int d = threadIdx.x;
+  for (int32_t r = 0; r < rows; ++r) {
+    if (!__syncthreads_or(d < dim && has(r, d))) continue;
+    const int32_t end = last(r);
+    float sums[N] = {};
+    for (int32_t y0 = 0; y0 < end; y0 += kChunk) {
+      Held mine{};
+      if (d < kChunk && y0 + d < end) mine.seen = weights(r, y0 + d, mine.w);
+      __syncthreads();
+      if (d < kChunk) held[d] = mine;
+      __syncthreads();
+      if (d >= dim) continue;
+      for (int32_t y = y0; y < min(end, y0 + kChunk); ++y)
+        if (held[y - y0].seen) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) sums[e] += held[y - y0].w[e] * static_cast<float>(row(e, y)[d]);
+        }
+    }
+    if (d < dim) write(r, d, sums);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float dot(const T *a, const T *b, int32_t dim) {
+  float s = 0.f;
+  for (int i = 0; i < dim; ++i) s = __builtin_fmaf(static_cast<float>(a[i]), static_cast<float>(b[i]), s);
+  return s;
+}
+
+constexpr int kQueries = kAttentionRows, kKeys = 64;       // of a workgroup; of a step
+
+}  // namespace
+}  // namespace train
+}  // namespace ones

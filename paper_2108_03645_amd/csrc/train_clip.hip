@@ -17,9 +17,8 @@ namespace {
 
 struct ClipArgs {
   void *p[kClipTable];
-  int64_t count[kClipTable];
   int32_t first[kClipTable + 1];              // piece of a tensor's first element
-  uint8_t type[kClipTable];
+  uint16_t last[kClipTable];                  // elements of its last piece less one, and its type above them
   int32_t tensors, part;                      // part: place of this launch's first sum
   int32_t parts;                              // of all launches
   float limit, eps;
@@ -53,40 +52,70 @@ __device__ __forceinline__ int tensor_of(const ClipArgs &a, int32_t piece) {
   return lo;
 }
 
-constexpr int kVec = 8;
+constexpr int kVec = 8, kRuns = static_cast<int>(kClipPiece / (256 * kVec));
+static_assert(kRuns * 256 * kVec == kClipPiece && kClipPiece <= 1 << 13);
 
+// A thread's elements of a piece: runs of eight, all of them loaded before the first is used.
 template <typename T>
-__device__ __forceinline__ double squares(const T *p, int64_t n) {
-  double s = 0.;
-  for (int64_t i = static_cast<int64_t>(threadIdx.x) * kVec; i < n; i += 256 * kVec) {
-    const Pack<T, kVec> v = load_some<T, kVec>(p + i, static_cast<int>(min(n - i, static_cast<int64_t>(kVec))));
+struct Runs {
+  Pack<T, kVec> v[kRuns];
+  __device__ __forceinline__ Runs(const T *p, int n) {
+    const int i = static_cast<int>(threadIdx.x) * kVec;
+    if (n == kClipPiece) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) { const double x = static_cast<double>(static_cast<float>(v.v[j])); s = __builtin_fma(x, x, s); }
+      for (int r = 0; r < kRuns; ++r) v[r] = load_pack<T, kVec>(p + r * 256 * kVec + i);
+    } else {
+#pragma unroll
+      for (int r = 0; r < kRuns; ++r) v[r] = load_some<T, kVec>(p + r * 256 * kVec + i, n - r * 256 * kVec - i);
+    }
   }
+};
+template <typename T>
+__device__ __forceinline__ double squares(const void *tensor, int64_t begin, int n) {
+  const Runs<T> runs(static_cast<const T *>(tensor) + begin, n);
+  double s = 0.;
+#pragma unroll
+  for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) { const double x = static_cast<double>(static_cast<float>(runs.v[r].v[j])); s = __builtin_fma(x, x, s); }
   return s;
 }
 template <typename T>
-__device__ __forceinline__ void scale(T *p, int64_t n, float factor) {
-  for (int64_t i = static_cast<int64_t>(threadIdx.x) * kVec; i < n; i += 256 * kVec) {
-    const int some = static_cast<int>(min(n - i, static_cast<int64_t>(kVec)));
-    const Pack<T, kVec> v = load_some<T, kVec>(p + i, some);
+__device__ __forceinline__ void scale(void *tensor, int64_t begin, int n, float factor) {
+  T *const p = static_cast<T *>(tensor) + begin;
+  const Runs<T> runs(p, n);
+#pragma unroll
+  for (int r = 0; r < kRuns; ++r) {
+    const int i = (r * 256 + static_cast<int>(threadIdx.x)) * kVec;
     float x[kVec];
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) x[j] = static_cast<float>(v.v[j]) * factor;
-    store_some<T, kVec>(p + i, x, some);
+    for (int j = 0; j < kVec; ++j) x[j] = static_cast<float>(runs.v[r].v[j]) * factor;
+    store_some<T, kVec>(p + i, x, n - i);
   }
 }
+// A piece: its tensor, type, first element and elements.
+struct Piece {
+  void *p;
+  int64_t begin;
+  int type, n;
+  __device__ __forceinline__ Piece(const ClipArgs &a, int32_t piece) {
+    const int t = tensor_of(a, piece);
+    p = a.p[t];
+    begin = static_cast<int64_t>(piece - a.first[t]) * kClipPiece;
+    n = piece + 1 == a.first[t + 1] ? (a.last[t] & (kClipPiece - 1)) + 1 : static_cast<int>(kClipPiece);
+    type = a.last[t] >> 13;
+  }
+};
 
 __global__ __launch_bounds__(256) void squares_kernel(ClipArgs a) {
   int32_t piece, end;
   pieces_of(a, piece, end);
   double s = 0.;
   for (; piece < end; ++piece) {
-    const int t = tensor_of(a, piece);
-    const int64_t begin = static_cast<int64_t>(piece - a.first[t]) * kClipPiece, n = min(a.count[t] - begin, kClipPiece);
-    if (a.type[t] == kF32) s += squares(static_cast<const float *>(a.p[t]) + begin, n);
-    else if (a.type[t] == kF16) s += squares(static_cast<const f16 *>(a.p[t]) + begin, n);
-    else s += squares(static_cast<const bf16 *>(a.p[t]) + begin, n);
+    const Piece at(a, piece);
+    if (at.type == kF32) s += squares<float>(at.p, at.begin, at.n);
+    else if (at.type == kF16) s += squares<f16>(at.p, at.begin, at.n);
+    else s += squares<bf16>(at.p, at.begin, at.n);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) a.sums[a.part + blockIdx.x] = s;
@@ -102,11 +131,10 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a) {
   int32_t begin, piece;
   pieces_of(a, begin, piece);
   while (--piece >= begin) {                  // from the last on, which the caches have yet
-    const int t = tensor_of(a, piece);
-    const int64_t first = static_cast<int64_t>(piece - a.first[t]) * kClipPiece, n = min(a.count[t] - first, kClipPiece);
-    if (a.type[t] == kF32) scale(static_cast<float *>(a.p[t]) + first, n, factor);
-    else if (a.type[t] == kF16) scale(static_cast<f16 *>(a.p[t]) + first, n, factor);
-    else scale(static_cast<bf16 *>(a.p[t]) + first, n, factor);
+    const Piece at(a, piece);
+    if (at.type == kF32) scale<float>(at.p, at.begin, at.n, factor);
+    else if (at.type == kF16) scale<f16>(at.p, at.begin, at.n, factor);
+    else scale<bf16>(at.p, at.begin, at.n, factor);
   }
 }
 
@@ -158,17 +186,17 @@ int ones_clip_gradients(void *const *gradients, const int64_t *counts, const int
   if (tensors)
     if (int rc = check_apart(gradients, counts, types, tensors)) return rc;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  // of the workgroups every launch has its share, by its pieces
+  // of the workgroups every launch has its share, by its pieces, or enough for most compute units
   auto table = [&](int64_t from, ClipArgs &a) {
     a.tensors = static_cast<int32_t>(std::min(tensors - from, kClipTable));
     a.first[0] = 0;
     for (int32_t i = 0; i < a.tensors; ++i) {
       a.p[i] = gradients[from + i];
-      a.count[i] = counts[from + i];
-      a.type[i] = static_cast<uint8_t>(types[from + i]);
+      a.last[i] = static_cast<uint16_t>(((counts[from + i] + kClipPiece - 1) % kClipPiece) | types[from + i] << 13);
       a.first[i + 1] = a.first[i] + static_cast<int32_t>(ceil_div(counts[from + i], kClipPiece));
     }
-    return std::min<int64_t>(a.first[a.tensors], a.first[a.tensors] * kClipBlocks / std::max<int64_t>(pieces, 1) + 1);
+    const int64_t mine = a.first[a.tensors];
+    return std::min(mine, std::max(kClipLeast, mine * kClipBlocks / std::max<int64_t>(pieces, 1)));
   };
   ClipArgs a{};
   a.limit = limit;

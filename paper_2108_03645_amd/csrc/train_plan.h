@@ -289,17 +289,18 @@ struct RotationPlan {
   int32_t vec, lanes, per, parts;             // pairs of a load (1: element by element), lanes of a row, loads of a lane; waves of a token
   int64_t blocks;
 };
-// Wide loads where the pairs that turn, and those that do not, are whole vectors; a power of two of lanes to a row.  A wave takes a
-// token, with few tokens a part of its heads.
-inline RotationPlan rotation_plan(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int64_t turned, bool neighbours, int64_t bytes, bool backward) {
+// Loads of 16 or 8 bytes where the pairs that turn, and those that do not, are whole vectors; a power of two of lanes to a row.  A wave takes
+// a token, with few tokens a part of its heads.
+inline RotationPlan rotation_plan(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int64_t turned, int64_t bytes, bool backward) {
   RotationPlan p{};
-  const int64_t vec = 16 / bytes, pairs = (dim + 1) / 2;
-  const bool wide = dim % (2 * vec) == 0 && turned % vec == 0;
-  p.vec = static_cast<int32_t>(wide ? vec : 1);
+  const int64_t pairs = (dim + 1) / 2;
+  int64_t vec = 16 / bytes;
+  while (vec > 1 && (dim % (2 * vec) || turned % vec || vec * 64 < pairs)) vec = vec > 8 / bytes ? 8 / bytes : 1;
+  p.vec = static_cast<int32_t>(vec);
   p.lanes = 16;
-  if (wide)
+  if (vec > 1)
     for (p.lanes = 4; p.lanes * vec < pairs; p.lanes *= 2) {}
-  p.per = static_cast<int32_t>(wide ? 1 : ceil_div(pairs, 16));
+  p.per = static_cast<int32_t>(vec > 1 ? 1 : ceil_div(pairs, 16));
   const int64_t rows = 64 / p.lanes, turns = ceil_div(heads, rows) + ceil_div(kv_heads, rows);
   p.parts = static_cast<int32_t>(tokens >= 2048 ? 1 : std::max<int64_t>(1, turns));
   const int64_t most = backward ? kRotationBlocks : 2048;
@@ -318,14 +319,11 @@ inline int check_rotation(int64_t tokens, int64_t heads, int64_t kv_heads, int64
 }
 
 // ---------------------------------------------------------------- attention --------
-#ifndef KEYROWS
-#define KEYROWS 64
-#endif
-constexpr int64_t kAttentionRows = 128, kAttentionKeys = KEYROWS;      // rows of a workgroup; of one of the keys' gradients
-#ifndef PARTS
-#define PARTS 2048
-#endif
-constexpr int64_t kPartsWanted = PARTS;        // workgroups of the keys' gradients
+constexpr int64_t kAttentionRows = 128, kAttentionKeys = 64;      // queries of a workgroup, or half of them; keys of one of their gradients
+constexpr int64_t kPartsWanted = 2048;        // workgroups of the keys' gradients
+
+// Whether workgroups of 128 queries are too few for the compute units, so that those of 64 carry more.
+inline bool attention_few(int64_t tokens, int64_t heads) { return ceil_div(tokens, kAttentionRows) * heads < 1024; }
 
 inline int check_attention(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, int64_t sequences, float scale) {
   if (tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || dim < 8 || dim % 8 || sequences < 0 || (type != ONES_F16 && type != ONES_BF16) ||
@@ -390,9 +388,11 @@ inline int check_step(int64_t batch, int64_t capacity, int64_t heads, int64_t kv
 }
 
 // ------------------------------------------------------- the global norm --------
-constexpr int64_t kClipTable = 128, kClipPiece = 8192, kClipBlocks = 1024;      // tensors of a launch; elements of a piece; workgroups of all launches
+// Tensors of a launch, whose addresses and sizes are its arguments; elements of a piece; workgroups of all launches, and of one at least if
+// it has the pieces.
+constexpr int64_t kClipTable = 256, kClipPiece = 8192, kClipBlocks = 1024, kClipLeast = 256;
 
-inline size_t clip_workspace(int64_t tensors) { return align_up(static_cast<size_t>(kClipBlocks + ceil_div(tensors, kClipTable)) * 8); }
+inline size_t clip_workspace(int64_t tensors) { return align_up(static_cast<size_t>(kClipBlocks + kClipLeast * ceil_div(tensors, kClipTable)) * 8); }
 
 }  // namespace train
 }  // namespace ones

@@ -263,29 +263,31 @@ void launch(const RotationArgs &a, bool backward, int64_t blocks, hipStream_t s)
   else hipLaunchKernelGGL((rotation_kernel<T, VEC, LANES, PER, NEIGHBOURS, false>), grid, block, 0, s, a);
 }
 
-template <typename T, bool NEIGHBOURS>
-void launch_lanes(RotationArgs a, bool backward, hipStream_t s) {
-  const RotationPlan p = rotation_plan(a.tokens, a.heads[0], a.heads[1], a.dim, a.turned, NEIGHBOURS, sizeof(T), backward);
-  a.parts = p.parts;
-  constexpr int vec = 16 / sizeof(T);
-  if (p.vec == 1) {
-    if (p.per <= 2) return launch<T, 1, 16, 2, NEIGHBOURS>(a, backward, p.blocks, s);
-    if (p.per <= 8) return launch<T, 1, 16, 8, NEIGHBOURS>(a, backward, p.blocks, s);
-    return launch<T, 1, 16, 16, NEIGHBOURS>(a, backward, p.blocks, s);
-  }
+template <typename T, int VEC, bool NEIGHBOURS>
+void launch_lanes(const RotationArgs &a, bool backward, const RotationPlan &p, hipStream_t s) {
   switch (p.lanes) {
-    case 4: return launch<T, vec, 4, 1, NEIGHBOURS>(a, backward, p.blocks, s);
-    case 8: return launch<T, vec, 8, 1, NEIGHBOURS>(a, backward, p.blocks, s);
-    case 16: return launch<T, vec, 16, 1, NEIGHBOURS>(a, backward, p.blocks, s);
-    case 32: return launch<T, vec, 32, 1, NEIGHBOURS>(a, backward, p.blocks, s);
-    default: return launch<T, vec, 64, 1, NEIGHBOURS>(a, backward, p.blocks, s);
+    case 4: return launch<T, VEC, 4, 1, NEIGHBOURS>(a, backward, p.blocks, s);
+    case 8: return launch<T, VEC, 8, 1, NEIGHBOURS>(a, backward, p.blocks, s);
+    case 16: return launch<T, VEC, 16, 1, NEIGHBOURS>(a, backward, p.blocks, s);
+    case 32: return launch<T, VEC, 32, 1, NEIGHBOURS>(a, backward, p.blocks, s);
+    default: return launch<T, VEC, 64, 1, NEIGHBOURS>(a, backward, p.blocks, s);
   }
+}
+template <typename T, bool NEIGHBOURS>
+void launch_vectors(RotationArgs a, bool backward, hipStream_t s) {
+  const RotationPlan p = rotation_plan(a.tokens, a.heads[0], a.heads[1], a.dim, a.turned, sizeof(T), backward);
+  a.parts = p.parts;
+  if (p.vec == 16 / sizeof(T)) return launch_lanes<T, 16 / sizeof(T), NEIGHBOURS>(a, backward, p, s);
+  if (p.vec == 8 / sizeof(T)) return launch_lanes<T, 8 / sizeof(T), NEIGHBOURS>(a, backward, p, s);
+  if (p.per <= 2) return launch<T, 1, 16, 2, NEIGHBOURS>(a, backward, p.blocks, s);
+  if (p.per <= 8) return launch<T, 1, 16, 8, NEIGHBOURS>(a, backward, p.blocks, s);
+  launch<T, 1, 16, 16, NEIGHBOURS>(a, backward, p.blocks, s);
 }
 
 void launch_type(const RotationArgs &a, int32_t type, bool neighbours, bool backward, hipStream_t s) {
-  if (type == ONES_F32) neighbours ? launch_lanes<float, true>(a, backward, s) : launch_lanes<float, false>(a, backward, s);
-  else if (type == ONES_F16) neighbours ? launch_lanes<f16, true>(a, backward, s) : launch_lanes<f16, false>(a, backward, s);
-  else neighbours ? launch_lanes<bf16, true>(a, backward, s) : launch_lanes<bf16, false>(a, backward, s);
+  if (type == ONES_F32) neighbours ? launch_vectors<float, true>(a, backward, s) : launch_vectors<float, false>(a, backward, s);
+  else if (type == ONES_F16) neighbours ? launch_vectors<f16, true>(a, backward, s) : launch_vectors<f16, false>(a, backward, s);
+  else neighbours ? launch_vectors<bf16, true>(a, backward, s) : launch_vectors<bf16, false>(a, backward, s);
 }
 
 RotationArgs arguments(const void *q, int64_t q_stride, int64_t q_head, const void *k, int64_t k_stride, int64_t k_head, int64_t tokens,
@@ -359,7 +361,7 @@ int ones_head_norm_rotation_backward(const void *dq_out, int64_t dq_stride, int6
   a.partial = static_cast<float *>(d_workspace);
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (any) launch_type(a, type, neighbours != 0, true, s);
-  const RotationPlan p = rotation_plan(tokens, heads, kv_heads, dim, pairs, neighbours != 0, type_bytes(type), true);
+  const RotationPlan p = rotation_plan(tokens, heads, kv_heads, dim, pairs, type_bytes(type), true);
   if (dq_weight || dk_weight)
     hipLaunchKernelGGL(rotation_reduce_kernel, dim3(static_cast<uint32_t>(ceil_div(2 * dim, 64))), dim3(1024), 0, s, a, any ? static_cast<int32_t>(p.blocks) : 0);
   return launched("head norm and rotation backward");

@@ -410,11 +410,14 @@ def orthogonal_update(grad, momentum=None, beta=0.95, nesterov=True, steps=5, co
 def _heads(t, kinds, name, tokens=None, dim=None, device=None, dtype=None):
     """Checked to be [tokens, heads, dim]; (t, elements between tokens, between heads), copied if its rows have gaps."""
     _check(t, name, None, kinds if dtype is None else (dtype,), device)
-    if t.dim() != 3 or (tokens is not None and t.shape[0] != tokens) or (dim is not None and t.shape[2] != dim):
-        raise ValueError(f"{name}: [{'tokens' if tokens is None else tokens}, heads, {'dim' if dim is None else dim}] is wanted, got {tuple(t.shape)}")
-    if (t.stride(2) != 1 and t.shape[2] > 1) or min(t.stride()) < 0:
+    shape = t.shape
+    if len(shape) != 3 or (tokens is not None and shape[0] != tokens) or (dim is not None and shape[2] != dim):
+        raise ValueError(f"{name}: [{'tokens' if tokens is None else tokens}, heads, {'dim' if dim is None else dim}] is wanted, got {tuple(shape)}")
+    stride, head, step = t.stride()
+    if step != 1 and shape[2] > 1:
         t = t.contiguous()
-    return t, t.stride(0), t.stride(1)
+        stride, head, step = t.stride()
+    return t, stride, head
 
 
 def _rotation_inputs(q, k, q_weight, k_weight, positions, frequencies):
@@ -488,12 +491,13 @@ def head_norm_rotation(q, k, q_weight, k_weight, positions, frequencies, eps=1e-
 
 # ---------------------------------------------------------- attention --------
 _STRIDE = 1 << 20                                 # of elements between tokens, at most
+_INDEX = (torch.int32,)
 
 
 def _attended(t, name, tokens=None, dim=None, like=None):
     """As _heads, copied as well if its rows cannot be loaded as they lie."""
     t, stride, head = _heads(t, _HALVES, name, tokens, dim, None if like is None else like.device, None if like is None else like.dtype)
-    if stride % 8 or head % 8 or stride > _STRIDE or stride < t.shape[2] or t.data_ptr() % 16:
+    if (stride | head) % 8 or stride > _STRIDE or stride < t.shape[2] or t.data_ptr() % 16:
         t = t.contiguous() if not t.is_contiguous() else t.clone()
         stride, head = t.shape[1] * t.shape[2], t.shape[2]
     return t, stride, head
@@ -504,18 +508,18 @@ def _attention_inputs(q, k, v, offsets, scale):
     tokens, heads, dim = q.shape
     k, k_stride, k_head = _attended(k, "k", tokens, dim, q)
     v, v_stride, v_head = _attended(v, "v", tokens, dim, q)
-    if k.shape[1] != v.shape[1] or not k.shape[1] or heads % k.shape[1]:
-        raise ValueError(f"{heads} query heads, {k.shape[1]} key heads and {v.shape[1]} value heads do not go together")
+    kv_heads = k.shape[1]
+    if kv_heads != v.shape[1] or not kv_heads or heads % kv_heads:
+        raise ValueError(f"{heads} query heads, {kv_heads} key heads and {v.shape[1]} value heads do not go together")
     if dim % 8:
         raise ValueError(f"dim: a multiple of 8 is wanted, got {dim}")
     if offsets is None:
         offsets = torch.zeros(2, dtype=torch.int32, device=q.device)
         offsets[1:].fill_(tokens)
-    _check(offsets, "offsets", None, (torch.int32,), q.device)
-    if offsets.dim() != 1 or not offsets.shape[0]:
+    offsets = _dense(offsets, "offsets", None, _INDEX, q.device)
+    if offsets.dim() != 1 or not len(offsets):
         raise ValueError("offsets: [sequences + 1] is wanted")
-    offsets = offsets.contiguous()
-    sizes = (tokens, heads, k.shape[1], dim, _TYPES[q.dtype], offsets.data_ptr(), offsets.shape[0] - 1, dim ** -0.5 if scale is None else scale)
+    sizes = (tokens, heads, kv_heads, dim, _TYPES[q.dtype], offsets.data_ptr(), len(offsets) - 1, dim ** -0.5 if scale is None else scale)
     return (q.data_ptr(), q_stride, q_head, k.data_ptr(), k_stride, k_head, v.data_ptr(), v_stride, v_head), sizes, (q, k, v, offsets)
 
 
@@ -623,21 +627,26 @@ def clip_gradients(gradients, limit, eps=1e-6):
     if not gradients:
         raise ValueError("gradients: one at least is wanted")
     first = gradients[0]
+    for g in gradients:
+        if not isinstance(g, torch.Tensor):
+            raise TypeError("gradients: tensors are wanted")
     _check(first, "gradients", None, _TYPES)
     device = first.device
-    for g in gradients:
-        _check(g, "gradients", None, _TYPES, device)
-        if not g.is_contiguous() and not _whole(g):
-            raise ValueError("gradients: updated in place, they may have no gaps")
+    # a call may have hundreds of them: what nearly all pass is asked for all at once
+    at, counts, kinds = [g.data_ptr() for g in gradients], [g.numel() for g in gradients], [g.dtype for g in gradients]
+    if set(map(torch.Tensor.get_device, gradients)) != {device.index} or not _TYPES.keys() >= set(kinds) or not all(map(torch.Tensor.is_contiguous, gradients)):
+        for g in gradients:
+            _check(g, "gradients", None, _TYPES, device)
+            if not g.is_contiguous() and not _whole(g):
+                raise ValueError("gradients: updated in place, they may have no gaps")
     n = len(gradients)
     norm = torch.empty((), dtype=torch.float32, device=device)
     L = load()
     nbytes = L.ones_clip_gradients_workspace_bytes(n)
     scratch = _scratch(nbytes, device)
-    _call(device, L.ones_clip_gradients, (C.c_void_p * n)(*[g.data_ptr() for g in gradients]), (C.c_int64 * n)(*[g.numel() for g in gradients]),
-          (C.c_int32 * n)(*[_TYPES[g.dtype] for g in gradients]), n, limit, eps, norm.data_ptr(), _ptr(scratch), nbytes)
-    for g in gradients:
-        _changed(g)
+    _call(device, L.ones_clip_gradients, (C.c_void_p * n)(*at), (C.c_int64 * n)(*counts), (C.c_int32 * n)(*map(_TYPES.get, kinds)), n, limit, eps,
+          norm.data_ptr(), _ptr(scratch), nbytes)
+    _changed(gradients)
     return norm
 
 

@@ -52,7 +52,7 @@ def check(train, gradients, limit, eps=1e-6):
     return norm
 
 
-SIZES = [[1], [7], [8191], [8192], [8193], [0, 5, 0], [100, 1, 3000, 77777], [3] * 129, [1000003], [11] * 400 + [50000], [0] * 130 + [9]]
+SIZES = [[1], [7], [8191], [8192], [8193], [0, 5, 0], [100, 1, 3000, 77777], [3] * 257, [1000003], [11] * 400 + [50000], [0] * 260 + [9]]
 
 
 @gpu
