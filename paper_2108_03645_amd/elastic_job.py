@@ -1,12 +1,12 @@
 """A job for the search: a small language model that trains at whatever local batch the winning schedule gives it.
 
-    python -m paper_2108_03645_amd.elastic_job
+    python -m paper_2108_03645_amd.elastic_job [--mixer recurrence|attention] [--clip LIMIT]
 
 One pass of the paper's loop (Section 3.1) with a real worker on one GPU: the job's steps are timed at a few local batches, a line
 through them gives the slope a and the offset d of its iteration time t(B, g) = a*B/g + c*log2(g) + d ("profiled online",
 Section 3.2.1), the search places it among other jobs, and the worker trains on at its share of the batch, with the learning rate
-scaled by the batch (Section 3.3.2).  Layer norm, recurrence and loss are ``train``'s and make a; the update of the matrices is
-``train``'s as well and belongs to d.  At the end the model continues a sequence token by token.
+scaled by the batch (Section 3.3.2).  Layer norm, recurrence or attention, and loss are ``train``'s and make a; the clipping of the gradients and
+the update of the matrices are ``train``'s as well and belong to d.  At the end the model continues a sequence token by token.
 
 Data: a synthetic language, in which every word has one usual successor."""
 from __future__ import annotations
@@ -20,22 +20,46 @@ from . import train, workloads
 
 
 class Model:
-    """Embedding, blocks of (layer norm, gated recurrence between projections), layer norm, output table."""
+    """Embedding, blocks of (layer norm, a mixer between projections), layer norm, output table.  The mixer is the gated recurrence, or causal
+    attention with two query heads of `dim` elements to a key head, their norms and the rotation by positions."""
 
-    def __init__(self, vocabulary=1000, width=256, blocks=2, device="cuda:0", seed=0):
+    def __init__(self, vocabulary=1000, width=256, blocks=2, device="cuda:0", seed=0, mixer="recurrence", dim=64):
+        if mixer not in ("recurrence", "attention"):
+            raise ValueError(f"mixer: recurrence or attention, not {mixer!r}")
+        if mixer == "attention" and width % (2 * dim):
+            raise ValueError(f"width: a multiple of {2 * dim} is wanted, got {width}")
         g = torch.Generator(device=device).manual_seed(seed)
         normal = lambda *shape, std: (torch.randn(*shape, generator=g, device=device) * std).requires_grad_()  # noqa: E731
         self.vocabulary, self.width, self.blocks = vocabulary, width, blocks
         self.embedding = normal(vocabulary, width, std=1.0)
         self.output = normal(vocabulary, width, std=width ** -0.5)
-        # the matrices of all blocks in one tensor (gate, value, out of each), so that one call updates them all
+        # the matrices of all blocks in one tensor (of each: gate, value, out; or queries, keys over values, out), so that one call updates them all
         self.matrices = normal(3 * blocks, width, width, std=width ** -0.5)
         self.norms = torch.ones(blocks + 1, 2, width, device=device)
         self.norms[:, 1] = 0
         self.norms.requires_grad_()
+        self.mixer, self.dim, self.heads = mixer, dim, width // dim
+        if mixer == "attention":
+            self.head_norms = torch.ones(blocks, 2, dim, device=device, requires_grad=True)
+            self.frequencies = 10000.0 ** (-torch.arange(0, dim, 2, device=device) / dim)
+
+    def parameters(self):
+        """The tensors that learn beside the matrices."""
+        return [self.embedding, self.output, self.norms] + ([self.head_norms] if self.mixer == "attention" else [])
+
+    def projected(self, k, y, positions, matrices):
+        """Queries, keys (normed and turned) and values of the rows y [tokens, width] in block k."""
+        queries, keys_values = matrices
+        q = (y @ queries.t()).view(-1, self.heads, self.dim)
+        keys, values = (y @ keys_values.t()).view(-1, 2, self.heads // 2, self.dim).unbind(1)
+        q, keys = train.head_norm_rotation(q, keys, self.head_norms[k, 0], self.head_norms[k, 1], positions, self.frequencies)
+        return q, keys, values
 
     def hidden(self, tokens, states=None):
-        """[batch, steps, width] after the last norm, and the blocks' states behind the last step."""
+        """[batch, steps, width] after the last norm, and the blocks' states behind the last step: of the recurrence, or the keys and values
+        [batch, steps, heads, dim] that attention met."""
+        if self.mixer == "attention":
+            return self.attended(tokens)
         x = self.embedding[tokens].bfloat16()
         ends = []
         for k in range(self.blocks):
@@ -46,6 +70,20 @@ class Model:
             ends.append(end)
         return train.layer_norm(x, self.norms[-1, 0], self.norms[-1, 1]), ends
 
+    def attended(self, tokens):
+        batch, steps = tokens.shape
+        x = self.embedding[tokens.reshape(-1)].bfloat16()
+        offsets = torch.arange(batch + 1, device=x.device, dtype=torch.int32) * steps
+        positions = torch.arange(steps, device=x.device, dtype=torch.int32).repeat(batch)
+        ends = []
+        for k in range(self.blocks):
+            *inner, out = self.matrices[3 * k:3 * k + 3].bfloat16()
+            y = train.layer_norm(x, self.norms[k, 0], self.norms[k, 1])
+            q, keys, values = self.projected(k, y, positions, inner)
+            x = x + train.attention(q, keys, values, offsets).flatten(1) @ out.t()
+            ends.append([t.unflatten(0, (batch, steps)) for t in (keys, values)])
+        return train.layer_norm(x, self.norms[-1, 0], self.norms[-1, 1]).view(batch, steps, -1), ends
+
     def loss(self, tokens):
         """The mean loss of every next token; tokens below 0 are padding."""
         y, _ = self.hidden(tokens[:, :-1].clamp(min=0))
@@ -55,31 +93,40 @@ class Model:
 
     @torch.no_grad()
     def continue_from(self, tokens, n):
-        """The n likeliest next tokens one after another, by single steps of the recurrence: [batch, n]."""
+        """The n likeliest next tokens one after another, by the mixer's single steps: [batch, n]."""
         y, states = self.hidden(tokens)
         y, found = y[:, -1], []
         weights = self.matrices.bfloat16()
         output = self.output.bfloat16()
+        if self.mixer == "attention":             # caches with room for what comes
+            batch, steps = tokens.shape
+            lengths = torch.full((batch,), steps, device=y.device, dtype=torch.int32)
+            states = [[torch.cat([t, t.new_empty(batch, n, *t.shape[2:])], 1) for t in state] for state in states]
         for _ in range(n):
             token = (y @ output.t()).argmax(1)
             found.append(token)
             x = self.embedding[token].bfloat16()
             for k in range(self.blocks):
                 y = train.layer_norm(x, self.norms[k, 0], self.norms[k, 1])
-                h = train.gated_recurrence_step(y @ weights[3 * k].t(), y @ weights[3 * k + 1].t(), states[k])
+                if self.mixer == "attention":
+                    h = train.attention_step(*self.projected(k, y, lengths, weights[3 * k:3 * k + 2]), *states[k], lengths).flatten(1)
+                else:
+                    h = train.gated_recurrence_step(y @ weights[3 * k].t(), y @ weights[3 * k + 1].t(), states[k])
                 x = x + h @ weights[3 * k + 2].t()
+            if self.mixer == "attention":
+                lengths += 1
             y = train.layer_norm(x, self.norms[-1, 0], self.norms[-1, 1])
         return torch.stack(found, 1)
 
 
 class Worker:
     """Trains a model at a local batch that may change between any two steps.  The learning rate is proportional to the batch: `rate` at
-    `per_sample_rate_at` sequences."""
+    `per_sample_rate_at` sequences.  clip: the norm that all gradients together are clipped to; None: they are not."""
 
-    def __init__(self, model, rate=0.02, per_sample_rate_at=512):
-        self.model, self.rate, self.at = model, rate, per_sample_rate_at
+    def __init__(self, model, rate=0.02, per_sample_rate_at=512, clip=None):
+        self.model, self.rate, self.at, self.clip = model, rate, per_sample_rate_at, clip
         self.momentum = torch.zeros_like(model.matrices)
-        self.others = torch.optim.AdamW([model.embedding, model.output, model.norms], lr=rate / 4, weight_decay=0.0)
+        self.others = torch.optim.AdamW(model.parameters(), lr=rate / 4, weight_decay=0.0)
 
     def rate_of(self, batch):
         return self.rate * batch / self.at
@@ -90,6 +137,8 @@ class Worker:
         self.others.zero_grad(set_to_none=True)
         loss = model.loss(tokens)
         loss.backward()
+        if self.clip is not None:
+            train.clip_gradients([model.matrices.grad] + [p.grad for p in model.parameters()], self.clip)
         update = train.orthogonal_update(model.matrices.grad, self.momentum)
         with torch.no_grad():
             model.matrices.add_(update, alpha=-rate)
@@ -167,9 +216,9 @@ def place(a, d, batches, generations=20, slot=0):
     return batch, int(samples[slot]), int(gpus[slot]), cluster.n_gpus
 
 
-def main(steps=60, generations=20, slot=0):
-    model = Model(vocabulary=4000, width=512)
-    worker, language = Worker(model), Language(model.vocabulary, 256)
+def main(steps=60, generations=20, slot=0, mixer="recurrence", clip=None):
+    model = Model(vocabulary=4000, width=512, mixer=mixer)
+    worker, language = Worker(model, clip=clip) if clip is not None else Worker(model), Language(model.vocabulary, 256)
     first = worker.step(language.batch(32)).item()
     batches = [32, 64, 128, 256, 512]
     seconds = measure(worker, language, batches)
@@ -194,4 +243,9 @@ def main(steps=60, generations=20, slot=0):
 
 
 if __name__ == "__main__":
-    main()
+    import argparse
+
+    parser = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    parser.add_argument("--mixer", choices=("recurrence", "attention"), default="recurrence")
+    parser.add_argument("--clip", type=float, metavar="LIMIT", help="clip the gradients to this norm")
+    main(**vars(parser.parse_args()))
