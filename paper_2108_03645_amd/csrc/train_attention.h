@@ -26,9 +26,12 @@ __device__ __forceinline__ void load_words_to_lds(const unsigned char *base, uin
 // number so that the lanes of a read meet different banks (of 64, 256 bytes at a time), whichever way they read: two pieces of eight rows, or
 // along the rows one piece of rows 0..3 and 12..15 with the next of rows 4..11 (lanes 0..3, 12..15 and 20..27 read at the same time).  (D 64: two
 // rows are 256 bytes.)
+// D: 32, 64, 96 or 128, of which dim may be less; a row has the room of 64 or 128.
+template <int D>
+constexpr int kPieces = D <= 64 ? 8 : 16;
 template <int D, int ROWS, int THREADS>
 struct RowTile {
-  static constexpr int row = D * 2, bytes = ROWS * row, pieces = D / 8, at_once = THREADS / pieces, loads = (ROWS + at_once - 1) / at_once;
+  static constexpr int pieces = kPieces<D>, row = pieces * 16, bytes = ROWS * row, at_once = THREADS / pieces, loads = (ROWS + at_once - 1) / at_once;
   static_assert(at_once % 16 == 0 && ROWS % 16 == 0);
   static constexpr uint32_t kOutside = 0x80000000;
   const unsigned char *base;                  // of the next tile's first row; the same for all threads

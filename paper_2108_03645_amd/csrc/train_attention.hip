@@ -9,6 +9,9 @@ namespace ones {
 namespace train {
 namespace {
 
+#ifndef FWD_VALUES
+#define FWD_VALUES 4
+#endif
 template <typename T, int D, int TN, bool REST>
 __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs a) {
   constexpr int kThreads = 256, kMine = 16 * TN, kRows = 4 * kMine;
@@ -64,16 +67,26 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
     }
     const int key = step * kKeys;
     if (key > first_row + kMine - 1) continue;       // keys behind all of the wave's rows
+    // LDS answers after some hundred cycles: every read is issued ahead of its product, eight of them before the first; those of the values
+    // before the exponentials.
+    constexpr int kSteps = D / 32, kBlocks = D / 16, kReads = 4 * kSteps, kAhead = kReads < 8 ? kReads : 8, kValues = kBlocks < FWD_VALUES ? kBlocks : FWD_VALUES;
+    s16x8 f[kAhead], fs[kValues];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) f[i] = Tile::read_along(ks, i / kSteps * 16, along[i % kSteps]);
+    __builtin_amdgcn_sched_barrier(0);
     f32x4 z[4][TN];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
 #pragma unroll
       for (int n = 0; n < TN; ++n) z[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        const s16x8 f = Tile::read_along(ks, b * 16, along[s]);
+      for (int s = 0; s < kSteps; ++s) {
+        const int i = b * kSteps + s, next = i + kAhead;
 #pragma unroll
-        for (int n = 0; n < TN; ++n) z[b][n] = mfma<T>(f, q[n][s], z[b][n]);
+        for (int n = 0; n < TN; ++n) z[b][n] = mfma<T>(f[i % kAhead], q[n][s], z[b][n]);
+        if (next < kReads) f[i % kAhead] = Tile::read_along(ks, next / kSteps * 16, along[next % kSteps]);
+        else if (next - kReads < kValues) fs[next - kReads] = Tile::read_across(vs, 0, across[next - kReads]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     if (key + kKeys - 1 > first_row) {
@@ -132,16 +145,15 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
       }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int i = 0; i < 2 * kBlocks; ++i) {
+      const int h = i / kBlocks, b = i % kBlocks, next = i + kValues;
 #pragma unroll
-      for (int b = 0; b < D / 16; ++b) {
-        const s16x8 f = Tile::read_across(vs, h * 32, across[b]);
-#pragma unroll
-        for (int n = 0; n < TN; ++n) {
-          acc[b][n] = mfma<T>(f, p[h][n], acc[b][n]);
-          if constexpr (REST) acc[b][n] = mfma<T>(f, lost[h][n], acc[b][n]);
-        }
+      for (int n = 0; n < TN; ++n) {
+        acc[b][n] = mfma<T>(fs[i % kValues], p[h][n], acc[b][n]);
+        if constexpr (REST) acc[b][n] = mfma<T>(fs[i % kValues], lost[h][n], acc[b][n]);
       }
+      if (next < 2 * kBlocks) fs[i % kValues] = Tile::read_across(vs, next / kBlocks * 32, across[next % kBlocks]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   float factor[TN];
@@ -184,7 +196,10 @@ void launch(const AttentionArgs &a, hipStream_t s) {
 }
 template <typename T>
 void launch(const AttentionArgs &a, hipStream_t s) {
-  a.dim <= 64 ? launch<T, 64>(a, s) : launch<T, 128>(a, s);
+  if (a.dim <= 32) return launch<T, 32>(a, s);
+  if (a.dim <= 64) return launch<T, 64>(a, s);
+  if (a.dim <= 96) return launch<T, 96>(a, s);
+  launch<T, 128>(a, s);
 }
 
 }  // namespace

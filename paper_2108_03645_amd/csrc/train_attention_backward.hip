@@ -8,7 +8,7 @@ namespace {
 // delta of every row of a slot and head, and its |do|; of a key head, the largest |v|.  (fp16 scales by the norms, see unit_of().)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
-  constexpr int lanes = D / 8, at_once = 256 / lanes;
+  constexpr int lanes = kPieces<D>, at_once = 256 / lanes;
   constexpr bool norms = __is_same(T, f16);
   __shared__ float part[4];
   const int32_t all = a.heads + (norms ? a.kv_heads : 0);
@@ -146,6 +146,17 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
       k.load(lds + (~step & 1) * Tile::bytes);
       v.load(lds + (2 + (~step & 1)) * Tile::bytes);
     }
+    // reads ahead of their products, as in gradient_of_keys
+    constexpr int kSteps = D / 32, kBlocks = D / 16, kAhead = D == 96 ? 3 : D == 32 ? 2 : 4, kEach = (kAhead + kSteps - 1) / kSteps;
+    s16x8 f[kSteps], e[kSteps], fs[kAhead];
+    const auto rows_at = [&](int b, int s) {
+      f[s] = Tile::read_along(ks, b * 16, along[s]);
+      e[s] = Tile::read_along(vs, b * 16, along[s]);
+    };
+    if (step * kKeys > first_row + kMine - 1) continue;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) rows_at(0, s);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int key = step * kKeys + h * 32;
@@ -156,35 +167,51 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
 #pragma unroll
         for (int n = 0; n < TN; ++n) z[b][n] = d[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-          const s16x8 f = Tile::read_along(ks, h * 32 + b * 16, along[s]), e = Tile::read_along(vs, h * 32 + b * 16, along[s]);
+        for (int s = 0; s < kSteps; ++s) {
 #pragma unroll
           for (int n = 0; n < TN; ++n) {
-            z[b][n] = mfma<T>(f, q[n][s], z[b][n]);
-            d[b][n] = mfma<T>(e, g[n][s], d[b][n]);
+            z[b][n] = mfma<T>(f[s], q[n][s], z[b][n]);
+            d[b][n] = mfma<T>(e[s], g[n][s], d[b][n]);
           }
+          if (b == 0) rows_at(h * 2 + 1, s);
+          else
+#pragma unroll
+            for (int i = s * kEach; i < min((s + 1) * kEach, kAhead); ++i) fs[i] = Tile::read_across(ks, h * 32, across[i]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       s16x8 ds[TN];
 #pragma unroll
       for (int n = 0; n < TN; ++n) {
-        const int row = first_row + n * 16 + (lane & 15) - key;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][n][r], c, -lse[n]));
-            const float s = p * (d[b][n][r] - delta[n]) * unit[n];
-            z[b][n][r] = b * 16 + (lane >> 4) * 4 + r > row ? 0.f : s;
+            z[b][n][r] = p * (d[b][n][r] - delta[n]);
+            if constexpr (__is_same(T, f16)) z[b][n][r] *= unit[n];
           }
+        if (key + 31 > first_row) {
+          const int row = first_row + n * 16 + (lane & 15) - key;
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (b * 16 + (lane >> 4) * 4 + r > row) z[b][n][r] = 0.f;
+        }
         ds[n] = rounded<T>(z[0][n], z[1][n]);
       }
 #pragma unroll
-      for (int b = 0; b < D / 16; ++b) {
-        const s16x8 f = Tile::read_across(ks, h * 32, across[b]);
+      for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
-        for (int n = 0; n < TN; ++n) acc[b][n] = mfma<T>(f, ds[n], acc[b][n]);
+        for (int n = 0; n < TN; ++n) acc[b][n] = mfma<T>(fs[b % kAhead], ds[n], acc[b][n]);
+        if (b + kAhead < kBlocks) fs[b % kAhead] = Tile::read_across(ks, h * 32, across[b + kAhead]);
+        else if (h == 0 && b - (kBlocks - kAhead) < kSteps) rows_at(2, b - (kBlocks - kAhead));
+        __builtin_amdgcn_sched_barrier(0);
       }
+      if (h == 0)
+#pragma unroll
+        for (int s = kAhead; s < kSteps; ++s) rows_at(2, s);
     }
   }
   write_rows<T, D, TN>(acc, factor, dq + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
@@ -290,20 +317,39 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     if (first + kStepRows - 1 < mine) continue;                              // queries in front of all of the wave's keys
     const bool border = first < mine + kMine - 1;
     asm volatile("" : "+v"(along0), "+v"(across0));      // places are formed from these two where they are needed: registers are short
+    // LDS answers after some hundred cycles, so every read is issued a phase ahead of its product, in this order: what the products of the
+    // second 16 queries need between those of the first, what those across the rows need between those of the second.
+    constexpr int kSteps = D / 32, kBlocks = D / 16, kAhead = D > 64 ? 3 : D == 32 ? 2 : 4, kEach = (kAhead + kSteps - 1) / kSteps;
+    s16x8 f[kSteps], e[kSteps], fs[kAhead], es[kAhead];
     Pack<T, 8> p[TN], ds[TN];
+    const auto rows_at = [&](int b, int s) {
+      f[s] = Tile::read_along(qs, b * 16, along0 ^ (s << 6));
+      e[s] = Tile::read_along(gs, b * 16, along0 ^ (s << 6));
+    };
+    const auto block_at = [&](int b) {
+      fs[b % kAhead] = Tile::read_across(gs, 0, across0 ^ (b << 5));
+      es[b % kAhead] = Tile::read_across(qs, 0, across0 ^ (b << 5));
+    };
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) rows_at(0, s);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       f32x4 z[TN], d[TN];
 #pragma unroll
       for (int n = 0; n < TN; ++n) z[n] = d[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        const s16x8 f = Tile::read_along(qs, b * 16, along0 ^ (s << 6)), e = Tile::read_along(gs, b * 16, along0 ^ (s << 6));
+      for (int s = 0; s < kSteps; ++s) {
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
-          z[n] = mfma<T>(f, k[n][s], z[n]);
-          d[n] = mfma<T>(e, v[n][s], d[n]);
+          z[n] = mfma<T>(f[s], k[n][s], z[n]);
+          d[n] = mfma<T>(e[s], v[n][s], d[n]);
         }
+        if (b == 0) rows_at(1, s);
+        else
+#pragma unroll
+          for (int i = s * kEach; i < min((s + 1) * kEach, kAhead); ++i) block_at(i);
+        __builtin_amdgcn_sched_barrier(0);
       }
       const f32x4 t0 = *reinterpret_cast<const f32x4 *>(ts + b * 32), t1 = *reinterpret_cast<const f32x4 *>(ts + b * 32 + 4);
       const float lse[4] = {t0[0], t0[2], t1[0], t1[2]}, delta[4] = {t0[1], t0[3], t1[1], t1[3]};
@@ -329,13 +375,14 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
       }
     }
 #pragma unroll
-    for (int b = 0; b < D / 16; ++b) {
-      const s16x8 f = Tile::read_across(gs, 0, across0 ^ (b << 5)), e = Tile::read_across(qs, 0, across0 ^ (b << 5));
+    for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
       for (int n = 0; n < TN; ++n) {
-        of_v[b][n] = mfma<T>(f, __builtin_bit_cast(s16x8, p[n]), of_v[b][n]);
-        of_k[b][n] = mfma<T>(e, __builtin_bit_cast(s16x8, ds[n]), of_k[b][n]);
+        of_v[b][n] = mfma<T>(fs[b % kAhead], __builtin_bit_cast(s16x8, p[n]), of_v[b][n]);
+        of_k[b][n] = mfma<T>(es[b % kAhead], __builtin_bit_cast(s16x8, ds[n]), of_k[b][n]);
       }
+      if (b + kAhead < kBlocks) block_at(b + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   float k_factor[TN], v_factor[TN];
@@ -441,7 +488,10 @@ void launch(const AttentionArgs &a, hipStream_t s) {
 }
 template <typename T>
 void launch(const AttentionArgs &a, hipStream_t s) {
-  a.dim <= 64 ? launch<T, 64>(a, s) : launch<T, 128>(a, s);
+  if (a.dim <= 32) return launch<T, 32>(a, s);
+  if (a.dim <= 64) return launch<T, 64>(a, s);
+  if (a.dim <= 96) return launch<T, 96>(a, s);
+  launch<T, 128>(a, s);
 }
 
 }  // namespace

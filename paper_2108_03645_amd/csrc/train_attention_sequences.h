@@ -82,6 +82,12 @@ __device__ __forceinline__ float dot(const T *a, const T *b, int32_t dim) {
   return s;
 }
 
+// A constant as an argument, so that a function's body is made for each of its values.
+template <bool VALUE>
+struct Flag {
+  static constexpr bool value = VALUE;
+};
+
 constexpr int kQueries = kAttentionRows, kKeys = 64;       // of a workgroup; of a step
 
 }  // namespace

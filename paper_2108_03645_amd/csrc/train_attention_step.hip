@@ -37,7 +37,7 @@ constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;      // as in train_atte
 template <int D>
 struct WaveTile {
   using Tile = RowTile<D, 32, 256>;           // places of the reads
-  static constexpr int bytes = Tile::bytes, pieces = D / 8, at_once = kWave / pieces, loads = 32 / at_once, kinds = 16 / at_once;
+  static constexpr int bytes = Tile::bytes, pieces = Tile::pieces, at_once = kWave / pieces, loads = 32 / at_once, kinds = 16 / at_once;
   static_assert(at_once == 4 || at_once == 8);
   uint32_t row_bytes, offset[kinds];
   __device__ __forceinline__ void start(int64_t stride, int32_t dim, int lane) {
@@ -132,8 +132,8 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_kernel(StepArgs a) {
         acc[i][r] = d < a.dim && weight != 0.f ? static_cast<float>(v_new[d]) * weight : 0.f;
       }
   }
-  if (split == 0 && of == 0 && threadIdx.x < 2 * (D / 8)) {
-    const int which = threadIdx.x / (D / 8), d = threadIdx.x % (D / 8) * 8;
+  if (split == 0 && of == 0 && threadIdx.x < 2 * Tile::pieces) {
+    const int which = threadIdx.x / Tile::pieces, d = threadIdx.x % Tile::pieces * 8;
     T *to = which ? static_cast<T *>(a.values) + b * a.values_batch + length * a.values_stride + kv * a.values_head
                   : static_cast<T *>(a.keys) + b * a.keys_batch + length * a.keys_stride + kv * a.keys_head;
     if (d < a.dim) *reinterpret_cast<Pack<uint32_t, 4> *>(to + d) = *reinterpret_cast<const Pack<uint32_t, 4> *>((which ? v_new : k_new) + d);
@@ -260,7 +260,9 @@ __global__ __launch_bounds__(1024) void step_join_kernel(StepArgs a) {
 template <typename T>
 void launch(const StepArgs &a, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(a.batch) * a.splits * a.blocks_of_heads * a.kv_heads)), block(kStepWaves * 64);
-  if (a.dim <= 64) hipLaunchKernelGGL((step_kernel<T, 64>), grid, block, 0, s, a);
+  if (a.dim <= 32) hipLaunchKernelGGL((step_kernel<T, 32>), grid, block, 0, s, a);
+  else if (a.dim <= 64) hipLaunchKernelGGL((step_kernel<T, 64>), grid, block, 0, s, a);
+  else if (a.dim <= 96) hipLaunchKernelGGL((step_kernel<T, 96>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((step_kernel<T, 128>), grid, block, 0, s, a);
   if (a.splits > 1) hipLaunchKernelGGL((step_join_kernel<T>), dim3(static_cast<uint32_t>(a.batch * a.heads)), dim3(1024), 0, s, a);
 }
