@@ -9,9 +9,6 @@ namespace ones {
 namespace train {
 namespace {
 
-#ifndef FWD_VALUES
-#define FWD_VALUES 4
-#endif
 template <typename T, int D, int TN, bool REST>
 __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs a) {
   constexpr int kThreads = 256, kMine = 16 * TN, kRows = 4 * kMine;
@@ -69,8 +66,8 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
     if (key > first_row + kMine - 1) continue;       // keys behind all of the wave's rows
     // LDS answers after some hundred cycles: every read is issued ahead of its product, eight of them before the first; those of the values
     // before the exponentials.
-    constexpr int kSteps = D / 32, kBlocks = D / 16, kReads = 4 * kSteps, kAhead = kReads < 8 ? kReads : 8, kValues = kBlocks < FWD_VALUES ? kBlocks : FWD_VALUES;
-    s16x8 f[kAhead], fs[kValues];
+    constexpr int kSteps = D / 32, kBlocks = D / 16, kReads = 4 * kSteps, kAhead = kReads < 8 ? kReads : 8;
+    s16x8 f[kAhead], fs[kBlocks];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) f[i] = Tile::read_along(ks, i / kSteps * 16, along[i % kSteps]);
     __builtin_amdgcn_sched_barrier(0);
@@ -85,7 +82,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
 #pragma unroll
         for (int n = 0; n < TN; ++n) z[b][n] = mfma<T>(f[i % kAhead], q[n][s], z[b][n]);
         if (next < kReads) f[i % kAhead] = Tile::read_along(ks, next / kSteps * 16, along[next % kSteps]);
-        else if (next - kReads < kValues) fs[next - kReads] = Tile::read_across(vs, 0, across[next - kReads]);
+        else if (next - kReads < kBlocks) fs[next - kReads] = Tile::read_across(vs, 0, across[next - kReads]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -146,13 +143,13 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
     }
 #pragma unroll
     for (int i = 0; i < 2 * kBlocks; ++i) {
-      const int h = i / kBlocks, b = i % kBlocks, next = i + kValues;
+      const int h = i / kBlocks, b = i % kBlocks;
 #pragma unroll
       for (int n = 0; n < TN; ++n) {
-        acc[b][n] = mfma<T>(fs[i % kValues], p[h][n], acc[b][n]);
-        if constexpr (REST) acc[b][n] = mfma<T>(fs[i % kValues], lost[h][n], acc[b][n]);
+        acc[b][n] = mfma<T>(fs[b], p[h][n], acc[b][n]);
+        if constexpr (REST) acc[b][n] = mfma<T>(fs[b], lost[h][n], acc[b][n]);
       }
-      if (next < 2 * kBlocks) fs[i % kValues] = Tile::read_across(vs, next / kBlocks * 32, across[next % kBlocks]);
+      if (h == 0) fs[b] = Tile::read_across(vs, 32, across[b]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }

@@ -99,11 +99,28 @@ struct Pairs {
   }
 };
 
-// The sum over the LANES lanes of a row.
+// The sum over the LANES lanes of a row, for all of them: between neighbours, pairs, the halves of 8 (mirrored: what they hold is the same by then)
+// and of 16, then between rows of 16 and between halves of the wave.
+template <int PATTERN>
+__device__ __forceinline__ float from_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), PATTERN, 0xf, 0xf, true));
+}
 template <int LANES>
 __device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int m = 1; m < LANES; m *= 2) v += __shfl_xor(v, m);
+  v += from_lane<0xb1>(v);
+  v += from_lane<0x4e>(v);
+  if constexpr (LANES > 4) v += from_lane<0x141>(v);
+  if constexpr (LANES > 8) v += from_lane<0x140>(v);
+  if constexpr (LANES > 16) {
+    const uint32_t b = __float_as_uint(v);
+    const auto h = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+  }
+  if constexpr (LANES > 32) {
+    const uint32_t b = __float_as_uint(v);
+    const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+  }
   return v;
 }
 
@@ -126,7 +143,7 @@ __global__ __launch_bounds__(256) void rotation_kernel(RotationArgs a) {
   using P = Pairs<VEC, LANES, PER, NEIGHBOURS>;
   constexpr int count = P::count, rows = kWave / LANES;      // rows of a wave at a time
   __shared__ float2 table[4][kMaxPairs];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const P pairs{a.dim, a.turned, lane % LANES};
   float w[2][2][count], dw[BACKWARD ? 2 : 1][2][count];
 #pragma unroll
@@ -138,8 +155,8 @@ __global__ __launch_bounds__(256) void rotation_kernel(RotationArgs a) {
       for (int i = 0; i < count; ++i) dw[k][0][i] = dw[k][1][i] = 0.f;
   }
   const float inverse = 1.f / static_cast<float>(a.dim);
-  const int64_t step = static_cast<int64_t>(gridDim.x) * 4;
-  for (int64_t job = static_cast<int64_t>(blockIdx.x) * 4 + wave; job < a.tokens * a.parts; job += step) {
+  const uint32_t jobs = static_cast<uint32_t>(a.tokens) * a.parts;          // parts above 1 only with few tokens
+  for (uint32_t job = blockIdx.x * 4 + wave; job < jobs; job += gridDim.x * 4) {
     const int64_t token = job / a.parts;
     const int part = static_cast<int>(job % a.parts);
     turns(a, token, table[wave]);
@@ -177,35 +194,35 @@ __global__ __launch_bounds__(256) void rotation_kernel(RotationArgs a) {
           }
         }
 #pragma unroll
-        for (int i = 0; i < count; ++i) square += x1[i] * x1[i] + x2[i] * x2[i];
+        for (int i = 0; i < count; ++i) square = __builtin_fmaf(x1[i], x1[i], __builtin_fmaf(x2[i], x2[i], square));
         const float r = rsqrtf(lanes_sum<LANES>(square) * inverse + a.eps);
         T *out = static_cast<T *>(a.out[k]) + (token * a.heads[k] + h) * a.dim;
         if constexpr (!BACKWARD) {
 #pragma unroll
           for (int i = 0; i < count; ++i) {
             const float n1 = x1[i] * r * w[k][0][i], n2 = x2[i] * r * w[k][1][i];
-            x1[i] = n1 * c[i] - n2 * s[i];
-            x2[i] = n2 * c[i] + n1 * s[i];
+            x1[i] = __builtin_fmaf(n1, c[i], -(n2 * s[i]));
+            x2[i] = __builtin_fmaf(n2, c[i], n1 * s[i]);
           }
           if (live) pairs.store(out, x1, x2, a.past);
         } else {
           float dot = 0.f;
 #pragma unroll
           for (int i = 0; i < count; ++i) {
-            const float b1 = g1[i] * c[i] + g2[i] * s[i], b2 = g2[i] * c[i] - g1[i] * s[i];
+            const float b1 = __builtin_fmaf(g1[i], c[i], g2[i] * s[i]), b2 = __builtin_fmaf(g2[i], c[i], -(g1[i] * s[i]));
             x1[i] *= r;
             x2[i] *= r;
-            dw[k][0][i] += b1 * x1[i];
-            dw[k][1][i] += b2 * x2[i];
+            dw[k][0][i] = __builtin_fmaf(b1, x1[i], dw[k][0][i]);
+            dw[k][1][i] = __builtin_fmaf(b2, x2[i], dw[k][1][i]);
             g1[i] = b1 * w[k][0][i];
             g2[i] = b2 * w[k][1][i];
-            dot += g1[i] * x1[i] + g2[i] * x2[i];
+            dot = __builtin_fmaf(g1[i], x1[i], __builtin_fmaf(g2[i], x2[i], dot));
           }
-          dot = lanes_sum<LANES>(dot) * inverse;
+          dot = lanes_sum<LANES>(dot) * -inverse;
 #pragma unroll
           for (int i = 0; i < count; ++i) {
-            g1[i] = r * (g1[i] - x1[i] * dot);
-            g2[i] = r * (g2[i] - x2[i] * dot);
+            g1[i] = r * __builtin_fmaf(x1[i], dot, g1[i]);
+            g2[i] = r * __builtin_fmaf(x2[i], dot, g2[i]);
           }
           if (live) pairs.store(out, g1, g2, a.past);
         }

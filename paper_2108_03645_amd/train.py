@@ -574,6 +574,8 @@ def _cache(t, name, batch, capacity, kv_heads, dim, like):
     """Checked: a cache is written in place, so its rows have to be loadable as they lie."""
     _check(t, name, (batch, capacity, kv_heads, dim), (like.dtype,), like.device)
     b, s, h, d = t.stride()
+    if not t.is_contiguous() and _overlaps(t):
+        raise ValueError(f"{name}: updated in place, no two of its places may be the same")
     if t.numel() and ((d != 1 and dim > 1) or (b | s | (h if kv_heads > 1 else 0)) % 8 or s < dim or s > _STRIDE or t.data_ptr() % 16):
         raise ValueError(f"{name}: updated in place; its base has to be a multiple of 16 bytes, strides of 8 elements, rows without gaps")
     return t.data_ptr(), b, s, h
@@ -648,6 +650,16 @@ def clip_gradients(gradients, limit, eps=1e-6):
           norm.data_ptr(), _ptr(scratch), nbytes)
     _changed(gradients)
     return norm
+
+
+def _overlaps(t):
+    """Whether two elements of t may lie in one place (or its strides do not rule it out in their order)."""
+    reach = 0
+    for stride, size in sorted((stride, size) for stride, size in zip(t.stride(), t.shape) if size > 1):
+        if stride <= reach:
+            return True
+        reach += stride * (size - 1)
+    return False
 
 
 def _whole(t):

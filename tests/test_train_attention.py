@@ -165,6 +165,19 @@ def test_attention(train, lengths, heads, kv, dim, dtype):
     check(train, q, k, v, offsets_of(lengths), do, rms=max(lengths) >= 64)
 
 
+# enough rows for workgroups of 128 queries; key heads of one and of more query heads (the parts of a group are summed behind, or there is one)
+LARGE = [([5000, 3001, 333], 16, 2, 128, BF16), ([4099, 0, 4100], 16, 16, 64, FP16), ([8222], 16, 1, 96, FP16), ([1] * 50 + [4200, 3983], 32, 16, 32, BF16)]
+
+
+@gpu
+@pytest.mark.parametrize("lengths,heads,kv,dim,dtype", LARGE, ids=["128", "64", "96", "32"])
+def test_attention_of_many_rows(train, lengths, heads, kv, dim, dtype):
+    n = sum(lengths) + 3
+    q, k, v, do = inputs(n + dim, n, heads, kv, dim, dtype)
+    check(train, q, k, v, offsets_of(lengths), do)
+    check(train, q, k, v, offsets_of(lengths))
+
+
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
 def test_rows_outside_all_sequences(train, dtype):
@@ -195,16 +208,16 @@ def test_a_sequence_does_not_see_its_neighbours(train):
 
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
-@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_a_row_does_not_see_what_comes_behind_it(train, bad, dtype):
+@pytest.mark.parametrize("bad,n,heads", [(float("nan"), 200, 2), (float("inf"), 200, 2), (-float("inf"), 200, 2), (float("nan"), 200, 1), (float("nan"), 2310, 64)])
+def test_a_row_does_not_see_what_comes_behind_it(train, bad, n, heads, dtype):
     """Infinities and NaN of a token reach its own row of o and dq and those behind it, its own of dk and dv and those before it, and no other.
     Rows that share a step with it are summed another way: either way is off by a share of h, so they differ by up to two (rest: by as much as o)."""
     def alike(got, right, what):
         size = want[0].float().norm() if what[1] == "rest" else right.float().norm()
         assert got.isfinite().all() and (got.float() - right.float()).norm() <= 2 * HALF[dtype] * size, what
 
-    n, at = 200, 77
-    clean = inputs(30, n, 2, 1, 128, dtype)
+    at = 77
+    clean = inputs(30, n, heads, 1, 128, dtype)
     ends = offsets_of([n])
     offsets = torch.tensor(ends, device="cuda", dtype=torch.int32)
     want = check(train, *clean[:3], ends, clean[3])
@@ -436,7 +449,9 @@ def test_a_step_without_room(train):
     with pytest.raises(ValueError):
         train.attention_step(q, k, v, keys[..., :63], values, torch.zeros(4, device="cuda", dtype=torch.int32))
     with pytest.raises(ValueError):
-        train.attention_step(q, k, v, keys.transpose(2, 3).contiguous().transpose(2, 3).expand(4, 40, 1, 64)[:, :, :, :], values.permute(3, 0, 1, 2).contiguous().permute(1, 2, 3, 0), torch.zeros(4, device="cuda", dtype=torch.int32))
+        train.attention_step(q, k, v, keys, values.permute(3, 0, 1, 2).contiguous().permute(1, 2, 3, 0), torch.zeros(4, device="cuda", dtype=torch.int32))
+    with pytest.raises(ValueError):                                  # one cache for all sequences: two would write one place
+        train.attention_step(q, k, v, keys[:1].expand(4, 40, 1, 64), values, torch.zeros(4, device="cuda", dtype=torch.int32))
     empty = torch.empty(4, 0, 1, 64, device="cuda", dtype=torch.bfloat16)
     assert train.attention_step(q, k, v, empty, empty, torch.zeros(4, device="cuda", dtype=torch.int32)).isnan().all()
     none = torch.empty(0, 2, 64, device="cuda", dtype=torch.bfloat16)
@@ -478,3 +493,73 @@ def test_a_cache_beyond_32_bits_of_offsets(train):
     want = train.attention_step(q, k, v, near_k, near_v, lengths)
     got = train.attention_step(q, k, v, keys, values, lengths)
     assert torch.equal(got, want) and torch.equal(keys, near_k) and torch.equal(values, near_v)
+
+
+SHIM = r"""
+#include "train_plan.h"
+using namespace ones::train;
+extern "C" {
+void attention(int64_t tokens, int64_t sequences, int64_t heads, int64_t kv, int64_t dim, int64_t *to) {
+  const AttentionPlan p = attention_plan(tokens, sequences, heads, kv, dim);
+  to[0] = attention_few(tokens, heads); to[1] = p.parts; to[2] = static_cast<int64_t>(p.bytes);
+}
+void step(int64_t batch, int64_t capacity, int64_t heads, int64_t kv, int64_t dim, int64_t *to) {
+  const StepPlan p = step_plan(batch, capacity, heads, kv, dim);
+  to[0] = p.splits; to[1] = p.blocks_of_heads; to[2] = static_cast<int64_t>(p.bytes);
+}
+void rotation(int64_t tokens, int64_t heads, int64_t kv, int64_t dim, int64_t pairs, int64_t bytes, int64_t backward, int64_t *to) {
+  const RotationPlan p = rotation_plan(tokens, heads, kv, dim, pairs, bytes, backward != 0);
+  to[0] = p.vec; to[1] = p.lanes; to[2] = p.per; to[3] = p.parts; to[4] = p.blocks;
+}
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plans(tmp_path_factory):
+    import os
+    import shutil
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    compiler = shutil.which("g++")
+    if not compiler:
+        pytest.skip("no g++")
+    at = tmp_path_factory.mktemp("plans")
+    (at / "shim.cpp").write_text(SHIM)
+    subprocess.check_call([compiler, "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{root}/include", f"-I{root}/paper_2108_03645_amd/csrc", str(at / "shim.cpp"),
+                           "-o", str(at / "shim.so")])
+    lib = C.CDLL(str(at / "shim.so"))
+
+    def ask(name, *sizes):
+        to = (C.c_int64 * 8)()
+        getattr(lib, name)(*[C.c_int64(v) for v in sizes], to)
+        return list(to)
+
+    return ask
+
+
+def test_the_sizes_above_reach_every_kernel_and_cut(plans):
+    """Workgroups of 64 and of 128 queries, one part of a group's heads and more, keys in one part and in more, loads of 16, 8 and less bytes."""
+    few = {(plans("attention", sum(s[0]), len(s[0]), *s[1:4])[0], (s[3] + 31) // 32) for s in SHAPES + LARGE}
+    assert few == {(a, b) for a in (0, 1) for b in (1, 2, 3, 4)}
+    parts = {(plans("attention", sum(s[0]), len(s[0]), *s[1:4])[1] > 1) for s in LARGE}
+    assert parts == {False, True}
+    assert {plans("step", len(s[0]), *s[1:])[0] > 1 for s in STEPS} == {False, True} == {plans("step", len(s[0]), *s[1:])[1] > 1 for s in STEPS}
+    from test_train_rotation import CASES
+    lanes = {(plans("rotation", *c[:5], b, back)[0] * b, back) for c in CASES for b in (2, 4) for back in (0, 1)}
+    assert lanes >= {(16, 0), (8, 0), (16, 1), (8, 1)} and any(plans("rotation", *c[:5], 2, 0)[0] == 1 for c in CASES)
+    assert {plans("rotation", *c[:5], 2, 1)[3] > 1 for c in CASES} == {False, True}
+
+
+def test_parts_and_splits_stay_within_bounds(plans):
+    import random
+    rng = random.Random(4)
+    for _ in range(3000):
+        kv, group, tokens = rng.randint(1, 64), rng.choice([1, 2, 3, 7, 16]), int(2 ** rng.uniform(0, 24))
+        _, parts, *_ = plans("attention", tokens, rng.randint(0, 100), kv * group, kv, 64)
+        assert 1 <= parts <= group and -(-group // -(-group // parts)) == parts          # no part without a head
+        splits, blocks, *_ = plans("step", rng.randint(1, 3000), int(2 ** rng.uniform(0, 26)), kv * group, kv, 64)
+        assert 1 <= splits <= 512 and (blocks - 1) * 16 < group <= blocks * 16
+        dim = rng.randint(1, 512)
+        vec, lanes, per, _, n, *_ = plans("rotation", tokens, kv * group, kv, dim, rng.randint(0, dim // 2), rng.choice([2, 4]), rng.randint(0, 1))
+        assert vec * lanes * per >= (dim + 1) // 2 and lanes in (4, 8, 16, 32, 64) and 1 <= n <= 2048 and (vec > 1 or (lanes == 16 and per <= 16))
