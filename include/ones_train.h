@@ -155,8 +155,8 @@ int ones_head_norm_rotation_backward(const void *dq_out, int64_t dq_stride, int6
  * keep them from its ends).  dim: 8 .. ONES_MAX_ATTENTION_DIM, a multiple of 8; bases multiples of 16 bytes, strides of 8 elements, between
  * tokens at least dim and at most 2^20.  heads: a multiple of kv_heads.  scale: 1e-30 to 1e30.
  * Backward: dout is the gradient of o; dk and dv are summed over the query heads of a key head.
- * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size or stride above its limit; (tokens / 128 + sequences + 2) * (heads + kv_heads)
- * of 2^24 or more), ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
+ * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size or stride above its limit; (tokens / 64 + sequences + 2) * heads of 2^23 or
+ * more), ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
 int ones_attention_forward(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride, int64_t k_head_stride,
                            const void *v, int64_t v_stride, int64_t v_head_stride, int64_t tokens, int64_t heads, int64_t kv_heads,
                            int64_t dim, int32_t type, const int32_t *offsets, int64_t sequences, float scale, void *o, void *rest,

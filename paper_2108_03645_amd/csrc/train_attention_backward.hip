@@ -464,27 +464,40 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   }
 }
 
-template <typename T, int D, int TN>
+template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char lds[4 * RowTile<D, kKeys, 256>::bytes];
-  gradient_of_queries<T, D, TN>(a, blockIdx.x, lds);
+  gradient_of_queries<T, D, 2>(a, blockIdx.x, lds);
 }
 template <typename T, int D>
-__global__ __launch_bounds__(4 * kKeyRows, 3) void attention_dkv_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(256, 3) void attention_dkv_kernel(AttentionArgs a) {
   __shared__ __attribute__((aligned(256))) unsigned char lds[kKeysLds<T, D>];
   gradient_of_keys<T, D>(a, blockIdx.x, lds);
+}
+// Both side by side, the first `keys` workgroups those of the keys: where either is few, the other fills what it leaves idle.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attention_gradients_kernel(AttentionArgs a, uint32_t keys) {
+  constexpr int bytes = 4 * RowTile<D, kKeys, 256>::bytes;
+  static_assert(kKeysLds<T, D> <= bytes);
+  __shared__ __attribute__((aligned(256))) unsigned char lds[bytes];
+  if (blockIdx.x < keys) gradient_of_keys<T, D>(a, blockIdx.x, lds);
+  else gradient_of_queries<T, D, 1>(a, blockIdx.x - keys, lds);
 }
 
 template <typename T, int D>
 void launch(const AttentionArgs &a, hipStream_t s) {
-  const int64_t slots = slots_of(a.tokens, a.sequences, kQueries), all = a.heads + (__is_same(T, f16) ? a.kv_heads : 0);
+  const int64_t slots = slots_of(a.tokens, a.sequences, kQueries), half_slots = slots_of(a.tokens, a.sequences, 64);
+  const int64_t all = a.heads + (__is_same(T, f16) ? a.kv_heads : 0);
+  const uint32_t keys = static_cast<uint32_t>(half_slots * a.kv_heads * a.parts);
+  static_assert(kKeyRows == 64);
   hipLaunchKernelGGL((attention_delta_kernel<T, D>), dim3(static_cast<uint32_t>(slots * all)), dim3(256), 0, s, a);
-  hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(static_cast<uint32_t>(slots_of(a.tokens, a.sequences, kKeyRows) * a.kv_heads * a.parts)), dim3(4 * kKeyRows), 0, s, a);
+  if (attention_few(a.tokens, a.heads)) {
+    hipLaunchKernelGGL((attention_gradients_kernel<T, D>), dim3(keys + static_cast<uint32_t>(half_slots * a.heads)), dim3(256), 0, s, a, keys);
+  } else {
+    hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(keys), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attention_dq_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.heads)), dim3(256), 0, s, a);
+  }
   if (a.parts > 1) hipLaunchKernelGGL((attention_join_kernel<T>), dim3(2048), dim3(256), 0, s, a);
-  const bool few = attention_few(a.tokens, a.heads);
-  const dim3 queries(static_cast<uint32_t>(slots_of(a.tokens, a.sequences, few ? 64 : 128) * a.heads));
-  if (few) hipLaunchKernelGGL((attention_dq_kernel<T, D, 1>), queries, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((attention_dq_kernel<T, D, 2>), queries, dim3(256), 0, s, a);
 }
 template <typename T>
 void launch(const AttentionArgs &a, hipStream_t s) {

@@ -332,7 +332,7 @@ inline int check_attention(int64_t tokens, int64_t heads, int64_t kv_heads, int6
     return ONES_E_INVALID_ARG;
   if (tokens > ONES_MAX_TOKENS || heads > ONES_MAX_HEADS || dim > ONES_MAX_ATTENTION_DIM || sequences > ONES_MAX_TOKENS) return ONES_E_BOUNDS;
   // threads of a launch, numbered in 32 bits
-  return std::max((tokens / kAttentionRows + sequences + 2) * (heads + kv_heads), (tokens / kAttentionKeys + sequences + 2) * heads) >= (int64_t{1} << 24) ? ONES_E_BOUNDS : ONES_OK;
+  return std::max((tokens / kAttentionRows + sequences + 2) * (heads + kv_heads), (tokens / kAttentionKeys + sequences + 2) * heads * 2) >= (int64_t{1} << 24) ? ONES_E_BOUNDS : ONES_OK;
 }
 // Rows that are loaded to LDS as they lie.
 inline int check_head_rows(const void *p, int64_t stride, int64_t head_stride, int64_t heads, int64_t dim) {
