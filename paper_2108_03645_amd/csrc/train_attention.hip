@@ -12,7 +12,8 @@ namespace {
 template <typename T, int D, int TN, bool REST>
 __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs a) {
   constexpr int kThreads = 256, kMine = 16 * TN, kRows = 4 * kMine;
-  using Tile = RowTile<D, kKeys, kThreads>;
+  constexpr int kStep = kKeys<TN>, kHalves = kStep / 32;                    // keys of a step, and runs of 32 of them
+  using Tile = RowTile<D, kStep, kThreads>;
   __shared__ __attribute__((aligned(256))) unsigned char lds[4 * Tile::bytes];
   const Turn turn = turn_of(blockIdx.x, a.heads, a.kv_heads);
   const int32_t last_slot = static_cast<int32_t>(slots_of(a.tokens, a.sequences, kRows)) - 1;
@@ -54,7 +55,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) acc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const int steps = (rows.at + count + kKeys - 1) / kKeys, first_row = rows.at + mine;
+  const int steps = (rows.at + count + kStep - 1) / kStep, first_row = rows.at + mine;
   for (int step = 0; step < steps; ++step) {
     meet<0>();
     const unsigned char *ks = lds + (step & 1) * Tile::bytes, *vs = ks + 2 * Tile::bytes;
@@ -62,18 +63,18 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
       k.load(lds + (~step & 1) * Tile::bytes);
       v.load(lds + (2 + (~step & 1)) * Tile::bytes);
     }
-    const int key = step * kKeys;
+    const int key = step * kStep;
     if (key > first_row + kMine - 1) continue;       // keys behind all of the wave's rows
     // LDS answers after some hundred cycles: every read is issued ahead of its product, eight of them before the first; those of the values
     // before the exponentials.
-    constexpr int kSteps = D / 32, kBlocks = D / 16, kReads = 4 * kSteps, kAhead = kReads < 8 ? kReads : 8;
+    constexpr int kSteps = D / 32, kBlocks = D / 16, kReads = 2 * kHalves * kSteps, kAhead = kReads < 8 ? kReads : 8;
     s16x8 f[kAhead], fs[kBlocks];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) f[i] = Tile::read_along(ks, i / kSteps * 16, along[i % kSteps]);
     __builtin_amdgcn_sched_barrier(0);
-    f32x4 z[4][TN];
+    f32x4 z[2 * kHalves][TN];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < 2 * kHalves; ++b) {
 #pragma unroll
       for (int n = 0; n < TN; ++n) z[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -86,12 +87,12 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (key + kKeys - 1 > first_row) {
+    if (key + kStep - 1 > first_row) {
 #pragma unroll
       for (int n = 0; n < TN; ++n) {
         const int row = first_row + n * 16 + (lane & 15) - key;
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < 2 * kHalves; ++b)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
             if (b * 16 + (lane >> 4) * 4 + r > row) z[b][n][r] = -INFINITY;
@@ -102,14 +103,15 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
     bool grown = false;
 #pragma unroll
     for (int n = 0; n < TN; ++n) {
-      float m[2] = {fmaxf(z[0][n][0], z[0][n][1]), fmaxf(z[1][n][0], z[1][n][1])};
+      float m[kHalves];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < kHalves; ++h) {
+        m[h] = fmaxf(z[h][n][0], z[h][n][1]);
         m[h] = fmaxf(fmaxf(m[h], z[h][n][2]), z[h][n][3]);
-        m[h] = fmaxf(fmaxf(m[h], z[2 + h][n][0]), z[2 + h][n][1]);
-        m[h] = fmaxf(fmaxf(m[h], z[2 + h][n][2]), z[2 + h][n][3]);
+        m[h] = fmaxf(fmaxf(m[h], z[kHalves + h][n][0]), z[kHalves + h][n][1]);
+        m[h] = fmaxf(fmaxf(m[h], z[kHalves + h][n][2]), z[kHalves + h][n][3]);
       }
-      most[n] = across_max(fmaxf(m[0], m[1]));
+      most[n] = across_max(fmaxf(m[0], m[kHalves - 1]));
       grown |= (most[n] - top[n]) * c > kSlack;
     }
     if (__any(grown)) {
@@ -122,13 +124,13 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
         top[n] = next;
       }
     }
-    s16x8 p[2][TN], lost[2][TN];              // lost: what the rounding takes from the exponentials
+    s16x8 p[kHalves][TN], lost[kHalves][TN];              // lost: what the rounding takes from the exponentials
 #pragma unroll
     for (int n = 0; n < TN; ++n) {
       const float base = (top[n] == -INFINITY ? 0.f : top[n] * c) - kShift<T>;
       float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+      for (int b = 0; b < 2 * kHalves; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           z[b][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][n][r], c, -base));
@@ -136,20 +138,20 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
         }
       sum[n] += (sums[0] + sums[1]) + (sums[2] + sums[3]);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < kHalves; ++h) {
         p[h][n] = rounded<T>(z[2 * h][n], z[2 * h + 1][n]);
         if constexpr (REST) lost[h][n] = remainder<T>(z[2 * h][n], z[2 * h + 1][n], p[h][n]);
       }
     }
 #pragma unroll
-    for (int i = 0; i < 2 * kBlocks; ++i) {
+    for (int i = 0; i < kHalves * kBlocks; ++i) {
       const int h = i / kBlocks, b = i % kBlocks;
 #pragma unroll
       for (int n = 0; n < TN; ++n) {
         acc[b][n] = mfma<T>(fs[b], p[h][n], acc[b][n]);
         if constexpr (REST) acc[b][n] = mfma<T>(fs[b], lost[h][n], acc[b][n]);
       }
-      if (h == 0) fs[b] = Tile::read_across(vs, 32, across[b]);
+      if (h + 1 < kHalves) fs[b] = Tile::read_across(vs, 32, across[b]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }

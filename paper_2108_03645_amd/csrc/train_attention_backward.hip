@@ -88,10 +88,11 @@ __device__ __forceinline__ float largest_norm(const float *norms, int32_t all, i
   return most;
 }
 
-template <typename T, int D, int TN>
+template <typename T, int D>
 __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint32_t id, unsigned char *lds) {
-  constexpr int kMine = 16 * TN, kRows = 4 * kMine;
-  using Tile = RowTile<D, kKeys, 256>;
+  constexpr int TN = 1, kMine = 16 * TN, kRows = 4 * kMine;
+  constexpr int kStep = kKeys<TN>, kHalves = kStep / 32;
+  using Tile = RowTile<D, kStep, 256>;
   const Turn turn = turn_of(id, a.heads, a.kv_heads);
   const int32_t slot = static_cast<int32_t>(slots_of(a.tokens, a.sequences, kRows)) - 1 - turn.slot;
   const Rows rows = rows_of<kRows>(a.offsets, a.sequences, a.tokens, slot);
@@ -138,7 +139,7 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
   for (int n = 0; n < TN; ++n)
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) acc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int steps = (rows.at + count + kKeys - 1) / kKeys, first_row = rows.at + mine;
+  const int steps = (rows.at + count + kStep - 1) / kStep, first_row = rows.at + mine;
   for (int step = 0; step < steps; ++step) {
     meet<0>();
     const unsigned char *ks = lds + (step & 1) * Tile::bytes, *vs = ks + 2 * Tile::bytes;
@@ -153,13 +154,13 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
       f[s] = Tile::read_along(ks, b * 16, along[s]);
       e[s] = Tile::read_along(vs, b * 16, along[s]);
     };
-    if (step * kKeys > first_row + kMine - 1) continue;
+    if (step * kStep > first_row + kMine - 1) continue;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) rows_at(0, s);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int key = step * kKeys + h * 32;
+    for (int h = 0; h < kHalves; ++h) {
+      const int key = step * kStep + h * 32;
       if (key > first_row + kMine - 1) break;
       f32x4 z[2][TN], d[2][TN];
 #pragma unroll
@@ -206,10 +207,10 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
 #pragma unroll
         for (int n = 0; n < TN; ++n) acc[b][n] = mfma<T>(fs[b % kAhead], ds[n], acc[b][n]);
         if (b + kAhead < kBlocks) fs[b % kAhead] = Tile::read_across(ks, h * 32, across[b + kAhead]);
-        else if (h == 0 && b - (kBlocks - kAhead) < kSteps) rows_at(2, b - (kBlocks - kAhead));
+        else if (h + 1 < kHalves && b - (kBlocks - kAhead) < kSteps) rows_at(2, b - (kBlocks - kAhead));
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (h == 0)
+      if (h + 1 < kHalves)
 #pragma unroll
         for (int s = kAhead; s < kSteps; ++s) rows_at(2, s);
     }
@@ -464,24 +465,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   }
 }
 
+// The gradients of keys and queries side by side, the first `keys` workgroups those of the keys: each fills what the other leaves idle.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionArgs a) {
-  __shared__ __attribute__((aligned(256))) unsigned char lds[4 * RowTile<D, kKeys, 256>::bytes];
-  gradient_of_queries<T, D, 2>(a, blockIdx.x, lds);
-}
-template <typename T, int D>
-__global__ __launch_bounds__(256, 3) void attention_dkv_kernel(AttentionArgs a) {
-  __shared__ __attribute__((aligned(256))) unsigned char lds[kKeysLds<T, D>];
-  gradient_of_keys<T, D>(a, blockIdx.x, lds);
-}
-// Both side by side, the first `keys` workgroups those of the keys: where either is few, the other fills what it leaves idle.
-template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attention_gradients_kernel(AttentionArgs a, uint32_t keys) {
-  constexpr int bytes = 4 * RowTile<D, kKeys, 256>::bytes;
-  static_assert(kKeysLds<T, D> <= bytes);
+__global__ __launch_bounds__(256, 3) void attention_gradients_kernel(AttentionArgs a, uint32_t keys) {
+  constexpr int queries = 4 * RowTile<D, kKeys<1>, 256>::bytes, bytes = queries > kKeysLds<T, D> ? queries : kKeysLds<T, D>;
   __shared__ __attribute__((aligned(256))) unsigned char lds[bytes];
   if (blockIdx.x < keys) gradient_of_keys<T, D>(a, blockIdx.x, lds);
-  else gradient_of_queries<T, D, 1>(a, blockIdx.x - keys, lds);
+  else gradient_of_queries<T, D>(a, blockIdx.x - keys, lds);
 }
 
 template <typename T, int D>
@@ -491,12 +481,7 @@ void launch(const AttentionArgs &a, hipStream_t s) {
   const uint32_t keys = static_cast<uint32_t>(half_slots * a.kv_heads * a.parts);
   static_assert(kKeyRows == 64);
   hipLaunchKernelGGL((attention_delta_kernel<T, D>), dim3(static_cast<uint32_t>(slots * all)), dim3(256), 0, s, a);
-  if (attention_few(a.tokens, a.heads)) {
-    hipLaunchKernelGGL((attention_gradients_kernel<T, D>), dim3(keys + static_cast<uint32_t>(half_slots * a.heads)), dim3(256), 0, s, a, keys);
-  } else {
-    hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(keys), dim3(256), 0, s, a);
-    hipLaunchKernelGGL((attention_dq_kernel<T, D>), dim3(static_cast<uint32_t>(slots * a.heads)), dim3(256), 0, s, a);
-  }
+  hipLaunchKernelGGL((attention_gradients_kernel<T, D>), dim3(keys + static_cast<uint32_t>(half_slots * a.heads)), dim3(256), 0, s, a, keys);
   if (a.parts > 1) hipLaunchKernelGGL((attention_join_kernel<T>), dim3(2048), dim3(256), 0, s, a);
 }
 template <typename T>

@@ -88,7 +88,10 @@ struct Flag {
   static constexpr bool value = VALUE;
 };
 
-constexpr int kQueries = kAttentionRows, kKeys = 64;       // of a workgroup; of a step
+constexpr int kQueries = kAttentionRows;
+// Keys of a step, by the rows of 16 of a wave's part: of 32 where there is one, so that more workgroups fit into a compute unit.
+template <int TN>
+constexpr int kKeys = TN == 1 ? 32 : 64;
 
 }  // namespace
 }  // namespace train

@@ -323,8 +323,9 @@ inline int check_rotation(int64_t tokens, int64_t heads, int64_t kv_heads, int64
 constexpr int64_t kAttentionRows = 128, kAttentionKeys = 64;      // queries of a workgroup, or half of them; keys of one of their gradients
 constexpr int64_t kPartsWanted = 2048;        // workgroups of the keys' gradients
 
-// Whether workgroups of 128 queries are too few for the compute units, so that those of 64 carry more.
-inline bool attention_few(int64_t tokens, int64_t heads) { return ceil_div(tokens, kAttentionRows) * heads < 1024; }
+// Whether workgroups of 128 queries are too few for the compute units, so that those of 64 carry more (forward, bf16, sequences x tokens, heads,
+// elements: 1 x 2048, 8, 128: 47 us against 42; 8 x 512, 16, 128: 22 and 22; 1 x 8192, 16, 128: 281 and 335).
+inline bool attention_few(int64_t tokens, int64_t heads) { return ceil_div(tokens, kAttentionRows) * heads < 512; }
 
 inline int check_attention(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, int64_t sequences, float scale) {
   if (tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || dim < 8 || dim % 8 || sequences < 0 || (type != ONES_F16 && type != ONES_BF16) ||
