@@ -280,41 +280,40 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
   for (int n = 0; n < TN; ++n)
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) of_k[b][n] = of_v[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // the queries from the tile's first key on, head after head
+  // The queries from the tile's first key on, the last ones first, of all heads before the next ones: the workgroups of a sequence end at different
+  // queries but begin at the same ones, so that they read the same rows at the same time, which then come from L2 (head after head
+  // from the first query on, 16 x 2048 x 16 over 2 x 128 read 4 GB from behind L2).
   const int32_t left = rows.length - rows.at;
   const int steps = (left + kStepRows - 1) / kStepRows, each = (group + a.parts - 1) / a.parts, head0 = kv * group + part * each;
   const int heads = min(each, group - part * each), all_steps = steps * max(heads, 0);
   Tile q, g;
-  const unsigned char *terms;
-  auto begin = [&](int head) {
-    q.start(at<T>(a.q, here, a.q_stride, head0 + head, a.q_head), a.q_stride, left, a.dim);
-    g.start(at<T>(a.dout, here, a.do_stride, head0 + head, a.do_head), a.do_stride, left, a.dim);
-    terms = reinterpret_cast<const unsigned char *>(a.terms + static_cast<int64_t>(head0 + head) * a.tokens + here);
-  };
-  auto load = [&](int to) {
+  q.start(at<T>(a.q, here, a.q_stride, head0, a.q_head), a.q_stride, left, a.dim);
+  g.start(at<T>(a.dout, here, a.do_stride, head0, a.do_head), a.do_stride, left, a.dim);
+  const unsigned char *const q0 = q.base, *const g0 = g.base, *const terms0 = reinterpret_cast<const unsigned char *>(a.terms + static_cast<int64_t>(head0) * a.tokens + here);
+  auto load = [&](int to, int step, int head) {
+    const int64_t row = step * kStepRows;
+    q.left = g.left = left - step * kStepRows;
+    q.base = q0 + row * q.row_bytes + head * a.q_head * 2;
+    g.base = g0 + row * g.row_bytes + head * a.do_head * 2;
     if (wave == 0) {
       const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LdsBytes *)(lds + 4 * Tile::bytes + to * kStepRows * 8)));
-      load_words_to_lds(terms, static_cast<uint32_t>(max(min(q.left, kStepRows), 0)) * 8, lane * 4, at);
+      load_words_to_lds(terms0 + (row + static_cast<int64_t>(head) * a.tokens) * 8, static_cast<uint32_t>(min(q.left, kStepRows)) * 8, lane * 4, at);
     }
-    terms += kStepRows * 8;
     q.load(lds + to * Tile::bytes);
     g.load(lds + (2 + to) * Tile::bytes);
   };
-  if (all_steps) {
-    begin(0);
-    load(0);
-  }
-  int head = 0, step = 0;
+  int head = 0, step = steps - 1;
+  if (all_steps) load(0, step, 0);
   for (int t = 0; t < all_steps; ++t) {
     meet<0>();
     const unsigned char *qs = lds + (t & 1) * Tile::bytes, *gs = qs + 2 * Tile::bytes;
     const float *ts = reinterpret_cast<const float *>(lds + 4 * Tile::bytes + (t & 1) * kStepRows * 8) + (lane >> 4) * 8;
     const int first = step * kStepRows;                                      // from the tile's first key on
-    if (++step == steps) {
-      step = 0;
-      if (++head < heads) begin(head);
+    if (++head == heads) {
+      head = 0;
+      --step;
     }
-    if (t + 1 < all_steps) load(~t & 1);
+    if (t + 1 < all_steps) load(~t & 1, step, head);
     if (first + kStepRows - 1 < mine) continue;                              // queries in front of all of the wave's keys
     const bool border = first < mine + kMine - 1;
     asm volatile("" : "+v"(along0), "+v"(across0));      // places are formed from these two where they are needed: registers are short

@@ -129,6 +129,7 @@ constexpr int kMaxPairs = ONES_MAX_HEAD_DIM / 2;
 // Cosines and sines of a token's pairs to LDS, a lane each.  The angle is formed in turns in 64 bits, so that far positions keep
 // theirs, and is at most half a turn in 32.
 __device__ __forceinline__ void turns(const RotationArgs &a, int64_t token, float2 *to) {
+  if (a.turned == 0) return;                  // then there may be no positions
   const double position = a.positions[token];
   for (int p = threadIdx.x % kWave; p < a.turned; p += kWave) {
     const double t = position * static_cast<double>(a.frequencies[p]) * 0.15915494309189535;

@@ -142,6 +142,16 @@ def test_rows_of_nothing_of_zeros_and_of_nan(train):
 
 
 @gpu
+def test_norms_alone_need_no_positions(train):
+    x, w = torch.randn(9, 2, 40, device="cuda"), torch.rand(40, device="cuda") + 0.5
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    rc = train.load().ones_head_norm_rotation_forward(x.data_ptr(), 80, 40, x.data_ptr(), 80, 40, 9, 2, 2, 40, 0, w.data_ptr(), w.data_ptr(), 0, 1e-6, None, None, 0, 0,
+                                                      y.data_ptr(), z.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(y, z)
+    near(y, x.double() * (x.double().pow(2).mean(-1, keepdim=True) + 1e-6) ** -0.5 * w.double(), x.double().abs() * 2, 64, "y")
+
+
+@gpu
 def test_gradients_under_autograd_against_differences(train):
     gen = torch.Generator(device="cuda").manual_seed(6)
     make = lambda *s: torch.randn(*s, generator=gen, device="cuda", requires_grad=True)  # noqa: E731
