@@ -3,6 +3,21 @@
 //   z_ij = scale q_i . k_j for j <= i, lse_i = log sum_j exp z_ij, p_ij = exp(z_ij - lse_i), o_i = sum_j p_ij v_j
 //   delta_i = do_i . o_i, ds_ij = p_ij (do_i . v_j - delta_i)
 //   dv_j = sum_i p_ij do_i, dk_j = scale sum_i ds_ij q_i (both over the heads of a group, too), dq_i = scale sum_j ds_ij k_j
+//
+// A workgroup takes 128 queries (64 where these would be too few workgroups) of one head and walks along the keys that they see, 64 (or 32) at a
+// step: keys and values come to LDS by direct loads into two places in turn, a wave keeps its 32 (16) queries, the largest score so far, the sum
+// of exponentials and o in registers.  Keys are the rows of the first product and the k of the second, so that exponentials go from one to the
+// other where they are.  Queries that end late are begun first.
+//
+// Exponentials are rounded to the operands' type for the product with the values: o is off by about as much again as by its own rounding.
+// For the gradients that is too much: delta_i = do_i . o_i is subtracted from numbers of its own size, and dq of short sequences would be off by
+// three times its rounding.  With `rest` wanted, what the rounding takes from the exponentials goes through a second product, and
+// what it takes from o is left behind.
+//
+// What bounds it: the matrix units, the exponentials, of which little hides behind them, and the power that both draw.  16384 tokens, 16 heads over 2 of 128, bf16: 1.01 to 1.09 ms, 1.0 to 1.1 PFLOP/s of the causal half (the same of zeros: 0.90 ms;
+// a library product of 8192 cubed: 1.27 to 1.35 PFLOP/s, of zeros 1.75); the matrix units are busy half of the cycles, the vector units 60 %, LDS
+// 25 %.  16 x 2048 tokens with `rest`: 0.46 ms.  Tried and not kept: four waves a SIMD with 16 queries each (1.17 ms), scores a run ahead
+// of the exponentials (1.10), wave priorities (1.08), groups of instructions set by hand (1.10 to 1.19).
 #include "train_attention_sequences.h"
 
 namespace ones {

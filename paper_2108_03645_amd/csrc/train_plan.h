@@ -321,11 +321,14 @@ inline int check_rotation(int64_t tokens, int64_t heads, int64_t kv_heads, int64
 
 // ---------------------------------------------------------------- attention --------
 constexpr int64_t kAttentionRows = 128, kAttentionKeys = 64;      // queries of a workgroup, or half of them; keys of one of their gradients
-constexpr int64_t kPartsWanted = 2048;        // workgroups of the keys' gradients
+// Workgroups of the keys' gradients: a group's heads are parted until there are so many, whose sums a small launch adds up (16 x 2048 tokens, 16
+// heads over 2 of 128, forward and backward: 512 workgroups 1.84 ms, 1024 1.76, 2048 1.70, 4096 1.72).
+constexpr int64_t kPartsWanted = 2048;
 
-// Whether workgroups of 128 queries are too few for the compute units, so that those of 64 carry more (forward, bf16, sequences x tokens, heads,
-// elements: 1 x 2048, 8, 128: 47 us against 42; 8 x 512, 16, 128: 22 and 22; 1 x 8192, 16, 128: 281 and 335).
-inline bool attention_few(int64_t tokens, int64_t heads) { return ceil_div(tokens, kAttentionRows) * heads < 512; }
+// Whether workgroups of 128 queries are too few for the compute units, so that those of 64 carry more (forward, sequences x tokens, heads,
+// elements, us of 128 and of 64: 1 x 2048, 8, 128: 47 and 42; 8 x 512, 16, 128: 22 and 22; 19 of 6007 tokens, 12, 80: 49 and 42;
+// 8 x 1024, 16, 128: 58 and 61; 1 x 8192, 16, 128: 281 and 335).
+inline bool attention_few(int64_t tokens, int64_t heads) { return ceil_div(tokens, kAttentionRows) * heads < 768; }
 
 inline int check_attention(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t dim, int32_t type, int64_t sequences, float scale) {
   if (tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || dim < 8 || dim % 8 || sequences < 0 || (type != ONES_F16 && type != ONES_BF16) ||
@@ -364,8 +367,11 @@ inline AttentionPlan attention_plan(int64_t tokens, int64_t sequences, int64_t h
 
 // ------------------------------------------- a token's attention over a cache --------
 constexpr int64_t kStepKeys = 32, kStepWaves = 2, kStepHeads = 16;         // keys of a wave's tile; waves; query heads of a workgroup
-constexpr int64_t kStepMaxSplits = 512;
+constexpr int64_t kStepMaxSplits = 512;       // workgroups wanted, and parts of a cache at most
 
+// A cache is parted until there are two workgroups of 64 KiB of LDS a compute unit, in parts of 512 places at least (a shorter cache takes one launch).
+// Waves of a workgroup and workgroups wanted, us: 32 sequences of 8192, 4 heads of 128 (a launch and the joining one): 4 and 256: 114; 4 and 512: 127;
+// 2 and 256: 122; 2 and 512: 109; 1 and 1024: 106; one sequence of 100003, 2 heads of 128: 31, 43, 39, 36, 42.
 struct StepPlan {
   int64_t blocks_of_heads, splits;
   size_t tops, sums, outputs, bytes;          // of the parts, where the keys are split

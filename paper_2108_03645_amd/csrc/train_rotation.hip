@@ -3,6 +3,13 @@
 //   n = x r w, r = (mean x^2 + eps)^-1/2 over a head's row; pairs of its first 2 F elements turn by position * frequency:
 //   y1 = n1 cos - n2 sin, y2 = n2 cos + n1 sin
 //   g = dy turned back, dw = sum over tokens and heads of g x r, u = g w, dx = r (u - x r mean(u x r))
+//
+// A wave takes a token: its cosines and sines are formed once, a lane each, and serve all heads, whose rows lie 4 to 64 lanes wide in the
+// wave; a lane has the same pairs in every row, so that weights, cosines and the sums of the weights' gradients stay in registers.  Backward forms r
+// again instead of reading it.  The sums of the workgroups are added up by a second launch.
+//
+// What bounds it is memory: 32768 tokens, 16 heads and 2 of 128, bf16: forward 54 us (302 MB, 5.6 TB/s), backward 96 us (453 MB, 4.7 TB/s) and 6 for the
+// weights' sums.  64 tokens: 4 us, a launch's own time and a chain of loads.
 #include "train_device.h"
 #include "train_host.h"
 
