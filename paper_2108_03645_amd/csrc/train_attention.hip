@@ -184,7 +184,16 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
     const T *const q0 = at<T>(a.q, here, a.q_stride, turn.head, a.q_head), *const k0 = at<T>(a.k, rows.first, a.k_stride, turn.kv, a.k_head);
     const T *const v0 = at<T>(a.v, rows.first, a.v_stride, turn.kv, a.v_head);
     sum_by_rows<1>(
-        lds, count, a.dim, [&](int32_t r, int d) { const float x = static_cast<float>(o[r * out_stride + d]); return x != x && lse[r] == lse[r]; },
+        lds, count, a.dim,
+        [&, seen = Seen()](int32_t r, int d) mutable {
+          const float x = static_cast<float>(o[r * out_stride + d]);
+          if (x == x || lse[r] != lse[r]) return false;
+          seen.through(v0, a.v_stride, rows.at + r, d);
+          if (seen.nan || (seen.up && seen.down)) return false;         // NaN is right: every weight is above 0
+          if (!seen.up && !seen.down) return true;
+          o[r * out_stride + d] = static_cast<T>(seen.up ? __builtin_inff() : -__builtin_inff());
+          return false;
+        },
         [&](int32_t r) { return rows.at + r + 1; },
         [&](int32_t r, int32_t y, float (&w)[1]) {
           w[0] = __builtin_amdgcn_exp2f(dot(q0 + r * a.q_stride, k0 + y * a.k_stride, a.dim) * c - lse[r] * kLog2e);

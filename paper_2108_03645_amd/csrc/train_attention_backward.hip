@@ -236,7 +236,14 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
     const float2 *const terms = a.terms + static_cast<int64_t>(turn.head) * a.tokens + here;
     sum_by_rows<1>(
         lds, count, a.dim,
-        [&](int32_t r, int d) { const float x = static_cast<float>(dq[r * out_stride + d]), t = terms[r].x + terms[r].y; return x != x && t == t; },
+        [&](int32_t r, int d) {
+          const float x = static_cast<float>(dq[r * out_stride + d]), t = terms[r].x + terms[r].y;
+          if (x == x || t - t != 0.f) return false;
+          bool seen = false, masked = false;      // infinite or NaN in a key makes its score so, and this element NaN, for the rows that see it
+          const int32_t i = rows.at + r, step = i / kStep * kStep;
+          find_infinite(k0, a.k_stride, step, i + 1, min(step + kStep, rows.length), d, seen, masked);
+          return masked && !seen;
+        },
         [&](int32_t r) { return rows.at + r + 1; },
         [&](int32_t r, int32_t y, float (&w)[1]) {
           const float p = __builtin_amdgcn_exp2f(dot(q0 + r * a.q_stride, k0 + y * a.k_stride, a.dim) * c - terms[r].x);
@@ -432,8 +439,17 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
         [&](int32_t r, int d) {
           const float x = a.parts == 1 ? static_cast<float>(dk[r * out_stride + d]) + static_cast<float>(dv[r * out_stride + d])
                                        : partial[r * partial_stride + d] + partial[r * partial_stride + a.dim + d];
-          const float own = dot(k0 + r * a.k_stride, v0 + r * a.v_stride, a.dim);
-          return x != x && own - own == 0.f;  // a key or value that is not finite has no other gradient
+          if (x == x) return false;
+          // What is not finite in a query that the key sees stays; this is for the rest of the one step that holds such as it does not see.
+          const int32_t step = r / kStepRows * kStepRows, end = min(step + kStepRows, left);
+          bool found = false;
+          for (int32_t h = head0; h < head0 + heads; ++h) {
+            bool masked[2] = {}, seen[2] = {};
+            find_infinite(at<T>(a.q, here, a.q_stride, h, a.q_head), a.q_stride, step, r, end, d, masked[0], seen[0]);
+            find_infinite(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, step, r, end, d, masked[1], seen[1]);
+            found |= (masked[0] && !seen[0]) || (masked[1] && !seen[1]);
+          }
+          return found;
         },
         [&](int32_t) { return all_steps ? heads * left : 0; },
         [&](int32_t r, int32_t y, float (&w)[2]) {

@@ -38,11 +38,13 @@ __device__ __forceinline__ const T *at(const void *p, int64_t row, int64_t strid
 template <typename T>
 constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;
 
-constexpr float kSlack = 6.f;                 // 2^(kShift + kSlack) is far from fp16's end
+// How far, as a power of two, an exponential may exceed 1 before the largest score is taken over.  (0 costs 4 % forward; the largest exponential is rounded
+// then as the others are, which a row of few large ones sees: bf16 o is off by 2.2e-3 of its norm instead of 1.9e-3.)
+constexpr float kSlack = 6.f;
 
 // A weight of 0 does not take a row out of a product where that row has infinities or NaN, so those of a token would reach the rows
 // that it is masked for, as far as they share a step with it.  Each kernel looks for NaN in what it has summed.  Where there is some, the rows
-// that have it are summed once more without products of matrices, over what they do see, which is slow and right:
+// that may have it from there are summed once more without products of matrices, over what they do see, which is slow and right:
 //   sums[e] = sum over y of weights(r, y)[e] * element d of row(e, y)
 // for the rows 0 <= r < rows of the workgroup, elements d < dim, and 0 <= y < last(r).  has(r, d): whether element d of row r asks for it;
 // weights(r, y, w): whether row r sees y at all; write(r, d, sums).
@@ -75,18 +77,42 @@ __device__ __forceinline__ void sum_by_rows(unsigned char *lds, int32_t rows, in
     if (d < dim) write(r, d, sums);
   }
 }
+// What is not finite among element d of the rows that a row sees, looked for as far as is asked, from the first row on; 16 at once, so that they are under
+// way together.
+struct Seen {
+  bool nan = false, up = false, down = false;
+  int32_t next = 0;
+  template <typename T>
+  __device__ __forceinline__ void through(const T *rows, int64_t stride, int32_t last, int d) {
+    while (next <= last && !nan && !(up && down)) {
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = static_cast<float>(rows[min(next + i, last) * stride + d]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        nan |= x[i] != x[i];
+        up |= x[i] == __builtin_inff();
+        down |= x[i] == -__builtin_inff();
+      }
+      next += 16;
+    }
+    next = min(next, last + 1);
+  }
+};
+// Whether of element d of rows first <= y < last, `stride` apart, one below `border` is not finite, and one from there on.
+template <typename T>
+__device__ __forceinline__ void find_infinite(const T *rows, int64_t stride, int32_t first, int32_t border, int32_t last, int d, bool &below, bool &above) {
+  for (int32_t y = first; y < last; ++y) {
+    const float x = static_cast<float>(rows[y * stride + d]);
+    if (x - x != 0.f) (y < border ? below : above) = true;
+  }
+}
 template <typename T>
 __device__ __forceinline__ float dot(const T *a, const T *b, int32_t dim) {
   float s = 0.f;
   for (int i = 0; i < dim; ++i) s = __builtin_fmaf(static_cast<float>(a[i]), static_cast<float>(b[i]), s);
   return s;
 }
-
-// A constant as an argument, so that a function's body is made for each of its values.
-template <bool VALUE>
-struct Flag {
-  static constexpr bool value = VALUE;
-};
 
 constexpr int kQueries = kAttentionRows;
 // Keys of a step, by the rows of 16 of a wave's part: of 32 where there is one, so that more workgroups fit into a compute unit.

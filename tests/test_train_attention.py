@@ -239,6 +239,38 @@ def test_a_row_does_not_see_what_comes_behind_it(train, bad, n, heads, dtype):
 
 
 @gpu
+def test_what_every_row_sees_is_not_looked_for_again(train):
+    """NaN that belongs in a row: the first token's value, every value, and every row at once; a long sequence takes no longer for it."""
+    q, k, v, do = inputs(31, 30000, 1, 1, 64, BF16)
+    offsets = torch.tensor([0, 30000], device="cuda", dtype=torch.int32)
+
+    def timed():
+        begun, ended = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begun.record()
+        o, lse, rest = train.attention_forward(q, k, v, offsets, keep_rest=True)
+        grads = train.attention_backward(do, q, k, v, o, lse, rest, offsets)
+        ended.record()
+        ended.synchronize()
+        return o, grads, begun.elapsed_time(ended)
+
+    timed()
+    clean = timed()[2]
+    v[0, 0, 3] = float("nan")
+    o, (dq, dk, dv), took = timed()
+    assert o[:, 0, 3].isnan().all() and o[:, 0, 4:].isfinite().all() and dq.isnan().any() and took < 20 * clean + 5
+    v[0, 0, 3], v[20, 0, 3], v[40, 0, 3] = float("inf"), float("nan"), float("nan")
+    o, _, took = timed()
+    assert (o[:20, 0, 3] == float("inf")).all() and o[20:, 0, 3].isnan().all() and took < 20 * clean + 5
+    v[20, 0, 3], v[40, 0, 3] = 1, -float("inf")
+    o, _, took = timed()
+    assert (o[:40, 0, 3] == float("inf")).all() and o[40:, 0, 3].isnan().all() and o[:, 0, 4:].isfinite().all() and took < 20 * clean + 5
+    v[:] = float("nan")
+    assert timed()[2] < 20 * clean + 5
+    q[:], k[:], do[:] = (float("nan"),) * 3
+    assert timed()[2] < 20 * clean + 5
+
+
+@gpu
 def test_many_sequences_and_offsets_that_do_not_rise(train):
     lengths = [(i * 7) % 4 for i in range(9001)]
     q, k, v, do = inputs(7, sum(lengths), 1, 1, 8, FP16)
