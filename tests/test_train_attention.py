@@ -127,14 +127,15 @@ def test_refusals_need_no_gpu(train):
         do, 256, 64, p, 256, 64, p, 128, 64, p, 128, 64, 1000, 4, 2, 64, 1, p, 3, 0.1, o, None, p, dq, p, p, ws, n, None)
     assert back(do=None) == back(dq=None) == back(o=None) == back(ws=None) == -1
     assert back(n=need - 1) == back(ws=C.c_void_p(0x1010)) == -5
-    step = lambda q=p, keys=p, b=2, cap=9, heads=4, kv=2, dim=64, kind=1, kb=9 * 128, ks=128, lengths=p, scale=0.1, o=p: L.ones_attention_step(  # noqa: E731
-        q, 256, 64, p, 128, 64, p, 128, 64, keys, kb, ks, 64, p, 9 * 128, 128, 64, lengths, b, cap, heads, kv, dim, kind, scale, o, None, 0, None)
+    step = lambda q=p, keys=p, b=2, cap=9, heads=4, kv=2, dim=64, kind=1, kb=9 * 128, ks=128, kh=64, lengths=p, scale=0.1, o=p: L.ones_attention_step(  # noqa: E731
+        q, 256, 64, p, 128, 64, p, 128, 64, keys, kb, ks, kh, p, 9 * 128, 128, 64, lengths, b, cap, heads, kv, dim, kind, scale, o, None, 0, None)
     for bad in (step(q=None), step(keys=None), step(b=-1), step(cap=-1), step(heads=3), step(dim=12), step(kind=0), step(kb=-8), step(kb=9), step(ks=32),
                 step(lengths=None), step(scale=0.0), step(o=None), step(keys=C.c_void_p(0x1008))):
         assert bad == -1
     assert step(b=65536) == step(cap=(1 << 30) + 1) == step(ks=(1 << 20) + 8) == step(b=60000, heads=128, kv=128) == step(kb=1 << 50) == -3
     assert step(b=0, q=None, keys=None, o=None) == 0
     assert L.ones_attention_step_workspace_bytes(1, 100000, 8, 2, 64) > 0 and L.ones_attention_step_workspace_bytes(1, 100, 8, 2, 64) == 0
+    assert step(kb=0) == step(kb=56) == step(kh=0) == step(kh=56) == -1     # two places of a cache in one
     assert step(b=1, cap=100000) == -1                               # split over the keys: a workspace is needed
 
 
