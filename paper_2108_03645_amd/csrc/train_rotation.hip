@@ -203,7 +203,9 @@ __global__ __launch_bounds__(256) void rotation_kernel(RotationArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < count; ++i) square = __builtin_fmaf(x1[i], x1[i], __builtin_fmaf(x2[i], x2[i], square));
-        const float r = rsqrtf(lanes_sum<LANES>(square) * inverse + a.eps);
+        square = lanes_sum<LANES>(square);
+        // What is no row has no norm: with eps 0 it would be infinite, and 0 times it NaN in the weights' gradients.
+        const float r = live ? rsqrtf(square * inverse + a.eps) : 0.f;
         T *out = static_cast<T *>(a.out[k]) + (token * a.heads[k] + h) * a.dim;
         if constexpr (!BACKWARD) {
 #pragma unroll

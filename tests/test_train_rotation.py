@@ -192,3 +192,30 @@ def test_a_stream_and_a_captured_graph_give_the_same(train):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(found, both(q + i))), i
+
+
+def both_ways(train, q, k, qw, kw, dq, dk, *args):
+    """Forward and backward against the formulas, equal bits from call to call."""
+    tokens, _, dim = q.shape
+    y = train.head_norm_rotation_forward(q, k, qw, kw, *args)
+    back = train.head_norm_rotation_backward(dq, dk, q, k, qw, kw, *args)
+    for x, w, dy, got, dx, dw in ((q, qw, dq, y[0], back[0], back[2]), (k, kw, dk, y[1], back[1], back[3])):
+        wy, wdx, wdw, sy, sdx, sdw = rotation64(x, w, *args, dy)
+        near(got, wy, sy, 32 + dim // 16, "y")
+        near(dx, wdx, sdx, 64 + dim // 8, "dx")
+        near(dw, wdw, sdw, 64 + tokens // 16, "dweight")
+    again = train.head_norm_rotation_backward(dq, dk, q, k, qw, kw, *args)
+    assert all(torch.equal(a, b) for a, b in zip(again, back))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("tokens,heads,kv,dim,pairs", [(33, 16, 2, 128, 64), (40, 16, 2, 64, 32), (5, 3, 1, 80, 20), (4, 2, 1, 17, 8), (2100, 5, 1, 96, 48), (9, 1, 1, 512, 256)])
+def test_norms_without_eps(train, tokens, heads, kv, dim, pairs, dtype):
+    """eps 0, and heads that do not fill the last rows of a wave: what is not there has no norm, and no part in the weights' gradients."""
+    gen = torch.Generator(device="cuda").manual_seed(tokens + dim)
+    make = lambda *s, std=1.0, mean=0.0: torch.randn(*s, generator=gen, device="cuda") * std + mean  # noqa: E731
+    q, k, dq, dk = (make(tokens, h, dim, std=1.5).to(dtype) for h in (heads, kv, heads, kv))
+    w = [make(dim, std=0.2, mean=1) for _ in range(2)]
+    positions = torch.arange(tokens, device="cuda", dtype=torch.int32)
+    both_ways(train, q, k, *w, dq, dk, positions, 100.0 ** (-torch.arange(pairs, device="cuda") / pairs), 0.0, False)
