@@ -66,6 +66,18 @@ __device__ __forceinline__ void arrived() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PENDING) : "memory");
 }
 
+// The workgroup's tiles of a cache that part `split` of `splits` has: whole ones, evenly over the parts.  A part may have none; the first has the new
+// token all the same.
+struct Part {
+  int32_t begin, end;
+  __device__ __forceinline__ Part(int32_t length, int32_t split, int32_t splits) {
+    const int64_t all = (length + kStepKeys * kStepWaves - 1) / (kStepKeys * kStepWaves);
+    begin = static_cast<int32_t>(all * split / splits);
+    end = static_cast<int32_t>(all * (split + 1) / splits);
+  }
+  __device__ __forceinline__ bool empty(int32_t split) const { return begin == end && split; }
+};
+
 template <typename T, int D>
 __global__ __launch_bounds__(kStepWaves * 64) void step_kernel(StepArgs a) {
   using Load = WaveTile<D>;
@@ -91,13 +103,9 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_kernel(StepArgs a) {
       for (int i = threadIdx.x; i < heads * a.dim; i += kStepWaves * 64) out[i] = static_cast<T>(fill);
     return;
   }
-  // whole tiles of the workgroup, evenly over the parts
-  const int32_t all = (length + kStepKeys * waves - 1) / (kStepKeys * waves);
-  const int32_t begin = static_cast<int32_t>(static_cast<int64_t>(all) * split / a.splits), end = static_cast<int32_t>(static_cast<int64_t>(all) * (split + 1) / a.splits);
-  if (begin == end && split) {
-    if (threadIdx.x < heads) a.tops[part0 + threadIdx.x * a.splits] = -INFINITY;
-    return;
-  }
+  const Part part(length, split, a.splits);
+  if (part.empty(split)) return;              // the joining launch knows
+  const int32_t begin = part.begin, end = part.end;
   const T *const k_new = static_cast<const T *>(a.k) + b * a.k_stride + kv * a.k_head, *const v_new = static_cast<const T *>(a.v) + b * a.v_stride + kv * a.v_head;
   const unsigned char *ks = reinterpret_cast<const unsigned char *>(static_cast<const T *>(a.keys) + b * a.keys_batch + kv * a.keys_head);
   const unsigned char *vs = reinterpret_cast<const unsigned char *>(static_cast<const T *>(a.values) + b * a.values_batch + kv * a.values_head);
@@ -224,7 +232,8 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_kernel(StepArgs a) {
   }
 }
 
-// The parts of a head: 128 elements by 8 groups of parts, added up in order.
+// The parts of a head: 128 elements by 8 groups of parts, added up in order.  Parts without keys left nothing behind; all others count, also where their
+// factor is 0: 0 times NaN is NaN.
 template <typename T>
 __global__ __launch_bounds__(1024) void step_join_kernel(StepArgs a) {
   __shared__ float factors[kStepMaxSplits], most_of[16], sums[8], outputs[8][128];
@@ -232,7 +241,8 @@ __global__ __launch_bounds__(1024) void step_join_kernel(StepArgs a) {
   if (length < 0 || length >= a.capacity) return;
   const int64_t at = static_cast<int64_t>(blockIdx.x) * a.splits;
   const int i = threadIdx.x, d = i % 128, group = i / 128;
-  const float top = i < a.splits ? a.tops[at + i] : -INFINITY;       // -infinity: a part without keys, whose sums are not there
+  const bool empty = i >= a.splits || Part(length, i, a.splits).empty(i);
+  const float top = empty ? -INFINITY : a.tops[at + i];
   float most = across_max(top);
 #pragma unroll
   for (int m = 1; m < 16; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
@@ -240,15 +250,15 @@ __global__ __launch_bounds__(1024) void step_join_kernel(StepArgs a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < 16; ++w) most = fmaxf(most, most_of[w]);
-  if (i < a.splits) factors[i] = i && top == -INFINITY ? 0.f : top == most ? 1.f : __builtin_amdgcn_exp2f((top - most) * (a.scale * kLog2e));
+  if (i < a.splits) factors[i] = empty ? -1.f : top == most ? 1.f : __builtin_amdgcn_exp2f((top - most) * (a.scale * kLog2e));
   __syncthreads();
   float sum = 0.f, x = 0.f;
   const int e = min(d, a.dim - 1);
 #pragma unroll 4
   for (int p = group; p < a.splits; p += 8) {
     const float f = factors[p], s = a.sums[at + p], y = a.outputs[(at + p) * a.dim + e];
-    sum += f == 0.f ? 0.f : s * f;
-    x += f == 0.f ? 0.f : y * f;
+    sum += f < 0.f ? 0.f : s * f;
+    x += f < 0.f ? 0.f : y * f;
   }
   outputs[group][d] = x;
   if (d == 0) sums[group] = sum;

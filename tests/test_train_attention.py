@@ -469,6 +469,40 @@ def test_attention_step(train, lengths, capacity, heads, kv, dim, dtype):
         assert torch.equal(cache.view(torch.int16), old.view(torch.int16))
 
 
+SEEN = [(40, [39, 20]), (700, [65, 300]), (2048, [2000, 700]), (8192, [513, 65]), (1024, [65, 1023])]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("capacity,lengths", SEEN, ids=[f"{s[1][0]}of{s[0]}" for s in SEEN])
+def test_a_step_keeps_the_nan_and_infinities_that_it_sees(train, capacity, lengths, dtype):
+    """In a key or a value of the first sequence's first key head: of the first place, the last one (alone in its part in some), many, the new token.  o is
+    what the formula gives, and the other sequence and key head keep their bits."""
+    b, heads, kv, dim = 2, 6, 2, 64
+    g = torch.Generator(device="cuda").manual_seed(capacity)
+    make = lambda *s, std=1.0: (torch.randn(*s, generator=g, device="cuda") * std).to(dtype)  # noqa: E731
+    clean = make(b, heads, dim, std=1.3), make(b, kv, dim, std=1.3), make(b, kv, dim), make(b, capacity, kv, dim, std=1.3), make(b, capacity, kv, dim)
+    at = torch.tensor(lengths, device="cuda", dtype=torch.int32)
+    right = train.attention_step(*(t.clone() for t in clean), at)
+    n = lengths[0]
+    z = step64(clean[0], *clean[3:], *clean[1:3], lengths, dim ** -0.5)[2]
+    for which in (0, 1):                                             # keys, values
+        for bad in (float("nan"), float("inf"), -float("inf")):
+            for places in (slice(0, 1), slice(n - 1, n), slice(n // 2, n), slice(0, n), None):
+                t = [x.clone() for x in clean]
+                (t[1 + which][0, 0] if places is None else t[3 + which][0, places, 0])[..., 5:7] = bad
+                want, sizes, _ = step64(t[0], *t[3:], *t[1:3], lengths, dim ** -0.5)
+                o = train.attention_step(*t, at)
+                what = f"{('keys', 'values')[which]} {bad} {places}"
+                assert torch.equal(o.isnan(), want.isnan()), what
+                assert torch.equal(o.double()[want.isinf()], want[want.isinf()]), what
+                good = want.isfinite()
+                assert good.any(), what
+                bound = sizes * (2 * HALF[dtype] + 2 * (dim + 32) * U32 * z + (n + 64) * U32)
+                held(o[good], want[good], bound[good], what, rms=False)
+                assert torch.equal(o[1], right[1]) and torch.equal(o[0, 3:], right[0, 3:]), what
+
+
 @gpu
 def test_a_step_without_room(train):
     g = torch.Generator(device="cuda").manual_seed(2)
