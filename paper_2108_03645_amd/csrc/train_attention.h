@@ -122,6 +122,32 @@ __device__ __forceinline__ bool any_nan(const f32x4 (&acc)[D / 16][TN]) {
   return found;
 }
 
+// What is not finite among element d of the rows that a row sees, looked for as far as is asked, from the first row on; 16 at once, so that they are under
+// way together.
+struct Seen {
+  bool nan = false, up = false, down = false;
+  int32_t next = 0;
+  __device__ __forceinline__ void add(float x) {
+    nan |= x != x;
+    up |= x == __builtin_inff();
+    down |= x == -__builtin_inff();
+  }
+  // Whether a sum over it, with weights above 0, is one infinity.
+  __device__ __forceinline__ bool infinite() const { return !nan && up != down; }
+  template <typename T>
+  __device__ __forceinline__ void through(const T *rows, int64_t stride, int32_t last, int d) {
+    while (next <= last && !nan && !(up && down)) {
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = static_cast<float>(rows[min(next + i, last) * stride + d]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) add(x[i]);
+      next += 16;
+    }
+    next = min(next, last + 1);
+  }
+};
+
 // Over the four lanes of a wave that hold the same n.
 __device__ __forceinline__ float across_max(float v) {
   const uint32_t b = __float_as_uint(v);

@@ -77,28 +77,6 @@ __device__ __forceinline__ void sum_by_rows(unsigned char *lds, int32_t rows, in
     if (d < dim) write(r, d, sums);
   }
 }
-// What is not finite among element d of the rows that a row sees, looked for as far as is asked, from the first row on; 16 at once, so that they are under
-// way together.
-struct Seen {
-  bool nan = false, up = false, down = false;
-  int32_t next = 0;
-  template <typename T>
-  __device__ __forceinline__ void through(const T *rows, int64_t stride, int32_t last, int d) {
-    while (next <= last && !nan && !(up && down)) {
-      float x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = static_cast<float>(rows[min(next + i, last) * stride + d]);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        nan |= x[i] != x[i];
-        up |= x[i] == __builtin_inff();
-        down |= x[i] == -__builtin_inff();
-      }
-      next += 16;
-    }
-    next = min(next, last + 1);
-  }
-};
 // Whether of element d of rows first <= y < last, `stride` apart, one below `border` is not finite, and one from there on.
 template <typename T>
 __device__ __forceinline__ void find_infinite(const T *rows, int64_t stride, int32_t first, int32_t border, int32_t last, int d, bool &below, bool &above) {

@@ -504,6 +504,29 @@ def test_a_step_keeps_the_nan_and_infinities_that_it_sees(train, capacity, lengt
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("capacity", [900, 4096])
+def test_a_step_keeps_what_it_sees_far_below_the_largest_score(train, capacity, dtype):
+    """Weights of e^-200 are 0 in 32 bits: what they stand for is seen all the same."""
+    n, dim = 700, 64
+    q, k, v = (torch.ones(1, h, dim, device="cuda", dtype=dtype) for h in (2, 1, 1))
+    keys, values = torch.ones(1, capacity, 1, dim, device="cuda", dtype=dtype), torch.ones(1, capacity, 1, dim, device="cuda", dtype=dtype)
+    keys[:, 300:] = -24                                              # scores 8 and -192
+    at = torch.tensor([n], device="cuda", dtype=torch.int32)
+    step = lambda: train.attention_step(q, k, v, keys, values, at)  # noqa: E731
+    assert torch.equal(step(), q)
+    values[0, 650, 0, 5], values[0, 651, 0, 6], values[0, 652, 0, 7] = float("inf"), -float("inf"), float("nan")
+    values[0, 660, 0, 8], values[0, 310, 0, 8] = float("inf"), -float("inf")
+    o = step()
+    assert (o[..., 5] == float("inf")).all() and (o[..., 6] == -float("inf")).all() and o[..., 7:9].isnan().all()
+    assert torch.equal(o[..., :5], q[..., :5]) and torch.equal(o[..., 9:], q[..., 9:])
+    k[:], v[0, 0, 9] = -24, -float("inf")                            # the new token's
+    assert (step()[..., 9] == -float("inf")).all() and torch.equal(step()[..., :5], q[..., :5])
+    keys[0, 690, 0, 3] = float("nan")
+    assert step().isnan().all()
+
+
+@gpu
 def test_a_step_without_room(train):
     g = torch.Generator(device="cuda").manual_seed(2)
     make = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
