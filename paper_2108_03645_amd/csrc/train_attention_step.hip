@@ -347,11 +347,13 @@ int ones_attention_step(const void *q, int64_t q_stride, int64_t q_head_stride, 
   if (capacity) {
     if (int rc = check_head_rows(keys, keys_stride, keys_head_stride, kv_heads, dim)) return rc;
     if (int rc = check_head_rows(values, values_stride, values_head_stride, kv_heads, dim)) return rc;
-    if (kv_heads > 1 && (keys_head_stride < dim || values_head_stride < dim)) return ONES_E_INVALID_ARG;     // places are written: no two are one
   }
   for (const int64_t stride : {keys_batch_stride, values_batch_stride})
-    if (batch > 1 && (stride < (capacity ? dim : 0) || stride % 8)) return ONES_E_INVALID_ARG;
+    if (batch > 1 && (stride < 0 || stride % 8)) return ONES_E_INVALID_ARG;
     else if (batch > 1 && stride > kMaxElements / batch) return ONES_E_BOUNDS;
+  if (capacity && (!places_apart(batch, keys_batch_stride, keys_stride, keys_head_stride, capacity, kv_heads, dim) ||
+                   !places_apart(batch, values_batch_stride, values_stride, values_head_stride, capacity, kv_heads, dim)))
+    return ONES_E_INVALID_ARG;                // places are written: no two may be one
   const StepPlan plan = step_plan(batch, capacity, heads, kv_heads, dim);
   if (int rc = check_workspace(d_workspace, workspace_bytes, plan.bytes)) return rc;
   unsigned char *const w = static_cast<unsigned char *>(d_workspace);

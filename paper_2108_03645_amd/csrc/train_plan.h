@@ -394,6 +394,19 @@ inline int check_step(int64_t batch, int64_t capacity, int64_t heads, int64_t kv
   if (int rc = check_attention(0, heads, kv_heads, dim, type, 0, scale)) return rc;
   return batch > ONES_MAX_BATCH || capacity > ONES_MAX_TOKENS || batch * heads > (int64_t{1} << 22) ? ONES_E_BOUNDS : ONES_OK;
 }
+// Whether no two places of a cache [batch][capacity][kv_heads] of rows of dim elements share an element, as far as the strides show it: in their order each
+// has to reach beyond all that the smaller ones do.  Strides and sizes are within their limits.
+inline bool places_apart(int64_t batch, int64_t batch_stride, int64_t stride, int64_t head_stride, int64_t capacity, int64_t kv_heads, int64_t dim) {
+  struct Axis { int64_t stride, size; } axes[3] = {{batch_stride, batch}, {stride, capacity}, {head_stride, kv_heads}};
+  std::sort(axes, axes + 3, [](const Axis &a, const Axis &b) { return a.stride < b.stride; });
+  int64_t reach = dim - 1;
+  for (const Axis &a : axes) {
+    if (a.size <= 1) continue;
+    if (a.stride <= reach) return false;
+    reach += a.stride * (a.size - 1);
+  }
+  return true;
+}
 
 // ------------------------------------------------------- the global norm --------
 // Tensors of a launch, whose addresses and sizes are its arguments; elements of a piece; workgroups of all launches, and of one at least if

@@ -601,6 +601,9 @@ void rotation(int64_t tokens, int64_t heads, int64_t kv, int64_t dim, int64_t pa
   const RotationPlan p = rotation_plan(tokens, heads, kv, dim, pairs, bytes, backward != 0);
   to[0] = p.vec; to[1] = p.lanes; to[2] = p.per; to[3] = p.parts; to[4] = p.blocks;
 }
+void apart(int64_t batch, int64_t batch_stride, int64_t stride, int64_t head_stride, int64_t capacity, int64_t kv, int64_t dim, int64_t *to) {
+  to[0] = places_apart(batch, batch_stride, stride, head_stride, capacity, kv, dim);
+}
 }
 """
 
@@ -626,6 +629,24 @@ def plans(tmp_path_factory):
         return list(to)
 
     return ask
+
+
+def test_caches_whose_places_are_shared_are_refused(train, plans):
+    """By the C entry too: two places of a cache, or of the two caches, in one would be written and read in the same launch."""
+    L, p = train.load(), C.c_void_p(0x1000)
+
+    def step(b=2, cap=9, kv=2, keys=(9 * 128, 128, 64), values=(9 * 128, 128, 64), at=0x1000, to=0x100000):
+        return L.ones_attention_step(p, 256, 64, p, 128, 64, p, 128, 64, C.c_void_p(at), *keys, C.c_void_p(to), *values, p, b, cap, 2 * kv, kv, 64, 1, 0.1, p, None, 0, None)
+
+    shared = [(9 * 128, 64, 64), (128, 128, 64), (64, 64, 9 * 64), (8 * 128, 128, 64), (9 * 128, 128, 128), (64 * 9, 128, 64), (9 * 128, 120, 64), (9 * 128, 128, 72), (72, 144, 8 * 144 + 64)]
+    for layout in shared:
+        assert step(keys=layout) == step(values=layout) == -1, layout
+        assert not plans("apart", 2, *layout, 9, 2, 64)[0], layout
+    for layout in [(9 * 128, 128, 64), (9 * 128, 64, 9 * 64), (128, 256, 64), (64, 256, 128), (64, 128, 9 * 128), (1 << 20, 1 << 10, 1 << 15)]:
+        assert plans("apart", 2, *layout, 9, 2, 64)[0], layout
+    assert plans("apart", 1, 0, 64, 0, 9, 1, 64)[0] and plans("apart", 1, 0, 64, 64, 1, 2, 64)[0] and plans("apart", 5, 64, 0, 64, 1, 1, 64)[0]
+    # the largest that is taken does not wrap
+    assert plans("apart", 65535, 1 << 30, 1 << 20, 1 << 40, 1 << 30, 1024, 128)[0] == 0
 
 
 def test_the_sizes_above_reach_every_kernel_and_cut(plans):
