@@ -173,7 +173,7 @@ int ones_attention_backward(const void *dout, int64_t do_stride, int64_t do_head
  * before the token; it is not changed.  Below 0: the sequence is left out, o is 0 and its cache stays; capacity or above: there is no room,
  * o is NaN and its cache stays.  Places behind lengths[b] are not read.  o [batch][heads][dim] has no gaps.  type, dim, heads, scale, bases
  * and strides as for ones_attention_forward (the caches' stride: between places; batch strides multiples of 8 elements;
- * no two places of a cache may overlap).
+ * no two places of a cache, or of the two caches, may overlap).
  * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size or stride, batch * heads above 2^22), ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
 size_t ones_attention_step_workspace_bytes(int64_t batch, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim);
 int ones_attention_step(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride, int64_t k_head_stride,

@@ -351,9 +351,12 @@ int ones_attention_step(const void *q, int64_t q_stride, int64_t q_head_stride, 
   for (const int64_t stride : {keys_batch_stride, values_batch_stride})
     if (batch > 1 && (stride < 0 || stride % 8)) return ONES_E_INVALID_ARG;
     else if (batch > 1 && stride > kMaxElements / batch) return ONES_E_BOUNDS;
-  if (capacity && (!places_apart(batch, keys_batch_stride, keys_stride, keys_head_stride, capacity, kv_heads, dim) ||
-                   !places_apart(batch, values_batch_stride, values_stride, values_head_stride, capacity, kv_heads, dim)))
-    return ONES_E_INVALID_ARG;                // places are written: no two may be one
+  if (capacity && batch) {                    // places are written: no two may be one
+    const Places of_keys(batch, keys_batch_stride, keys_stride, keys_head_stride, capacity, kv_heads, dim);
+    const Places of_values(batch, values_batch_stride, values_stride, values_head_stride, capacity, kv_heads, dim);
+    const int64_t behind = (reinterpret_cast<intptr_t>(values) - reinterpret_cast<intptr_t>(keys)) / 2;
+    if (!of_keys.apart() || !of_values.apart() || !of_keys.apart_from(of_values, behind)) return ONES_E_INVALID_ARG;
+  }
   const StepPlan plan = step_plan(batch, capacity, heads, kv_heads, dim);
   if (int rc = check_workspace(d_workspace, workspace_bytes, plan.bytes)) return rc;
   unsigned char *const w = static_cast<unsigned char *>(d_workspace);

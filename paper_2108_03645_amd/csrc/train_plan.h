@@ -394,19 +394,43 @@ inline int check_step(int64_t batch, int64_t capacity, int64_t heads, int64_t kv
   if (int rc = check_attention(0, heads, kv_heads, dim, type, 0, scale)) return rc;
   return batch > ONES_MAX_BATCH || capacity > ONES_MAX_TOKENS || batch * heads > (int64_t{1} << 22) ? ONES_E_BOUNDS : ONES_OK;
 }
-// Whether no two places of a cache [batch][capacity][kv_heads] of rows of dim elements share an element, as far as the strides show it: in their order each
-// has to reach beyond all that the smaller ones do.  Strides and sizes are within their limits.
-inline bool places_apart(int64_t batch, int64_t batch_stride, int64_t stride, int64_t head_stride, int64_t capacity, int64_t kv_heads, int64_t dim) {
-  struct Axis { int64_t stride, size; } axes[3] = {{batch_stride, batch}, {stride, capacity}, {head_stride, kv_heads}};
-  std::sort(axes, axes + 3, [](const Axis &a, const Axis &b) { return a.stride < b.stride; });
-  int64_t reach = dim - 1;
-  for (const Axis &a : axes) {
-    if (a.size <= 1) continue;
-    if (a.stride <= reach) return false;
-    reach += a.stride * (a.size - 1);
+// The places of a cache [batch][capacity][kv_heads] of rows of dim elements, strides in elements, within their limits; axes of one place have none.
+struct Places {
+  struct Axis { int64_t stride, size; } axes[3];            // the smallest stride first
+  int64_t dim;
+  Places(int64_t batch, int64_t batch_stride, int64_t stride, int64_t head_stride, int64_t capacity, int64_t kv_heads, int64_t d)
+      : axes{{batch > 1 ? batch_stride : 0, batch}, {capacity > 1 ? stride : 0, capacity}, {kv_heads > 1 ? head_stride : 0, kv_heads}}, dim(d) {
+    std::sort(axes, axes + 3, [](const Axis &a, const Axis &b) { return a.stride < b.stride; });
   }
-  return true;
-}
+  // Whether no two of them share an element, as far as the strides show it: in their order each has to reach beyond all that the smaller ones do.
+  bool apart() const {
+    int64_t reach = dim - 1;
+    for (const Axis &a : axes) {
+      if (a.size <= 1) continue;
+      if (a.stride <= reach) return false;
+      reach += a.stride * (a.size - 1);
+    }
+    return true;
+  }
+  // Whether one of them and one that lies `delta` elements from another of them share an element (of places that are apart): then delta is a sum of
+  // steps along the axes and less than a row, and of an axis only the two steps next to what is left can be in it.
+  bool meets(int64_t delta, int axis = 2) const {
+    if (axis < 0) return -dim < delta && delta < dim;
+    const Axis &a = axes[axis];
+    if (a.size <= 1) return meets(delta, axis - 1);
+    const int64_t steps = delta / a.stride - (delta % a.stride < 0);
+    for (const int64_t n : {steps, steps + 1})
+      if (-a.size < n && n < a.size && meets(delta - n * a.stride, axis - 1)) return true;
+    return false;
+  }
+  // Whether no place is one of the others', which lie `delta` elements behind; layouts of different strides are only known to meet at their bases.
+  bool apart_from(const Places &other, int64_t delta) const {
+    if (delta == 0) return false;
+    for (int i = 0; i < 3; ++i)
+      if (axes[i].size != other.axes[i].size || axes[i].stride != other.axes[i].stride) return true;
+    return !meets(delta);
+  }
+};
 
 // ------------------------------------------------------- the global norm --------
 // Tensors of a launch, whose addresses and sizes are its arguments; elements of a piece; workgroups of all launches, and of one at least if

@@ -584,7 +584,8 @@ def _cache(t, name, batch, capacity, kv_heads, dim, like):
 def attention_step(q, k, v, keys, values, lengths, scale=None):
     """ones_attention_step: one more token of every sequence.  k, v [batch, kv_heads, dim] are written to place lengths[b] of keys, values
     [batch, capacity, kv_heads, dim], and q [batch, heads, dim] attends over places 0 .. lengths[b]; returns o, shaped like q.  lengths (int32
-    [batch]) is not changed; below 0 a sequence is left out (o is 0), at capacity and above it has no room (o is NaN)."""
+    [batch]) is not changed; below 0 a sequence is left out (o is 0), at capacity and above it has no room (o is NaN).  No two places of the caches may
+    share memory."""
     q, q_stride, q_head = _step_rows(q, "q")
     batch, heads, dim = q.shape
     k, k_stride, k_head = _step_rows(k, "k", batch, dim, q)

@@ -602,7 +602,10 @@ void rotation(int64_t tokens, int64_t heads, int64_t kv, int64_t dim, int64_t pa
   to[0] = p.vec; to[1] = p.lanes; to[2] = p.per; to[3] = p.parts; to[4] = p.blocks;
 }
 void apart(int64_t batch, int64_t batch_stride, int64_t stride, int64_t head_stride, int64_t capacity, int64_t kv, int64_t dim, int64_t *to) {
-  to[0] = places_apart(batch, batch_stride, stride, head_stride, capacity, kv, dim);
+  to[0] = Places(batch, batch_stride, stride, head_stride, capacity, kv, dim).apart();
+}
+void meets(int64_t batch, int64_t batch_stride, int64_t stride, int64_t head_stride, int64_t capacity, int64_t kv, int64_t dim, int64_t delta, int64_t *to) {
+  to[0] = Places(batch, batch_stride, stride, head_stride, capacity, kv, dim).meets(delta);
 }
 }
 """
@@ -647,6 +650,34 @@ def test_caches_whose_places_are_shared_are_refused(train, plans):
     assert plans("apart", 1, 0, 64, 0, 9, 1, 64)[0] and plans("apart", 1, 0, 64, 64, 1, 2, 64)[0] and plans("apart", 5, 64, 0, 64, 1, 1, 64)[0]
     # the largest that is taken does not wrap
     assert plans("apart", 65535, 1 << 30, 1 << 20, 1 << 40, 1 << 30, 1024, 128)[0] == 0
+
+
+def test_keys_and_values_that_share_places_are_refused(train, plans):
+    """One tensor for both, or values that begin inside the keys; places that lie between each other are two."""
+    L, p = train.load(), C.c_void_p(0x1000)
+
+    def step(keys, values, at, to, b=2, cap=9, kv=2):
+        return L.ones_attention_step(p, 256, 64, p, 128, 64, p, 128, 64, C.c_void_p(at), *keys, C.c_void_p(to), *values, p, b, cap, 2 * kv, kv, 64, 1, 0.1, p, None, 0, None)
+
+    dense, at = (9 * 128, 128, 64), 1 << 20
+    for behind in (0, 8, 64, -64, 128, 9 * 128, -9 * 128, 17 * 128, -(17 * 128 + 64)):
+        assert step(dense, dense, at, at + 2 * behind) == -1, behind
+    between = (2 * 9 * 128, 128, 64)
+    assert step(between, between, at, at + 2 * 128) == step(between, dense, at, at) == -1
+    import itertools
+    import random
+    rng = random.Random(1)
+    for _ in range(300):                                             # against the elements themselves
+        sizes, dim = [rng.randint(1, 3) for _ in range(3)], rng.choice([8, 16])
+        order, strides, reach = rng.sample(range(3), 3), [0] * 3, dim
+        for axis in order:
+            strides[axis] = reach + 8 * rng.choice([0, 0, 1, 2, 5])
+            reach += strides[axis] * (sizes[axis] - 1)
+        places = {sum(i * s for i, s in zip(at, strides)) + d for at in itertools.product(*map(range, sizes)) for d in range(dim)}
+        layout = (sizes[0], *strides, *sizes[1:], dim)
+        assert plans("apart", *layout)[0] == 1
+        for delta in [8 * rng.randint(-reach // 8 - 1, reach // 8 + 1) for _ in range(30)]:
+            assert plans("meets", *layout, delta)[0] == any(x + delta in places for x in places), (layout, delta)
 
 
 def test_the_sizes_above_reach_every_kernel_and_cut(plans):
