@@ -84,8 +84,8 @@ __device__ __forceinline__ double squares(const void *tensor, int64_t begin, int
     for (int j = 0; j < kVec; ++j) { const double x = static_cast<double>(static_cast<float>(runs.v[r].v[j])); s = __builtin_fma(x, x, s); }
   return s;
 }
-template <typename T>
-__device__ __forceinline__ void scale(void *tensor, int64_t begin, int n, float factor) {
+template <typename T, typename F>
+__device__ __forceinline__ void scale(void *tensor, int64_t begin, int n, F factor) {
   T *const p = static_cast<T *>(tensor) + begin;
   const Runs<T> runs(p, n);
 #pragma unroll
@@ -93,7 +93,7 @@ __device__ __forceinline__ void scale(void *tensor, int64_t begin, int n, float 
     const int i = (r * 256 + static_cast<int>(threadIdx.x)) * kVec;
     float x[kVec];
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) x[j] = static_cast<float>(runs.v[r].v[j]) * factor;
+    for (int j = 0; j < kVec; ++j) x[j] = static_cast<float>(static_cast<F>(static_cast<float>(runs.v[r].v[j])) * factor);
     store_some<T, kVec>(p + i, x, n - i);
   }
 }
@@ -110,6 +110,19 @@ struct Piece {
     type = a.last[t] >> 13;
   }
 };
+
+// The workgroup's pieces times factor, from the last one on, which the caches have yet.
+template <typename F>
+__device__ __forceinline__ void scale_pieces(const ClipArgs &a, F factor) {
+  int32_t begin, piece;
+  pieces_of(a, begin, piece);
+  while (--piece >= begin) {
+    const Piece at(a, piece);
+    if (at.type == kF32) scale<float>(at.p, at.begin, at.n, factor);
+    else if (at.type == kF16) scale<f16>(at.p, at.begin, at.n, factor);
+    else scale<bf16>(at.p, at.begin, at.n, factor);
+  }
+}
 
 __global__ __launch_bounds__(256) void squares_kernel(ClipArgs a) {
   int32_t piece, end;
@@ -131,15 +144,10 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a) {
   const double norm = sqrt(block_sum(s)), with = norm + a.eps;
   if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = static_cast<float>(norm);
   if (!(with > a.limit) || !(norm < static_cast<double>(INFINITY))) return;
-  const float factor = static_cast<float>(a.limit / with);
-  int32_t begin, piece;
-  pieces_of(a, begin, piece);
-  while (--piece >= begin) {                  // from the last on, which the caches have yet
-    const Piece at(a, piece);
-    if (at.type == kF32) scale<float>(at.p, at.begin, at.n, factor);
-    else if (at.type == kF16) scale<f16>(at.p, at.begin, at.n, factor);
-    else scale<bf16>(at.p, at.begin, at.n, factor);
-  }
+  // A factor that is no normal float, of a norm beyond 1e38 as it is with ordinary limits, would lose its bits in 32.
+  const double factor = a.limit / with;
+  if (factor < 0x1p-126) scale_pieces(a, factor);
+  else scale_pieces(a, static_cast<float>(factor));
 }
 
 struct Span {

@@ -128,3 +128,17 @@ def test_equal_bits_streams_and_graphs(train):
         torch.cuda.synchronize()
         norm = train.clip_gradients(eager, 1.5)
         assert torch.equal(found, norm) and all(torch.equal(a, b) for a, b in zip(held, eager)), i
+
+
+@gpu
+@pytest.mark.parametrize("limit", [1.0, 1e-3, 1e-6])
+def test_factors_that_32_bits_do_not_hold(train, limit):
+    """A million elements of 3e38 (norm 3e41): limit / norm is no normal float, every element times it is."""
+    for dtype in (FP32, BF16):
+        g = [torch.full((1000000,), 3e38, device="cuda", dtype=dtype), torch.full((30,), -1e37, device="cuda", dtype=dtype)]
+        exact = [t.double() for t in g]
+        norm = math.sqrt(sum(t.pow(2).sum().item() for t in exact))
+        assert train.clip_gradients(g, limit).isinf()
+        for t, e in zip(g, exact):
+            want = e * (limit / (norm + 1e-6))
+            assert ((t.double() - want).abs() <= (HALF[dtype] + 4 * U32) * want.abs()).all()
