@@ -125,18 +125,16 @@ __device__ __forceinline__ bool any_nan(const f32x4 (&acc)[D / 16][TN]) {
 // What is not finite among element d of the rows that a row sees, looked for as far as is asked, from the first row on; 16 at once, so that they are under
 // way together.
 struct Seen {
-  bool nan = false, up = false, down = false;
+  uint32_t bits = 0;                          // 1: NaN, 2: infinity, 4: -infinity
   int32_t next = 0;
-  __device__ __forceinline__ void add(float x) {
-    nan |= x != x;
-    up |= x == __builtin_inff();
-    down |= x == -__builtin_inff();
-  }
-  // Whether a sum over it, with weights above 0, is one infinity.
-  __device__ __forceinline__ bool infinite() const { return !nan && up != down; }
+  __device__ __forceinline__ bool up() const { return bits & 2; }
+  __device__ __forceinline__ void add(float x) { bits |= x != x ? 1 : x == __builtin_inff() ? 2 : x == -__builtin_inff() ? 4 : 0; }
+  // Whether a sum over it, with weights above 0, is NaN; whether it is one infinity.
+  __device__ __forceinline__ bool no_number() const { return (bits & 1) || bits == 6; }
+  __device__ __forceinline__ bool infinite() const { return bits == 2 || bits == 4; }
   template <typename T>
   __device__ __forceinline__ void through(const T *rows, int64_t stride, int32_t last, int d) {
-    while (next <= last && !nan && !(up && down)) {
+    while (next <= last && !no_number()) {
       float x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = static_cast<float>(rows[min(next + i, last) * stride + d]);

@@ -189,9 +189,9 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
           const float x = static_cast<float>(o[r * out_stride + d]);
           if (x == x || lse[r] != lse[r]) return false;
           seen.through(v0, a.v_stride, rows.at + r, d);
-          if (seen.nan || (seen.up && seen.down)) return false;         // NaN is right: every weight is above 0
-          if (!seen.up && !seen.down) return true;
-          o[r * out_stride + d] = static_cast<T>(seen.up ? __builtin_inff() : -__builtin_inff());
+          if (seen.no_number()) return false;         // NaN is right: every weight is above 0
+          if (!seen.bits) return true;
+          o[r * out_stride + d] = static_cast<T>(seen.up() ? __builtin_inff() : -__builtin_inff());
           return false;
         },
         [&](int32_t r) { return rows.at + r + 1; },
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
           return true;
         },
         [&](int, int32_t y) { return v0 + y * a.v_stride; },
-        [&](int32_t r, int d, const float (&sums)[1]) {
+        [&](int32_t r, int d, const float (&sums)[1], int) {
           o[r * out_stride + d] = static_cast<T>(sums[0]);
           if (rest) rest[r * out_stride + d] = static_cast<T>(sums[0] - static_cast<float>(static_cast<T>(sums[0])));
         });

@@ -236,13 +236,14 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
     const float2 *const terms = a.terms + static_cast<int64_t>(turn.head) * a.tokens + here;
     sum_by_rows<1>(
         lds, count, a.dim,
-        [&](int32_t r, int d) {
+        [&, seen = Seen()](int32_t r, int d) mutable {
           const float x = static_cast<float>(dq[r * out_stride + d]), t = terms[r].x + terms[r].y;
           if (x == x || t - t != 0.f) return false;
-          bool seen = false, masked = false;      // infinite or NaN in a key makes its score so, and this element NaN, for the rows that see it
-          const int32_t i = rows.at + r, step = i / kStep * kStep;
-          find_infinite(k0, a.k_stride, step, i + 1, min(step + kStep, rows.length), d, seen, masked);
-          return masked && !seen;
+          const int32_t i = rows.at + r, end = min(i / kStep * kStep + kStep, rows.length);
+          if (!any_infinite(k0, a.k_stride, i + 1, end, d)) return false;
+          // infinite or NaN in a key makes its score so, and this element NaN, for the rows that see it
+          if (!seen.bits) seen.through(k0, a.k_stride, i, d);
+          return !seen.bits;
         },
         [&](int32_t r) { return rows.at + r + 1; },
         [&](int32_t r, int32_t y, float (&w)[1]) {
@@ -251,7 +252,7 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
           return true;
         },
         [&](int, int32_t y) { return k0 + y * a.k_stride; },
-        [&](int32_t r, int d, const float (&sums)[1]) { dq[r * out_stride + d] = static_cast<T>(sums[0] * a.scale); });
+        [&](int32_t r, int d, const float (&sums)[1], int) { dq[r * out_stride + d] = static_cast<T>(sums[0] * a.scale); });
   }
 }
 
@@ -433,23 +434,51 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
   if (__syncthreads_or(any_nan<D, TN>(of_k) || any_nan<D, TN>(of_v))) {
     __syncthreads();
     const T *const k0 = at<T>(a.k, here, a.k_stride, kv, a.k_head), *const v0 = at<T>(a.v, here, a.v_stride, kv, a.v_head);
+    // What the queries from .. to - 1 of all heads hold: NaN in lse, which makes both results of a key that sees it NaN, and in delta, all of dk; and what is not
+    // finite in element d of do, which goes into that element of dv.
+    constexpr uint32_t kLse = 1, kDelta = 2, kUp = 8, kDown = 16, kDout = 28;          // (of do as in Seen)
+    auto look = [&](int32_t from, int32_t to, int d) __attribute__((always_inline)) {
+      uint32_t held = 0;
+      for (int32_t h = head0; h < head0 + heads; ++h) {
+        const float2 *const terms = a.terms + static_cast<int64_t>(h) * a.tokens + here;
+        for (int32_t i = from; i < to && !(held & kLse); i += 16)
+#pragma unroll
+          for (int n = 0; n < 16; ++n) {
+            const float2 t = terms[min(i + n, to - 1)];
+            held |= (t.x != t.x ? kLse : 0) | (t.y != t.y ? kDelta : 0);
+          }
+        Seen dout;
+        dout.next = from;
+        dout.through(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, to - 1, d);
+        held |= dout.bits << 2;
+      }
+      return held;
+    };
     // the queries of all heads in a row, from the tile's first key on
     sum_by_rows<2>(
         lds, count, a.dim,
-        [&](int32_t r, int d) {
-          const float x = a.parts == 1 ? static_cast<float>(dk[r * out_stride + d]) + static_cast<float>(dv[r * out_stride + d])
-                                       : partial[r * partial_stride + d] + partial[r * partial_stride + a.dim + d];
-          if (x == x) return false;
-          // What is not finite in a query that the key sees stays; this is for the rest of the one step that holds such as it does not see.
-          const int32_t step = r / kStepRows * kStepRows, end = min(step + kStepRows, left);
-          bool found = false;
+        [&, behind = 0u, looked = false](int32_t r, int d) mutable {
+          const float of_k = a.parts == 1 ? static_cast<float>(dk[r * out_stride + d]) : partial[r * partial_stride + d];
+          const float of_v = a.parts == 1 ? static_cast<float>(dv[r * out_stride + d]) : partial[r * partial_stride + a.dim + d];
+          // only of queries and gradients that the key does not see, in the one step that it shares with them
+          bool k_asks = false, v_asks = false;
+          const int32_t step = r / kStepRows * kStepRows;
           for (int32_t h = head0; h < head0 + heads; ++h) {
-            bool masked[2] = {}, seen[2] = {};
-            find_infinite(at<T>(a.q, here, a.q_stride, h, a.q_head), a.q_stride, step, r, end, d, masked[0], seen[0]);
-            find_infinite(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, step, r, end, d, masked[1], seen[1]);
-            found |= (masked[0] && !seen[0]) || (masked[1] && !seen[1]);
+            if (of_k != of_k) k_asks |= any_infinite(at<T>(a.q, here, a.q_stride, h, a.q_head), a.q_stride, step, r, d);
+            if (of_v != of_v) v_asks |= any_infinite(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, step, r, d);
           }
-          return found;
+          if (!k_asks && !v_asks) return 0;
+          const int32_t tile = min(kKeyRows, left);
+          if (!looked) behind = look(tile, left, d);
+          looked = true;
+          const uint32_t held = behind | look(r, tile, d), dout = held & kDout;
+          if (held & kLse) return 0;
+          if (v_asks && (dout == kUp || dout == kDown)) {
+            const float all = dout == kUp ? __builtin_inff() : -__builtin_inff();
+            if (a.parts == 1) dv[r * out_stride + d] = static_cast<T>(all);
+            else partial[r * partial_stride + a.dim + d] = all;
+          }
+          return (k_asks && !(held & kDelta) ? 1 : 0) + (v_asks && !dout ? 2 : 0);
         },
         [&](int32_t) { return all_steps ? heads * left : 0; },
         [&](int32_t r, int32_t y, float (&w)[2]) {
@@ -463,13 +492,12 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
         [&](int e, int32_t y) {
           return e ? at<T>(a.dout, here + y % left, a.do_stride, head0 + y / left, a.do_head) : at<T>(a.q, here + y % left, a.q_stride, head0 + y / left, a.q_head);
         },
-        [&](int32_t r, int d, const float (&sums)[2]) {
-          if (a.parts > 1) {
-            partial[r * partial_stride + d] = sums[0];
-            partial[r * partial_stride + a.dim + d] = sums[1];
-          } else {
-            dk[r * out_stride + d] = static_cast<T>(sums[0]);
-            dv[r * out_stride + d] = static_cast<T>(sums[1]);
+        [&](int32_t r, int d, const float (&sums)[2], int asks) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            if (!(asks >> e & 1)) continue;
+            if (a.parts > 1) partial[r * partial_stride + e * a.dim + d] = sums[e];
+            else (e ? dv : dk)[r * out_stride + d] = static_cast<T>(sums[e]);
           }
         });
   }

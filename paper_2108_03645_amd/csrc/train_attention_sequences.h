@@ -46,8 +46,8 @@ constexpr float kSlack = 6.f;
 // that it is masked for, as far as they share a step with it.  Each kernel looks for NaN in what it has summed.  Where there is some, the rows
 // that may have it from there are summed once more without products of matrices, over what they do see, which is slow and right:
 //   sums[e] = sum over y of weights(r, y)[e] * element d of row(e, y)
-// for the rows 0 <= r < rows of the workgroup, elements d < dim, and 0 <= y < last(r).  has(r, d): whether element d of row r asks for it;
-// weights(r, y, w): whether row r sees y at all; write(r, d, sums).
+// for the rows 0 <= r < rows of the workgroup, elements d < dim, and 0 <= y < last(r).  has(r, d): what of element d of row r asks for it, 0 if nothing
+// does; weights(r, y, w): whether row r sees y at all; write(r, d, sums, what asked).
 template <int N, class Has, class Last, class Weights, class Row, class Write>
 __device__ __forceinline__ void sum_by_rows(unsigned char *lds, int32_t rows, int32_t dim, Has has, Last last, Weights weights, Row row, Write write) {
   struct Held {
@@ -58,7 +58,8 @@ __device__ __forceinline__ void sum_by_rows(unsigned char *lds, int32_t rows, in
   Held *const held = reinterpret_cast<Held *>(lds);
   const int d = threadIdx.x;
   for (int32_t r = 0; r < rows; ++r) {
-    if (!__syncthreads_or(d < dim && has(r, d))) continue;
+    const int asks = d < dim ? has(r, d) : 0;
+    if (!__syncthreads_or(asks)) continue;
     const int32_t end = last(r);
     float sums[N] = {};
     for (int32_t y0 = 0; y0 < end; y0 += kChunk) {
@@ -74,16 +75,18 @@ __device__ __forceinline__ void sum_by_rows(unsigned char *lds, int32_t rows, in
           for (int e = 0; e < N; ++e) sums[e] += held[y - y0].w[e] * static_cast<float>(row(e, y)[d]);
         }
     }
-    if (d < dim) write(r, d, sums);
+    if (asks) write(r, d, sums, asks);
   }
 }
-// Whether of element d of rows first <= y < last, `stride` apart, one below `border` is not finite, and one from there on.
+// Whether of element d of rows first <= y < last, `stride` apart, one is not finite.
 template <typename T>
-__device__ __forceinline__ void find_infinite(const T *rows, int64_t stride, int32_t first, int32_t border, int32_t last, int d, bool &below, bool &above) {
+__device__ __forceinline__ bool any_infinite(const T *rows, int64_t stride, int32_t first, int32_t last, int d) {
+  bool found = false;
   for (int32_t y = first; y < last; ++y) {
     const float x = static_cast<float>(rows[y * stride + d]);
-    if (x - x != 0.f) (y < border ? below : above) = true;
+    found |= x - x != 0.f;
   }
+  return found;
 }
 template <typename T>
 __device__ __forceinline__ float dot(const T *a, const T *b, int32_t dim) {

@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_kernel(StepArgs a) {
       if (y == y || !(all_sum > 0.f)) continue;
       if (seen.next == 0) seen.add(static_cast<float>(v_new[d]));
       seen.through(reinterpret_cast<const T *>(vs), a.values_stride, length - 1, d);
-      if (seen.infinite()) out[h * a.dim + d] = static_cast<T>(seen.up ? __builtin_inff() : -__builtin_inff());
+      if (seen.infinite()) out[h * a.dim + d] = static_cast<T>(seen.up() ? __builtin_inff() : -__builtin_inff());
     }
   }
 }
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(1024) void step_join_kernel(StepArgs a) {
     const T *const values = static_cast<const T *>(a.values) + b * a.values_batch + (blockIdx.x % a.heads) / (a.heads / a.kv_heads) * a.values_head;
     seen.through(values + group * a.values_stride, 8 * a.values_stride, (length + 8 - group) / 8 - 1, d);       // with the new token's, which is there by now
   }
-  outputs[group][d] = static_cast<float>(seen.nan | seen.up << 1 | seen.down << 2);
+  outputs[group][d] = static_cast<float>(seen.bits);
   __syncthreads();
   if (!lost) return;
   int32_t found = 0;

@@ -240,6 +240,44 @@ def test_a_row_does_not_see_what_comes_behind_it(train, bad, n, heads, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("n,heads,kv", [(200, 2, 1), (200, 1, 1), (2310, 64, 8)])
+def test_what_keys_see_behind_what_they_do_not(train, n, heads, kv, bad, dtype):
+    """Infinities and NaN in gradients at places that share a step with keys behind them, and at later ones that these keys see: dv holds what is seen, in
+    that element and no other, and keys behind all of it are as they were."""
+    q, k, v, do = inputs(33, n, heads, kv, 128, dtype)
+    offsets = torch.tensor([0, n], device="cuda", dtype=torch.int32)
+    o, lse, rest = train.attention_forward(q, k, v, offsets, keep_rest=True)
+    clean = train.attention_backward(do, q, k, v, o, lse, rest, offsets)
+    up = float("inf")
+    for first, then in ((70, 90), (70, 150), (64, 127)):             # in one step of 32, in another tile, at a tile's ends
+        g = do.clone()
+        g[first, 0, 5], g[then, 0, 5], g[then, 0, 9] = bad, up, -up
+        _, dk, dv = train.attention_backward(g, q, k, v, o, lse, rest, offsets)
+        before = dv[:first + 1, 0, 5]
+        assert (before == up).all() if bad == up else before.isnan().all()
+        assert (dv[first + 1:then + 1, 0, 5] == up).all() and (dv[:then + 1, 0, 9] == -up).all()
+        others = [d for d in range(128) if d not in (5, 9)]
+        assert dv[:, 0, others].isfinite().all() and torch.equal(dv[:, 1:], clean[2][:, 1:]) and torch.equal(dk[:, 1:], clean[1][:, 1:])
+        for got, right in ((dv[:, 0, others], clean[2][:, 0, others]), (dv[then + 1:], clean[2][then + 1:]), (dk[then + 1:], clean[1][then + 1:])):
+            assert (got.float() - right.float()).norm() <= 2 * HALF[dtype] * right.float().norm()
+    # in every step of 32: every key sees some, most do not see one of their own step
+    for t, which in ((do, 0), (q, 1)):
+        bads = t.clone()
+        bads[::32, 0, 5] = bad
+        last = (n - 1) // 32 * 32
+        if which == 0:
+            _, dk, dv = train.attention_backward(bads, q, k, v, o, lse, rest, offsets)
+            seen = dv[:last + 1, 0, 5]
+            assert (seen.isnan() if bad != bad else seen == bad).all() and dv[:, 0, others].isfinite().all()
+        else:
+            _, dk, dv = train.attention_backward(do, bads, k, v, *train.attention_forward(bads, k, v, offsets, keep_rest=True), offsets)
+            assert not dk[:last + 1, 0].isfinite().any() and not dv[:last + 1, 0].isfinite().any()
+        assert dk[last + 1:].isfinite().all() and dv[last + 1:].isfinite().all()
+
+
+@gpu
 def test_what_every_row_sees_is_not_looked_for_again(train):
     """NaN that belongs in a row: the first token's value, every value, and every row at once; a long sequence takes no longer for it."""
     q, k, v, do = inputs(31, 30000, 1, 1, 64, BF16)
