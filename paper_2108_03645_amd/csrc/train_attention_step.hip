@@ -210,46 +210,35 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_kernel(StepArgs a) {
   for (int i = 0; i < D / 16; ++i)
     *reinterpret_cast<f32x4 *>(parts + ((wave * 16 + (lane & 15)) * D + i * 16 + (lane >> 4) * 4)) = acc[i];
   __syncthreads();
-  auto join = [&](int h, int d, float &most, float &all_sum) {
-    most = tops[0][h];
+  Seen seen;                                  // among the values of element of_d
+  int of_d = -1;
+  for (int i = threadIdx.x; i < heads * D; i += kStepWaves * 64) {
+    const int h = i / D, d = i % D;
+    float most = tops[0][h];
 #pragma unroll
     for (int w = 1; w < waves; ++w) most = fmaxf(most, tops[w][h]);
-    float x = all_sum = 0.f;
+    float all_sum = 0.f, x = 0.f;
 #pragma unroll
     for (int w = 0; w < waves; ++w) {
       const float f = tops[w][h] == most ? 1.f : __builtin_amdgcn_exp2f((tops[w][h] - most) * c);
       all_sum += sums[w][h] * f;
       x += parts[(w * 16 + h) * D + d] * f;
     }
-    return x;
-  };
-  bool lost = false;
-  for (int i = threadIdx.x; i < heads * D; i += kStepWaves * 64) {
-    const int h = i / D, d = i % D;
-    float most, all_sum;
-    const float x = join(h, d, most, all_sum);
     if (d >= a.dim) continue;
     if (a.splits == 1) {
-      const float y = x / all_sum;
-      lost |= y != y && all_sum > 0.f;
-      out[h * a.dim + d] = static_cast<T>(y);
+      x /= all_sum;
+      if (x != x && all_sum > 0.f) {          // a weight that is 0 in 32 bits is above 0 all the same: one infinity that it met is the result, not NaN
+        if (d != of_d) seen = Seen();
+        of_d = d;
+        seen.add(static_cast<float>(v_new[d]));
+        seen.through(reinterpret_cast<const T *>(vs), a.values_stride, length - 1, d);
+        if (seen.infinite()) x = seen.up() ? __builtin_inff() : -__builtin_inff();
+      }
+      out[h * a.dim + d] = static_cast<T>(x);
     } else {
       const int64_t at = part0 + static_cast<int64_t>(h) * a.splits;
       a.outputs[at * a.dim + d] = x;
       if (d == 0) { a.tops[at] = most; a.sums[at] = all_sum; }
-    }
-  }
-  // A weight that is 0 in 32 bits is above 0 all the same: infinities that it met, of one sign, are the result, not NaN.
-  if (a.splits > 1 || !__syncthreads_or(lost)) return;
-  for (int d = threadIdx.x; d < a.dim; d += kStepWaves * 64) {
-    Seen seen;
-    for (int h = 0; h < heads; ++h) {
-      float most, all_sum;
-      const float y = join(h, d, most, all_sum) / all_sum;
-      if (y == y || !(all_sum > 0.f)) continue;
-      if (seen.next == 0) seen.add(static_cast<float>(v_new[d]));
-      seen.through(reinterpret_cast<const T *>(vs), a.values_stride, length - 1, d);
-      if (seen.infinite()) out[h * a.dim + d] = static_cast<T>(seen.up() ? __builtin_inff() : -__builtin_inff());
     }
   }
 }
@@ -285,29 +274,17 @@ __global__ __launch_bounds__(1024) void step_join_kernel(StepArgs a) {
   outputs[group][d] = x;
   if (d == 0) sums[group] = sum;
   __syncthreads();
-  T *const out = static_cast<T *>(a.o) + static_cast<int64_t>(blockIdx.x) * a.dim + d;
-  bool lost = false;
-  if (group == 0 && d < a.dim) {
-    sum = sums[0];
+  if (group || d >= a.dim) return;
+  sum = sums[0];
 #pragma unroll
-    for (int g = 1; g < 8; ++g) { x += outputs[g][d]; sum += sums[g]; }
-    x /= sum;
-    *out = static_cast<T>(x);
-    lost = x != x && sum > 0.f;
+  for (int g = 1; g < 8; ++g) { x += outputs[g][d]; sum += sums[g]; }
+  x /= sum;
+  if (x != x && sum > 0.f) {                  // as in step_kernel; the new token's value is in its place by now
+    Seen seen;
+    seen.through(static_cast<const T *>(a.values) + b * a.values_batch + (blockIdx.x % a.heads) / (a.heads / a.kv_heads) * a.values_head, a.values_stride, length, d);
+    if (seen.infinite()) x = seen.up() ? __builtin_inff() : -__builtin_inff();
   }
-  if (!__syncthreads_or(lost)) return;        // else as in step_kernel: the values are looked through, every eighth by a group
-  Seen seen;
-  if (d < a.dim) {
-    const T *const values = static_cast<const T *>(a.values) + b * a.values_batch + (blockIdx.x % a.heads) / (a.heads / a.kv_heads) * a.values_head;
-    seen.through(values + group * a.values_stride, 8 * a.values_stride, (length + 8 - group) / 8 - 1, d);       // with the new token's, which is there by now
-  }
-  outputs[group][d] = static_cast<float>(seen.bits);
-  __syncthreads();
-  if (!lost) return;
-  int32_t found = 0;
-#pragma unroll
-  for (int g = 0; g < 8; ++g) found |= static_cast<int32_t>(outputs[g][d]);
-  if (found == 2 || found == 4) *out = static_cast<T>(found == 2 ? __builtin_inff() : -__builtin_inff());
+  static_cast<T *>(a.o)[static_cast<int64_t>(blockIdx.x) * a.dim + d] = static_cast<T>(x);
 }
 
 template <typename T>
