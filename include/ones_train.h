@@ -149,7 +149,7 @@ int ones_head_norm_rotation_backward(const void *dq_out, int64_t dq_stride, int6
  * offsets[s + 1] - 1, none or more.  For a row i of it, over the rows j <= i of the same sequence:
  *   z_j = scale * q_i . k_j, lse_i = log sum_j exp z_j, o_i = sum_j exp(z_j - lse_i) v_j
  * lse: float [heads][tokens].  Rows in front of the first and behind the last sequence are not read; o and the gradients are 0 there and
- * lse is -infinity.  rest, or NULL: what the rounding took from o, in its type; backward takes it for the sums that it needs o for (without it
+ * lse is -infinity.  rest, or NULL: what the rounding took from o, in its type (0 of an infinity); backward takes it for the sums that it needs o for (without it
  * the gradients of short sequences are off by up to three times their own rounding).  o, rest, dq, dk, dv have no gaps.
  * type: ONES_F16 or ONES_BF16; exponentials and the scores' gradients are rounded to it where a product takes them (in fp16 in units that
  * keep them from its ends).  dim: 8 .. ONES_MAX_ATTENTION_DIM, a multiple of 8; bases multiples of 16 bytes, strides of 8 elements, between

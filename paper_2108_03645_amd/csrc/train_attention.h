@@ -212,6 +212,13 @@ __device__ __forceinline__ Turn turn_of(uint32_t id, int32_t heads, int32_t kv_h
   return Turn{static_cast<int32_t>(id / heads), kv * (heads / kv_heads) + in / kv_heads, kv};
 }
 
+// What rounding takes from x: nothing of an infinity.
+template <typename T>
+__device__ __forceinline__ float lost(float x) {
+  const float r = static_cast<float>(static_cast<T>(x));
+  return fabsf(r) == INFINITY ? 0.f : x - r;
+}
+
 // acc[block][n] is C with m = 16 block + ..., of an output's rows n: out[first + 16 n + lane % 16][m] = factor[n] * acc, rounded, and
 // what the rounding took if `rest`.  Rows from `rows` on and elements from dim on are not there.
 template <typename T, int D, int TN, bool REST = false>
@@ -229,7 +236,7 @@ __device__ __forceinline__ void write_rows(const f32x4 (&acc)[D / 16][TN], const
       if (inside) *reinterpret_cast<Pack<uint32_t, 4> *>(out + r * stride + at) = v;
       if constexpr (REST) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i] -= static_cast<float>(static_cast<T>(x[i])); y[i] -= static_cast<float>(static_cast<T>(y[i])); }
+        for (int i = 0; i < 4; ++i) { x[i] = lost<T>(x[i]); y[i] = lost<T>(y[i]); }
         const Pack<uint32_t, 4> w = swapped<T>(x, y);
         if (inside && rest) *reinterpret_cast<Pack<uint32_t, 4> *>(rest + r * stride + at) = w;
       }

@@ -192,6 +192,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
           if (seen.no_number()) return false;         // NaN is right: every weight is above 0
           if (!seen.bits) return true;
           o[r * out_stride + d] = static_cast<T>(seen.up() ? __builtin_inff() : -__builtin_inff());
+          if (rest) rest[r * out_stride + d] = static_cast<T>(0.f);
           return false;
         },
         [&](int32_t r) { return rows.at + r + 1; },
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
         [&](int, int32_t y) { return v0 + y * a.v_stride; },
         [&](int32_t r, int d, const float (&sums)[1], int) {
           o[r * out_stride + d] = static_cast<T>(sums[0]);
-          if (rest) rest[r * out_stride + d] = static_cast<T>(sums[0] - static_cast<float>(static_cast<T>(sums[0])));
+          if (rest) rest[r * out_stride + d] = static_cast<T>(lost<T>(sums[0]));
         });
   }
 }

@@ -278,6 +278,18 @@ def test_what_keys_see_behind_what_they_do_not(train, n, heads, kv, bad, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+def test_infinite_results_have_no_rest(train, dtype):
+    """Nothing is rounded off infinity: o + rest is o there, in rows that saw it in a product and in rows that are summed again."""
+    q, k, v, do = inputs(34, 300, 2, 1, 64, dtype)
+    v[100, 0, 3], v[40, 0, 7] = float("inf"), -float("inf")
+    k[40] = -30 * q[40:41, :1].sign()                                 # and one that most weights are small for
+    o, _, rest = train.attention_forward(q, k, v, torch.tensor([0, 300], device="cuda", dtype=torch.int32), keep_rest=True)
+    assert (o[100:, :, 3] == float("inf")).all() and (o[40:, :, 7] == -float("inf")).all()
+    assert not rest[100:, :, 3].any() and not rest[40:, :, 7].any() and rest.isfinite().all() and rest.any()
+
+
+@gpu
 def test_what_every_row_sees_is_not_looked_for_again(train):
     """NaN that belongs in a row: the first token's value, every value, and every row at once; a long sequence takes no longer for it."""
     q, k, v, do = inputs(31, 30000, 1, 1, 64, BF16)
