@@ -106,29 +106,37 @@ struct Pairs {
   }
 };
 
-// The sum over the LANES lanes of a row, for all of them: between neighbours, pairs, the halves of 8 (mirrored: what they hold is the same by then)
-// and of 16, then between rows of 16 and between halves of the wave.
+// What `both` makes of the values of the LANES lanes of a row, for all of them: between neighbours, pairs, the halves of 8 (mirrored: what they hold is the
+// same by then) and of 16, then between rows of 16 and between halves of the wave.
 template <int PATTERN>
 __device__ __forceinline__ float from_lane(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), PATTERN, 0xf, 0xf, true));
 }
-template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v) {
-  v += from_lane<0xb1>(v);
-  v += from_lane<0x4e>(v);
-  if constexpr (LANES > 4) v += from_lane<0x141>(v);
-  if constexpr (LANES > 8) v += from_lane<0x140>(v);
+template <int LANES, class Both>
+__device__ __forceinline__ float of_lanes(float v, Both both) {
+  v = both(v, from_lane<0xb1>(v));
+  v = both(v, from_lane<0x4e>(v));
+  if constexpr (LANES > 4) v = both(v, from_lane<0x141>(v));
+  if constexpr (LANES > 8) v = both(v, from_lane<0x140>(v));
   if constexpr (LANES > 16) {
     const uint32_t b = __float_as_uint(v);
     const auto h = __builtin_amdgcn_permlane16_swap(b, b, false, false);
-    v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+    v = both(__uint_as_float(h[0]), __uint_as_float(h[1]));
   }
   if constexpr (LANES > 32) {
     const uint32_t b = __float_as_uint(v);
     const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-    v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+    v = both(__uint_as_float(h[0]), __uint_as_float(h[1]));
   }
   return v;
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+  return of_lanes<LANES>(v, [](float a, float b) { return a + b; });
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float v) {
+  return of_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
 constexpr int kMaxPairs = ONES_MAX_HEAD_DIM / 2;
@@ -146,8 +154,10 @@ __device__ __forceinline__ void turns(const RotationArgs &a, int64_t token, floa
   }
 }
 
+// Forward the grid is eight waves a SIMD, which have to fit at once: up to four pairs a lane do (22453 tokens of 15 x 88 fp16: 22.6 us; with 65 registers, and
+// so seven waves, 25.8).
 template <typename T, int VEC, int LANES, int PER, bool NEIGHBOURS, bool BACKWARD>
-__global__ __launch_bounds__(256) void rotation_kernel(RotationArgs a) {
+__global__ __launch_bounds__(256, !BACKWARD && VEC * PER <= 4 ? 8 : 1) void rotation_kernel(RotationArgs a) {
   using P = Pairs<VEC, LANES, PER, NEIGHBOURS>;
   constexpr int count = P::count, rows = kWave / LANES;      // rows of a wave at a time
   __shared__ float2 table[4][kMaxPairs];
@@ -203,9 +213,32 @@ __global__ __launch_bounds__(256) void rotation_kernel(RotationArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < count; ++i) square = __builtin_fmaf(x1[i], x1[i], __builtin_fmaf(x2[i], x2[i], square));
-        square = lanes_sum<LANES>(square);
+        float mean = lanes_sum<LANES>(square) * inverse + a.eps, unit = 1.f;
+        // Rows whose squares 32 bits do not hold, or not with all of their bits, are taken in a unit of their own, a power of two by their largest element
+        // (or eps), and every other row of the wave as it is.
+        const bool beyond = live && !(mean > 0x1p-100f && mean < 0x1p100f);
+        if (__builtin_expect(__any(beyond), 0)) {
+          float most = sqrtf(a.eps);
+#pragma unroll
+          for (int i = 0; i < count; ++i) most = fmaxf(most, fmaxf(fabsf(x1[i]), fabsf(x2[i])));
+          most = lanes_max<LANES>(most);
+          if (beyond && most > 0.f && most < INFINITY) {
+            int e;
+            frexpf(most, &e);
+            unit = ldexpf(1.f, min(-e, 126));
+          }
+          square = 0.f;
+#pragma unroll
+          for (int i = 0; i < count; ++i) {
+            x1[i] *= unit;
+            x2[i] *= unit;
+            square = __builtin_fmaf(x1[i], x1[i], __builtin_fmaf(x2[i], x2[i], square));
+          }
+          square = lanes_sum<LANES>(square);
+          if (unit != 1.f) mean = square * inverse + a.eps * unit * unit;
+        }
         // What is no row has no norm: with eps 0 it would be infinite, and 0 times it NaN in the weights' gradients.
-        const float r = live ? rsqrtf(square * inverse + a.eps) : 0.f;
+        const float r = live ? rsqrtf(mean) : 0.f;
         T *out = static_cast<T *>(a.out[k]) + (token * a.heads[k] + h) * a.dim;
         if constexpr (!BACKWARD) {
 #pragma unroll
@@ -229,10 +262,11 @@ __global__ __launch_bounds__(256) void rotation_kernel(RotationArgs a) {
             dot = __builtin_fmaf(g1[i], x1[i], __builtin_fmaf(g2[i], x2[i], dot));
           }
           dot = lanes_sum<LANES>(dot) * -inverse;
+          const float of_x = r * unit;
 #pragma unroll
           for (int i = 0; i < count; ++i) {
-            g1[i] = r * __builtin_fmaf(x1[i], dot, g1[i]);
-            g2[i] = r * __builtin_fmaf(x2[i], dot, g2[i]);
+            g1[i] = of_x * __builtin_fmaf(x1[i], dot, g1[i]);
+            g2[i] = of_x * __builtin_fmaf(x2[i], dot, g2[i]);
           }
           if (live) pairs.store(out, g1, g2, a.past);
         }

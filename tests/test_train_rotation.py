@@ -219,3 +219,22 @@ def test_norms_without_eps(train, tokens, heads, kv, dim, pairs, dtype):
     w = [make(dim, std=0.2, mean=1) for _ in range(2)]
     positions = torch.arange(tokens, device="cuda", dtype=torch.int32)
     both_ways(train, q, k, *w, dq, dk, positions, 100.0 ** (-torch.arange(pairs, device="cuda") / pairs), 0.0, False)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dim,interleaved", [(128, False), (80, True), (17, False), (512, False)])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_rows_whose_squares_are_no_floats(train, dim, interleaved, dtype, eps):
+    """Elements of 1e21 and 1e30, and without eps of 1e-21 and 1e-30, beside ordinary ones: norms as of all others."""
+    gen = torch.Generator(device="cuda").manual_seed(dim)
+    make = lambda *s, std=1.0, mean=0.0: torch.randn(*s, generator=gen, device="cuda") * std + mean  # noqa: E731
+    size = torch.tensor([1.0, 1e21, 1e30, 1e19] + ([1e-21, 1e-30, 1e-19] if eps == 0 else []), device="cuda")[:, None, None]
+    n = len(size)
+    q, k = (make(n, h, dim).mul(size).to(dtype) for h in (5, 2))
+    q[1, 0, 1:], k[2, 1, 2:] = 0, 0                                  # most of a row nothing
+    # gradients of the sizes that such rows give and take: dx stays within the type
+    dq, dk = (make(n, h, dim).mul(size.clamp(1e-3, 1e3)).to(dtype) for h in (5, 2))
+    w = [make(dim, std=0.2, mean=1) for _ in range(2)]
+    positions = torch.arange(n, device="cuda", dtype=torch.int32)
+    both_ways(train, q, k, *w, dq, dk, positions, 100.0 ** (-torch.arange(dim // 4, device="cuda") / (dim // 4)), eps, interleaved)
