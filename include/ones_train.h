@@ -128,8 +128,8 @@ int ones_orthogonal_update(const void *grad, float *momentum, int64_t count, int
  *   angle position * frequencies[i]: y1 = n1 cos - n2 sin, y2 = n2 cos + n1 sin; the others as they are.
  * Pairs are elements (i, i + pairs), or with `neighbours` (2 i, 2 i + 1).  q: [tokens][heads][dim], k: [tokens][kv_heads][dim], with
  * strides between tokens and between heads; outputs without gaps.  type: any; q_weight, k_weight: dim elements of weight_type, type or
- * ONES_F32.  Rows of any finite size have their norm.  positions: int32 [tokens], any; frequencies: float [pairs], radians a position (the angle is formed in 64 bits: off by
- * less than 2^-24 turns up to 2^29 turns).  0 <= 2 * pairs <= dim <= ONES_MAX_HEAD_DIM.
+ * ONES_F32.  Rows of any finite size have their norm.  positions: int32 [tokens], any; frequencies: float [pairs], radians a position
+ * (the angle is formed in 64 bits: off by less than 2^-24 turns up to 2^29 turns).  0 <= 2 * pairs <= dim <= ONES_MAX_HEAD_DIM.
  * Backward: dq_out, dk_out are the gradients of the results; dq, dk and the sums over tokens and heads dq_weight, dk_weight are written
  * (the latter may be NULL).  Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS, ONES_E_WORKSPACE_TOO_SMALL, ONES_E_HIP. */
 int ones_head_norm_rotation_forward(const void *q, int64_t q_stride, int64_t q_head_stride, const void *k, int64_t k_stride,

@@ -57,8 +57,10 @@ class Model:
 
     def hidden(self, tokens, states=None):
         """[batch, steps, width] after the last norm, and the blocks' states behind the last step: of the recurrence, or the keys and values
-        [batch, steps, heads, dim] that attention met."""
+        [batch, steps, heads, dim] that attention met.  states: what the recurrence goes on from."""
         if self.mixer == "attention":
+            if states is not None:
+                raise ValueError("states: attention begins a sequence anew; attention_step continues one")
             return self.attended(tokens)
         x = self.embedding[tokens].bfloat16()
         ends = []

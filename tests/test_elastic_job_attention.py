@@ -92,3 +92,10 @@ def test_the_job_runs_with_attention(capsys):
     losses, right = elastic_job.main(steps=3, generations=2, mixer="attention", clip=1.0)
     print(capsys.readouterr().out)
     assert all(loss == loss and abs(loss) < 100 for loss in losses) and 0 <= right <= 1
+
+
+def test_states_of_another_kind_are_refused():
+    """Attention begins a sequence anew: what the recurrence would go on from has no place in it."""
+    model = elastic_job.Model(7, 128, 1, device="cpu", mixer="attention")
+    with pytest.raises(ValueError):
+        model.hidden(torch.zeros(1, 3, dtype=torch.int64), [torch.zeros(1, 128)])
