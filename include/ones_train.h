@@ -152,7 +152,8 @@ int ones_head_norm_rotation_backward(const void *dq_out, int64_t dq_stride, int6
  * lse is -infinity.  rest, or NULL: what the rounding took from o, in its type (0 of an infinity); backward takes it for the sums that it needs o for (without it
  * the gradients of short sequences are off by up to three times their own rounding).  o, rest, dq, dk, dv have no gaps.
  * type: ONES_F16 or ONES_BF16; exponentials and the scores' gradients are rounded to it where a product takes them (in fp16 in units that
- * keep them from its ends).  dim: 8 .. ONES_MAX_ATTENTION_DIM, a multiple of 8; bases multiples of 16 bytes, strides of 8 elements, between
+ * keep them from its ends: dk is as exact as fp16 is for keys whose queries' |dout| are within 2^-26 of the largest from the key's block of 128
+ * rows on, dq for queries whose values are within 2^-26 of the largest up to the end of the query's block).  dim: 8 .. ONES_MAX_ATTENTION_DIM, a multiple of 8; bases multiples of 16 bytes, strides of 8 elements, between
  * tokens at least dim and at most 2^20.  heads: a multiple of kv_heads.  scale: 1e-30 to 1e30.
  * Backward: dout is the gradient of o; dk and dv are summed over the query heads of a key head.
  * Errors: ONES_E_INVALID_ARG, ONES_E_BOUNDS (a size or stride above its limit; (tokens / 64 + sequences + 2) * heads of 2^23 or

@@ -83,8 +83,9 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(AttentionArgs a) {
   }
 }
 
-// The unit that ds is held in where it is rounded to fp16: a power of two that brings |ds| <= 2 |do| |v| to at most 2^14.  (bf16 has the
-// exponents of 32 bits: 1.)
+// The unit that ds is held in where it is rounded to fp16: a power of two that brings |ds| <= 2 |do| |v| to at most 2^14.  |do| is a query's own, for keys
+// the largest of the queries from their slot on, |v| the largest up to a query's slot, for keys of the sequence; what is more than 2^27 below such
+// a bound loses bits.  (bf16 has the exponents of 32 bits: 1.)
 __device__ __forceinline__ float unit_of(float bound) {
   if (!(bound > 0.f) || !(bound < INFINITY)) return 1.f;
   int e;
@@ -125,7 +126,7 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
   float v_most = 0.f;
   if constexpr (__is_same(T, f16)) {
     const int32_t all = a.heads + a.kv_heads;
-    v_most = largest_norm(a.v_norm, all, a.heads + turn.kv, 1, slot_of<kQueries>(rows.sequence, rows.first), (rows.length + kQueries - 1) / kQueries);
+    v_most = largest_norm(a.v_norm, all, a.heads + turn.kv, 1, slot_of<kQueries>(rows.sequence, rows.first), (rows.at + count + kQueries - 1) / kQueries);
   }
   s16x8 q[TN][D / 32], g[TN][D / 32];
   float lse[TN], delta[TN], unit[TN], factor[TN];
@@ -285,7 +286,8 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
   float unit = 1.f;
   if constexpr (__is_same(T, f16)) {
     const int32_t all = a.heads + a.kv_heads, first = slot_of<kQueries>(rows.sequence, rows.first), slots = (rows.length + kQueries - 1) / kQueries;
-    unit = unit_of(2.f * largest_norm(a.v_norm, all, kv * group, group, first, slots) * largest_norm(a.v_norm, all, a.heads + kv, 1, first, slots));
+    const int32_t front = rows.at / kQueries;        // slots whose queries do not see the tile's keys; the others' o has values of all
+    unit = unit_of(2.f * largest_norm(a.v_norm, all, kv * group, group, first + front, slots - front) * largest_norm(a.v_norm, all, a.heads + kv, 1, first, slots));
   }
   constexpr float kWeights = __is_same(T, f16) ? 16384.f : 1.f;       // the unit of p, at most 1 and a rounding
   s16x8 k[TN][D / 32], v[TN][D / 32];

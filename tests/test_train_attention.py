@@ -408,6 +408,29 @@ def test_fp16_gradients_of_very_different_sizes(train):
 
 
 @gpu
+def test_fp16_gradients_far_below_those_in_front(train):
+    """Units go by what a tile's rows see: keys whose queries all have gradients of 2^-15 keep fp16's precision behind queries with gradients of 2^14, and
+    queries whose values are of 2^-12 in front of values of 2^12."""
+    q, k, v, do = inputs(35, 900, 4, 2, 64, FP16)
+    offsets = torch.tensor([0, 900], device="cuda", dtype=torch.int32)
+    for which in ("dk", "dv", "dq"):
+        g, u = do.float() / 0.05, v.float()
+        if which == "dq":
+            u[:512], u[512:] = u[:512] * 2.0 ** -12, u[512:] * 2.0 ** 12
+            rows = slice(0, 512)
+        else:
+            g[:512], g[512:] = (g[:512] * 2.0 ** 14).clamp(-60000, 60000), g[512:] * 2.0 ** -15
+            rows = slice(512, 900)
+        t = q, k, u.half()
+        g = g.half()
+        r = attention64(*t, [0, 900], 0.125, g)
+        got = dict(zip(("dq", "dk", "dv"), train.attention_backward(g, *t, *train.attention_forward(*t, offsets, keep_rest=True), offsets)))[which]
+        want, part = r[which][rows], got[rows].double()
+        # as above: of its norm the products' roundings, and its own where that is fp16's smallest
+        assert (part - want).norm() <= HALF[FP16] * want.norm() + 2.0 ** -25 * want.numel() ** 0.5, which
+
+
+@gpu
 def test_gradients_under_autograd_against_differences(train):
     q, k, v, do = inputs(12, 90, 4, 2, 32, FP16, std=0.5)
     q, k, v = (t.requires_grad_() for t in (q, k, v))
