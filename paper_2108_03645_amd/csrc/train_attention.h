@@ -14,6 +14,12 @@ namespace ones {
 namespace train {
 namespace {
 
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// fp16 keeps 2^-24 and up: the exponentials below the row's largest are held in units of 2^-8.
+template <typename T>
+constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;
+
 // As load_to_lds, four bytes a lane.
 __device__ __forceinline__ void load_words_to_lds(const unsigned char *base, uint32_t bytes, uint32_t offset, uint32_t to) {
   const uint64_t at = reinterpret_cast<uintptr_t>(base);
@@ -125,13 +131,20 @@ __device__ __forceinline__ bool any_nan(const f32x4 (&acc)[D / 16][TN]) {
 // What is not finite among element d of the rows that a row sees, looked for as far as is asked, from the first row on; 16 at once, so that they are under
 // way together.
 struct Seen {
-  uint32_t bits = 0;                          // 1: NaN, 2: infinity, 4: -infinity
+  float most = 0.f, least = 0.f;
+  uint32_t size = 0;                          // the largest, as bits without the sign: NaN lies above infinity
   int32_t next = 0;
-  __device__ __forceinline__ bool up() const { return bits & 2; }
-  __device__ __forceinline__ void add(float x) { bits |= x != x ? 1 : x == __builtin_inff() ? 2 : x == -__builtin_inff() ? 4 : 0; }
+  __device__ __forceinline__ void add(float x) {
+    most = fmaxf(most, x);
+    least = fminf(least, x);
+    size = max(size, __float_as_uint(x) & 0x7fffffff);
+  }
+  __device__ __forceinline__ bool up() const { return most == __builtin_inff(); }
+  __device__ __forceinline__ bool down() const { return least == -__builtin_inff(); }
+  __device__ __forceinline__ bool finite() const { return size < 0x7f800000; }
   // Whether a sum over it, with weights above 0, is NaN; whether it is one infinity.
-  __device__ __forceinline__ bool no_number() const { return (bits & 1) || bits == 6; }
-  __device__ __forceinline__ bool infinite() const { return bits == 2 || bits == 4; }
+  __device__ __forceinline__ bool no_number() const { return size > 0x7f800000 || (up() && down()); }
+  __device__ __forceinline__ bool infinite() const { return size == 0x7f800000 && up() != down(); }
   template <typename T>
   __device__ __forceinline__ void through(const T *rows, int64_t stride, int32_t last, int d) {
     while (next <= last && !no_number()) {

@@ -190,7 +190,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(AttentionArgs
           if (x == x || lse[r] != lse[r]) return false;
           seen.through(v0, a.v_stride, rows.at + r, d);
           if (seen.no_number()) return false;         // NaN is right: every weight is above 0
-          if (!seen.bits) return true;
+          if (seen.finite()) return true;
           o[r * out_stride + d] = static_cast<T>(seen.up() ? __builtin_inff() : -__builtin_inff());
           if (rest) rest[r * out_stride + d] = static_cast<T>(0.f);
           return false;

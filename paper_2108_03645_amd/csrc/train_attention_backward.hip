@@ -104,8 +104,8 @@ __device__ __forceinline__ float largest_norm(const float *norms, int32_t all, i
 
 template <typename T, int D>
 __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint32_t id, unsigned char *lds) {
-  constexpr int TN = 1, kMine = 16 * TN, kRows = 4 * kMine;
-  constexpr int kStep = kKeys<TN>, kHalves = kStep / 32;
+  constexpr int kMine = 16, kRows = 4 * kMine, kStep = kKeys<1>;
+  static_assert(kStep == 32);
   using Tile = RowTile<D, kStep, 256>;
   const Turn turn = turn_of(id, a.heads, a.kv_heads);
   const int32_t slot = static_cast<int32_t>(slots_of(a.tokens, a.sequences, kRows)) - 1 - turn.slot;
@@ -128,31 +128,22 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
     const int32_t all = a.heads + a.kv_heads;
     v_most = largest_norm(a.v_norm, all, a.heads + turn.kv, 1, slot_of<kQueries>(rows.sequence, rows.first), (rows.at + count + kQueries - 1) / kQueries);
   }
-  s16x8 q[TN][D / 32], g[TN][D / 32];
-  float lse[TN], delta[TN], unit[TN], factor[TN];
-#pragma unroll
-  for (int n = 0; n < TN; ++n) {
-    const int r = mine + n * 16;
-    read_rows<D>(at<T>(a.q, here + r, a.q_stride, turn.head, a.q_head), a.q_stride, count - r, a.dim, lane, q[n]);
-    read_rows<D>(at<T>(a.dout, here + r, a.do_stride, turn.head, a.do_head), a.do_stride, count - r, a.dim, lane, g[n]);
-    const int64_t i = static_cast<int64_t>(turn.head) * a.tokens + here + min(r + (lane & 15), count - 1);
-    const float2 terms = a.terms[i];
-    lse[n] = terms.x;
-    delta[n] = terms.y;
-    unit[n] = 1.f;
-    if constexpr (__is_same(T, f16)) unit[n] = unit_of(2.f * a.dout_norm[i] * v_most);
-    factor[n] = a.scale / unit[n];
-  }
+  s16x8 q[D / 32], g[D / 32];
+  read_rows<D>(at<T>(a.q, here + mine, a.q_stride, turn.head, a.q_head), a.q_stride, count - mine, a.dim, lane, q);
+  read_rows<D>(at<T>(a.dout, here + mine, a.do_stride, turn.head, a.do_head), a.do_stride, count - mine, a.dim, lane, g);
+  const int64_t term = static_cast<int64_t>(turn.head) * a.tokens + here + min(mine + (lane & 15), count - 1);
+  const float lse = a.terms[term].x, delta = a.terms[term].y;
+  float unit = 1.f;
+  if constexpr (__is_same(T, f16)) unit = unit_of(2.f * a.dout_norm[term] * v_most);
+  const float factor[1] = {a.scale / unit};
   int along[D / 32], across[D / 16];
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) along[s] = Tile::along(lane, s);
 #pragma unroll
   for (int b = 0; b < D / 16; ++b) across[b] = Tile::across(lane, b);
-  f32x4 acc[D / 16][TN];
+  f32x4 acc[D / 16][1];
 #pragma unroll
-  for (int n = 0; n < TN; ++n)
-#pragma unroll
-    for (int b = 0; b < D / 16; ++b) acc[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int b = 0; b < D / 16; ++b) acc[b][0] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int steps = (rows.at + count + kStep - 1) / kStep, first_row = rows.at + mine;
   for (int step = 0; step < steps; ++step) {
     meet<0>();
@@ -168,69 +159,52 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
       f[s] = Tile::read_along(ks, b * 16, along[s]);
       e[s] = Tile::read_along(vs, b * 16, along[s]);
     };
-    if (step * kStep > first_row + kMine - 1) continue;
+    const int key = step * kStep;
+    if (key > first_row + kMine - 1) continue;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) rows_at(0, s);
     __builtin_amdgcn_sched_barrier(0);
+    f32x4 z[2], d[2];
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
-      const int key = step * kStep + h * 32;
-      if (key > first_row + kMine - 1) break;
-      f32x4 z[2][TN], d[2][TN];
+    for (int b = 0; b < 2; ++b) {
+      z[b] = d[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int s = 0; s < kSteps; ++s) {
+        z[b] = mfma<T>(f[s], q[s], z[b]);
+        d[b] = mfma<T>(e[s], g[s], d[b]);
+        if (b == 0) rows_at(1, s);
+        else
 #pragma unroll
-        for (int n = 0; n < TN; ++n) z[b][n] = d[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-#pragma unroll
-          for (int n = 0; n < TN; ++n) {
-            z[b][n] = mfma<T>(f[s], q[n][s], z[b][n]);
-            d[b][n] = mfma<T>(e[s], g[n][s], d[b][n]);
-          }
-          if (b == 0) rows_at(h * 2 + 1, s);
-          else
-#pragma unroll
-            for (int i = s * kEach; i < min((s + 1) * kEach, kAhead); ++i) fs[i] = Tile::read_across(ks, h * 32, across[i]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-      s16x8 ds[TN];
-#pragma unroll
-      for (int n = 0; n < TN; ++n) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][n][r], c, -lse[n]));
-            z[b][n][r] = p * (d[b][n][r] - delta[n]);
-            if constexpr (__is_same(T, f16)) z[b][n][r] *= unit[n];
-          }
-        if (key + 31 > first_row) {
-          const int row = first_row + n * 16 + (lane & 15) - key;
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (b * 16 + (lane >> 4) * 4 + r > row) z[b][n][r] = 0.f;
-        }
-        ds[n] = rounded<T>(z[0][n], z[1][n]);
-      }
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-#pragma unroll
-        for (int n = 0; n < TN; ++n) acc[b][n] = mfma<T>(fs[b % kAhead], ds[n], acc[b][n]);
-        if (b + kAhead < kBlocks) fs[b % kAhead] = Tile::read_across(ks, h * 32, across[b + kAhead]);
-        else if (h + 1 < kHalves && b - (kBlocks - kAhead) < kSteps) rows_at(2, b - (kBlocks - kAhead));
+          for (int i = s * kEach; i < min((s + 1) * kEach, kAhead); ++i) fs[i] = Tile::read_across(ks, 0, across[i]);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (h + 1 < kHalves)
+    }
 #pragma unroll
-        for (int s = kAhead; s < kSteps; ++s) rows_at(2, s);
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][r], c, -lse));
+        z[b][r] = p * (d[b][r] - delta);
+        if constexpr (__is_same(T, f16)) z[b][r] *= unit;
+      }
+    if (key + kStep - 1 > first_row) {
+      const int row = first_row + (lane & 15) - key;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (b * 16 + (lane >> 4) * 4 + r > row) z[b][r] = 0.f;
+    }
+    const s16x8 ds = rounded<T>(z[0], z[1]);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      acc[b][0] = mfma<T>(fs[b % kAhead], ds, acc[b][0]);
+      if (b + kAhead < kBlocks) fs[b % kAhead] = Tile::read_across(ks, 0, across[b + kAhead]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  write_rows<T, D, TN>(acc, factor, dq + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
-  if (__syncthreads_or(any_nan<D, TN>(acc))) {
+  write_rows<T, D, 1>(acc, factor, dq + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+  if (__syncthreads_or(any_nan<D, 1>(acc))) {
     __syncthreads();
     const T *const q0 = at<T>(a.q, here, a.q_stride, turn.head, a.q_head), *const k0 = at<T>(a.k, rows.first, a.k_stride, turn.kv, a.k_head);
     const T *const g0 = at<T>(a.dout, here, a.do_stride, turn.head, a.do_head), *const v0 = at<T>(a.v, rows.first, a.v_stride, turn.kv, a.v_head);
@@ -243,8 +217,8 @@ __device__ __forceinline__ void gradient_of_queries(const AttentionArgs &a, uint
           const int32_t i = rows.at + r, end = min(i / kStep * kStep + kStep, rows.length);
           if (!any_infinite(k0, a.k_stride, i + 1, end, d)) return false;
           // infinite or NaN in a key makes its score so, and this element NaN, for the rows that see it
-          if (!seen.bits) seen.through(k0, a.k_stride, i, d);
-          return !seen.bits;
+          if (seen.finite()) seen.through(k0, a.k_stride, i, d);
+          return seen.finite();
         },
         [&](int32_t r) { return rows.at + r + 1; },
         [&](int32_t r, int32_t y, float (&w)[1]) {
@@ -264,7 +238,7 @@ constexpr int kKeysLds = 4 * RowTile<D, kStepRows, 4 * kKeyRows>::bytes + 2 * kS
 
 template <typename T, int D>
 __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_t id, unsigned char *lds) {
-  constexpr int TN = 1, kMine = 16;
+  constexpr int kMine = 16;
   using Tile = RowTile<D, kStepRows, 4 * kKeyRows>;
   const int32_t kv = static_cast<int32_t>(id % a.kv_heads), group = a.heads / a.kv_heads;
   id /= a.kv_heads;
@@ -290,19 +264,13 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     unit = unit_of(2.f * largest_norm(a.v_norm, all, kv * group, group, first + front, slots - front) * largest_norm(a.v_norm, all, a.heads + kv, 1, first, slots));
   }
   constexpr float kWeights = __is_same(T, f16) ? 16384.f : 1.f;       // the unit of p, at most 1 and a rounding
-  s16x8 k[TN][D / 32], v[TN][D / 32];
-#pragma unroll
-  for (int n = 0; n < TN; ++n) {
-    const int r = mine + n * 16;
-    read_rows<D>(at<T>(a.k, here + r, a.k_stride, kv, a.k_head), a.k_stride, count - r, a.dim, lane, k[n]);
-    read_rows<D>(at<T>(a.v, here + r, a.v_stride, kv, a.v_head), a.v_stride, count - r, a.dim, lane, v[n]);
-  }
+  s16x8 k[D / 32], v[D / 32];
+  read_rows<D>(at<T>(a.k, here + mine, a.k_stride, kv, a.k_head), a.k_stride, count - mine, a.dim, lane, k);
+  read_rows<D>(at<T>(a.v, here + mine, a.v_stride, kv, a.v_head), a.v_stride, count - mine, a.dim, lane, v);
   int along0 = Tile::along(lane, 0), across0 = Tile::across(lane, 0);
-  f32x4 of_k[D / 16][TN], of_v[D / 16][TN];
+  f32x4 of_k[D / 16][1], of_v[D / 16][1];
 #pragma unroll
-  for (int n = 0; n < TN; ++n)
-#pragma unroll
-    for (int b = 0; b < D / 16; ++b) of_k[b][n] = of_v[b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int b = 0; b < D / 16; ++b) of_k[b][0] = of_v[b][0] = f32x4{0.f, 0.f, 0.f, 0.f};
   // The queries from the tile's first key on, the last ones first, of all heads before the next ones: the workgroups of a sequence end at different
   // queries but begin at the same ones, so that they read the same rows at the same time, which then come from L2 (head after head
   // from the first query on, 16 x 2048 x 16 over 2 x 128 read 4 GB from behind L2).
@@ -344,7 +312,7 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     // second 16 queries need between those of the first, what those across the rows need between those of the second.
     constexpr int kSteps = D / 32, kBlocks = D / 16, kAhead = D > 64 ? 3 : D == 32 ? 2 : 4, kEach = (kAhead + kSteps - 1) / kSteps;
     s16x8 f[kSteps], e[kSteps], fs[kAhead], es[kAhead];
-    Pack<T, 8> p[TN], ds[TN];
+    Pack<T, 8> p, ds;
     const auto rows_at = [&](int b, int s) {
       f[s] = Tile::read_along(qs, b * 16, along0 ^ (s << 6));
       e[s] = Tile::read_along(gs, b * 16, along0 ^ (s << 6));
@@ -358,16 +326,11 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      f32x4 z[TN], d[TN];
-#pragma unroll
-      for (int n = 0; n < TN; ++n) z[n] = d[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 z{0.f, 0.f, 0.f, 0.f}, d = z;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
-#pragma unroll
-        for (int n = 0; n < TN; ++n) {
-          z[n] = mfma<T>(f[s], k[n][s], z[n]);
-          d[n] = mfma<T>(e[s], v[n][s], d[n]);
-        }
+        z = mfma<T>(f[s], k[s], z);
+        d = mfma<T>(e[s], v[s], d);
         if (b == 0) rows_at(1, s);
         else
 #pragma unroll
@@ -377,89 +340,76 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
       const f32x4 t0 = *reinterpret_cast<const f32x4 *>(ts + b * 32), t1 = *reinterpret_cast<const f32x4 *>(ts + b * 32 + 4);
       const float lse[4] = {t0[0], t0[2], t1[0], t1[2]}, delta[4] = {t0[1], t0[3], t1[1], t1[3]};
 #pragma unroll
-      for (int n = 0; n < TN; ++n) {
+      for (int r = 0; r < 4; ++r) {
+        z[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[r], c, -lse[r]));
+        d[r] = z[r] * (d[r] - delta[r]);
+        if constexpr (__is_same(T, f16)) { z[r] *= kWeights; d[r] *= unit; }
+      }
+      if (border) {
+        const int row = mine + (lane & 15) - first - b * 16 - (lane >> 4) * 4;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          z[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[n][r], c, -lse[r]));
-          d[n][r] = z[n][r] * (d[n][r] - delta[r]);
-          if constexpr (__is_same(T, f16)) { z[n][r] *= kWeights; d[n][r] *= unit; }
-        }
-        if (border) {
-          const int row = mine + n * 16 + (lane & 15) - first - b * 16 - (lane >> 4) * 4;
+        for (int r = 0; r < 4; ++r)
+          if (r < row) z[r] = d[r] = 0.f;
+      }
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (r < row) z[n][r] = d[n][r] = 0.f;
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          p[n].v[b * 4 + r] = static_cast<T>(z[n][r]);
-          ds[n].v[b * 4 + r] = static_cast<T>(d[n][r]);
-        }
+      for (int r = 0; r < 4; ++r) {
+        p.v[b * 4 + r] = static_cast<T>(z[r]);
+        ds.v[b * 4 + r] = static_cast<T>(d[r]);
       }
     }
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-#pragma unroll
-      for (int n = 0; n < TN; ++n) {
-        of_v[b][n] = mfma<T>(fs[b % kAhead], __builtin_bit_cast(s16x8, p[n]), of_v[b][n]);
-        of_k[b][n] = mfma<T>(es[b % kAhead], __builtin_bit_cast(s16x8, ds[n]), of_k[b][n]);
-      }
+      of_v[b][0] = mfma<T>(fs[b % kAhead], __builtin_bit_cast(s16x8, p), of_v[b][0]);
+      of_k[b][0] = mfma<T>(es[b % kAhead], __builtin_bit_cast(s16x8, ds), of_k[b][0]);
       if (b + kAhead < kBlocks) block_at(b + kAhead);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  float k_factor[TN], v_factor[TN];
-#pragma unroll
-  for (int n = 0; n < TN; ++n) {
-    k_factor[n] = a.scale / unit;
-    v_factor[n] = 1.f / kWeights;
-  }
+  const float k_factor[1] = {a.scale / unit}, v_factor[1] = {1.f / kWeights};
   if (a.parts == 1) {
-    write_rows<T, D, TN>(of_k, k_factor, dk + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
-    write_rows<T, D, TN>(of_v, v_factor, dv + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+    write_rows<T, D, 1>(of_k, k_factor, dk + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
+    write_rows<T, D, 1>(of_v, v_factor, dv + mine * out_stride, nullptr, out_stride, count - mine, a.dim, lane);
   }
   float *const partial = a.partial + ((static_cast<int64_t>(part) * a.tokens + here) * a.kv_heads + kv) * 2 * a.dim;
   const int64_t partial_stride = static_cast<int64_t>(a.kv_heads) * 2 * a.dim;
-#pragma unroll
-  for (int n = 0; n < TN; ++n) {
-    const int r = mine + n * 16 + (lane & 15);
-    if (a.parts == 1 || r >= count) continue;
-    float *to = partial + r * partial_stride;
+  if (const int r = mine + (lane & 15); a.parts > 1 && r < count) {
+    float *const to = partial + r * partial_stride;
 #pragma unroll
     for (int b = 0; b < D / 16; ++b) {
       const int i = b * 16 + (lane >> 4) * 4;
       if (i >= a.dim) continue;
-      *reinterpret_cast<f32x4 *>(to + i) = of_k[b][n] * k_factor[n];
-      *reinterpret_cast<f32x4 *>(to + a.dim + i) = of_v[b][n] * v_factor[n];
+      *reinterpret_cast<f32x4 *>(to + i) = of_k[b][0] * k_factor[0];
+      *reinterpret_cast<f32x4 *>(to + a.dim + i) = of_v[b][0] * v_factor[0];
     }
   }
-  if (__syncthreads_or(any_nan<D, TN>(of_k) || any_nan<D, TN>(of_v))) {
+  if (__syncthreads_or(any_nan<D, 1>(of_k) || any_nan<D, 1>(of_v))) {
     __syncthreads();
     const T *const k0 = at<T>(a.k, here, a.k_stride, kv, a.k_head), *const v0 = at<T>(a.v, here, a.v_stride, kv, a.v_head);
     // What the queries from .. to - 1 of all heads hold: NaN in lse, which makes both results of a key that sees it NaN, and in delta, all of dk; and what is not
     // finite in element d of do, which goes into that element of dv.
-    constexpr uint32_t kLse = 1, kDelta = 2, kUp = 8, kDown = 16, kDout = 28;          // (of do as in Seen)
-    auto look = [&](int32_t from, int32_t to, int d) __attribute__((always_inline)) {
-      uint32_t held = 0;
+    struct Held {
+      uint32_t lse, delta;                    // as Seen::size
+      Seen dout;
+    };
+    auto look = [&](int32_t from, int32_t to, int d, Held held) __attribute__((always_inline)) {
       for (int32_t h = head0; h < head0 + heads; ++h) {
         const float2 *const terms = a.terms + static_cast<int64_t>(h) * a.tokens + here;
-        for (int32_t i = from; i < to && !(held & kLse); i += 16)
+        for (int32_t i = from; i < to && held.lse <= 0x7f800000; i += 8)
 #pragma unroll
-          for (int n = 0; n < 16; ++n) {
+          for (int n = 0; n < 8; ++n) {
             const float2 t = terms[min(i + n, to - 1)];
-            held |= (t.x != t.x ? kLse : 0) | (t.y != t.y ? kDelta : 0);
+            held.lse = max(held.lse, __float_as_uint(t.x) & 0x7fffffff);
+            held.delta = max(held.delta, __float_as_uint(t.y) & 0x7fffffff);
           }
-        Seen dout;
-        dout.next = from;
-        dout.through(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, to - 1, d);
-        held |= dout.bits << 2;
+        held.dout.next = from;
+        held.dout.through(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, to - 1, d);
       }
       return held;
     };
     // the queries of all heads in a row, from the tile's first key on
     sum_by_rows<2>(
         lds, count, a.dim,
-        [&, behind = 0u, looked = false](int32_t r, int d) mutable {
+        [&, behind = Held{}, looked = false](int32_t r, int d) mutable {
           const float of_k = a.parts == 1 ? static_cast<float>(dk[r * out_stride + d]) : partial[r * partial_stride + d];
           const float of_v = a.parts == 1 ? static_cast<float>(dv[r * out_stride + d]) : partial[r * partial_stride + a.dim + d];
           // only of queries and gradients that the key does not see, in the one step that it shares with them
@@ -471,16 +421,20 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
           }
           if (!k_asks && !v_asks) return 0;
           const int32_t tile = min(kKeyRows, left);
-          if (!looked) behind = look(tile, left, d);
+          Held held = behind;                   // of the queries behind the tile, which all of its keys see; looked for once
+#pragma unroll 1
+          for (int turn = looked; turn < 2; ++turn) {
+            held = look(turn ? r : tile, turn ? tile : left, d, held);
+            if (turn == 0) behind = held;
+          }
           looked = true;
-          const uint32_t held = behind | look(r, tile, d), dout = held & kDout;
-          if (held & kLse) return 0;
-          if (v_asks && (dout == kUp || dout == kDown)) {
-            const float all = dout == kUp ? __builtin_inff() : -__builtin_inff();
+          if (held.lse > 0x7f800000) return 0;
+          if (v_asks && held.dout.infinite()) {
+            const float all = held.dout.up() ? __builtin_inff() : -__builtin_inff();
             if (a.parts == 1) dv[r * out_stride + d] = static_cast<T>(all);
             else partial[r * partial_stride + a.dim + d] = all;
           }
-          return (k_asks && !(held & kDelta) ? 1 : 0) + (v_asks && !dout ? 2 : 0);
+          return (k_asks && held.delta <= 0x7f800000 ? 1 : 0) + (v_asks && held.dout.finite() ? 2 : 0);
         },
         [&](int32_t) { return all_steps ? heads * left : 0; },
         [&](int32_t r, int32_t y, float (&w)[2]) {

@@ -13,8 +13,6 @@ namespace ones {
 namespace train {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
 struct AttentionArgs {
   const void *q, *k, *v, *dout;
   int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head, do_stride, do_head;      // elements
@@ -33,10 +31,6 @@ template <typename T>
 __device__ __forceinline__ const T *at(const void *p, int64_t row, int64_t stride, int32_t head, int64_t head_stride) {
   return static_cast<const T *>(p) + row * stride + head * head_stride;
 }
-
-// fp16 keeps 2^-24 and up: the exponentials below the row's largest are held in units of 2^-8.
-template <typename T>
-constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;
 
 // How far, as a power of two, an exponential may exceed 1 before the largest score is taken over.  (0 costs 4 % forward; the largest exponential is rounded
 // then as the others are, which a row of few large ones sees: bf16 o is off by 2.2e-3 of its norm instead of 1.9e-3.)

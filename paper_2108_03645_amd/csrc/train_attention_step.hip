@@ -20,8 +20,6 @@ namespace ones {
 namespace train {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-
 struct StepArgs {
   const void *q, *k, *v;
   void *keys, *values, *o;
@@ -32,9 +30,6 @@ struct StepArgs {
   int32_t batch, capacity, heads, kv_heads, dim, blocks_of_heads, splits;
   float scale;
 };
-
-template <typename T>
-constexpr float kShift = __is_same(T, f16) ? 8.f : 0.f;      // as in train_attention.hip
 
 // A wave's tile of 32 rows: like RowTile, but a load of the wave fills fewer than 16 rows, so that the exchange differs from load to load.
 template <int D>
