@@ -419,7 +419,10 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
             if (of_k != of_k) k_asks |= any_infinite(at<T>(a.q, here, a.q_stride, h, a.q_head), a.q_stride, step, r, d);
             if (of_v != of_v) v_asks |= any_infinite(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, step, r, d);
           }
-          if (!k_asks && !v_asks) return 0;
+          // And the rows behind the sequence that its last step has are zeros, but their scores with a key that has infinities NaN: where nothing else
+          // that the key sees is, its own scores were all -infinity.
+          const bool behind_end = left % kStepRows != 0;
+          if (!k_asks && !v_asks && (!behind_end || (of_k == of_k && of_v == of_v))) return 0;
           const int32_t tile = min(kKeyRows, left);
           Held held = behind;                   // of the queries behind the tile, which all of its keys see; looked for once
 #pragma unroll 1
@@ -434,6 +437,9 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
             if (a.parts == 1) dv[r * out_stride + d] = static_cast<T>(all);
             else partial[r * partial_stride + a.dim + d] = all;
           }
+          const bool from_there = behind_end && max(held.lse, held.delta) < 0x7f800000;
+          k_asks |= from_there && of_k != of_k;
+          v_asks |= from_there && of_v != of_v;
           return (k_asks && held.delta <= 0x7f800000 ? 1 : 0) + (v_asks && held.dout.finite() ? 2 : 0);
         },
         [&](int32_t) { return all_steps ? heads * left : 0; },

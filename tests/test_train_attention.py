@@ -290,6 +290,23 @@ def test_infinite_results_have_no_rest(train, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("n", [128, 130, 159, 300])
+def test_keys_of_minus_infinity_have_no_weight(train, n, dtype):
+    """A score of -infinity is a weight of 0: nothing of the key reaches o, its dk and dv are 0, whatever the length leaves of the last step."""
+    q, k, v, do = inputs(36, n, 2, 1, 64, dtype)
+    q = q.abs() + 1
+    k[[5, 70, n - 1], 0, 3] = -float("inf")
+    offsets = torch.tensor([0, n], device="cuda", dtype=torch.int32)
+    o, lse, rest = train.attention_forward(q, k, v, offsets, keep_rest=True)
+    _, dk, dv = train.attention_backward(do, q, k, v, o, lse, rest, offsets)
+    assert all(t.isfinite().all() for t in (o, lse, rest, dk, dv))
+    for key in (5, 70, n - 1):
+        assert not dk[key].any() and not dv[key].any()
+    assert dv[6].any() and dk[6].any()
+
+
+@gpu
 def test_what_every_row_sees_is_not_looked_for_again(train):
     """NaN that belongs in a row: the first token's value, every value, and every row at once; a long sequence takes no longer for it."""
     q, k, v, do = inputs(31, 30000, 1, 1, 64, BF16)
