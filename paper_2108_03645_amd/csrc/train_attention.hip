@@ -16,7 +16,7 @@
 //
 // What bounds it: the matrix units, the exponentials, of which little hides behind them, and the power that both draw.  16384 tokens, 16 heads over 2 of 128, bf16: 1.01 to 1.09 ms, 1.0 to 1.1 PFLOP/s of the causal half (the same of zeros: 0.90 ms;
 // a library product of 8192 cubed: 1.27 to 1.35 PFLOP/s, of zeros 1.75); the matrix units are busy half of the cycles, the vector units 60 %, LDS
-// 25 %.  16 x 2048 tokens with `rest`: 0.46 ms.  Tried and not kept: four waves a SIMD with 16 queries each (1.17 ms), scores a run ahead
+// 25 %.  16 x 2048 tokens with `rest`: 0.47 ms.  Tried and not kept: four waves a SIMD with 16 queries each (1.17 ms), scores a run ahead
 // of the exponentials (1.10), wave priorities (1.08), groups of instructions set by hand (1.10 to 1.19).
 #include "train_attention_sequences.h"
 

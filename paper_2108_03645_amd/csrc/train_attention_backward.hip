@@ -9,9 +9,9 @@
 // SIMD fit then; with 32 keys a wave it is two, whose registers spill (the keys' part alone, sizes as below: 754 us against 720).  In fp16 the
 // scores' gradients are held in units that follow from the norms of do and v (unit_of()).
 //
-// What bounds it: the matrix units are busy 46 % of the cycles, LDS 49 % (every row of the other side is read for 16 of this one), the vector units 44 %; waits
-// between them are the rest.  16 x 2048 tokens, 16 heads over 2 of 128, bf16: delta 73 us (402 MB, 5.5 TB/s), gradients 1.03 ms (0.96 PFLOP/s of
-// seven products), the parts' sums 31 us.
+// What bounds it: the matrix units are busy 48 % of the cycles, LDS 51 % (every row of the other side is read for 16 of this one), the vector units 46 %; waits
+// between them are the rest.  16 x 2048 tokens, 16 heads over 2 of 128, bf16: delta 74 us (402 MB, 5.5 TB/s), gradients 1.03 to 1.06 ms (0.91 to 0.94
+// PFLOP/s of seven products), the parts' sums 30 us.
 #include "train_attention_sequences.h"
 
 namespace ones {

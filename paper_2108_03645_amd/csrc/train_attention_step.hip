@@ -7,7 +7,7 @@
 // on.  The sums of the waves, then those of the parts, are joined at the end.  The new token's key and value are
 // arguments; the wave that begins the cache begins with them, and the same workgroup writes them to the cache.
 //
-// What bounds it is memory: 32 sequences of 8192 places, 4 key heads of 128, 8 query heads each, bf16: 109 us and 6 for the joining launch, 537 MB, 4.9
+// What bounds it is memory: 32 sequences of 8192 places, 4 key heads of 128, 8 query heads each, bf16: 107 us and 6 for the joining launch, 537 MB, 5.0
 // TB/s.  One sequence of 100003 places, 2 heads: 25 us and 5.  Eight short sequences: 8 us, a chain of loads one behind the other.
 #include "train_attention.h"
 #include "train_host.h"

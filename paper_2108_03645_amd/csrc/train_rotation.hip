@@ -8,8 +8,8 @@
 // wave; a lane has the same pairs in every row, so that weights, cosines and the sums of the weights' gradients stay in registers.  Backward forms r
 // again instead of reading it.  The sums of the workgroups are added up by a second launch.
 //
-// What bounds it is memory: 32768 tokens, 16 heads and 2 of 128, bf16: forward 54 us (302 MB, 5.6 TB/s), backward 96 us (453 MB, 4.7 TB/s) and 6 for the
-// weights' sums.  64 tokens: 4 us, a launch's own time and a chain of loads.
+// What bounds it is memory: 32768 tokens, 16 heads and 2 of 128, bf16: forward 54 us (302 MB, 5.6 TB/s), backward 97 us (453 MB, 4.7 TB/s) and 6 for the
+// weights' sums; fp32: 115 us (604 MB, 5.3 TB/s), 163 (906 MB, 5.6 TB/s) and 6.  64 tokens: 4 us, a launch's own time and a chain of loads.
 #include "train_device.h"
 #include "train_host.h"
 
