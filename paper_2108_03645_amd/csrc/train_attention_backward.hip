@@ -385,6 +385,7 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
   if (__syncthreads_or(any_nan<D, 1>(of_k) || any_nan<D, 1>(of_v))) {
     __syncthreads();
     const T *const k0 = at<T>(a.k, here, a.k_stride, kv, a.k_head), *const v0 = at<T>(a.v, here, a.v_stride, kv, a.v_head);
+    const auto is_nan = [](auto x) { const float v = static_cast<float>(x); return v != v ? 1 : 0; };
     // What the queries from .. to - 1 of all heads hold: NaN in lse, which makes both results of a key that sees it NaN, and in delta, all of dk; and what is not
     // finite in element d of do, which goes into that element of dv.
     struct Held {
@@ -394,9 +395,9 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     auto look = [&](int32_t from, int32_t to, int d, Held held) __attribute__((always_inline)) {
       for (int32_t h = head0; h < head0 + heads; ++h) {
         const float2 *const terms = a.terms + static_cast<int64_t>(h) * a.tokens + here;
-        for (int32_t i = from; i < to && held.lse <= 0x7f800000; i += 8)
+        for (int32_t i = from; i < to && held.lse <= 0x7f800000; i += 4)
 #pragma unroll
-          for (int n = 0; n < 8; ++n) {
+          for (int n = 0; n < 4; ++n) {
             const float2 t = terms[min(i + n, to - 1)];
             held.lse = max(held.lse, __float_as_uint(t.x) & 0x7fffffff);
             held.delta = max(held.delta, __float_as_uint(t.y) & 0x7fffffff);
@@ -410,19 +411,17 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
     sum_by_rows<2>(
         lds, count, a.dim,
         [&, behind = Held{}, looked = false](int32_t r, int d) mutable {
-          const float of_k = a.parts == 1 ? static_cast<float>(dk[r * out_stride + d]) : partial[r * partial_stride + d];
-          const float of_v = a.parts == 1 ? static_cast<float>(dv[r * out_stride + d]) : partial[r * partial_stride + a.dim + d];
-          // only of queries and gradients that the key does not see, in the one step that it shares with them
-          bool k_asks = false, v_asks = false;
+          // which of dk and dv are NaN
+          const int nan = a.parts == 1 ? is_nan(dk[r * out_stride + d]) + 2 * is_nan(dv[r * out_stride + d])
+                                       : is_nan(partial[r * partial_stride + d]) + 2 * is_nan(partial[r * partial_stride + a.dim + d]);
+          if (!nan) return 0;
+          // from queries and gradients that the key does not see, in the one step that it shares with them
+          int asks = 0;
           const int32_t step = r / kStepRows * kStepRows;
           for (int32_t h = head0; h < head0 + heads; ++h) {
-            if (of_k != of_k) k_asks |= any_infinite(at<T>(a.q, here, a.q_stride, h, a.q_head), a.q_stride, step, r, d);
-            if (of_v != of_v) v_asks |= any_infinite(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, step, r, d);
+            if (nan & 1) asks |= any_infinite(at<T>(a.q, here, a.q_stride, h, a.q_head), a.q_stride, step, r, d) ? 1 : 0;
+            if (nan & 2) asks |= any_infinite(at<T>(a.dout, here, a.do_stride, h, a.do_head), a.do_stride, step, r, d) ? 2 : 0;
           }
-          // And the rows behind the sequence that its last step has are zeros, but their scores with a key that has infinities NaN: where nothing else
-          // that the key sees is, its own scores were all -infinity.
-          const bool behind_end = left % kStepRows != 0;
-          if (!k_asks && !v_asks && (!behind_end || (of_k == of_k && of_v == of_v))) return 0;
           const int32_t tile = min(kKeyRows, left);
           Held held = behind;                   // of the queries behind the tile, which all of its keys see; looked for once
 #pragma unroll 1
@@ -431,16 +430,15 @@ __device__ __forceinline__ void gradient_of_keys(const AttentionArgs &a, uint32_
             if (turn == 0) behind = held;
           }
           looked = true;
-          if (held.lse > 0x7f800000) return 0;
-          if (v_asks && held.dout.infinite()) {
+          if ((nan & 2) && held.lse <= 0x7f800000 && held.dout.infinite()) {        // also where weights are 0 in 32 bits
             const float all = held.dout.up() ? __builtin_inff() : -__builtin_inff();
             if (a.parts == 1) dv[r * out_stride + d] = static_cast<T>(all);
             else partial[r * partial_stride + a.dim + d] = all;
           }
-          const bool from_there = behind_end && max(held.lse, held.delta) < 0x7f800000;
-          k_asks |= from_there && of_k != of_k;
-          v_asks |= from_there && of_v != of_v;
-          return (k_asks && held.delta <= 0x7f800000 ? 1 : 0) + (v_asks && held.dout.finite() ? 2 : 0);
+          // The rows behind the sequence that its last step has are zeros, but their scores with a key that has infinities NaN: where all that the key
+          // sees is finite, its own scores were -infinity.
+          if (left % kStepRows && max(held.lse, held.delta) < 0x7f800000) asks = nan;
+          return held.lse > 0x7f800000 ? 0 : asks & ((held.delta <= 0x7f800000 ? 1 : 0) | (held.dout.finite() ? 2 : 0));
         },
         [&](int32_t) { return all_steps ? heads * left : 0; },
         [&](int32_t r, int32_t y, float (&w)[2]) {

@@ -307,6 +307,27 @@ def test_keys_of_minus_infinity_have_no_weight(train, n, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("n,heads", [(128, 1), (300, 1), (300, 4)])
+def test_keys_far_below_the_largest_score_see_infinities(train, n, heads, dtype):
+    """Weights of e^-200 are 0 in 32 bits: infinities in o's gradient reach dv, and those of values o, all the same."""
+    q, do = torch.ones(n, heads, 64, device="cuda", dtype=dtype), torch.ones(n, heads, 64, device="cuda", dtype=dtype)
+    k, v = torch.ones(n, 1, 64, device="cuda", dtype=dtype), torch.ones(n, 1, 64, device="cuda", dtype=dtype)
+    k[10] = -24                                                      # scores 8 and -192
+    offsets = torch.tensor([0, n], device="cuda", dtype=torch.int32)
+    o, lse, rest = train.attention_forward(q, k, v, offsets, keep_rest=True)
+    do[50, 0, 5], do[60, 0, 6], do[70, 0, 7], do[80, 0, 7] = float("inf"), -float("inf"), float("inf"), -float("inf")
+    dv = train.attention_backward(do, q, k, v, o, lse, rest, offsets)[2]
+    for key in (0, 10):
+        assert dv[key, 0, 5] == float("inf") and dv[key, 0, 6] == -float("inf") and dv[key, 0, 7].isnan()
+        assert dv[key, 0, 8:].isfinite().all() and dv[key, 0, :5].isfinite().all()
+    assert dv[90:].isfinite().all() and not dv[10, 0, 8:].any()
+    v[10, 0, 3] = float("inf")
+    o = train.attention_forward(q, k, v, offsets)[0]
+    assert (o[10:, :, 3] == float("inf")).all() and torch.equal(o[:10], q[:10]) and torch.equal(o[..., 4:], q[..., 4:])
+
+
+@gpu
 def test_what_every_row_sees_is_not_looked_for_again(train):
     """NaN that belongs in a row: the first token's value, every value, and every row at once; a long sequence takes no longer for it."""
     q, k, v, do = inputs(31, 30000, 1, 1, 64, BF16)
